@@ -59,6 +59,10 @@ enum {
                                 as ONE persistent kernel with grid-wide barriers, so that the weight stream does not stop
                                 at kernel boundaries; implies the folded RMSNorm.  head_dim 128 only; larger steps and
                                 captured streams take the ordinary path                                       */
+  RECG_FLAG_KV_4BIT = 64,    /* the KV pool holds 4 bits a value, about a quarter of the bytes: every kv head's K row and V row
+                                of a token is 16 levels from its smallest value m in steps of s = bf16((max - m) / 15), each
+                                value taken to the nearest (ties to the even level); a row with a value that is not finite
+                                reads back as NaN.  recg_kv_pool_bytes() and everything that takes the pool follow it   */
   RECG_FLAG_DEBUG_CHECKS = 8 /* guard bands behind every workspace region, checked by recg_sync() (RECG_ERR_INTERNAL
                                 if a kernel wrote past the end of one), and a host check that no page which receives
                                 new rows is named by two requests (RECG_ERR_INVALID_ARG)          */
@@ -239,6 +243,17 @@ recg_status recg_kv_write(recg_ctx *ctx, void *kv_pool, int64_t kv_pool_pages, i
 recg_status recg_kv_read(recg_ctx *ctx, const void *kv_pool, int64_t kv_pool_pages, int32_t layer,
                          const int32_t *page_table_row, int32_t n_table, int32_t pos0, int32_t n_pos,
                          void *k, void *v);
+
+/*
+ * Move the K/V rows of a batch into / out of the pool: row t of k and v belongs to row t of the ragged batch, at cache position
+ * L_r + (its row within the request) (ctx_len = 0 and verify_len = n: the first n positions of every request).  k, v: DEVICE bf16,
+ * [T, n_kv_heads, head_dim] with row_stride elements from one row to the next (0: n_kv_heads * head_dim; slices of a projection's
+ * output have more), 16-byte aligned, row_stride a multiple of 8.  batch == NULL: the batch laid out last (by any entry point that
+ * took one with a KV pool).  recg_kv_rows() leaves what lies between the rows as it was.  No slot may be named twice by a batch
+ * that is appended.
+ */
+recg_status recg_kv_append(recg_ctx *ctx, const recg_batch *batch, int32_t layer, const void *k, const void *v, int64_t row_stride);
+recg_status recg_kv_rows(recg_ctx *ctx, const recg_batch *batch, int32_t layer, void *k, void *v, int64_t row_stride);
 
 /*
  * y[M, N] = x[M, K] . w[N, K]^T, the projection kernel without an epilogue (for checking it alone).

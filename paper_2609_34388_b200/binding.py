@@ -20,6 +20,7 @@ RECG_OK = 0
 DTYPE_BF16, DTYPE_F32 = 0, 1
 MEM_DEVICE, MEM_HOST = 0, 1
 FLAG_LOGITS_BF16, FLAG_SIMT_GEMM, FLAG_SIMT_ATTENTION, FLAG_DEBUG_CHECKS, FLAG_FOLD_NORM, FLAG_CHAIN = 1, 2, 4, 8, 16, 32
+FLAG_KV_4BIT = 64
 STATUS_NAMES = {0: "RECG_OK", 1: "RECG_ERR_INVALID_ARG", 2: "RECG_ERR_SHAPE", 3: "RECG_ERR_CAPACITY",
                 4: "RECG_ERR_CUDA", 5: "RECG_ERR_TIMEOUT", 6: "RECG_ERR_INTERNAL"}
 
@@ -107,6 +108,9 @@ def lib() -> C.CDLL:
                 C.c_void_p]
         L.recg_kv_write.argtypes = kvio
         L.recg_kv_read.argtypes = kvio
+        rows = [C.c_void_p, C.POINTER(recg_batch), C.c_int32, C.c_void_p, C.c_void_p, C.c_int64]
+        L.recg_kv_append.argtypes = rows
+        L.recg_kv_rows.argtypes = rows
         L.recg_linear.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         L.recg_debug_buffer.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_void_p), C.POINTER(C.c_int32),
                                         C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
@@ -128,7 +132,7 @@ def lib() -> C.CDLL:
         L.recg_debug_map_cache_selftest.argtypes = [C.c_int32, C.POINTER(C.c_int32)]
         L.recg_debug_map_cache_selftest.restype = C.c_int32
         for f in ("recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write", "recg_kv_read",
-                  "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_timing_enable", "recg_timing_read",
+                  "recg_kv_append", "recg_kv_rows", "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_timing_enable", "recg_timing_read",
                   "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
                   "recg_step_device", "recg_next_round"):
             getattr(L, f).restype = C.c_int32
@@ -137,7 +141,7 @@ def lib() -> C.CDLL:
 
 
 EXPORTS = ("recg_kv_pool_bytes", "recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write",
-           "recg_kv_read", "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_last_error",
+           "recg_kv_read", "recg_kv_append", "recg_kv_rows", "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_last_error",
            "recg_timing_enable", "recg_timing_read", "recg_row_stats_static", "recg_row_stats_static_error",
            "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
            "recg_debug_map_cache_selftest", "recg_step_device", "recg_next_round")
@@ -265,6 +269,7 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("recg needs a CUDA device (there is no CPU fallback)")
         self.cfg = cfg
+        self._last_rows = 0
         self._keep = weights
         self.h = C.c_void_p()
         wptr = None
@@ -294,6 +299,7 @@ class Context:
     def recg_step(self, batch: Batch):
         """Returns a torch view [T, vocab] of the library-owned logits (valid until the next step)."""
         lg = recg_logits()
+        self._n_tok(batch)
         self._check(lib().recg_step(self.h, C.byref(batch.c), C.byref(lg)))
         return lg
 
@@ -338,6 +344,35 @@ class Context:
                                        k.data_ptr(), v.data_ptr()))
         return k, v
 
+    def _kv_rows_args(self, batch: Optional[Batch], k: torch.Tensor, v: torch.Tensor):
+        want = (self._n_tok(batch), self.cfg.n_kv_heads, self.cfg.head_dim)
+        for t in (k, v):
+            if t.dtype != torch.bfloat16 or not t.is_cuda or t.shape != want or t.stride()[1:] != (want[2], 1):
+                raise ValueError(f"k and v must be CUDA bf16 {list(want)} with contiguous rows")
+        if k.stride(0) != v.stride(0) and want[0] > 1:
+            raise ValueError("the rows of k and v must be equally far apart")
+        return C.byref(batch.c) if batch is not None else None, k.data_ptr(), v.data_ptr(), k.stride(0) if want[0] > 1 else 0
+
+    def _n_tok(self, batch: Optional[Batch]) -> int:
+        """Rows of the batch, or of the one that an operation was given last."""
+        if batch is not None:
+            self._last_rows = batch.n_tok
+        return self._last_rows
+
+    def recg_kv_append(self, batch: Optional[Batch], layer: int, k: torch.Tensor, v: torch.Tensor):
+        """k, v [T, n_kv_heads, head_dim]: rows of the batch (None: the one laid out last); rows may lie in a wider array."""
+        b, kp, vp, stride = self._kv_rows_args(batch, k, v)
+        self._check(lib().recg_kv_append(self.h, b, layer, kp, vp, stride))
+
+    def recg_kv_rows(self, batch: Optional[Batch], layer: int, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
+        """The K and V rows of the batch as the pool holds them, into k and v or into new tensors."""
+        if k is None or v is None:
+            k = torch.empty((self._n_tok(batch), self.cfg.n_kv_heads, self.cfg.head_dim), dtype=torch.bfloat16, device="cuda")
+            v = torch.empty_like(k)
+        b, kp, vp, stride = self._kv_rows_args(batch, k, v)
+        self._check(lib().recg_kv_rows(self.h, b, layer, kp, vp, stride))
+        return k, v
+
     def recg_linear(self, x: torch.Tensor, w: torch.Tensor, out_dtype=torch.float32) -> torch.Tensor:
         M, K = x.shape
         N = w.shape[0]
@@ -374,6 +409,7 @@ class Context:
 
     def recg_step_device(self, batch: "DeviceBatch"):
         lg = recg_logits()
+        self._last_rows = self.cfg.max_tokens
         self._check(lib().recg_step_device(self.h, C.byref(batch.c), C.byref(lg)))
         return lg
 

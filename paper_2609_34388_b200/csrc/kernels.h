@@ -257,4 +257,11 @@ void launch_policy(const BatchLayout& bl, const PolicyTable& tb, float* e1, floa
 void launch_kv_io(bool write, void* pool, int64_t n_pages, int layer, const Dims& dm, const int* page_row, int pos0, int n_pos,
                   void* k, void* v, cudaStream_t st);
 
+// K/V rows of a pool in 4 bits: positions of a request, like launch_kv_io
+void launch_kv4_io(bool write, void* pool, int64_t n_pages, int layer, const Dims& dm, const int* page_row, int pos0, int n_pos,
+                   void* k, void* v, cudaStream_t st);
+// K/V rows of the batch laid out last, rows row_stride elements apart, to or from their slots; four: a pool in 4 bits
+void launch_kv_rows(bool write, bool four, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, void* k,
+                    void* v, int64_t row_stride, cudaStream_t st);
+
 }  // namespace recg

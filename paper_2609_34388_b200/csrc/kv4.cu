@@ -1,0 +1,162 @@
+// Rows into and out of the KV pool: a request's positions for a pool in 4 bits (recg_kv_write, recg_kv_read), and the rows of a
+// batch for either kind of pool (recg_kv_append, recg_kv_rows).
+//
+// Nothing is computed that counts, so the bytes bound it: 4 d in, d + 8 out per position and head (K and V) to write, the reverse
+// to read.  The d / 8 lanes that share a row take eight values of it each, one 16-byte access, and reduce minimum and maximum by
+// shuffles; each makes one word of codes.
+#include "kernels.h"
+#include "kv4.cuh"
+
+namespace recg {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kIoPages = 896;        // page ids that travel with a launch: 3.5 of the 4 KB of kernel parameters
+struct IoPages {
+  int first;                         // logical page of ids[0]
+  int ids[kIoPages];
+};
+
+// Positions [pos0, pos0 + n_pos) of a request; k, v [n_pos][n_kv][D].  Two positions of a token pair (2 p, 2 p + 1) and one head
+// are 2 D / 8 consecutive lanes, so that a word of V, which holds both, is put together by one shuffle.
+template <int D, bool WRITE>
+__global__ void __launch_bounds__(kThreads) kv4_io_kernel(uint8_t* pool, int64_t n_pages, int layer, int n_kv,
+                                                          const __grid_constant__ IoPages pages, int pos0, int n_pos,
+                                                          uint4* __restrict__ k, uint4* __restrict__ v) {
+  constexpr int kLanes = D / 8;
+  griddep_launch();
+  const int unit = (int)((blockIdx.x * (unsigned)kThreads + threadIdx.x) / (2 * kLanes));
+  const int half = (threadIdx.x / kLanes) & 1, j = threadIdx.x % kLanes;
+  const int first_pair = pos0 >> 1, n_pairs = ((pos0 + n_pos - 1) >> 1) - first_pair + 1;
+  const int pair = unit / n_kv, h = unit - pair * n_kv;
+  const int pos = 2 * (first_pair + pair) + half, i = pos - pos0;
+  const bool mine = pair < n_pairs && i >= 0 && i < n_pos;
+  const int tok = pos & (kPageSize - 1);
+  uint8_t* block = nullptr;
+  if (mine) block = pool + kv4_block_base(n_pages, n_kv, D, layer, pages.ids[pos / kPageSize - pages.first], h);
+  const size_t at = mine ? ((size_t)i * n_kv + h) * kLanes + j : 0;
+  griddep_wait();
+  if (WRITE) {
+    const uint4 kr = mine ? k[at] : make_uint4(0, 0, 0, 0), vr = mine ? v[at] : make_uint4(0, 0, 0, 0);
+    uint32_t kp, vp;
+    const uint32_t kw = kv4_quantise<kLanes>(kr, &kp), vw = kv4_quantise<kLanes>(vr, &vp);
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, vw, kLanes);
+    const bool both = __shfl_xor_sync(0xffffffffu, (int)mine, kLanes) && mine;
+    if (!mine) return;
+    *reinterpret_cast<uint32_t*>(block + kv4_k_word(tok, j, D)) = kw;
+    if (both) {       // the even position stores the word of the even values, the odd one that of the odd values
+      *reinterpret_cast<uint32_t*>(block + kv4_v_word(tok, j, half, D)) = half ? __byte_perm(other, vw, 0x7632) : __byte_perm(vw, other, 0x5410);
+    } else {
+      *reinterpret_cast<uint16_t*>(block + kv4_v_word(tok, j, 0, D) + 2 * half) = (uint16_t)vw;
+      *reinterpret_cast<uint16_t*>(block + kv4_v_word(tok, j, 1, D) + 2 * half) = (uint16_t)(vw >> 16);
+    }
+    if (j == 0) {
+      *reinterpret_cast<uint32_t*>(block + kv4_k_pairs(D) + 4 * tok) = kp;
+      *reinterpret_cast<uint32_t*>(block + kv4_v_pairs(D) + 4 * tok) = vp;
+    }
+  } else if (mine) {
+    const uint32_t kw = *reinterpret_cast<const uint32_t*>(block + kv4_k_word(tok, j, D));
+    const uint2 w = *reinterpret_cast<const uint2*>(block + kv4_v_word(tok, j, 0, D));
+    const uint32_t kp = *reinterpret_cast<const uint32_t*>(block + kv4_k_pairs(D) + 4 * tok);
+    const uint32_t vp = *reinterpret_cast<const uint32_t*>(block + kv4_v_pairs(D) + 4 * tok);
+    k[at] = kv4_values(kw, kp);
+    v[at] = kv4_values(half ? __byte_perm(w.x, w.y, 0x7632) : __byte_perm(w.x, w.y, 0x5410), vp);
+  }
+}
+
+// The rows of a batch, row t to or from slot tok_slot[t]; rows row_stride elements apart.  FOUR: a pool in 4 bits.
+template <int D, bool FOUR, bool WRITE>
+__global__ void __launch_bounds__(kThreads) kv_rows_kernel(uint8_t* pool, int64_t n_pages, int layer, int n_kv, const int* __restrict__ tok_slot,
+                                                           int n_tok, const int* dyn, uint8_t* k, uint8_t* v, int64_t row_stride) {
+  constexpr int kLanes = D / 8;
+  griddep_launch();
+  const int64_t unit = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes;
+  const int j = threadIdx.x % kLanes;
+  const int t = (int)(unit / n_kv), h = (int)(unit - (int64_t)t * n_kv);
+  const size_t at = ((size_t)t * row_stride + (size_t)h * D + 8 * j) * 2;
+  griddep_wait();
+  if (dyn) n_tok = dyn[0];
+  const int slot = t < n_tok ? tok_slot[t] : -1;
+  const bool mine = slot >= 0;                     // (a slot of a bad page is -1: the layout kernel has said so)
+  const int tok = slot & (kPageSize - 1);
+  const int64_t page = slot / kPageSize;
+  if (FOUR) {
+    uint8_t* block = mine ? pool + kv4_block_base(n_pages, n_kv, D, layer, page, h) : nullptr;
+    if (WRITE) {
+      const uint4 none = make_uint4(0, 0, 0, 0);
+      const uint4 kr = mine ? *reinterpret_cast<const uint4*>(k + at) : none, vr = mine ? *reinterpret_cast<const uint4*>(v + at) : none;
+      uint32_t kp, vp;
+      const uint32_t kw = kv4_quantise<kLanes>(kr, &kp), vw = kv4_quantise<kLanes>(vr, &vp);
+      if (!mine) return;
+      *reinterpret_cast<uint32_t*>(block + kv4_k_word(tok, j, D)) = kw;
+      *reinterpret_cast<uint16_t*>(block + kv4_v_word(tok, j, 0, D) + 2 * (tok & 1)) = (uint16_t)vw;
+      *reinterpret_cast<uint16_t*>(block + kv4_v_word(tok, j, 1, D) + 2 * (tok & 1)) = (uint16_t)(vw >> 16);
+      if (j == 0) {
+        *reinterpret_cast<uint32_t*>(block + kv4_k_pairs(D) + 4 * tok) = kp;
+        *reinterpret_cast<uint32_t*>(block + kv4_v_pairs(D) + 4 * tok) = vp;
+      }
+    } else if (mine) {
+      const uint32_t kw = *reinterpret_cast<const uint32_t*>(block + kv4_k_word(tok, j, D));
+      const uint2 w = *reinterpret_cast<const uint2*>(block + kv4_v_word(tok, j, 0, D));
+      const uint32_t kp = *reinterpret_cast<const uint32_t*>(block + kv4_k_pairs(D) + 4 * tok);
+      const uint32_t vp = *reinterpret_cast<const uint32_t*>(block + kv4_v_pairs(D) + 4 * tok);
+      *reinterpret_cast<uint4*>(k + at) = kv4_values(kw, kp);
+      *reinterpret_cast<uint4*>(v + at) = kv4_values((tok & 1) ? __byte_perm(w.x, w.y, 0x7632) : __byte_perm(w.x, w.y, 0x5410), vp);
+    }
+  } else if (mine) {
+    uint8_t* tile = pool + 2 * (kv_tile_base(n_pages, n_kv, D, layer, page, h) + kv_tile_offset(tok, 8 * j, D));
+    uint8_t* vtile = tile + 2 * kv_tile_elems(D);
+    if (WRITE) {
+      *reinterpret_cast<uint4*>(tile) = *reinterpret_cast<const uint4*>(k + at);
+      *reinterpret_cast<uint4*>(vtile) = *reinterpret_cast<const uint4*>(v + at);
+    } else {
+      *reinterpret_cast<uint4*>(k + at) = *reinterpret_cast<const uint4*>(tile);
+      *reinterpret_cast<uint4*>(v + at) = *reinterpret_cast<const uint4*>(vtile);
+    }
+  }
+}
+
+using IoKernel = void (*)(uint8_t*, int64_t, int, int, const IoPages, int, int, uint4*, uint4*);
+using RowsKernel = void (*)(uint8_t*, int64_t, int, int, const int*, int, const int*, uint8_t*, uint8_t*, int64_t);
+template <int D>
+RowsKernel rows_kernel(bool four, bool write) {
+  if (four) return write ? kv_rows_kernel<D, true, true> : kv_rows_kernel<D, true, false>;
+  return write ? kv_rows_kernel<D, false, true> : kv_rows_kernel<D, false, false>;
+}
+
+}  // namespace
+
+void launch_kv4_io(bool write, void* pool, int64_t n_pages, int layer, const Dims& dm, const int* page_row, int pos0, int n_pos,
+                   void* k, void* v, cudaStream_t st) {
+  uint4 *kp = static_cast<uint4*>(k), *vp = static_cast<uint4*>(v);
+  const size_t row = (size_t)dm.n_kv * (dm.head_dim / 8);
+  IoPages pg;
+  while (n_pos > 0) {
+    pg.first = pos0 / kPageSize;
+    int n = (pg.first + kIoPages) * kPageSize - pos0;          // positions that the launch's page ids cover (whole pairs: a page is even)
+    if (n > n_pos) n = n_pos;
+    const int last = (pos0 + n - 1) / kPageSize;
+    for (int i = pg.first; i <= last; ++i) pg.ids[i - pg.first] = page_row[i];
+    const size_t pairs = ((pos0 + n - 1) >> 1) - (pos0 >> 1) + 1, threads = pairs * dm.n_kv * (dm.head_dim / 4);
+    const dim3 grid((unsigned)((threads + kThreads - 1) / kThreads));
+    IoKernel kernel = dm.head_dim == 128 ? (write ? kv4_io_kernel<128, true> : kv4_io_kernel<128, false>)
+                                         : (write ? kv4_io_kernel<64, true> : kv4_io_kernel<64, false>);
+    launch_pdl(kernel, grid, dim3(kThreads), 0, st, static_cast<uint8_t*>(pool), n_pages, layer, dm.n_kv, pg, pos0, n, kp, vp);
+    pos0 += n;
+    n_pos -= n;
+    kp += n * row;
+    vp += n * row;
+  }
+}
+
+void launch_kv_rows(bool write, bool four, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, void* k,
+                    void* v, int64_t row_stride, cudaStream_t st) {
+  const int64_t threads = (int64_t)bl.n_tok * dm.n_kv * (dm.head_dim / 8);
+  const dim3 grid((unsigned)((threads + kThreads - 1) / kThreads));
+  RowsKernel kernel = dm.head_dim == 128 ? rows_kernel<128>(four, write) : rows_kernel<64>(four, write);
+  launch_pdl(kernel, grid, dim3(kThreads), 0, st, static_cast<uint8_t*>(pool), n_pages, layer, dm.n_kv, (const int*)bl.tok_slot,
+             bl.n_tok, bl.dyn, static_cast<uint8_t*>(k), static_cast<uint8_t*>(v), row_stride);
+}
+
+}  // namespace recg

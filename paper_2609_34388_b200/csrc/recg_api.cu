@@ -7,6 +7,7 @@
 #include "../../include/recg.h"
 #include "common.cuh"
 #include "kernels.h"
+#include "kv4.cuh"
 
 using namespace recg;
 
@@ -327,6 +328,7 @@ recg_status pack_batch(recg_ctx* ctx, const recg_batch* b, bool need_pages, bool
 // projections: whoever writes the residual stream also writes x = bf16(h * gain of the next norm) and partial sums of squares
 // per row, and the projection that reads x scales its accumulator rows by the row's rstd; the mma.sync projections of
 // RECG_FLAG_SIMT_GEMM run it as a kernel of its own).
+bool four_bits(const recg_ctx* ctx) { return ctx->cfg.flags & RECG_FLAG_KV_4BIT; }
 bool folds_norm(const recg_ctx* ctx) { return ctx->tc_state && !(ctx->cfg.flags & RECG_FLAG_SIMT_GEMM); }
 void embed_tokens(recg_ctx* ctx, int64_t n_pages) {
   const Dims& d = ctx->dm;
@@ -400,6 +402,8 @@ extern "C" {
 
 size_t recg_kv_pool_bytes(const recg_config* cfg, int64_t n_pages) {
   if (!cfg || n_pages <= 0) return 0;
+  if (cfg->flags & RECG_FLAG_KV_4BIT)
+    return (size_t)cfg->n_layers * (size_t)n_pages * cfg->n_kv_heads * kv4_block_bytes(cfg->head_dim);
   return (size_t)cfg->n_layers * (size_t)n_pages * cfg->n_kv_heads * 2 * kPageSize * cfg->head_dim * 2;
 }
 
@@ -423,6 +427,8 @@ recg_status recg_init(recg_ctx** out, const recg_config* cfg, const recg_weights
   if (g.hidden % 64 || g.ffn % 64 || g.vocab % 16 || ((g.n_q_heads + 2 * g.n_kv_heads) * g.head_dim) % 128)
     return fail(ctx, RECG_ERR_SHAPE, "recg_init: hidden and ffn must be multiples of 64, vocab of 16, qkv width of 128");
   if (g.mask_token_id >= g.vocab) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_init: mask_token_id outside the vocabulary");
+  if (w && (g.flags & RECG_FLAG_KV_4BIT))
+    return fail(ctx, RECG_ERR_INVALID_ARG, "recg_init: RECG_FLAG_KV_4BIT is for contexts without weights");
   if (w && g.n_layers > 0 &&
       (!w->embed || !w->final_norm || !w->lm_head || !w->attn_norm || !w->wqkv || !w->wo || !w->ffn_norm ||
        !w->w_gate_up || !w->w_down))
@@ -914,6 +920,7 @@ recg_status recg_policy_step(recg_ctx* ctx, const recg_policy_state* state, cons
 recg_status recg_attention(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, void* o) {
   if (!ctx || !q || !o) return RECG_ERR_INVALID_ARG;
   if (layer < 0 || (ctx->cfg.n_layers > 0 && layer >= ctx->cfg.n_layers) ) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_attention: layer out of range");
+  if (four_bits(ctx)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_attention: not available for a pool in 4 bits");
   if (batch) {
     recg_status s = upload_and_layout(ctx, batch, true, false);
     if (s != RECG_OK) return s;
@@ -939,7 +946,7 @@ static recg_status kv_io(recg_ctx* ctx, bool write, void* pool, int64_t n_pool_p
   if ((pos0 + n_pos - 1) / kPageSize >= n_table) return fail(ctx, RECG_ERR_CAPACITY, "recg_kv_*: positions beyond the page table row");
   for (int i = pos0 / kPageSize; i <= (pos0 + n_pos - 1) / kPageSize; ++i)
     if (row[i] < 0 || row[i] >= n_pool_pages) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_*: page id outside the pool");
-  launch_kv_io(write, pool, n_pool_pages, layer, ctx->dm, row, pos0, n_pos, k, v, ctx->stream);
+  (four_bits(ctx) ? launch_kv4_io : launch_kv_io)(write, pool, n_pool_pages, layer, ctx->dm, row, pos0, n_pos, k, v, ctx->stream);
   CU(cudaGetLastError());
   return RECG_OK;
 }
@@ -952,6 +959,40 @@ recg_status recg_kv_write(recg_ctx* ctx, void* kv_pool, int64_t kv_pool_pages, i
 recg_status recg_kv_read(recg_ctx* ctx, const void* kv_pool, int64_t kv_pool_pages, int32_t layer, const int32_t* page_table_row,
                          int32_t n_table, int32_t pos0, int32_t n_pos, void* k, void* v) {
   return kv_io(ctx, false, const_cast<void*>(kv_pool), kv_pool_pages, layer, page_table_row, n_table, pos0, n_pos, k, v);
+}
+
+// The batch of a standalone operation on the pool: the one given, or the one laid out last.
+static recg_status operation_batch(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const char* who) {
+  if (layer < 0 || (ctx->cfg.n_layers > 0 && layer >= ctx->cfg.n_layers))
+    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": layer out of range");
+  if (batch) {
+    recg_status s = upload_and_layout(ctx, batch, true, false);
+    if (s == RECG_OK) ctx->logits_valid = false;
+    return s;
+  }
+  if (!ctx->layout_valid || !ctx->layout_has_pages || !ctx->last_pool)
+    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": no batch given and none with a KV pool laid out before");
+  return RECG_OK;
+}
+
+static recg_status kv_rows(recg_ctx* ctx, bool write, const recg_batch* batch, int32_t layer, void* k, void* v, int64_t row_stride,
+                           const char* who) {
+  if (!ctx || !k || !v) return RECG_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)ctx->dm.n_kv * ctx->dm.head_dim;
+  if (row_stride == 0) row_stride = width;
+  if (row_stride < width || row_stride % 8 || ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15))
+    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": rows must be 16-byte aligned and at least n_kv_heads * head_dim elements apart");
+  recg_status s = operation_batch(ctx, batch, layer, who);
+  if (s != RECG_OK) return s;
+  launch_kv_rows(write, four_bits(ctx), ctx->bl, ctx->last_pool, ctx->last_pool_pages, layer, ctx->dm, k, v, row_stride, ctx->stream);
+  CU(cudaGetLastError());
+  return RECG_OK;
+}
+recg_status recg_kv_append(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* k, const void* v, int64_t row_stride) {
+  return kv_rows(ctx, true, batch, layer, const_cast<void*>(k), const_cast<void*>(v), row_stride, "recg_kv_append");
+}
+recg_status recg_kv_rows(recg_ctx* ctx, const recg_batch* batch, int32_t layer, void* k, void* v, int64_t row_stride) {
+  return kv_rows(ctx, false, batch, layer, k, v, row_stride, "recg_kv_rows");
 }
 
 recg_status recg_linear(recg_ctx* ctx, const void* x, const void* w, void* y, int32_t M, int32_t N, int32_t K,

@@ -108,3 +108,12 @@ def test_product_does_not_import_the_oracle():
             if f.endswith((".py", ".cu", ".cuh", ".h")):
                 src = open(os.path.join(dirpath, f)).read()
                 assert "oracle" not in src.replace("the CPU oracle", "").replace("CPU oracle", ""), f
+
+
+def test_pool_bytes_of_a_4_bit_pool():
+    lib = binding.lib()
+    cfg = binding.recg_config(32, 4096, 32, 8, 128, 14336, 128256, 5e5, 1e-5, -1, 16, 16, 1024, 600, binding.FLAG_KV_4BIT)
+    # per token and head: 2 x 64 bytes of codes and 2 x 4 bytes of {step, minimum}
+    assert lib.recg_kv_pool_bytes(C.byref(cfg), 10) == 10 * 16 * 32 * 8 * 136
+    cfg.head_dim = 64
+    assert lib.recg_kv_pool_bytes(C.byref(cfg), 10) == 10 * 16 * 32 * 8 * 72
