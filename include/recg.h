@@ -231,6 +231,8 @@ recg_status recg_verify(recg_ctx *ctx, const recg_batch *batch, const void *logi
  * positions of every request must already be in layer `layer` of the pool.
  */
 recg_status recg_attention(recg_ctx *ctx, const recg_batch *batch, int32_t layer, const void *q, void *o);
+/* The same, and lse[t, h] = ln of the sum over the visible positions of exp(q . k / sqrt(head_dim)): DEVICE float32 [T, n_q_heads]. */
+recg_status recg_attention_lse(recg_ctx *ctx, const recg_batch *batch, int32_t layer, const void *q, void *o, float *lse);
 
 /*
  * Move logical K/V rows of one request into / out of the pool.  k, v: DEVICE bf16

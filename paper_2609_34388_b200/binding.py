@@ -104,6 +104,7 @@ def lib() -> C.CDLL:
         L.recg_step.argtypes = [C.c_void_p, C.POINTER(recg_batch), C.POINTER(recg_logits)]
         L.recg_verify.argtypes = [C.c_void_p, C.POINTER(recg_batch), C.c_void_p, C.c_int32, C.POINTER(recg_verify_out)]
         L.recg_attention.argtypes = [C.c_void_p, C.POINTER(recg_batch), C.c_int32, C.c_void_p, C.c_void_p]
+        L.recg_attention_lse.argtypes = L.recg_attention.argtypes + [C.c_void_p]
         kvio = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                 C.c_void_p]
         L.recg_kv_write.argtypes = kvio
@@ -132,7 +133,7 @@ def lib() -> C.CDLL:
         L.recg_debug_map_cache_selftest.argtypes = [C.c_int32, C.POINTER(C.c_int32)]
         L.recg_debug_map_cache_selftest.restype = C.c_int32
         for f in ("recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write", "recg_kv_read",
-                  "recg_kv_append", "recg_kv_rows", "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_timing_enable", "recg_timing_read",
+                  "recg_attention_lse", "recg_kv_append", "recg_kv_rows", "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_timing_enable", "recg_timing_read",
                   "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
                   "recg_step_device", "recg_next_round"):
             getattr(L, f).restype = C.c_int32
@@ -141,7 +142,7 @@ def lib() -> C.CDLL:
 
 
 EXPORTS = ("recg_kv_pool_bytes", "recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write",
-           "recg_kv_read", "recg_kv_append", "recg_kv_rows", "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_last_error",
+           "recg_attention_lse", "recg_kv_read", "recg_kv_append", "recg_kv_rows", "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_last_error",
            "recg_timing_enable", "recg_timing_read", "recg_row_stats_static", "recg_row_stats_static_error",
            "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
            "recg_debug_map_cache_selftest", "recg_step_device", "recg_next_round")
@@ -326,9 +327,16 @@ class Context:
         self._check(lib().recg_verify(self.h, C.byref(batch.c) if batch is not None else None, lp, dt, C.byref(out.c)))
         return out.views()
 
-    def recg_attention(self, batch: Optional[Batch], layer: int, q: torch.Tensor, o: torch.Tensor):
-        self._check(lib().recg_attention(self.h, C.byref(batch.c) if batch is not None else None, layer, q.data_ptr(),
-                                         o.data_ptr()))
+    def recg_attention(self, batch: Optional[Batch], layer: int, q: torch.Tensor, o: torch.Tensor, lse: Optional[torch.Tensor] = None):
+        """lse (float32 [T, n_q_heads], optional) receives the log-sum-exp of every row's scores."""
+        n_tok = self._n_tok(batch)
+        b = C.byref(batch.c) if batch is not None else None
+        if lse is None:
+            self._check(lib().recg_attention(self.h, b, layer, q.data_ptr(), o.data_ptr()))
+            return
+        if lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.numel() != n_tok * self.cfg.n_q_heads:
+            raise ValueError(f"lse must be contiguous CUDA float32 [{n_tok}, {self.cfg.n_q_heads}]")
+        self._check(lib().recg_attention_lse(self.h, b, layer, q.data_ptr(), o.data_ptr(), lse.data_ptr()))
 
     def recg_kv_write(self, pool: torch.Tensor, n_pages: int, layer: int, page_row, pos0: int, k: torch.Tensor,
                       v: torch.Tensor):

@@ -42,6 +42,7 @@ struct AttnParams {
   const int* tok_hi;
   const __nv_bfloat16* q;
   __nv_bfloat16* o;
+  float* lse;         // log-sum-exp of every row and head (null: not wanted)
   const __nv_bfloat16* pool;
   int64_t n_pages;
   int layer, n_q, n_kv, group;
@@ -346,6 +347,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P
 #pragma unroll
           for (int i = 0; i < D / 8; ++i)
             dst[i * 4 + q4] = pack_bf16(o[i][2 * hh] * inv, o[i][2 * hh + 1] * inv);
+          if (P.lse && q4 == 0) P.lse[(size_t)qrow_tok[hh] * P.n_q + qrow_head[hh]] = log_sum_exp(m_run[hh], l_run[hh]);
         } else {
           float2* dst = reinterpret_cast<float2*>(P.part_o + ((size_t)w.part * 128 + rho) * D);
 #pragma unroll
@@ -376,7 +378,7 @@ __global__ void __launch_bounds__(512, MODE == kDeepRows ? 1 : 2) attention_comb
                                                                 const int* __restrict__ counts, int n_q, int group,
                                                                 const float* __restrict__ part_o,
                                                                 const float* __restrict__ part_ml,
-                                                                __nv_bfloat16* __restrict__ o, int list_settled, int log_split) {
+                                                                __nv_bfloat16* __restrict__ o, float* __restrict__ lse, int list_settled, int log_split) {
   constexpr int E = D / 32;
   constexpr bool SPLIT = MODE == kSplitRows;
   constexpr int kRows = MODE == kDeepRows ? 18 : 6;     // partial rows in flight
@@ -464,7 +466,9 @@ __global__ void __launch_bounds__(512, MODE == kDeepRows ? 1 : 2) attention_comb
     if (live && my == 0) {
       const float inv = l > 0.f ? 1.f / l : 0.f;
       const int j = rho / group, hg = rho % group;
-      __nv_bfloat16* dst = o + ((size_t)(tl.tok0 + j) * n_q + tl.kv_head * group + hg) * D + lane * E;
+      const size_t row = (size_t)(tl.tok0 + j) * n_q + tl.kv_head * group + hg;
+      __nv_bfloat16* dst = o + row * D + lane * E;
+      if (lse && lane == 0) lse[row] = log_sum_exp(m, l);
       if constexpr (E == 4) {
         uint2 pk;
         pk.x = pack_bf16(acc[0] * inv, acc[1] * inv);
@@ -502,7 +506,15 @@ auto combine_kernel(int tiles, int log_s, int n_sm) {
 }
 
 template <int D>
-void launch_attention_t(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, const void* kv_pool,
+void launch_combine(const BatchLayout& bl, const Dims& dm, void* o, float* lse, const float* part_o, const float* part_ml, int n_sm,
+                    cudaStream_t st, int tiles, bool step, int list_settled) {
+  const int log_s = combine_split(tiles, n_sm, step);
+  launch_pdl(combine_kernel<D>(tiles, log_s, n_sm), dim3(combine_ctas(tiles, log_s, n_sm)), dim3(512), 0, st, (const AttnTile*)bl.tiles,
+             (const int*)bl.counts, dm.n_q, dm.n_q / dm.n_kv, part_o, part_ml, static_cast<__nv_bfloat16*>(o), lse, list_settled, log_s);
+}
+
+template <int D>
+void launch_attention_t(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
                         int64_t n_pages, float* part_o, float* part_ml, int tok_per_tile, int n_sm, int* status,
                         cudaStream_t st, bool whole, int tiles, bool step) {
   static bool configured[kMaxDevices] = {false};
@@ -519,6 +531,7 @@ void launch_attention_t(const BatchLayout& bl, const Dims& dm, int layer, const 
   P.tok_hi = bl.tok_hi;
   P.q = static_cast<const __nv_bfloat16*>(q);
   P.o = static_cast<__nv_bfloat16*>(o);
+  P.lse = lse;
   P.pool = static_cast<const __nv_bfloat16*>(kv_pool);
   P.n_pages = n_pages;
   P.layer = layer;
@@ -530,11 +543,7 @@ void launch_attention_t(const BatchLayout& bl, const Dims& dm, int layer, const 
   P.part_ml = part_ml;
   P.status = status;
   launch_pdl(attention_kernel<D>, dim3(n_sm), dim3(kAttnThreads), AttnSmem<D>::kTotal, st, P);
-  if (whole) return;
-  const int log_s = combine_split(tiles, n_sm, step);
-  launch_pdl(combine_kernel<D>(tiles, log_s, n_sm), dim3(combine_ctas(tiles, log_s, n_sm)), dim3(512), 0, st,
-             (const AttnTile*)bl.tiles, (const int*)bl.counts, dm.n_q, P.group, (const float*)part_o, (const float*)part_ml,
-             static_cast<__nv_bfloat16*>(o), 0, log_s);
+  if (!whole) launch_combine<D>(bl, dm, o, lse, part_o, part_ml, n_sm, st, tiles, step, 0);
 }
 
 }  // namespace
@@ -545,20 +554,18 @@ size_t attention_smem_bytes(int head_dim) {
 
 void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, const void* kv_pool,
                       int64_t n_pages, float* part_o, float* part_ml, int tok_per_tile, int n_sm, int* status,
-                      cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step) {
-  if (use_tc && dm.head_dim == 128) {
-    launch_attention_tc_main(bl, dm, layer, q, o, kv_pool, n_pages, part_o, part_ml, n_sm, status, st, layout_settled);
-    if (whole) return;
-    const int log_s = combine_split(tiles, n_sm, step);
-    launch_pdl(combine_kernel<128>(tiles, log_s, n_sm), dim3(combine_ctas(tiles, log_s, n_sm)), dim3(512), 0, st,
-               (const AttnTile*)bl.tiles, (const int*)bl.counts, dm.n_q, dm.n_q / dm.n_kv, (const float*)part_o, (const float*)part_ml,
-               static_cast<__nv_bfloat16*>(o), 1, log_s);    // (the kernel in front signals its dependents when the list is settled)
+                      cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, bool four, float* lse) {
+  if (four || (use_tc && dm.head_dim == 128)) {
+    if (four) launch_attention_kv4(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st);
+    else launch_attention_tc_main(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st, layout_settled);
+    // (the kernel in front signals its dependents when the list is settled)
+    if (!whole) (dm.head_dim == 64 ? launch_combine<64> : launch_combine<128>)(bl, dm, o, lse, part_o, part_ml, n_sm, st, tiles, step, 1);
     return;
   }
   if (dm.head_dim == 64)
-    launch_attention_t<64>(bl, dm, layer, q, o, kv_pool, n_pages, part_o, part_ml, tok_per_tile, n_sm, status, st, whole, tiles, step);
+    launch_attention_t<64>(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, tok_per_tile, n_sm, status, st, whole, tiles, step);
   else
-    launch_attention_t<128>(bl, dm, layer, q, o, kv_pool, n_pages, part_o, part_ml, tok_per_tile, n_sm, status, st, whole, tiles, step);
+    launch_attention_t<128>(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, tok_per_tile, n_sm, status, st, whole, tiles, step);
 }
 
 }  // namespace recg

@@ -89,6 +89,7 @@ struct TcAttnParams {
   const int* tok_lo;
   const int* tok_hi;
   __nv_bfloat16* o;
+  float* lse;         // log-sum-exp of every row and head (null: not wanted)
   const __nv_bfloat16* pool;
   int64_t n_pages;
   int layer, n_q, n_kv, group;
@@ -687,6 +688,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             __syncwarp();
           }
         }
+        if (P.lse && g == 0 && rvalid && w.part < 0)
+          P.lse[(size_t)(w.tok0 + j) * P.n_q + w.kv_head * P.group + hg] = log_sum_exp(m_all, l_all);
         if (g == 0 && rvalid && w.part >= 0) {
           P.part_ml[((size_t)w.part * 128 + row) * 2 + 0] = m_all;
           P.part_ml[((size_t)w.part * 128 + row) * 2 + 1] = l_all;
@@ -774,7 +777,7 @@ bool q_tensor_map(const void* q, int n_tok, int n_q, int group, CUtensorMap* out
 
 }  // namespace
 
-void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o,
+void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse,
                               const void* kv_pool, int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status,
                               cudaStream_t st, bool layout_settled) {
   static bool configured[kMaxDevices] = {false};
@@ -790,6 +793,7 @@ void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, 
   P.tok_lo = bl.tok_lo;
   P.tok_hi = bl.tok_hi;
   P.o = static_cast<__nv_bfloat16*>(o);
+  P.lse = lse;
   P.pool = static_cast<const __nv_bfloat16*>(kv_pool);
   P.n_pages = n_pages;
   P.layer = layer;

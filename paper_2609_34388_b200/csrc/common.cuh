@@ -120,6 +120,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 __device__ __forceinline__ float bf16_bits_to_float(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
 
+// ln sum exp of a row from its reference maximum (powers of two) and its sum relative to that; -inf for a row without tokens
+__device__ __forceinline__ float log_sum_exp(float ref, float sum) { return (ref + log2f(sum)) * 0.69314718056f; }
+
 // two fp32 operations per instruction
 __device__ __forceinline__ float2 fma2(const float2& a, const float2& b, const float2& c) {
   uint64_t d;

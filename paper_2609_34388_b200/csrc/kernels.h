@@ -218,10 +218,14 @@ bool launch_gemm_chain(void* s, const ChainOp* ops, int n_ops, int M, const Chai
 // tiles: the row tiles of all kv heads, cut or not (0: known on the device only); step: a projection follows
 void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, const void* kv_pool,
                       int64_t n_pages, float* part_o, float* part_ml, int tok_per_tile, int n_sm, int* status,
-                      cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step);
-void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o,
+                      cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, bool four = false,
+                      float* lse = nullptr);
+void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse,
                               const void* kv_pool, int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status,
                               cudaStream_t st, bool layout_settled);
+// the same over a pool in 4 bits
+void launch_attention_kv4(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
+                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status, cudaStream_t st);
 size_t attention_smem_bytes(int head_dim);
 
 // S9b + S10

@@ -199,6 +199,8 @@ size_t carve(recg_ctx* c, DeviceArena& A) {
   return A.used + 256;
 }
 
+bool four_bits(const recg_ctx* ctx) { return ctx->cfg.flags & RECG_FLAG_KV_4BIT; }
+
 // Rows of request r: verify tokens, continuation masks and the correction branches (replacement + masks each).
 static inline int request_rows(const recg_batch* b, int r) {
   const int nc = b->n_corr ? b->n_corr[r] : 0;
@@ -214,6 +216,8 @@ recg_status pack_batch(recg_ctx* ctx, const recg_batch* b, bool need_pages, bool
   const bool pages = b->page_table != nullptr;
   if (need_pages && (!pages || !b->kv_pool || b->kv_pool_pages <= 0))
     return fail(ctx, RECG_ERR_INVALID_ARG, "batch: page_table and kv_pool are required");
+  if (four_bits(ctx) && (reinterpret_cast<uintptr_t>(b->kv_pool) & 15))
+    return fail(ctx, RECG_ERR_INVALID_ARG, "batch: a KV pool in 4 bits must be 16-byte aligned");
   if (pages && (b->page_table_stride <= 0 || b->page_table_stride > ctx->cfg.max_pages_per_request))
     return fail(ctx, RECG_ERR_CAPACITY, "batch: page_table_stride exceeds max_pages_per_request");
   if (b->n_corr && (!b->corr_index || !b->corr_token || !b->corr_block))
@@ -328,7 +332,6 @@ recg_status pack_batch(recg_ctx* ctx, const recg_batch* b, bool need_pages, bool
 // projections: whoever writes the residual stream also writes x = bf16(h * gain of the next norm) and partial sums of squares
 // per row, and the projection that reads x scales its accumulator rows by the row's rstd; the mma.sync projections of
 // RECG_FLAG_SIMT_GEMM run it as a kernel of its own).
-bool four_bits(const recg_ctx* ctx) { return ctx->cfg.flags & RECG_FLAG_KV_4BIT; }
 bool folds_norm(const recg_ctx* ctx) { return ctx->tc_state && !(ctx->cfg.flags & RECG_FLAG_SIMT_GEMM); }
 void embed_tokens(recg_ctx* ctx, int64_t n_pages) {
   const Dims& d = ctx->dm;
@@ -917,23 +920,41 @@ recg_status recg_policy_step(recg_ctx* ctx, const recg_policy_state* state, cons
   return RECG_OK;
 }
 
-recg_status recg_attention(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, void* o) {
-  if (!ctx || !q || !o) return RECG_ERR_INVALID_ARG;
-  if (layer < 0 || (ctx->cfg.n_layers > 0 && layer >= ctx->cfg.n_layers) ) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_attention: layer out of range");
-  if (four_bits(ctx)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_attention: not available for a pool in 4 bits");
+// The batch of a standalone operation on the pool: the one given, or the one laid out last.
+static recg_status operation_batch(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const char* who) {
+  if (layer < 0 || (ctx->cfg.n_layers > 0 && layer >= ctx->cfg.n_layers))
+    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": layer out of range");
   if (batch) {
     recg_status s = upload_and_layout(ctx, batch, true, false);
-    if (s != RECG_OK) return s;
-    ctx->logits_valid = false;
-  } else if (!ctx->layout_valid || !ctx->layout_has_pages || !ctx->last_pool) {
-    return fail(ctx, RECG_ERR_INVALID_ARG, "recg_attention: no batch given and none with a KV pool laid out before");
+    if (s == RECG_OK) ctx->logits_valid = false;
+    return s;
   }
+  if (!ctx->layout_valid || !ctx->layout_has_pages || !ctx->last_pool)
+    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": no batch given and none with a KV pool laid out before");
+  return RECG_OK;
+}
+
+static bool aligned16(const void* a, const void* b) { return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15) == 0; }
+
+static recg_status attention(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, void* o, float* lse, const char* who) {
+  if (four_bits(ctx) && !aligned16(q, o)) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": q and o must be 16-byte aligned");
+  recg_status s = operation_batch(ctx, batch, layer, who);
+  if (s != RECG_OK) return s;
   launch_attention(ctx->bl, ctx->dm, layer, q, o, ctx->last_pool, ctx->last_pool_pages, ctx->part_o, ctx->part_ml,
                    ctx->tok_per_tile, ctx->n_sm, ctx->d_status, ctx->stream, !(ctx->cfg.flags & RECG_FLAG_SIMT_ATTENTION),
-                   ctx->list_settled, ctx->layout_whole, ctx->layout_tiles, false);
+                   ctx->list_settled, ctx->layout_whole, ctx->layout_tiles, false, four_bits(ctx), lse);
   CU(cudaGetLastError());
   ctx->list_settled = true;
   return RECG_OK;
+}
+
+recg_status recg_attention(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, void* o) {
+  if (!ctx || !q || !o) return RECG_ERR_INVALID_ARG;
+  return attention(ctx, batch, layer, q, o, nullptr, "recg_attention");
+}
+recg_status recg_attention_lse(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, void* o, float* lse) {
+  if (!ctx || !q || !o || !lse) return RECG_ERR_INVALID_ARG;
+  return attention(ctx, batch, layer, q, o, lse, "recg_attention_lse");
 }
 
 static recg_status kv_io(recg_ctx* ctx, bool write, void* pool, int64_t n_pool_pages, int32_t layer,
@@ -942,6 +963,8 @@ static recg_status kv_io(recg_ctx* ctx, bool write, void* pool, int64_t n_pool_p
   if (pos0 < 0 || n_pos < 0 || n_table <= 0 || n_table > ctx->cfg.max_pages_per_request || layer < 0 ||
       (ctx->cfg.n_layers > 0 && layer >= ctx->cfg.n_layers) || n_pool_pages <= 0)
     return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_*: bad position range, layer or table length");
+  if (four_bits(ctx) && (!aligned16(k, v) || !aligned16(pool, pool)))
+    return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_*: k, v and the pool must be 16-byte aligned");
   if (n_pos == 0) return RECG_OK;
   if ((pos0 + n_pos - 1) / kPageSize >= n_table) return fail(ctx, RECG_ERR_CAPACITY, "recg_kv_*: positions beyond the page table row");
   for (int i = pos0 / kPageSize; i <= (pos0 + n_pos - 1) / kPageSize; ++i)
@@ -961,26 +984,12 @@ recg_status recg_kv_read(recg_ctx* ctx, const void* kv_pool, int64_t kv_pool_pag
   return kv_io(ctx, false, const_cast<void*>(kv_pool), kv_pool_pages, layer, page_table_row, n_table, pos0, n_pos, k, v);
 }
 
-// The batch of a standalone operation on the pool: the one given, or the one laid out last.
-static recg_status operation_batch(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const char* who) {
-  if (layer < 0 || (ctx->cfg.n_layers > 0 && layer >= ctx->cfg.n_layers))
-    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": layer out of range");
-  if (batch) {
-    recg_status s = upload_and_layout(ctx, batch, true, false);
-    if (s == RECG_OK) ctx->logits_valid = false;
-    return s;
-  }
-  if (!ctx->layout_valid || !ctx->layout_has_pages || !ctx->last_pool)
-    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": no batch given and none with a KV pool laid out before");
-  return RECG_OK;
-}
-
 static recg_status kv_rows(recg_ctx* ctx, bool write, const recg_batch* batch, int32_t layer, void* k, void* v, int64_t row_stride,
                            const char* who) {
   if (!ctx || !k || !v) return RECG_ERR_INVALID_ARG;
   const int64_t width = (int64_t)ctx->dm.n_kv * ctx->dm.head_dim;
   if (row_stride == 0) row_stride = width;
-  if (row_stride < width || row_stride % 8 || ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15))
+  if (row_stride < width || row_stride % 8 || !aligned16(k, v))
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": rows must be 16-byte aligned and at least n_kv_heads * head_dim elements apart");
   recg_status s = operation_batch(ctx, batch, layer, who);
   if (s != RECG_OK) return s;

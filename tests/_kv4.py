@@ -42,3 +42,42 @@ def attention(q, k, v, see):
         o[:, h] = (p / p.sum(-1, keepdims=True)) @ np.where(see.any(0)[:, None], v[:, h // g], 0.0)
         lse[:, h] = (top + np.log(p.sum(-1, keepdims=True)))[:, 0]
     return o, lse
+
+
+def visible(L, v, b, corr=(), bc=0):
+    """[n, L + n] bool: what each new row of a request sees (corr: draft indices its branches replace, bc masks each)."""
+    n = v + b + len(corr) * (1 + bc)
+    see = np.zeros((n, L + n), dtype=bool)
+    for i in range(v):
+        see[i, :L + i + 1] = True
+    see[v:v + b, :L + v + b] = True
+    for k, i in enumerate(corr):
+        first = v + b + k * (1 + bc)
+        see[first:first + 1 + bc, :L + i] = True
+        see[first, L + first] = True
+        see[first + 1:first + 1 + bc, L + first:L + first + 1 + bc] = True
+    return see
+
+
+def attention_bounds(q, k_codes, v_codes, see):
+    """How far kernels may be from `attention` (o before its own rounding, and lse): p times a step is rounded to bf16 once
+    (2^-8 of every term p s |c - 8|), everything else is fp32: a score's sum of exact products takes eight steps in an accumulator
+    that drops what is below 2^-22 of its largest term, and 2^x and its argument are good to 2^-21 of the exponents."""
+    (ck, sk, mk), (cv, sv, mv) = k_codes, v_codes
+    n, nq, d = q.shape
+    g = nq // ck.shape[1]
+    o_err, lse_err = np.zeros((n, nq, d)), np.zeros((n, nq))
+    for h in range(nq):
+        kh = h // g
+        size = (np.abs(q[:, h]) @ (sk[:, kh] * np.abs(ck[:, kh] - 8)).T
+                + np.abs(q[:, h]).sum(-1, keepdims=True) * np.abs(mk[:, kh] + 8 * sk[:, kh]).T) / math.sqrt(d)
+        score = np.where(see, size * 2.0 ** -19 + 2.0 ** -21, 0.0).max(-1)               # absolute error of any visible score
+        z = np.where(see, q[:, h] @ (mk[:, kh] + sk[:, kh] * ck[:, kh]).T / math.sqrt(d), -np.inf)
+        top = z.max(-1, keepdims=True)
+        p = np.exp(z - top)
+        p /= p.sum(-1, keepdims=True)
+        coded = p @ np.where(see.any(0)[:, None], sv[:, kh] * np.abs(cv[:, kh] - 8), 0.0)
+        rest = p @ np.where(see.any(0)[:, None], np.abs(mv[:, kh] + 8 * sv[:, kh]), 0.0)
+        o_err[:, h] = 2.0 ** -8 * coded + (2.0 ** -17 + 4 * score)[:, None] * (coded + rest)
+        lse_err[:, h] = score + 2.0 ** -20 * (1 + np.abs(top[:, 0]) + math.log(see.shape[1]))
+    return o_err, lse_err
