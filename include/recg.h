@@ -258,6 +258,52 @@ recg_status recg_kv_append(recg_ctx *ctx, const recg_batch *batch, int32_t layer
 recg_status recg_kv_rows(recg_ctx *ctx, const recg_batch *batch, int32_t layer, void *k, void *v, int64_t row_stride);
 
 /*
+ * The attention weight that the cached tokens of a batch gather in one layer (what an eviction goes by).  Per request, kv head
+ * and cache position j < L_r + n_r, in float32:
+ *   weights_out[j] = (j < L_r ? decay * weights_in[j] : 0) + sum over the rows t of the request and the query heads that share the
+ *                    kv head of row_weight[t] * exp(q . k_j / sqrt(head_dim) - lse[t])       (rows that see j: the mask of Eq. 1)
+ *   q [T, n_q_heads, head_dim] bf16 and lse [T, n_q_heads] as recg_attention_lse() had and gave them; row_weight float32 [T] or
+ *   NULL (1 each; 0 leaves a row out: mask rows, drafts that verification rejected); decay >= 0; all DEVICE.
+ * weights_in, weights_out: DEVICE float32 [n_layers, kv_pool_pages, n_kv_heads, 16], entry (layer, page, head, offset) for the
+ * token in that slot; they may be the same array.  weights_in == NULL: nothing gathered so far.  Entries of other slots are left as they are.
+ * batch == NULL: the batch laid out last.
+ */
+recg_status recg_kv_weights(recg_ctx *ctx, const recg_batch *batch, int32_t layer, const void *q, const float *lse,
+                            const float *row_weight, float decay, const float *weights_in, float *weights_out);
+
+/*
+ * Eviction by gathered weight.  Every request r is cut to kept_r = min(ctx_len[r], budget[r]) committed positions, per layer and
+ * kv head its own: the first n_sink, the last n_recent, and of the others those with the largest weight (the lowest position
+ * among equals; NaN ranks last).  They stay in their order, so that kept_r is the request's new ctx_len.  K keeps the rotation of its
+ * original position.
+ *   ctx_len, budget [n_req]; page_table [n_req, page_table_stride]: HOST.  A budget that cuts must be at least n_sink + n_recent.
+ *   dst_page_table [n_req, dst_stride]: HOST, pages that take what stays, which must be no page of the sources (pages that
+ *                  requests share, as a common prefix, stay whole that way); NULL: in place, no page named twice
+ *   weights        DEVICE float32, as for recg_kv_weights(), 16-byte aligned
+ *   layer_begin, layer_end  the layers [begin, end)
+ * recg_kv_select() writes keep: DEVICE int32 [layer_end - layer_begin, n_req, n_kv_heads, keep_stride], the positions that stay in
+ * ascending order, -1 behind the last.  kv_pool is not read.
+ * recg_kv_compact() moves K, V and weight (weights may be NULL) of position keep[i] to position i.  keep may be any list of
+ * positions below ctx_len, in place with keep[i] >= i; an entry that is not sets the device status word (recg_sync() returns
+ * RECG_ERR_INTERNAL) and its position is left as it was.
+ * Both copy the HOST arrays and do not synchronise; they are refused while the stream is being captured.
+ */
+typedef struct {
+  int32_t n_req, n_sink, n_recent;
+  const int32_t *ctx_len, *budget;
+  const int32_t *page_table;
+  int32_t page_table_stride;
+  const int32_t *dst_page_table;
+  int32_t dst_stride;
+  void *kv_pool;
+  int64_t kv_pool_pages;
+  float *weights;
+  int32_t layer_begin, layer_end;
+} recg_eviction;
+recg_status recg_kv_select(recg_ctx *ctx, const recg_eviction *eviction, int32_t *keep, int32_t keep_stride);
+recg_status recg_kv_compact(recg_ctx *ctx, const recg_eviction *eviction, const int32_t *keep, int32_t keep_stride);
+
+/*
  * y[M, N] = x[M, K] . w[N, K]^T, the projection kernel without an epilogue (for checking it alone).
  * x, w: DEVICE bf16, 16-byte aligned, K a multiple of 64 and N a multiple of 16; y: DEVICE, out_dtype, 8-byte aligned for
  * bf16 (16-byte: the tcgen05 kernel, else the mma.sync one), 4-byte for fp32 (16-byte with RECG_FLAG_SIMT_GEMM).  Pointers

@@ -86,6 +86,13 @@ class recg_round_log(C.Structure):
                 ("entropy_mean", C.c_void_p)]
 
 
+class recg_eviction(C.Structure):
+    _fields_ = [("n_req", C.c_int32), ("n_sink", C.c_int32), ("n_recent", C.c_int32), ("ctx_len", C.c_void_p), ("budget", C.c_void_p),
+                ("page_table", C.c_void_p), ("page_table_stride", C.c_int32), ("dst_page_table", C.c_void_p), ("dst_stride", C.c_int32),
+                ("kv_pool", C.c_void_p), ("kv_pool_pages", C.c_int64), ("weights", C.c_void_p), ("layer_begin", C.c_int32),
+                ("layer_end", C.c_int32)]
+
+
 _lib = None
 
 
@@ -112,6 +119,10 @@ def lib() -> C.CDLL:
         rows = [C.c_void_p, C.POINTER(recg_batch), C.c_int32, C.c_void_p, C.c_void_p, C.c_int64]
         L.recg_kv_append.argtypes = rows
         L.recg_kv_rows.argtypes = rows
+        L.recg_kv_weights.argtypes = [C.c_void_p, C.POINTER(recg_batch), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+                                      C.c_void_p, C.c_void_p]
+        L.recg_kv_select.argtypes = [C.c_void_p, C.POINTER(recg_eviction), C.c_void_p, C.c_int32]
+        L.recg_kv_compact.argtypes = L.recg_kv_select.argtypes
         L.recg_linear.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         L.recg_debug_buffer.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_void_p), C.POINTER(C.c_int32),
                                         C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
@@ -133,7 +144,8 @@ def lib() -> C.CDLL:
         L.recg_debug_map_cache_selftest.argtypes = [C.c_int32, C.POINTER(C.c_int32)]
         L.recg_debug_map_cache_selftest.restype = C.c_int32
         for f in ("recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write", "recg_kv_read",
-                  "recg_attention_lse", "recg_kv_append", "recg_kv_rows", "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_timing_enable", "recg_timing_read",
+                  "recg_attention_lse", "recg_kv_append", "recg_kv_rows", "recg_kv_weights", "recg_kv_select", "recg_kv_compact",
+           "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_timing_enable", "recg_timing_read",
                   "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
                   "recg_step_device", "recg_next_round"):
             getattr(L, f).restype = C.c_int32
@@ -142,7 +154,8 @@ def lib() -> C.CDLL:
 
 
 EXPORTS = ("recg_kv_pool_bytes", "recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write",
-           "recg_attention_lse", "recg_kv_read", "recg_kv_append", "recg_kv_rows", "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_last_error",
+           "recg_attention_lse", "recg_kv_read", "recg_kv_append", "recg_kv_rows", "recg_kv_weights", "recg_kv_select", "recg_kv_compact",
+           "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_last_error",
            "recg_timing_enable", "recg_timing_read", "recg_row_stats_static", "recg_row_stats_static_error",
            "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
            "recg_debug_map_cache_selftest", "recg_step_device", "recg_next_round")
@@ -198,6 +211,27 @@ class Batch:
             self.rows = self.rows + self.n_corr * (1 + self.corr_block)
         self.n_tok = int(self.rows.sum())
         self.n_ver = int(self.verify_len.sum())
+
+
+class Eviction:
+    """Holds the host arrays of one recg_eviction alive.  dst_page_table None: in place; layers: the range [begin, end)."""
+
+    def __init__(self, ctx_len, budget, page_table, kv_pool: Optional[torch.Tensor], kv_pool_pages: int, weights: Optional[torch.Tensor],
+                 n_sink: int = 0, n_recent: int = 0, dst_page_table=None, layers=(0, 1)):
+        self.ctx_len, self.budget, self.page_table = _i32(ctx_len), _i32(budget), _i32(page_table)
+        self.dst_page_table = None if dst_page_table is None else _i32(dst_page_table)
+        n = len(self.ctx_len)
+        for name, a, ndim in (("budget", self.budget, 1), ("page_table", self.page_table, 2), ("dst_page_table", self.dst_page_table, 2)):
+            if a is not None and (a.ndim != ndim or len(a) != n):
+                raise ValueError(f"{name} must have one entry per request")
+        if weights is not None and (weights.dtype != torch.float32 or not weights.is_cuda or not weights.is_contiguous()):
+            raise ValueError("weights must be contiguous CUDA float32")
+        self.kv_pool, self.weights, self.layers = kv_pool, weights, (int(layers[0]), int(layers[1]))
+        self.kept = np.minimum(self.ctx_len, self.budget)              # the requests' new ctx_len
+        self.c = recg_eviction(n, n_sink, n_recent, _ptr(self.ctx_len), _ptr(self.budget), _ptr(self.page_table),
+                               int(self.page_table.shape[1]), _ptr(self.dst_page_table),
+                               0 if dst_page_table is None else int(self.dst_page_table.shape[1]), _ptr(kv_pool), int(kv_pool_pages),
+                               _ptr(weights), *self.layers)
 
 
 class DeviceBatch:
@@ -270,7 +304,7 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("recg needs a CUDA device (there is no CPU fallback)")
         self.cfg = cfg
-        self._last_rows = 0
+        self._last_rows = self._last_pages = 0
         self._keep = weights
         self.h = C.c_void_p()
         wptr = None
@@ -364,7 +398,7 @@ class Context:
     def _n_tok(self, batch: Optional[Batch]) -> int:
         """Rows of the batch, or of the one that an operation was given last."""
         if batch is not None:
-            self._last_rows = batch.n_tok
+            self._last_rows, self._last_pages = batch.n_tok, int(batch.c.kv_pool_pages)
         return self._last_rows
 
     def recg_kv_append(self, batch: Optional[Batch], layer: int, k: torch.Tensor, v: torch.Tensor):
@@ -380,6 +414,44 @@ class Context:
         b, kp, vp, stride = self._kv_rows_args(batch, k, v)
         self._check(lib().recg_kv_rows(self.h, b, layer, kp, vp, stride))
         return k, v
+
+    def _floats(self, name: str, t: Optional[torch.Tensor], n: Optional[int] = None):
+        if t is None:
+            return None
+        if t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n):
+            raise ValueError(f"{name} must be contiguous CUDA float32" + (f" of {n} elements" if n is not None else ""))
+        return t.data_ptr()
+
+    def recg_kv_weights(self, batch: Optional[Batch], layer: int, q: torch.Tensor, lse: torch.Tensor,
+                        weights_in: Optional[torch.Tensor], weights_out: torch.Tensor, row_weight: Optional[torch.Tensor] = None,
+                        decay: float = 1.0):
+        """Attention weight gathered by the cached tokens; weights [n_layers, pages, n_kv_heads, 16] float32 (in and out may be one array)."""
+        n = self._n_tok(batch)
+        if q.dtype != torch.bfloat16 or not q.is_cuda or not q.is_contiguous() or q.numel() != n * self.cfg.n_q_heads * self.cfg.head_dim:
+            raise ValueError(f"q must be contiguous CUDA bf16 [{n}, {self.cfg.n_q_heads}, {self.cfg.head_dim}]")
+        if weights_in is not None and weights_in.numel() != weights_out.numel():
+            raise ValueError("weights_in and weights_out must have one shape")
+        if self._last_pages and weights_out.numel() != self.cfg.n_layers * self._last_pages * self.cfg.n_kv_heads * 16:
+            raise ValueError("weights must be [n_layers, pages of the pool, n_kv_heads, 16]")
+        self._check(lib().recg_kv_weights(self.h, C.byref(batch.c) if batch is not None else None, layer, q.data_ptr(),
+                                          self._floats("lse", lse, n * self.cfg.n_q_heads), self._floats("row_weight", row_weight, n),
+                                          float(decay), self._floats("weights_in", weights_in), self._floats("weights_out", weights_out)))
+
+    def _keep_args(self, ev: Eviction, keep: torch.Tensor):
+        want = (ev.layers[1] - ev.layers[0], ev.c.n_req, self.cfg.n_kv_heads)
+        if keep.dtype != torch.int32 or not keep.is_cuda or not keep.is_contiguous() or keep.ndim != 4 or keep.shape[:3] != want:
+            raise ValueError(f"keep must be contiguous CUDA int32 {list(want)} + [positions]")
+        if ev.weights is not None and ev.weights.numel() != self.cfg.n_layers * int(ev.c.kv_pool_pages) * self.cfg.n_kv_heads * 16:
+            raise ValueError("weights must be [n_layers, pages of the pool, n_kv_heads, 16]")
+        return C.byref(ev.c), keep.data_ptr(), keep.shape[3]
+
+    def recg_kv_select(self, ev: Eviction, keep: torch.Tensor):
+        """keep int32 [layers, n_req, n_kv_heads, positions] receives what stays, in ascending order, -1 behind the last."""
+        self._check(lib().recg_kv_select(self.h, *self._keep_args(ev, keep)))
+
+    def recg_kv_compact(self, ev: Eviction, keep: torch.Tensor):
+        """Moves K, V and weights of the positions in keep to the front of the request's pages, or to the destination pages."""
+        self._check(lib().recg_kv_compact(self.h, *self._keep_args(ev, keep)))
 
     def recg_linear(self, x: torch.Tensor, w: torch.Tensor, out_dtype=torch.float32) -> torch.Tensor:
         M, K = x.shape
@@ -417,7 +489,7 @@ class Context:
 
     def recg_step_device(self, batch: "DeviceBatch"):
         lg = recg_logits()
-        self._last_rows = self.cfg.max_tokens
+        self._last_rows, self._last_pages = self.cfg.max_tokens, int(batch.c.kv_pool_pages)
         self._check(lib().recg_step_device(self.h, C.byref(batch.c), C.byref(lg)))
         return lg
 

@@ -268,4 +268,22 @@ void launch_kv4_io(bool write, void* pool, int64_t n_pages, int layer, const Dim
 void launch_kv_rows(bool write, bool four, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, void* k,
                     void* v, int64_t row_stride, cudaStream_t st);
 
+// Attention weight gathered by the cached tokens of the batch laid out last; row_weight and in may be null
+void launch_kv_weights(const BatchLayout& bl, const Dims& dm, int layer, const void* q, const float* lse, const float* row_weight,
+                       float decay, const float* in, float* out, const void* pool, int64_t n_pages, bool four, int n_sm, int* status,
+                       cudaStream_t st);
+
+// Eviction: arrays on the device, written by the API from the caller's host arrays
+struct EvictDesc {
+  int n_req, n_sink, n_recent, layer_begin, pt_stride, dst_stride, splits;
+  const int* ctx_len;      // [n_req]
+  const int* kept;         // [n_req] min(ctx_len, budget)
+  const int* page_table;   // [n_req][pt_stride]
+  const int* dst_table;    // [n_req][dst_stride], or null: in place
+};
+void launch_kv_select(const EvictDesc& E, const float* weights, int64_t n_pages, int n_kv, int n_layers, int* keep, int keep_stride,
+                      cudaStream_t st);
+void launch_kv_compact(EvictDesc E, const Dims& dm, void* pool, float* weights, int64_t n_pages, bool four, int n_layers, int max_keep,
+                       const int* keep, int keep_stride, int* status, cudaStream_t st);
+
 }  // namespace recg

@@ -1,4 +1,5 @@
 // The C ABI: context, workspace, descriptor validation and the per-step launch sequence.
+#include <algorithm>
 #include <cstdio>
 #include <cstring>
 #include <string>
@@ -93,6 +94,10 @@ struct recg_ctx {
   std::vector<int> h_rows;
   SmallDesc small_desc{};        // the descriptor laid out last, where it is small enough to travel with the launches (n > 0)
   std::vector<int> h_page_owner;   // debug checks: which request names a page
+  int* d_evict = nullptr;          // eviction: the descriptor uploaded last, and on the host
+  std::vector<int> h_evict;
+  std::vector<int> h_page_seen;    // eviction: per page the call (times two, plus one where it is a destination) that named it last
+  int evict_calls = 0;
   // optional per-class timing
   bool timing = false;
   std::vector<cudaEvent_t> ev_pool;
@@ -149,6 +154,7 @@ size_t carve(recg_ctx* c, DeviceArena& A) {
   bl.tiles = A.take<AttnTile>(max_tiles);
   bl.cta_off = A.take<int>(4 * (c->target_items + 1));
   bl.counts = A.take<int>(4);
+  c->d_evict = A.take<int>(2 * Cm + 2 * Cm * Pm);
   c->d_status = A.take<int>(1);
   c->d_dyn = A.take<int>(4);
   c->d_policy = A.take<int>(8 + 8 + 64 + RECG_POLICY_MAX_BLOCKS * RECG_POLICY_MAX_BINS * RECG_POLICY_MAX_BLOCKS * 2);
@@ -989,7 +995,7 @@ static recg_status kv_rows(recg_ctx* ctx, bool write, const recg_batch* batch, i
   if (!ctx || !k || !v) return RECG_ERR_INVALID_ARG;
   const int64_t width = (int64_t)ctx->dm.n_kv * ctx->dm.head_dim;
   if (row_stride == 0) row_stride = width;
-  if (row_stride < width || row_stride % 8 || !aligned16(k, v))
+  if (row_stride < width || row_stride > INT32_MAX || row_stride % 8 || !aligned16(k, v))
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": rows must be 16-byte aligned and at least n_kv_heads * head_dim elements apart");
   recg_status s = operation_batch(ctx, batch, layer, who);
   if (s != RECG_OK) return s;
@@ -1002,6 +1008,122 @@ recg_status recg_kv_append(recg_ctx* ctx, const recg_batch* batch, int32_t layer
 }
 recg_status recg_kv_rows(recg_ctx* ctx, const recg_batch* batch, int32_t layer, void* k, void* v, int64_t row_stride) {
   return kv_rows(ctx, false, batch, layer, k, v, row_stride, "recg_kv_rows");
+}
+
+recg_status recg_kv_weights(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, const float* lse,
+                            const float* row_weight, float decay, const float* weights_in, float* weights_out) {
+  if (!ctx || !q || !lse || !weights_out) return RECG_ERR_INVALID_ARG;
+  if (!(decay >= 0.f && decay <= 3e38f)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: decay must be a finite number >= 0");
+  if (!aligned16(q, q)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: q must be 16-byte aligned");
+  recg_status s = operation_batch(ctx, batch, layer, "recg_kv_weights");
+  if (s != RECG_OK) return s;
+  if (!aligned16(ctx->last_pool, ctx->last_pool)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: the KV pool must be 16-byte aligned");
+  launch_kv_weights(ctx->bl, ctx->dm, layer, q, lse, row_weight, decay, weights_in, weights_out, ctx->last_pool, ctx->last_pool_pages,
+                    four_bits(ctx), ctx->n_sm, ctx->d_status, ctx->stream);
+  CU(cudaGetLastError());
+  return RECG_OK;
+}
+
+// Validates an eviction and leaves its descriptor [ctx_len | kept | page table | destination table] on the device.
+static recg_status evict_batch(recg_ctx* ctx, const recg_eviction* e, int32_t keep_stride, bool moves, const char* who, EvictDesc* out,
+                               int* max_keep) {
+  const std::string name(who);
+  if (!e || e->n_req <= 0 || !e->ctx_len || !e->budget || !e->page_table || e->kv_pool_pages <= 0)
+    return fail(ctx, RECG_ERR_INVALID_ARG, name + ": null array, n_req <= 0 or no pages");
+  const int C = e->n_req;
+  if (C > ctx->cfg.max_requests) return fail(ctx, RECG_ERR_CAPACITY, name + ": n_req exceeds max_requests");
+  if (e->layer_begin < 0 || e->layer_end <= e->layer_begin || e->layer_end > (ctx->cfg.n_layers > 0 ? ctx->cfg.n_layers : 1) ||
+      e->layer_end - e->layer_begin > 65535)
+    return fail(ctx, RECG_ERR_INVALID_ARG, name + ": layer range");
+  if (e->n_sink < 0 || e->n_recent < 0) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": negative n_sink or n_recent");
+  const bool other = e->dst_page_table != nullptr;
+  if (e->page_table_stride <= 0 || e->page_table_stride > ctx->cfg.max_pages_per_request ||
+      (other && (e->dst_stride <= 0 || e->dst_stride > ctx->cfg.max_pages_per_request)))
+    return fail(ctx, RECG_ERR_CAPACITY, name + ": page table stride exceeds max_pages_per_request");
+  if (moves && (reinterpret_cast<uintptr_t>(e->kv_pool) & 15 || !e->kv_pool))
+    return fail(ctx, RECG_ERR_INVALID_ARG, name + ": the KV pool is null or not 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(e->weights) & 15) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": weights must be 16-byte aligned");
+  std::vector<int> d(2 * (size_t)C + (size_t)C * (e->page_table_stride + (other ? e->dst_stride : 0)));
+  if (moves) {
+    if (ctx->h_page_seen.size() < (size_t)e->kv_pool_pages) ctx->h_page_seen.resize((size_t)e->kv_pool_pages, 0);
+    if (++ctx->evict_calls > 0x3ffffff0) {
+      ctx->evict_calls = 1;
+      std::fill(ctx->h_page_seen.begin(), ctx->h_page_seen.end(), 0);
+    }
+  }
+  *max_keep = 0;
+  for (int r = 0; r < C; ++r) {
+    const int L = e->ctx_len[r], b = e->budget[r];
+    if (L < 0 || b < 0) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": negative ctx_len or budget");
+    if (L > b && (long long)e->n_sink + e->n_recent > b)
+      return fail(ctx, RECG_ERR_INVALID_ARG, name + ": a budget below n_sink + n_recent");
+    const int kept = L < b ? L : b;
+    if (kept > *max_keep) *max_keep = kept;
+    const long long need = ((long long)L + kPageSize - 1) / kPageSize, dst_need = (kept + kPageSize - 1) / kPageSize;
+    if (need > e->page_table_stride || (other && dst_need > e->dst_stride))
+      return fail(ctx, RECG_ERR_CAPACITY, name + ": a page table row does not cover its positions");
+    d[r] = L;
+    d[C + r] = kept;
+    int* pt = d.data() + 2 * (size_t)C + (size_t)r * e->page_table_stride;
+    for (int i = 0; i < e->page_table_stride; ++i) {
+      pt[i] = e->page_table[(size_t)r * e->page_table_stride + i];
+      if (i >= need) continue;
+      if (pt[i] < 0 || pt[i] >= e->kv_pool_pages) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": page id outside the pool");
+      if (!moves) continue;
+      int& seen = ctx->h_page_seen[pt[i]];
+      // (requests may share source pages where nothing is written to them)
+      if (!other && seen >> 1 == ctx->evict_calls) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": in place, a page is named twice");
+      seen = ctx->evict_calls << 1;
+    }
+  }
+  if (other)
+    for (int r = 0; r < C; ++r) {
+      int* pt = d.data() + 2 * (size_t)C + (size_t)C * e->page_table_stride + (size_t)r * e->dst_stride;
+      for (int i = 0; i < e->dst_stride; ++i) {
+        pt[i] = e->dst_page_table[(size_t)r * e->dst_stride + i];
+        if (i >= (d[C + r] + kPageSize - 1) / kPageSize) continue;
+        if (pt[i] < 0 || pt[i] >= e->kv_pool_pages) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": page id outside the pool");
+        if (!moves) continue;
+        int& seen = ctx->h_page_seen[pt[i]];
+        if (seen >> 1 == ctx->evict_calls) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": a destination page is named twice or is a source");
+        seen = ctx->evict_calls << 1;
+      }
+    }
+  if (keep_stride < *max_keep || keep_stride <= 0) return fail(ctx, RECG_ERR_CAPACITY, name + ": keep_stride is below the positions that stay");
+  cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+  CU(cudaStreamIsCapturing(ctx->stream, &cap));
+  if (cap != cudaStreamCaptureStatusNone) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": not while the stream is being captured");
+  if (d != ctx->h_evict) {            // (a selection and its move come with the same descriptor)
+    ctx->h_evict.clear();
+    CU(cudaMemcpyAsync(ctx->d_evict, d.data(), d.size() * sizeof(int), cudaMemcpyHostToDevice, ctx->stream));
+    ctx->h_evict.swap(d);
+  }
+  const int* at = ctx->d_evict;
+  *out = EvictDesc{C, e->n_sink, e->n_recent, e->layer_begin, e->page_table_stride, other ? e->dst_stride : 0, 1, at, at + C, at + 2 * C,
+                   other ? at + 2 * C + (size_t)C * e->page_table_stride : nullptr};
+  return RECG_OK;
+}
+recg_status recg_kv_select(recg_ctx* ctx, const recg_eviction* e, int32_t* keep, int32_t keep_stride) {
+  if (!ctx || !keep) return RECG_ERR_INVALID_ARG;
+  if (e && !e->weights) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_select: weights is null");
+  EvictDesc E;
+  int max_keep = 0;
+  recg_status s = evict_batch(ctx, e, keep_stride, false, "recg_kv_select", &E, &max_keep);
+  if (s != RECG_OK) return s;
+  launch_kv_select(E, e->weights, e->kv_pool_pages, ctx->dm.n_kv, e->layer_end - e->layer_begin, keep, keep_stride, ctx->stream);
+  CU(cudaGetLastError());
+  return RECG_OK;
+}
+recg_status recg_kv_compact(recg_ctx* ctx, const recg_eviction* e, const int32_t* keep, int32_t keep_stride) {
+  if (!ctx || !keep) return RECG_ERR_INVALID_ARG;
+  EvictDesc E;
+  int max_keep = 0;
+  recg_status s = evict_batch(ctx, e, keep_stride, true, "recg_kv_compact", &E, &max_keep);
+  if (s != RECG_OK) return s;
+  launch_kv_compact(E, ctx->dm, e->kv_pool, e->weights, e->kv_pool_pages, four_bits(ctx), e->layer_end - e->layer_begin, max_keep, keep,
+                    keep_stride, ctx->d_status, ctx->stream);
+  CU(cudaGetLastError());
+  return RECG_OK;
 }
 
 recg_status recg_linear(recg_ctx* ctx, const void* x, const void* w, void* y, int32_t M, int32_t N, int32_t K,

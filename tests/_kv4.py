@@ -81,3 +81,22 @@ def attention_bounds(q, k_codes, v_codes, see):
         o_err[:, h] = 2.0 ** -8 * coded + (2.0 ** -17 + 4 * score)[:, None] * (coded + rest)
         lse_err[:, h] = score + 2.0 ** -20 * (1 + np.abs(top[:, 0]) + math.log(see.shape[1]))
     return o_err, lse_err
+
+
+def gathered(q, k, see, lse, row_weight):
+    """Weight that every position receives, [nkv, L], and how far kernels may be from it: a probability is 2^(score - lse) with both
+    in fp32 (a score's sum: see attention_bounds), and at most n * group of them are added up."""
+    n, nq, d = q.shape
+    nkv = k.shape[1]
+    g = nq // nkv
+    out, err = np.zeros((nkv, k.shape[0])), np.zeros((nkv, k.shape[0]))
+    for h in range(nq):
+        with np.errstate(all="ignore"):
+            z = q[:, h] @ k[:, h // g].T / math.sqrt(d)
+            size = np.abs(q[:, h]) @ np.abs(k[:, h // g]).T / math.sqrt(d)
+            use = see & (row_weight != 0)[:, None]
+            p = np.where(use, np.exp(z - lse[:, h:h + 1]) * row_weight[:, None], 0.0)
+            rel = np.where(use, 3 * size * 2.0 ** -19 + 2.0 ** -20 * (1 + np.abs(z) + np.abs(lse[:, h:h + 1])), 0.0)
+        out[h // g] += p.sum(0)
+        err[h // g] += (np.abs(p) * (rel + n * g * 2.0 ** -23)).sum(0)
+    return out, err
