@@ -226,6 +226,9 @@ void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, 
 // the same over a pool in 4 bits
 void launch_attention_kv4(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
                           int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status, cudaStream_t st);
+// ... on the tcgen05 tensor cores (head_dim 128); false: not launched (no tensor map over q)
+bool launch_attention_kv4_tc(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
+                             int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status, cudaStream_t st);
 size_t attention_smem_bytes(int head_dim);
 
 // S9b + S10
