@@ -1,22 +1,31 @@
 // Hybrid-mask paged attention over a pool in 4 bits on the 5th-generation tensor cores (head_dim 128, many query rows per kv head).
 //
-// Work items, masks and the combine kernel are those of attention_tc.cu, the mathematics are those of attention_kv4.cu: the tensor
-// cores multiply codes (c - 8 as bf16, exact), steps and minima enter in fp32 beside the softmax,
-//   score = s_K (q . (c_K - 8)) + (m_K + 8 s_K) sum(q),    o = sum_j (p_j s_Vj) (c_Vj - 8) + sum_j p_j (m_Vj + 8 s_Vj).
-// Values with their steps applied would have to be rounded to bf16 before the products, K and V both: an error of 3.2e-3 against
-// 2.3e-3 for scores of unit variance, and a log-sum-exp that is good to 1e-4 only.
+// Work items, masks and the combine kernel are those of attention_tc.cu.  The operands are fp16: with x = m + s c (kv4.cuh) a product
+// s (c - 8) of an 8-bit step and a code has 11 significant bits, which is what fp16 holds, and so have q and m.  Hence
+//   score = q . (s_K (c_K - 8))  +  (m_K + 8 s_K) sum(q)
+// is exact up to fp32 sums: the second term is one more step of 16 of the contraction, in which both factors stand as sums of
+// two fp16 numbers.  (K as m + s c rounded to 16 bits would leave the log-sum-exp of a few tokens good to 1e-4 only; steps applied
+// in fp32 behind the product have to be broadcast to every row's thread, and that alone took more of the shared memory's
+// bandwidth than all operands: 325 us instead of %SELF% for 1001 rows over 6000 tokens of 40 / 8 heads.)  V stands as m + s c
+// rounded once, and P as fp16 too: 2^-12 of each term, a sixteenth of the rounding of the result.
+//
+// Range.  fp16 has five bits of exponent, so everything is scaled by powers of two: a query row by its own largest value, K and V
+// of 32 tokens by theirs, in steps of 2^8.  The scale of a row of Q and of 32 tokens of K is one factor of the score.  The scale of V
+// joins the exponent of the probabilities, relative to the largest one so far (O is rescaled when that grows).  Values next to others
+// that are 2^25 times as large lose bits, as in any fp32 sum of both.
 //
 // Per CTA (16 warps = 4 warpgroups, one CTA per SM, persistent over the work list), stages of 128 tokens:
 //   warp 0     streams the blocks of the pool (codes and pairs of a page and head: one bulk copy) into a ring of two raw stages, and
 //              the item's Q rows by TMA
-//   warps 4-7  turn a raw stage into the operands: K (K-major) and V (MN-major), 16 tokens x 128 values in 128-byte-swizzled atoms as
-//              the tensor core reads them, and the steps and minima as fp32 pairs.  Every lane turns words of eight codes into
-//              16-byte stores; words of a lane are taken in an order in which no two lanes of a store meet a bank.
-//   warp 1     one elected lane issues S = Q C_K^T (two stages ahead) and per softmax group O_g += P_g C_V (P from TMEM)
+//   warps 4-7  turn a raw stage into the operands, 32 tokens a warp: K (K-major) and V (MN-major), 16 tokens x 128 values in 128-byte-
+//              swizzled atoms as the tensor core reads them; and the rows of Q, one a thread.  Every lane turns words of eight
+//              codes into 16-byte stores; the words of a lane are taken in an order in which no two lanes of a store meet a bank.
+//   warp 1     one elected lane issues S = Q K^T (two stages ahead) and per softmax group O_g += P_g V_g (P from TMEM)
 //   warps 8-11 and 12-15  two softmax groups: group g takes tokens [64 g, 64 g + 64) of every stage, one thread one query row, its
-//              own O accumulator and running (reference maximum, sum, sum of p m); merged at the end of an item.
+//              own O accumulator and running (reference maximum, sum); merged at the end of an item.
 // The registers are moved to the softmax warps: 4 x (88 + 88 + 168 + 168) x 32 = 16 x 128 x 32 of the launch.
 // Every wait is bounded; a wait that runs out raises a CTA-wide flag after which no wait blocks, so the kernel always ends.
+#include <cuda_fp16.h>
 #include <cstdio>
 
 #include "attention_tc.cuh"
@@ -34,24 +43,28 @@ constexpr int kBlock = kv4_block_bytes(D);       // 2176
 constexpr int kRawBytes = kPages * kBlock;
 constexpr int kOperand = kBT * D * 2;            // 32 KB: K or V of a stage, or Q
 constexpr int kRaw = 2, kRing = 2;               // raw stages; stages of K and of V operands
-constexpr int kParams = 4;                       // stages of steps and minima (see the writer)
-constexpr int kParamBytes = (kBT / 2) * 32;      // per token pair {s_K, s_K', m_K, m_K'} and {s_V, s_V', m_V, m_V'}
+constexpr int kInfo = 4;                         // stages of what the softmax needs to know of 32 tokens (see the writer)
+constexpr int kExt = 128 * 32;                   // the 16 further values of the contraction: 128 rows x 32 bytes, not swizzled
 constexpr int kThreads = 512;
 constexpr uint32_t kSpin = 1u << 22;
 constexpr int kTmemCols = 512;                   // two S buffers of 128 columns; O of group g at 256 + 128 g
 constexpr int kTmemO = 2 * kBT;
-constexpr float kNoRef = -1e30f;
-constexpr float kHeadroom = 8.f;
+constexpr float kNoRef = -1e30f;       // reference maximum of a row that has seen no token yet
+constexpr float kHeadroom = 8.f;       // a row's reference maximum moves when it is outgrown by more than 2^8
+constexpr float kLift = 7.f;           // probabilities stand as 2^7 p: at most 2^15, and 2^-31 of the reference is not lost yet
 
 constexpr int kOffQ = 0;
 constexpr int kOffK = kOffQ + kOperand;
 constexpr int kOffV = kOffK + kRing * kOperand;
-constexpr int kOffRaw = kOffV + kRing * kOperand;
-constexpr int kOffParam = kOffRaw + kRaw * kRawBytes;
-constexpr int kOffScratch = kOffParam + kParams * kParamBytes;     // 2 KB per softmax warp: partial rows on their way out
-constexpr int kOffML = kOffScratch + 8 * 2048;                     // float4 [2 groups][128 rows]: reference, sum, sum of p m
-constexpr int kOffBar = kOffML + 2 * 128 * 16;
-constexpr int kNumBars = 2 * kRaw + 4 * kRing + 2 + 2 + 4 + 3;
+constexpr int kOffQExt = kOffV + kRing * kOperand;
+constexpr int kOffKExt = kOffQExt + kExt;
+constexpr int kOffRaw = kOffKExt + kRing * kExt;
+constexpr int kOffScratch = kOffRaw + kRaw * kRawBytes;            // 2 KB per softmax warp: partial rows on their way out
+constexpr int kOffML = kOffScratch + 8 * 2048;                     // per row, both groups: reference; sum; scale of O
+constexpr int kOffQF = kOffML + 3 * 2 * 128 * 4;                   // per row: the factor of its scores
+constexpr int kOffInfo = kOffQF + 128 * 4;                         // TokenInfo [kInfo][4]
+constexpr int kOffBar = kOffInfo + kInfo * 4 * 16;
+constexpr int kNumBars = 2 * kRaw + 4 * kRing + 3 + 2 + 4 + 3;
 constexpr int kSmemBytes = kOffBar + kNumBars * 8 + 16;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
 
@@ -79,13 +92,52 @@ template <int N>
 __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-__device__ __forceinline__ float2 mul2(const float2& a, const float2& b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
-  return reinterpret_cast<float2&>(d);
+
+constexpr uint32_t kIdescF16QK = kIdescQK & ~((1u << 7) | (1u << 10));      // fp16 operands
+constexpr uint32_t kIdescF16PV = kIdescPV & ~((1u << 7) | (1u << 10));
+// K-major operand of 16 values per row without swizzle: 8 rows x 16 bytes make a core matrix, the second one 128 bytes behind the
+// first, the next 8 rows 256 bytes
+__device__ __forceinline__ uint64_t desc_ext(uint32_t addr) {
+  return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46);
 }
-// eight values c - 8 as four bf16 pairs
-__device__ __forceinline__ uint4 word_values(uint32_t w) { return make_uint4(kv4_pair(w, 0), kv4_pair(w, 1), kv4_pair(w, 2), kv4_pair(w, 3)); }
+__device__ __forceinline__ int ext_row(int row) { return (row >> 3) * 256 + (row & 7) * 16; }
+
+struct TokenInfo {       // of 32 tokens
+  float k_scale;         // K stands scaled by 1 / k_scale
+  int v_exp;             // V stands scaled by 2^-v_exp
+  uint32_t v_bad;        // tokens whose V is not finite: it stands as zero, and a row that sees one of them is NaN
+  int pad;
+};
+
+// Multiples of eight E with 2^-E v in [1, 2^8) for the v whose exponent field is `field` (clamped where a factor 2^E or 2^-E would
+// not be a normal number, or products of two not)
+__device__ __forceinline__ int scale_exp(int field) { return max(-56, min(120, ((field - 127) >> 3) << 3)); }
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
+__device__ __forceinline__ uint32_t h2_bits(const __half2& h) { return reinterpret_cast<const uint32_t&>(h); }
+__device__ __forceinline__ __half2 bits_h2(uint32_t u) { return reinterpret_cast<const __half2&>(u); }
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
+// the pairs of a word of codes as fp16 c + off: 1024 + c is 0x6400 | c, 1024 + 16 c is 0x6400 | (c << 4)
+template <int OFF>
+__device__ __forceinline__ void word_codes(uint32_t w, __half2 (&x)[4]) {
+  const __half2 a = __half2half2(__float2half_rn((float)(OFF - 1024))), b = __half2half2(__float2half_rn((float)(OFF - 64))),
+                sixteenth = __half2half2(__float2half_rn(0.0625f));
+  const uint32_t v = w >> 8;
+  x[0] = __hadd2(bits_h2((w & 0x000f000fu) | 0x64006400u), a);
+  x[1] = __hfma2(bits_h2((w & 0x00f000f0u) | 0x64006400u), sixteenth, b);
+  x[2] = __hadd2(bits_h2((v & 0x000f000fu) | 0x64006400u), a);
+  x[3] = __hfma2(bits_h2((v & 0x00f000f0u) | 0x64006400u), sixteenth, b);
+}
+// s (c - 8), exact; m + s c, rounded once
+__device__ __forceinline__ uint4 k_values(uint32_t w, const __half2& s) {
+  __half2 x[4];
+  word_codes<-8>(w, x);
+  return make_uint4(h2_bits(__hmul2(x[0], s)), h2_bits(__hmul2(x[1], s)), h2_bits(__hmul2(x[2], s)), h2_bits(__hmul2(x[3], s)));
+}
+__device__ __forceinline__ uint4 v_values(uint32_t w, const __half2& s, const __half2& m) {
+  __half2 x[4];
+  word_codes<0>(w, x);
+  return make_uint4(h2_bits(__hfma2(x[0], s, m)), h2_bits(__hfma2(x[1], s, m)), h2_bits(__hfma2(x[2], s, m)), h2_bits(__hfma2(x[3], s, m)));
+}
 
 __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __grid_constant__ CUtensorMap qmap, Params P) {
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -101,15 +153,17 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
   uint64_t* v_full = k_empty + kRing;
   uint64_t* v_empty = v_full + kRing;
   uint64_t* q_full = v_empty + kRing;            // [1]
-  uint64_t* q_empty = q_full + 1;                // [1]   the item's last S product, and the eight softmax warps (sum of the row)
-  uint64_t* s_full = q_empty + 1;                // [2]   per S buffer
+  uint64_t* q_empty = q_full + 1;                // [1]   the item's last S product, and the eight softmax warps (factor of the row)
+  uint64_t* q_ready = q_empty + 1;               // [1]   the four converting warps
+  uint64_t* s_full = q_ready + 1;                // [2]   per S buffer
   uint64_t* p_full = s_full + 2;                 // [4]   2 g + (stage & 1)
   uint64_t* pv_done = p_full + 4;
   uint64_t* o_full = pv_done + 1;
   uint64_t* o_empty = o_full + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  float4* ml_smem = reinterpret_cast<float4*>(smem + kOffML);
+  float* ml_smem = reinterpret_cast<float*>(smem + kOffML);
+  float* qf_smem = reinterpret_cast<float*>(smem + kOffQF);
   auto bwait = [&](uint64_t* bar, uint32_t parity, int code) {
     if (mbar_test_wait(bar, parity) || *abort_flag) return;
     if (!mbar_wait(bar, parity, kSpin)) {
@@ -132,6 +186,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
     }
     mbar_init(q_full, 1);
     mbar_init(q_empty, 9);
+    mbar_init(q_ready, 4);
     for (int s = 0; s < 2; ++s) mbar_init(&s_full[s], 1);
     for (int s = 0; s < 4; ++s) mbar_init(&p_full[s], 4);
     mbar_init(pv_done, 1);
@@ -140,6 +195,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
     fence_barrier_init();
     asm volatile("prefetch.tensormap [%0];" ::"l"(&qmap) : "memory");
   }
+  for (int i = threadIdx.x; i < (1 + kRing) * kExt / 16; i += kThreads)     // (12 of the 16 further values stay zero)
+    reinterpret_cast<uint4*>(smem + kOffQExt)[i] = make_uint4(0, 0, 0, 0);
+  fence_proxy_async();
   if (warp == 1) {
     tmem_alloc(tmem_slot, kTmemCols);
     tmem_relinquish();
@@ -214,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
       // ------------------------------------ MMA issuer ------------------------------------
       if (elect_one()) {
         uint32_t blk = 0;
-        const uint64_t dq0 = desc_kmajor(smem_base + kOffQ);
+        const uint64_t dq0 = desc_kmajor(smem_base + kOffQ), dq1 = desc_ext(smem_base + kOffQExt);
         for (int item = 0; item < item_end; ++item) {
           const AttnItem w = P.items[item_at(item)];
           const int nblk = stages_of(w);
@@ -226,12 +284,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
               umma_bf16(tmem_base + (b & 1) * kBT, dq0 + (uint64_t)((((kk >> 2) * (128 * 128)) + (kk & 3) * 32) >> 4),
-                        dk0 + (uint64_t)((((kk >> 2) * 1024) + (kk & 3) * 32) >> 4), kIdescQK, kk ? 1u : 0u);
+                        dk0 + (uint64_t)((((kk >> 2) * 1024) + (kk & 3) * 32) >> 4), kIdescF16QK, kk ? 1u : 0u);
+            umma_bf16(tmem_base + (b & 1) * kBT, dq1, desc_ext(smem_base + kOffKExt + s * kExt), kIdescF16QK, 1u);
             umma_commit(&s_full[b & 1]);
             umma_commit(&k_empty[s]);
             if (last) umma_commit(q_empty);
           };
-          bwait(q_full, item & 1, DEV_TIMEOUT_FULL);
+          bwait(q_ready, item & 1, DEV_TIMEOUT_FULL);
           tc_fence_after();
           issue_qk(blk, nblk == 1);
           if (nblk > 1) issue_qk(blk + 1, nblk == 2);
@@ -249,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
 #pragma unroll
               for (int kk = 0; kk < 4; ++kk)
                 umma_bf16_ts(tmem_base + kTmemO + g * D, tmem_base + (blk & 1) * kBT + g * 64 + kk * 8,
-                             dv0 + (uint64_t)(((4 * g + kk) * 4096) >> 4), kIdescPV, (n | kk) ? 1u : 0u);
+                             dv0 + (uint64_t)(((4 * g + kk) * 4096) >> 4), kIdescF16PV, (n | kk) ? 1u : 0u);
             }
             umma_commit(pv_done);
             umma_commit(&v_empty[s]);
@@ -262,62 +321,116 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
   } else if (warp < 8) {
     // ------------------------------------ codes to operands ------------------------------------
     regs_dec<88>();
-    const int tid = threadIdx.x - 128;
+    const int wq = warp - 4;                     // takes tokens [32 wq, 32 wq + 32) of every stage, and rows 32 wq .. of Q
     uint32_t blk = 0;
     for (int item = 0; item < item_end; ++item) {
       const AttnItem w = P.items[item_at(item)];
       const int nblk = stages_of(w), tok_begin = w.blk_begin * 64, tok_end = min(w.blk_end * 64, w.kv_len);
       for (int n = 0; n < nblk; ++n, ++blk) {
         const int rs = blk % kRaw, s = blk % kRing;
-        const uint8_t* raw = smem + kOffRaw + rs * kRawBytes;
+        const uint8_t* raw = smem + kOffRaw + rs * kRawBytes + 2 * wq * kBlock;
         bwait(&raw_full[rs], (blk / kRaw) & 1, DEV_TIMEOUT_FULL);
         bwait(&k_empty[s], ((blk / kRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
-        // Steps and minima: thread = token.  The ring of them is four deep: the V operands of the stage before this one went where the P V
-        // product of stage blk - 3 had read, which waited for every softmax warp to be done with stage blk - 3.
-        {
-          const uint8_t* pg = raw + (tid >> 4) * kBlock;
-          const bool there = tok_begin + n * kBT + tid < tok_end;          // what is not there counts nothing, whatever the slot holds
-          const uint32_t kp = there ? *reinterpret_cast<const uint32_t*>(pg + kv4_k_pairs(D) + 4 * (tid & 15)) : 0u;
-          const uint32_t vp = there ? *reinterpret_cast<const uint32_t*>(pg + kv4_v_pairs(D) + 4 * (tid & 15)) : 0u;
-          float* out = reinterpret_cast<float*>(smem + kOffParam + (blk % kParams) * kParamBytes) + (tid >> 1) * 8 + (tid & 1);
-          out[0] = kv4_step(kp) * P.scale_log2;
-          out[2] = fmaf(8.f, kv4_step(kp), kv4_min(kp)) * P.scale_log2;
-          out[4] = kv4_step(vp);
-          out[6] = fmaf(8.f, kv4_step(vp), kv4_min(vp));
+        // ---- steps and minima, a token a lane: what is not there, or not finite, counts nothing ----
+        const uint8_t* pg = raw + (lane >> 4) * kBlock;
+        const bool there = tok_begin + n * kBT + 32 * wq + lane < tok_end;
+        const uint32_t kp = there ? *reinterpret_cast<const uint32_t*>(pg + kv4_k_pairs(D) + 4 * (lane & 15)) : 0u;
+        uint32_t vp = there ? *reinterpret_cast<const uint32_t*>(pg + kv4_v_pairs(D) + 4 * (lane & 15)) : 0u;
+        const bool k_bad = (kp & 0x7f80u) == 0x7f80u, v_bad = (vp & 0x7f80u) == 0x7f80u;
+        if (v_bad) vp = 0;
+        const float k_mid = fmaf(8.f, kv4_step(kp), kv4_min(kp));                       // m + 8 s
+        const float k_top = k_bad ? 0.f : fmaxf(fabsf(k_mid), 8.f * kv4_step(kp));
+        const float v_top = fmaxf(fabsf(kv4_min(vp)), fabsf(fmaf(15.f, kv4_step(vp), kv4_min(vp))));
+        const int ke = scale_exp(__reduce_max_sync(0xffffffffu, __float_as_int(k_top) >> 23));
+        const int ve = scale_exp(__reduce_max_sync(0xffffffffu, __float_as_int(v_top) >> 23));
+        const float ks = pow2(-ke), vs = pow2(-ve);
+        const unsigned bad = __ballot_sync(0xffffffffu, v_bad);
+        // The ring is four stages deep: the V operands of the stage before this one went where the P V product of stage blk - 3 had
+        // read, which waited for every softmax warp to be done with stage blk - 3.
+        if (lane == 0) {
+          TokenInfo* info = reinterpret_cast<TokenInfo*>(smem + kOffInfo) + (blk % kInfo) * 4 + wq;
+          *reinterpret_cast<int4*>(info) = make_int4(__float_as_int(pow2(ke)), ve, (int)bad, 0);
         }
-        uint8_t* kdst = smem + kOffK + s * kOperand;
+        {
+          const float mid = k_mid * ks, hi = __half2float(__float2half_rn(mid));
+          const uint32_t terms = pack_f16(hi, mid - hi);                                // met by {a, a, b, b} of the row's sum a + b
+          *reinterpret_cast<uint4*>(smem + kOffKExt + s * kExt + ext_row(32 * wq + lane)) = make_uint4(terms, terms, 0, 0);
+        }
+        const uint32_t k_step = pack_f16(kv4_step(kp) * ks, kv4_step(kp) * ks);
+        const uint32_t v_pair = pack_f16(kv4_step(vp) * vs, kv4_min(vp) * vs);
+        uint8_t* kdst = smem + kOffK + s * kOperand + wq * 8192;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           // unit: 16 bytes = values [32 q, 32 q + 32) of a token; atom (token group, q >> 1), chunks (q & 1) * 4 + word
-          const int i = u * 128 + tid, tok = i >> 2, q = i & 3;
+          const int tok = u * 8 + (lane >> 2), q = lane & 3;
+          const __half2 step = bits_h2(__shfl_sync(0xffffffffu, k_step, tok));
           uint4 v = *reinterpret_cast<const uint4*>(raw + (tok >> 4) * kBlock + (tok & 15) * (D / 2) + q * 16);
           if (q & 2) v = make_uint4(v.z, v.w, v.x, v.y);
           const uint32_t word[4] = {v.x, v.y, v.z, v.w};
           uint8_t* row = kdst + (tok >> 3) * 2048 + (q >> 1) * 1024 + (tok & 7) * 128;
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            *reinterpret_cast<uint4*>(row + ((((q & 1) * 4 + (x ^ (q & 2))) ^ (tok & 7)) << 4)) = word_values(word[x]);
+            *reinterpret_cast<uint4*>(row + ((((q & 1) * 4 + (x ^ (q & 2))) ^ (tok & 7)) << 4)) = k_values(word[x], step);
         }
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&k_full[s]);
+        if (n == 0) {
+          // ---- Q: one row a thread, scaled by its largest value, in place; its sum; the factor of its scores ----
+          const int row = 32 * wq + lane;
+          uint8_t* qrow = smem + kOffQ + row * 128;
+          bwait(q_full, item & 1, DEV_TIMEOUT_FULL);
+          uint32_t top = 0;
+          float sum = 0.f;
+#pragma unroll 4
+          for (int c = 0; c < 16; ++c) {
+            const uint4 v = *reinterpret_cast<const uint4*>(qrow + (c >> 3) * (kOperand / 2) + (((c & 7) ^ (row & 7)) << 4));
+            const uint32_t e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              top = max(top, max(e[i] & 0x7fffu, (e[i] >> 16) & 0x7fffu));
+              sum += __uint_as_float(e[i] << 16) + __uint_as_float(e[i] & 0xffff0000u);
+            }
+          }
+          const int qe = scale_exp((int)(top >> 7));
+          const float qs = pow2(-qe);
+#pragma unroll 4
+          for (int c = 0; c < 16; ++c) {
+            uint4* at = reinterpret_cast<uint4*>(qrow + (c >> 3) * (kOperand / 2) + (((c & 7) ^ (row & 7)) << 4));
+            uint4 v = *at;
+            v.x = pack_f16(__uint_as_float(v.x << 16) * qs, __uint_as_float(v.x & 0xffff0000u) * qs);
+            v.y = pack_f16(__uint_as_float(v.y << 16) * qs, __uint_as_float(v.y & 0xffff0000u) * qs);
+            v.z = pack_f16(__uint_as_float(v.z << 16) * qs, __uint_as_float(v.z & 0xffff0000u) * qs);
+            v.w = pack_f16(__uint_as_float(v.w << 16) * qs, __uint_as_float(v.w & 0xffff0000u) * qs);
+            *at = v;
+          }
+          sum *= qs;
+          const float hi = __half2float(__float2half_rn(sum)), lo = sum - hi;
+          *reinterpret_cast<uint4*>(smem + kOffQExt + ext_row(row)) = make_uint4(pack_f16(hi, hi), pack_f16(lo, lo), 0, 0);
+          qf_smem[row] = P.scale_log2 * pow2(qe);
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(q_ready);
+        }
         bwait(&v_empty[s], ((blk / kRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
-        uint8_t* vdst = smem + kOffV + s * kOperand;
+        uint8_t* vdst = smem + kOffV + s * kOperand + wq * 8192;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           // unit: 16 bytes = values [16 g, 16 g + 16) of a token pair, chunks 2 g and 2 g + 1 of both tokens
-          const int i = u * 128 + tid, pair = i >> 3, g = i & 7;
+          const int pair = u * 4 + (lane >> 3), g = lane & 7;
           uint4 v = *reinterpret_cast<const uint4*>(raw + (pair >> 3) * kBlock + kv4_v_codes(D) + (pair & 7) * D + g * 16);
           if (g & 4) v = make_uint4(v.z, v.w, v.x, v.y);
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int tok = 2 * pair + e;
+            const __half2 sm = bits_h2(__shfl_sync(0xffffffffu, v_pair, tok));
+            const __half2 step = __low2half2(sm), low = __high2half2(sm);
             uint8_t* row = vdst + (tok >> 3) * 2048 + (g >> 2) * 1024 + (tok & 7) * 128;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const uint32_t a = x ? v.z : v.x, b = x ? v.w : v.y;
               *reinterpret_cast<uint4*>(row + (((2 * (g & 3) + (x ^ (g >> 2))) ^ (tok & 7)) << 4)) =
-                  word_values(e ? __byte_perm(a, b, 0x7632) : __byte_perm(a, b, 0x5410));
+                  v_values(e ? __byte_perm(a, b, 0x7632) : __byte_perm(a, b, 0x5410), step, low);
             }
           }
         }
@@ -350,137 +463,111 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
         vlo = P.tok_lo[t];
         vhi = P.tok_hi[t];
       }
-      // the sum of the row's query values
-      float qsum = 0.f;
-      bwait(q_full, item & 1, DEV_TIMEOUT_FULL);
-      if (rvalid) {
-#pragma unroll 4
-        for (int c = 0; c < 16; ++c) {
-          const uint4 v = *reinterpret_cast<const uint4*>(smem + kOffQ + (c >> 3) * (kOperand / 2) + row * 128 + (((c & 7) ^ (row & 7)) << 4));
-          const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) qsum += __uint_as_float(u[i] << 16) + __uint_as_float(u[i] & 0xffff0000u);
-        }
-      }
+      bwait(q_ready, item & 1, DEV_TIMEOUT_FULL);
+      const float qf = qf_smem[row];               // (a row that does not exist: whatever)
       __syncwarp();
       if (lane == 0) mbar_arrive(q_empty);
-      float m_ref = rvalid ? kNoRef : 0.f, l_run = 0.f, om_run = 0.f;
+      // Reference maximum (powers of two, a whole number: adding exponents to it is exact) and sum of the row; and the scale of O, which
+      // all of a group's rows share.
+      float m_ref = rvalid ? kNoRef : 0.f, l_run = 0.f;
+      int o_exp = -1000;
 
       for (int n = 0; n < nblk; ++n, ++cs) {
         const uint32_t s_buf = s_addr + (cs & 1) * kBT;
         bwait(&s_full[cs & 1], (cs >> 1) & 1, DEV_TIMEOUT_MMA);
         tc_fence_after();
         const int pos0 = tok_begin + n * kBT + g * 64;
-        const float4* param = reinterpret_cast<const float4*>(smem + kOffParam + (cs % kParams) * kParamBytes) + g * 64;
         if (warp_valid) {
-          uint32_t sr[2][32];   // 64 products of this thread's row
+          const int4* info = reinterpret_cast<const int4*>(smem + kOffInfo) + (cs % kInfo) * 4 + 2 * g;
+          const int4 i0 = info[0], i1 = info[1];
+          const float f[2] = {qf * __int_as_float(i0.x), qf * __int_as_float(i1.x)};
+          uint32_t sr[2][32];   // the S row of this thread: 64 scores, in units of 1 / f
 #pragma unroll
           for (int c = 0; c < 2; ++c) tmem_ld32_nowait(s_buf + c * 32, sr[c]);
           tmem_ld_wait();
           const int lim = min(climit, tok_end - 1);
           const bool need_mask = __any_sync(0xffffffffu, rvalid && (pos0 + 63 > lim));
-          unsigned long long see = ~0ull;          // visible tokens of this row within the 64: [0, a] and [b, c)
+          unsigned bad[2] = {(unsigned)i0.z, (unsigned)i1.z};
           if (need_mask) {
+            // visible tokens of this row within the 64: [0, a] and [b, c), as a 64-bit mask over tokens
             const int a = lim - pos0, b = vlo - pos0, cc = min(vhi, tok_end) - pos0;
             auto ones = [](int k) -> unsigned long long { return k <= 0 ? 0ull : (k >= 64 ? ~0ull : ((1ull << k) - 1ull)); };
-            see = ones(a + 1) | (ones(cc) & ~ones(b));
-          }
-          const float2 qsum2 = make_float2(qsum, qsum);
-          // scores (in powers of two) of tokens i, i + 1 of half c, less `ref`
-          auto score2 = [&](int c, int i, const float2& neg_ref2) {
-            const float4 kp = param[2 * ((c * 32 + i) >> 1)];
-            return fma2(make_float2(__uint_as_float(sr[c][i]), __uint_as_float(sr[c][i + 1])), make_float2(kp.x, kp.y),
-                        fma2(make_float2(kp.z, kp.w), qsum2, neg_ref2));
-          };
-          auto row_max = [&]() {
-            float mx = -INFINITY;
-            const float2 none = make_float2(0.f, 0.f);
-#pragma unroll 1
+            const unsigned long long see = ones(a + 1) | (ones(cc) & ~ones(b));
+            bad[0] &= (unsigned)see;
+            bad[1] &= (unsigned)(see >> 32);
+#pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-              for (int i = 0; i < 32; i += 2) {
-                const float4 kp = param[2 * ((c * 32 + i) >> 1)];
-                const float2 t = c ? make_float2(__uint_as_float(sr[1][i]), __uint_as_float(sr[1][i + 1]))
-                                   : make_float2(__uint_as_float(sr[0][i]), __uint_as_float(sr[0][i + 1]));
-                const float2 y = fma2(t, make_float2(kp.x, kp.y), fma2(make_float2(kp.z, kp.w), qsum2, none));
-                const unsigned bits = (unsigned)(see >> (c * 32 + i)) & 3u;
-                if (bits & 1u) mx = fmaxf(mx, y.x);
-                if (bits & 2u) mx = fmaxf(mx, y.y);
-              }
-            return mx;
-          };
-          if (__any_sync(0xffffffffu, m_ref == kNoRef)) {      // a row that has seen no token yet: what it has summed up is nothing
-            const float mx = row_max();
-            if (m_ref == kNoRef && mx > m_ref) m_ref = mx;
+              for (int i = 0; i < 32; ++i)
+                if (((see >> (c * 32 + i)) & 1ull) == 0ull) sr[c][i] = 0xff800000u;   // -inf
           }
+          if (__any_sync(0xffffffffu, m_ref == kNoRef)) {      // a row that has seen no token yet: what it has summed up is nothing
+            float mx[2][2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              mx[c][0] = mx[c][1] = -INFINITY;
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                mx[c][0] = fmaxf(mx[c][0], fmaxf(__uint_as_float(sr[c][i]), __uint_as_float(sr[c][i + 1])));
+                mx[c][1] = fmaxf(mx[c][1], fmaxf(__uint_as_float(sr[c][i + 2]), __uint_as_float(sr[c][i + 3])));
+              }
+            }
+            const float z = fmaxf(__fmul_rn(fmaxf(mx[0][0], mx[0][1]), f[0]), __fmul_rn(fmaxf(mx[1][0], mx[1][1]), f[1]));
+            if (m_ref == kNoRef && z > m_ref) m_ref = rintf(z);
+          }
+          const int e_new = max(o_exp, max(i0.y, i1.y));
+          bool rescale = n > 0 && e_new != o_exp;
           // (see attention_tc.cu: probabilities relative to the standing reference; a stage in which a row outgrows it is done again)
 #pragma unroll 1
           for (int pass = 0; pass < 2; ++pass) {
-            const float2 neg_ref2 = make_float2(-m_ref, -m_ref);
-            float2 lsa[2] = {}, oma[2] = {};
-            float mxa[2] = {-INFINITY, -INFINITY};
+            float2 lsa[2][2] = {};
+            float mxa[2][2];
+            const int lower[2] = {max(-64, i0.y - e_new), max(-64, i1.y - e_new)};     // (at -64 nothing of P is left)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              uint32_t pk[16];
-              if (!need_mask) {
+              const float2 f2 = make_float2(f[c], f[c]);
+              const float shift = kLift + (float)lower[c] - m_ref;
+              const float2 shift2 = make_float2(shift, shift);
+              mxa[c][0] = mxa[c][1] = -INFINITY;
+              uint32_t pk[16];     // 32 tokens -> 16 packed columns over the start of this S buffer
 #pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                  const int k = (i >> 1) & 1;
-                  const float2 y = score2(c, i, neg_ref2);
-                  const float4 vp = param[2 * ((c * 32 + i) >> 1) + 1];
-                  mxa[k] = fmaxf(mxa[k], fmaxf(y.x, y.y));
-                  const float2 p = make_float2(exp2f(y.x), exp2f(y.y));
-                  lsa[k] = add2(lsa[k], p);
-                  oma[k] = fma2(p, make_float2(vp.z, vp.w), oma[k]);
-                  const float2 ps = mul2(p, make_float2(vp.x, vp.y));
-                  pk[i >> 1] = pack_bf16(ps.x, ps.y);
-                }
-              } else {
-#pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                  const int k = (i >> 1) & 1;
-                  float2 y = score2(c, i, neg_ref2);
-                  const bool s0 = (see >> (c * 32 + i)) & 1ull, s1 = (see >> (c * 32 + i + 1)) & 1ull;
-                  if (!s0) y.x = -INFINITY;
-                  if (!s1) y.y = -INFINITY;
-                  const float4 vp = param[2 * ((c * 32 + i) >> 1) + 1];
-                  mxa[k] = fmaxf(mxa[k], fmaxf(y.x, y.y));
-                  const float2 p = make_float2(exp2f(y.x), exp2f(y.y));
-                  lsa[k] = add2(lsa[k], p);
-                  // (a token that this row does not see may hold anything, infinities too)
-                  oma[k] = add2(oma[k], make_float2(s0 ? p.x * vp.z : 0.f, s1 ? p.y * vp.w : 0.f));
-                  pk[i >> 1] = pack_bf16(s0 ? p.x * vp.x : 0.f, s1 ? p.y * vp.y : 0.f);
-                }
+              for (int i = 0; i < 32; i += 2) {
+                const int k = (i >> 1) & 1;
+                const float2 t = make_float2(__uint_as_float(sr[c][i]), __uint_as_float(sr[c][i + 1])), y = fma2(t, f2, shift2);
+                mxa[c][k] = fmaxf(mxa[c][k], fmaxf(t.x, t.y));
+                const float2 p = make_float2(exp2f(y.x), exp2f(y.y));   // exp2(-inf) = 0 for masked
+                lsa[c][k] = add2(lsa[c][k], p);
+                pk[i >> 1] = pack_f16(p.x, p.y);
               }
               tmem_st16(s_buf + c * 16, pk);
             }
-            const bool grow = rvalid && n > 0 && fmaxf(mxa[0], mxa[1]) > kHeadroom;
-            if (pass == 1 || !__any_sync(0xffffffffu, grow)) {
-              const float2 ls = add2(lsa[0], lsa[1]), os = add2(oma[0], oma[1]);
-              l_run += ls.x + ls.y;
-              om_run += os.x + os.y;
+            const float z = fmaxf(__fmul_rn(fmaxf(mxa[0][0], mxa[0][1]), f[0]), __fmul_rn(fmaxf(mxa[1][0], mxa[1][1]), f[1]));
+            const bool grow = rvalid && n > 0 && z > m_ref + kHeadroom;
+            if (pass == 1 || !__any_sync(0xffffffffu, grow || rescale)) {
+              const float2 l0 = add2(lsa[0][0], lsa[0][1]), l1 = add2(lsa[1][0], lsa[1][1]);
+              l_run += (l0.x + l0.y) * pow2(-lower[0]) + (l1.x + l1.y) * pow2(-lower[1]);
               break;
             }
             // O is rescaled in TMEM, once the group's P V of the previous stage has completed
             bwait(pv_done, (cs - 1) & 1, DEV_TIMEOUT_MMA);
             tc_fence_after();
-            const float mx = row_max();
-            const float m_new = grow ? fmaxf(m_ref, mx) : m_ref;
-            const float f = exp2f(m_ref - m_new);
+            const float m_new = grow ? rintf(z) : m_ref;
+            const float fl = exp2f(m_ref - m_new), fo = rescale ? fl * pow2(max(-120, o_exp - e_new)) : fl;
             m_ref = m_new;
-            l_run *= f;
-            om_run *= f;
+            l_run *= fl;
 #pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
               uint32_t r[16];
               tmem_ld16(o_addr + c * 16, r);
               tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+              for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * fo);
               tmem_st16(o_addr + c * 16, r);
             }
             tmem_st_wait();
           }
+          o_exp = e_new;
+          if (bad[0] | bad[1]) l_run = __int_as_float(0x7fc00000);      // the row sees V that is not finite
           tmem_st_wait();
         }
         tc_fence_before();
@@ -491,30 +578,30 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
       // ---- merge the two groups' partial attentions and write out: this group finishes dims [64 g, 64 g + 64) ----
       bwait(o_full, item & 1, DEV_TIMEOUT_MMA);
       tc_fence_after();
-      ml_smem[g * 128 + row] = make_float4(m_ref, l_run, om_run, 0.f);
+      // (the sum is of lifted probabilities, relative to a reference lower by as much)
+      ml_smem[g * 128 + row] = m_ref - kLift;
+      ml_smem[256 + g * 128 + row] = l_run;
+      ml_smem[512 + g * 128 + row] = pow2(max(-56, o_exp));
       softmax_bar();
       if (warp_valid) {
-        const float4 a0 = ml_smem[row], a1 = ml_smem[128 + row];
-        const float m_all = fmaxf(a0.x, a1.x);
-        float f0 = exp2f(a0.x - m_all), f1 = exp2f(a1.x - m_all);
-        const float l_all = a0.y * f0 + a1.y * f1;
-        const float inv = (w.part < 0) ? (l_all > 0.f ? 1.f / l_all : 0.f) : 1.f;
-        f0 *= inv;
-        f1 *= inv;
-        const float om = a0.z * f0 + a1.z * f1;
+        const float r0 = ml_smem[row], r1 = ml_smem[128 + row], m_all = fmaxf(r0, r1);
+        const float w0 = exp2f(r0 - m_all), w1 = exp2f(r1 - m_all);
+        const float l_all = ml_smem[256 + row] * w0 + ml_smem[384 + row] * w1;
+        const float inv = (w.part < 0) ? (l_all > 0.f ? 1.f / l_all : 0.f * l_all) : (l_all == l_all ? 1.f : l_all);
+        const float f0 = w0 * ml_smem[512 + row] * inv, f1 = w1 * ml_smem[640 + row] * inv;
         const size_t orow = (size_t)(w.tok0 + row / P.group) * P.n_q + w.kv_head * P.group + row % P.group;
         float4* s4 = reinterpret_cast<float4*>(smem + kOffScratch + (warp - 8) * 2048);
         const int nrow = min(32, R - quad * 32);
 #pragma unroll 1
         for (int cc = 0; cc < 4; ++cc) {
           const int c = 4 * g + cc;               // 16-dim chunk of the output row
-          uint32_t r[16], r1[16];
-          tmem_ld16(lane_addr + kTmemO + c * 16, r);
-          tmem_ld16(lane_addr + kTmemO + D + c * 16, r1);
+          uint32_t ra[16], rb[16];
+          tmem_ld16(lane_addr + kTmemO + c * 16, ra);
+          tmem_ld16(lane_addr + kTmemO + D + c * 16, rb);
           tmem_ld_wait();
           float v[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = fmaf(__uint_as_float(r1[i]), f1, fmaf(__uint_as_float(r[i]), f0, om));
+          for (int i = 0; i < 16; ++i) v[i] = fmaf(__uint_as_float(rb[i]), f1, __uint_as_float(ra[i]) * f0);
           if (w.part < 0) {
             if (rvalid) {
               uint4* dst = reinterpret_cast<uint4*>(P.o + orow * D + c * 16);
