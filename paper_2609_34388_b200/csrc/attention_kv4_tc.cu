@@ -14,16 +14,17 @@
 // joins the exponent of the probabilities, relative to the largest one so far (O is rescaled when that grows).  Values next to others
 // that are 2^25 times as large lose bits, as in any fp32 sum of both.
 //
-// Per CTA (16 warps = 4 warpgroups, one CTA per SM, persistent over the work list), stages of 128 tokens:
+// Per CTA (20 warps = 5 warpgroups, one CTA per SM, persistent over the work list), stages of 128 tokens:
 //   warp 0     streams the blocks of the pool (codes and pairs of a page and head: one bulk copy) into a ring of two raw stages, and
 //              the item's Q rows by TMA
-//   warps 4-7  turn a raw stage into the operands, 32 tokens a warp: K (K-major) and V (MN-major), 16 tokens x 128 values in 128-byte-
-//              swizzled atoms as the tensor core reads them; and the rows of Q, one a thread.  Every lane turns words of eight
-//              codes into 16-byte stores; the words of a lane are taken in an order in which no two lanes of a store meet a bank.
+//   warps 4-7  turn a raw stage into the operand K (K-major) and warps 8-11 into V (MN-major), 32 tokens a warp: 16 tokens x 128 values
+//              in 128-byte-swizzled atoms as the tensor core reads them.  Every lane turns words of eight codes into 16-byte stores;
+//              the words of a lane are taken in an order in which no two lanes of a store meet a bank.  Warps 4-7 also turn the
+//              rows of Q, one a thread.  (One warpgroup for both had a chain of latencies longer than a stage: 272 us.)
 //   warp 1     one elected lane issues S = Q K^T (two stages ahead) and per softmax group O_g += P_g V_g (P from TMEM)
-//   warps 8-11 and 12-15  two softmax groups: group g takes tokens [64 g, 64 g + 64) of every stage, one thread one query row, its
+//   warps 12-15 and 16-19  two softmax groups: group g takes tokens [64 g, 64 g + 64) of every stage, one thread one query row, its
 //              own O accumulator and running (reference maximum, sum); merged at the end of an item.
-// The registers are moved to the softmax warps: 4 x (88 + 88 + 168 + 168) x 32 = 16 x 128 x 32 of the launch.
+// The registers are moved to the softmax warps: 4 x (56 + 64 + 64 + 144 + 144) x 32 of the 20 x 96 x 32 of the launch.
 // Every wait is bounded; a wait that runs out raises a CTA-wide flag after which no wait blocks, so the kernel always ends.
 #include <cuda_fp16.h>
 #include <cstdio>
@@ -45,7 +46,7 @@ constexpr int kOperand = kBT * D * 2;            // 32 KB: K or V of a stage, or
 constexpr int kRaw = 2, kRing = 2;               // raw stages; stages of K and of V operands
 constexpr int kInfo = 4;                         // stages of what the softmax needs to know of 32 tokens (see the writer)
 constexpr int kExt = 128 * 32;                   // the 16 further values of the contraction: 128 rows x 32 bytes, not swizzled
-constexpr int kThreads = 512;
+constexpr int kThreads = 640;
 constexpr uint32_t kSpin = 1u << 22;
 constexpr int kTmemCols = 512;                   // two S buffers of 128 columns; O of group g at 256 + 128 g
 constexpr int kTmemO = 2 * kBT;
@@ -113,6 +114,12 @@ struct TokenInfo {       // of 32 tokens
 // not be a normal number, or products of two not)
 __device__ __forceinline__ int scale_exp(int field) { return max(-56, min(120, ((field - 127) >> 3) << 3)); }
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
+// the scale of V of the 32 tokens whose {step, minimum} a warp's lanes hold
+__device__ __forceinline__ int v_scale(uint32_t pair, bool* bad) {
+  *bad = (pair & 0x7f80u) == 0x7f80u;
+  const float top = *bad ? 0.f : fmaxf(fabsf(kv4_min(pair)), fabsf(fmaf(15.f, kv4_step(pair), kv4_min(pair))));
+  return scale_exp(__reduce_max_sync(0xffffffffu, __float_as_int(top) >> 23));
+}
 __device__ __forceinline__ uint32_t h2_bits(const __half2& h) { return reinterpret_cast<const uint32_t&>(h); }
 __device__ __forceinline__ __half2 bits_h2(uint32_t u) { return reinterpret_cast<const __half2&>(u); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
@@ -147,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
   }
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBar);
   uint64_t* raw_full = bars;                     // [kRaw]
-  uint64_t* raw_empty = raw_full + kRaw;         // [kRaw]   the four converting warps
+  uint64_t* raw_empty = raw_full + kRaw;         // [kRaw]   the eight converting warps
   uint64_t* k_full = raw_empty + kRaw;           // [kRing]
   uint64_t* k_empty = k_full + kRing;
   uint64_t* v_full = k_empty + kRing;
@@ -176,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
     *abort_flag = 0;
     for (int s = 0; s < kRaw; ++s) {
       mbar_init(&raw_full[s], 1);
-      mbar_init(&raw_empty[s], 4);
+      mbar_init(&raw_empty[s], 8);
     }
     for (int s = 0; s < kRing; ++s) {
       mbar_init(&k_full[s], 4);
@@ -216,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
   auto stages_of = [&](const AttnItem& w) { return (min(w.blk_end * 64, w.kv_len) - w.blk_begin * 64 + kBT - 1) / kBT; };
 
   if (warp < 4) {
-    regs_dec<88>();
+    regs_dec<56>();
     if (warp == 0) {
       // ------------------------------------ producer: raw stages and Q ------------------------------------
       uint32_t blk = 0;
@@ -319,8 +326,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
       }
     }
   } else if (warp < 8) {
-    // ------------------------------------ codes to operands ------------------------------------
-    regs_dec<88>();
+    // ------------------------------------ codes to K; the rows of Q ------------------------------------
+    regs_dec<64>();
     const int wq = warp - 4;                     // takes tokens [32 wq, 32 wq + 32) of every stage, and rows 32 wq .. of Q
     uint32_t blk = 0;
     for (int item = 0; item < item_end; ++item) {
@@ -330,48 +337,44 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
         const int rs = blk % kRaw, s = blk % kRing;
         const uint8_t* raw = smem + kOffRaw + rs * kRawBytes + 2 * wq * kBlock;
         bwait(&raw_full[rs], (blk / kRaw) & 1, DEV_TIMEOUT_FULL);
-        bwait(&k_empty[s], ((blk / kRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
         // ---- steps and minima, a token a lane: what is not there, or not finite, counts nothing ----
         const uint8_t* pg = raw + (lane >> 4) * kBlock;
         const bool there = tok_begin + n * kBT + 32 * wq + lane < tok_end;
         const uint32_t kp = there ? *reinterpret_cast<const uint32_t*>(pg + kv4_k_pairs(D) + 4 * (lane & 15)) : 0u;
-        uint32_t vp = there ? *reinterpret_cast<const uint32_t*>(pg + kv4_v_pairs(D) + 4 * (lane & 15)) : 0u;
-        const bool k_bad = (kp & 0x7f80u) == 0x7f80u, v_bad = (vp & 0x7f80u) == 0x7f80u;
-        if (v_bad) vp = 0;
+        const uint32_t vp = there ? *reinterpret_cast<const uint32_t*>(pg + kv4_v_pairs(D) + 4 * (lane & 15)) : 0u;
         const float k_mid = fmaf(8.f, kv4_step(kp), kv4_min(kp));                       // m + 8 s
-        const float k_top = k_bad ? 0.f : fmaxf(fabsf(k_mid), 8.f * kv4_step(kp));
-        const float v_top = fmaxf(fabsf(kv4_min(vp)), fabsf(fmaf(15.f, kv4_step(vp), kv4_min(vp))));
+        const float k_top = (kp & 0x7f80u) == 0x7f80u ? 0.f : fmaxf(fabsf(k_mid), 8.f * kv4_step(kp));
         const int ke = scale_exp(__reduce_max_sync(0xffffffffu, __float_as_int(k_top) >> 23));
-        const int ve = scale_exp(__reduce_max_sync(0xffffffffu, __float_as_int(v_top) >> 23));
-        const float ks = pow2(-ke), vs = pow2(-ve);
+        const float ks = pow2(-ke);
+        bool v_bad;
+        const int ve = v_scale(vp, &v_bad);
         const unsigned bad = __ballot_sync(0xffffffffu, v_bad);
-        // The ring is four stages deep: the V operands of the stage before this one went where the P V product of stage blk - 3 had
-        // read, which waited for every softmax warp to be done with stage blk - 3.
-        if (lane == 0) {
-          TokenInfo* info = reinterpret_cast<TokenInfo*>(smem + kOffInfo) + (blk % kInfo) * 4 + wq;
-          *reinterpret_cast<int4*>(info) = make_int4(__float_as_int(pow2(ke)), ve, (int)bad, 0);
-        }
-        {
-          const float mid = k_mid * ks, hi = __half2float(__float2half_rn(mid));
-          const uint32_t terms = pack_f16(hi, mid - hi);                                // met by {a, a, b, b} of the row's sum a + b
-          *reinterpret_cast<uint4*>(smem + kOffKExt + s * kExt + ext_row(32 * wq + lane)) = make_uint4(terms, terms, 0, 0);
-        }
+        const float mid = k_mid * ks, hi = __half2float(__float2half_rn(mid));
+        const uint32_t terms = pack_f16(hi, mid - hi);                                  // met by {a, a, b, b} of the row's sum a + b
         const uint32_t k_step = pack_f16(kv4_step(kp) * ks, kv4_step(kp) * ks);
-        const uint32_t v_pair = pack_f16(kv4_step(vp) * vs, kv4_min(vp) * vs);
-        uint8_t* kdst = smem + kOffK + s * kOperand + wq * 8192;
-#pragma unroll
+        bwait(&k_empty[s], ((blk / kRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
+        // (A ring of four stages is enough: the S product of stage blk - 2, whose K stood here, was issued behind the P V products of
+        // stage blk - 4, which had waited for every softmax warp.)
+        if (lane == 0)
+          reinterpret_cast<int4*>(smem + kOffInfo)[(blk % kInfo) * 4 + wq] = make_int4(__float_as_int(pow2(ke)), ve, (int)bad, 0);
+        *reinterpret_cast<uint4*>(smem + kOffKExt + s * kExt + ext_row(32 * wq + lane)) = make_uint4(terms, terms, 0, 0);
+        // unit: 16 bytes = values [32 q, 32 q + 32) of a token; atom (token group, q >> 1), chunks (q & 1) * 4 + word
+        const int q = lane & 3, r = lane >> 2;
+        const uint8_t* src = raw + r * (D / 2) + q * 16;
+        uint8_t* dst = smem + kOffK + s * kOperand + wq * 8192 + (q >> 1) * 1024 + r * 128;
+        uint4 next = *reinterpret_cast<const uint4*>(src);
+#pragma unroll 1
         for (int u = 0; u < 4; ++u) {
-          // unit: 16 bytes = values [32 q, 32 q + 32) of a token; atom (token group, q >> 1), chunks (q & 1) * 4 + word
-          const int tok = u * 8 + (lane >> 2), q = lane & 3;
-          const __half2 step = bits_h2(__shfl_sync(0xffffffffu, k_step, tok));
-          uint4 v = *reinterpret_cast<const uint4*>(raw + (tok >> 4) * kBlock + (tok & 15) * (D / 2) + q * 16);
-          if (q & 2) v = make_uint4(v.z, v.w, v.x, v.y);
+          const uint4 v = (q & 2) ? make_uint4(next.z, next.w, next.x, next.y) : next;
+          if (u < 3) next = *reinterpret_cast<const uint4*>(src + ((u + 1) >> 1) * kBlock + ((u + 1) & 1) * (4 * D));
+          const __half2 step = bits_h2(__shfl_sync(0xffffffffu, k_step, u * 8 + r));
           const uint32_t word[4] = {v.x, v.y, v.z, v.w};
-          uint8_t* row = kdst + (tok >> 3) * 2048 + (q >> 1) * 1024 + (tok & 7) * 128;
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            *reinterpret_cast<uint4*>(row + ((((q & 1) * 4 + (x ^ (q & 2))) ^ (tok & 7)) << 4)) = k_values(word[x], step);
+            *reinterpret_cast<uint4*>(dst + u * 2048 + ((((q & 1) * 4 + (x ^ (q & 2))) ^ r) << 4)) = k_values(word[x], step);
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&raw_empty[rs]);
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&k_full[s]);
@@ -412,40 +415,59 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
           __syncwarp();
           if (lane == 0) mbar_arrive(q_ready);
         }
+      }
+    }
+  } else if (warp < 12) {
+    // ------------------------------------ codes to V ------------------------------------
+    regs_dec<64>();
+    const int wq = warp - 8;
+    uint32_t blk = 0;
+    for (int item = 0; item < item_end; ++item) {
+      const AttnItem w = P.items[item_at(item)];
+      const int nblk = stages_of(w), tok_begin = w.blk_begin * 64, tok_end = min(w.blk_end * 64, w.kv_len);
+      for (int n = 0; n < nblk; ++n, ++blk) {
+        const int rs = blk % kRaw, s = blk % kRing;
+        const uint8_t* raw = smem + kOffRaw + rs * kRawBytes + 2 * wq * kBlock;
+        bwait(&raw_full[rs], (blk / kRaw) & 1, DEV_TIMEOUT_FULL);
+        const bool there = tok_begin + n * kBT + 32 * wq + lane < tok_end;
+        uint32_t vp = there ? *reinterpret_cast<const uint32_t*>(raw + (lane >> 4) * kBlock + kv4_v_pairs(D) + 4 * (lane & 15)) : 0u;
+        bool v_bad;
+        const float vs = pow2(-v_scale(vp, &v_bad));
+        if (v_bad) vp = 0;
+        const uint32_t v_pair = pack_f16(kv4_step(vp) * vs, kv4_min(vp) * vs);
         bwait(&v_empty[s], ((blk / kRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
-        uint8_t* vdst = smem + kOffV + s * kOperand + wq * 8192;
-#pragma unroll
+        // unit: 16 bytes = values [16 g, 16 g + 16) of a token pair, chunks 2 g and 2 g + 1 of both tokens
+        const int g = lane & 7, r = lane >> 3;
+        const uint8_t* src = raw + kv4_v_codes(D) + r * D + g * 16;
+        uint8_t* dst = smem + kOffV + s * kOperand + wq * 8192 + (g >> 2) * 1024 + 2 * r * 128;
+        uint4 next = *reinterpret_cast<const uint4*>(src);
+#pragma unroll 1
         for (int u = 0; u < 4; ++u) {
-          // unit: 16 bytes = values [16 g, 16 g + 16) of a token pair, chunks 2 g and 2 g + 1 of both tokens
-          const int pair = u * 4 + (lane >> 3), g = lane & 7;
-          uint4 v = *reinterpret_cast<const uint4*>(raw + (pair >> 3) * kBlock + kv4_v_codes(D) + (pair & 7) * D + g * 16);
-          if (g & 4) v = make_uint4(v.z, v.w, v.x, v.y);
+          const uint4 v = (g & 4) ? make_uint4(next.z, next.w, next.x, next.y) : next;
+          if (u < 3) next = *reinterpret_cast<const uint4*>(src + ((u + 1) >> 1) * kBlock + ((u + 1) & 1) * (4 * D));
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int tok = 2 * pair + e;
-            const __half2 sm = bits_h2(__shfl_sync(0xffffffffu, v_pair, tok));
+            const __half2 sm = bits_h2(__shfl_sync(0xffffffffu, v_pair, u * 8 + 2 * r + e));
             const __half2 step = __low2half2(sm), low = __high2half2(sm);
-            uint8_t* row = vdst + (tok >> 3) * 2048 + (g >> 2) * 1024 + (tok & 7) * 128;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const uint32_t a = x ? v.z : v.x, b = x ? v.w : v.y;
-              *reinterpret_cast<uint4*>(row + (((2 * (g & 3) + (x ^ (g >> 2))) ^ (tok & 7)) << 4)) =
+              *reinterpret_cast<uint4*>(dst + u * 2048 + e * 128 + (((2 * (g & 3) + (x ^ (g >> 2))) ^ (2 * r + e)) << 4)) =
                   v_values(e ? __byte_perm(a, b, 0x7632) : __byte_perm(a, b, 0x5410), step, low);
             }
           }
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&raw_empty[rs]);
         fence_proxy_async();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&v_full[s]);
-          mbar_arrive(&raw_empty[rs]);
-        }
+        if (lane == 0) mbar_arrive(&v_full[s]);
       }
     }
   } else {
     // ------------------------------------ softmax ------------------------------------
-    regs_inc<168>();
-    const int g = (warp - 8) >> 2;             // softmax group: takes tokens [64 g, 64 g + 64) of every stage
+    regs_inc<144>();
+    const int g = (warp - 12) >> 2;             // softmax group: takes tokens [64 g, 64 g + 64) of every stage
     const int quad = warp & 3;
     const int row = quad * 32 + lane;          // query row of the tile = TMEM lane
     const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
@@ -590,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
         const float inv = (w.part < 0) ? (l_all > 0.f ? 1.f / l_all : 0.f * l_all) : (l_all == l_all ? 1.f : l_all);
         const float f0 = w0 * ml_smem[512 + row] * inv, f1 = w1 * ml_smem[640 + row] * inv;
         const size_t orow = (size_t)(w.tok0 + row / P.group) * P.n_q + w.kv_head * P.group + row % P.group;
-        float4* s4 = reinterpret_cast<float4*>(smem + kOffScratch + (warp - 8) * 2048);
+        float4* s4 = reinterpret_cast<float4*>(smem + kOffScratch + (warp - 12) * 2048);
         const int nrow = min(32, R - quad * 32);
 #pragma unroll 1
         for (int cc = 0; cc < 4; ++cc) {
