@@ -47,7 +47,7 @@ constexpr int kRaw = 2, kRing = 2;               // raw stages; stages of K and 
 constexpr int kInfo = 4;                         // stages of what the softmax needs to know of 32 tokens (see the writer)
 constexpr int kExt = 128 * 32;                   // the 16 further values of the contraction: 128 rows x 32 bytes, not swizzled
 constexpr int kThreads = 640;
-constexpr uint32_t kSpin = 1u << 22;
+constexpr uint32_t kSpin = 1u << 22;             // polls of a wait
 constexpr int kTmemCols = 512;                   // two S buffers of 128 columns; O of group g at 256 + 128 g
 constexpr int kTmemO = 2 * kBT;
 constexpr float kNoRef = -1e30f;       // reference maximum of a row that has seen no token yet
@@ -103,6 +103,17 @@ __device__ __forceinline__ uint64_t desc_ext(uint32_t addr) {
 }
 __device__ __forceinline__ int ext_row(int row) { return (row >> 3) * 256 + (row & 7) * 16; }
 
+// A bounded wait that sleeps NS nanoseconds between polls: 20 warps that poll take issue slots from those that work.
+template <int NS>
+__device__ __forceinline__ bool wait_asleep(uint64_t* bar, uint32_t parity) {
+#pragma unroll 1
+  for (uint32_t i = 0; i < kSpin; ++i) {
+    __nanosleep(NS);
+    if (mbar_test_wait(bar, parity)) return true;
+  }
+  return false;
+}
+
 struct TokenInfo {       // of 32 tokens
   float k_scale;         // K stands scaled by 1 / k_scale
   int v_exp;             // V stands scaled by 2^-v_exp
@@ -121,29 +132,59 @@ __device__ __forceinline__ int v_scale(uint32_t pair, bool* bad) {
   return scale_exp(__reduce_max_sync(0xffffffffu, __float_as_int(top) >> 23));
 }
 __device__ __forceinline__ uint32_t h2_bits(const __half2& h) { return reinterpret_cast<const uint32_t&>(h); }
-__device__ __forceinline__ __half2 bits_h2(uint32_t u) { return reinterpret_cast<const __half2&>(u); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
+__device__ __forceinline__ uint32_t add_h2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t fma_h2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+// The constants of a conversion.  They are made where the compiler does not see their values: it would split every (word & mask) |
+// exponent into two instructions with an immediate each.
+struct CodeConst {
+  uint32_t exponent, whole, part, sixteenth;      // 1024 in both halves; off - 1024, off - 64; 1 / 16
+};
+__device__ __forceinline__ uint32_t opaque(uint32_t v) {
+  uint32_t d;
+  asm volatile("mov.b32 %0, %1;" : "=r"(d) : "r"(v));
+  return d;
+}
+__device__ __forceinline__ CodeConst code_const(float off) {
+  return CodeConst{opaque(0x64006400u), opaque(pack_f16(off - 1024.f, off - 1024.f)), opaque(pack_f16(off - 64.f, off - 64.f)), opaque(0x2c002c00u)};
+}
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t code_bits(uint32_t w, uint32_t exponent) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(w), "n"(MASK), "r"(exponent));     // (w & MASK) | exponent
+  return d;
+}
 // the pairs of a word of codes as fp16 c + off: 1024 + c is 0x6400 | c, 1024 + 16 c is 0x6400 | (c << 4)
-template <int OFF>
-__device__ __forceinline__ void word_codes(uint32_t w, __half2 (&x)[4]) {
-  const __half2 a = __half2half2(__float2half_rn((float)(OFF - 1024))), b = __half2half2(__float2half_rn((float)(OFF - 64))),
-                sixteenth = __half2half2(__float2half_rn(0.0625f));
+__device__ __forceinline__ void word_codes(uint32_t w, const CodeConst& k, uint32_t (&x)[4]) {
   const uint32_t v = w >> 8;
-  x[0] = __hadd2(bits_h2((w & 0x000f000fu) | 0x64006400u), a);
-  x[1] = __hfma2(bits_h2((w & 0x00f000f0u) | 0x64006400u), sixteenth, b);
-  x[2] = __hadd2(bits_h2((v & 0x000f000fu) | 0x64006400u), a);
-  x[3] = __hfma2(bits_h2((v & 0x00f000f0u) | 0x64006400u), sixteenth, b);
+  x[0] = add_h2(code_bits<0x000f000fu>(w, k.exponent), k.whole);
+  x[1] = fma_h2(code_bits<0x00f000f0u>(w, k.exponent), k.sixteenth, k.part);
+  x[2] = add_h2(code_bits<0x000f000fu>(v, k.exponent), k.whole);
+  x[3] = fma_h2(code_bits<0x00f000f0u>(v, k.exponent), k.sixteenth, k.part);
 }
 // s (c - 8), exact; m + s c, rounded once
-__device__ __forceinline__ uint4 k_values(uint32_t w, const __half2& s) {
-  __half2 x[4];
-  word_codes<-8>(w, x);
-  return make_uint4(h2_bits(__hmul2(x[0], s)), h2_bits(__hmul2(x[1], s)), h2_bits(__hmul2(x[2], s)), h2_bits(__hmul2(x[3], s)));
+__device__ __forceinline__ uint4 k_values(uint32_t w, const CodeConst& k, uint32_t s) {
+  uint32_t x[4];
+  word_codes(w, k, x);
+  return make_uint4(mul_h2(x[0], s), mul_h2(x[1], s), mul_h2(x[2], s), mul_h2(x[3], s));
 }
-__device__ __forceinline__ uint4 v_values(uint32_t w, const __half2& s, const __half2& m) {
-  __half2 x[4];
-  word_codes<0>(w, x);
-  return make_uint4(h2_bits(__hfma2(x[0], s, m)), h2_bits(__hfma2(x[1], s, m)), h2_bits(__hfma2(x[2], s, m)), h2_bits(__hfma2(x[3], s, m)));
+__device__ __forceinline__ uint4 v_values(uint32_t w, const CodeConst& k, uint32_t s, uint32_t m) {
+  uint32_t x[4];
+  word_codes(w, k, x);
+  return make_uint4(fma_h2(x[0], s, m), fma_h2(x[1], s, m), fma_h2(x[2], s, m), fma_h2(x[3], s, m));
 }
 
 __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __grid_constant__ CUtensorMap qmap, Params P) {
@@ -171,9 +212,17 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* ml_smem = reinterpret_cast<float*>(smem + kOffML);
   float* qf_smem = reinterpret_cast<float*>(smem + kOffQF);
+  // (the MMA issuer and the softmax warps, whom the stage waits for, poll more often)
   auto bwait = [&](uint64_t* bar, uint32_t parity, int code) {
     if (mbar_test_wait(bar, parity) || *abort_flag) return;
-    if (!mbar_wait(bar, parity, kSpin)) {
+    if (!wait_asleep<20>(bar, parity)) {
+      set_status(P.status, code);
+      *abort_flag = 1;
+    }
+  };
+  auto lazy_wait = [&](uint64_t* bar, uint32_t parity, int code) {
+    if (mbar_test_wait(bar, parity) || *abort_flag) return;
+    if (!wait_asleep<100>(bar, parity)) {
       set_status(P.status, code);
       *abort_flag = 1;
     }
@@ -244,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
             my_pg = -1;
           }
           const int s = blk % kRaw;
-          bwait(&raw_empty[s], ((blk / kRaw) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
+          lazy_wait(&raw_empty[s], ((blk / kRaw) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
           const unsigned mask = __ballot_sync(0xffffffffu, my_pg >= 0);
           if (lane == 0) {
             if (mask == 0) mbar_arrive(&raw_full[s]);
@@ -257,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
           __syncwarp();
           if (n == 0) {
             // Q rows of the item (see attention_tc.cu); the first raw stage went ahead, since the item before may still read its Q
-            bwait(q_empty, (item & 1) ^ 1, DEV_TIMEOUT_EMPTY);
+            lazy_wait(q_empty, (item & 1) ^ 1, DEV_TIMEOUT_EMPTY);
             if (lane == 0) {
               mbar_arrive_expect_tx(q_full, 2u * 128u * (uint32_t)(P.group * (128 / P.group)));
               tma_load_3d(smem_base + kOffQ, &qmap, 0, w.kv_head * P.group, w.tok0, q_full);
@@ -328,6 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
   } else if (warp < 8) {
     // ------------------------------------ codes to K; the rows of Q ------------------------------------
     regs_dec<64>();
+    const CodeConst kc = code_const(-8.f);
     const int wq = warp - 4;                     // takes tokens [32 wq, 32 wq + 32) of every stage, and rows 32 wq .. of Q
     uint32_t blk = 0;
     for (int item = 0; item < item_end; ++item) {
@@ -336,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
       for (int n = 0; n < nblk; ++n, ++blk) {
         const int rs = blk % kRaw, s = blk % kRing;
         const uint8_t* raw = smem + kOffRaw + rs * kRawBytes + 2 * wq * kBlock;
-        bwait(&raw_full[rs], (blk / kRaw) & 1, DEV_TIMEOUT_FULL);
+        lazy_wait(&raw_full[rs], (blk / kRaw) & 1, DEV_TIMEOUT_FULL);
         // ---- steps and minima, a token a lane: what is not there, or not finite, counts nothing ----
         const uint8_t* pg = raw + (lane >> 4) * kBlock;
         const bool there = tok_begin + n * kBT + 32 * wq + lane < tok_end;
@@ -352,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
         const float mid = k_mid * ks, hi = __half2float(__float2half_rn(mid));
         const uint32_t terms = pack_f16(hi, mid - hi);                                  // met by {a, a, b, b} of the row's sum a + b
         const uint32_t k_step = pack_f16(kv4_step(kp) * ks, kv4_step(kp) * ks);
-        bwait(&k_empty[s], ((blk / kRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
+        lazy_wait(&k_empty[s], ((blk / kRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
         // (A ring of four stages is enough: the S product of stage blk - 2, whose K stood here, was issued behind the P V products of
         // stage blk - 4, which had waited for every softmax warp.)
         if (lane == 0)
@@ -367,11 +417,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
         for (int u = 0; u < 4; ++u) {
           const uint4 v = (q & 2) ? make_uint4(next.z, next.w, next.x, next.y) : next;
           if (u < 3) next = *reinterpret_cast<const uint4*>(src + ((u + 1) >> 1) * kBlock + ((u + 1) & 1) * (4 * D));
-          const __half2 step = bits_h2(__shfl_sync(0xffffffffu, k_step, u * 8 + r));
+          const uint32_t step = __shfl_sync(0xffffffffu, k_step, u * 8 + r);
           const uint32_t word[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            *reinterpret_cast<uint4*>(dst + u * 2048 + ((((q & 1) * 4 + (x ^ (q & 2))) ^ r) << 4)) = k_values(word[x], step);
+            *reinterpret_cast<uint4*>(dst + u * 2048 + ((((q & 1) * 4 + (x ^ (q & 2))) ^ r) << 4)) = k_values(word[x], kc, step);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&raw_empty[rs]);
@@ -382,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
           // ---- Q: one row a thread, scaled by its largest value, in place; its sum; the factor of its scores ----
           const int row = 32 * wq + lane;
           uint8_t* qrow = smem + kOffQ + row * 128;
-          bwait(q_full, item & 1, DEV_TIMEOUT_FULL);
+          lazy_wait(q_full, item & 1, DEV_TIMEOUT_FULL);
           uint32_t top = 0;
           float sum = 0.f;
 #pragma unroll 4
@@ -420,6 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
   } else if (warp < 12) {
     // ------------------------------------ codes to V ------------------------------------
     regs_dec<64>();
+    const CodeConst vc = code_const(0.f);
     const int wq = warp - 8;
     uint32_t blk = 0;
     for (int item = 0; item < item_end; ++item) {
@@ -428,14 +479,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
       for (int n = 0; n < nblk; ++n, ++blk) {
         const int rs = blk % kRaw, s = blk % kRing;
         const uint8_t* raw = smem + kOffRaw + rs * kRawBytes + 2 * wq * kBlock;
-        bwait(&raw_full[rs], (blk / kRaw) & 1, DEV_TIMEOUT_FULL);
+        lazy_wait(&raw_full[rs], (blk / kRaw) & 1, DEV_TIMEOUT_FULL);
         const bool there = tok_begin + n * kBT + 32 * wq + lane < tok_end;
         uint32_t vp = there ? *reinterpret_cast<const uint32_t*>(raw + (lane >> 4) * kBlock + kv4_v_pairs(D) + 4 * (lane & 15)) : 0u;
         bool v_bad;
         const float vs = pow2(-v_scale(vp, &v_bad));
         if (v_bad) vp = 0;
         const uint32_t v_pair = pack_f16(kv4_step(vp) * vs, kv4_min(vp) * vs);
-        bwait(&v_empty[s], ((blk / kRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
+        lazy_wait(&v_empty[s], ((blk / kRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
         // unit: 16 bytes = values [16 g, 16 g + 16) of a token pair, chunks 2 g and 2 g + 1 of both tokens
         const int g = lane & 7, r = lane >> 3;
         const uint8_t* src = raw + kv4_v_codes(D) + r * D + g * 16;
@@ -447,13 +498,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
           if (u < 3) next = *reinterpret_cast<const uint4*>(src + ((u + 1) >> 1) * kBlock + ((u + 1) & 1) * (4 * D));
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const __half2 sm = bits_h2(__shfl_sync(0xffffffffu, v_pair, u * 8 + 2 * r + e));
-            const __half2 step = __low2half2(sm), low = __high2half2(sm);
+            const uint32_t sm = __shfl_sync(0xffffffffu, v_pair, u * 8 + 2 * r + e);
+            const uint32_t step = __byte_perm(sm, sm, 0x1010), low = __byte_perm(sm, sm, 0x3232);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const uint32_t a = x ? v.z : v.x, b = x ? v.w : v.y;
               *reinterpret_cast<uint4*>(dst + u * 2048 + e * 128 + (((2 * (g & 3) + (x ^ (g >> 2))) ^ (2 * r + e)) << 4)) =
-                  v_values(e ? __byte_perm(a, b, 0x7632) : __byte_perm(a, b, 0x5410), step, low);
+                  v_values(e ? __byte_perm(a, b, 0x7632) : __byte_perm(a, b, 0x5410), vc, step, low);
             }
           }
         }
