@@ -552,13 +552,15 @@ size_t attention_smem_bytes(int head_dim) {
   return head_dim == 64 ? AttnSmem<64>::kTotal : AttnSmem<128>::kTotal;
 }
 
+// (rule to be measured)
+constexpr int kFewRows = 16;
 void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, const void* kv_pool,
                       int64_t n_pages, float* part_o, float* part_ml, int tok_per_tile, int n_sm, int* status,
-                      cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, bool four, float* lse) {
+                      cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, bool four, float* lse, int max_rows) {
   if (four || (use_tc && dm.head_dim == 128)) {
-    if (four && use_tc && dm.head_dim == 128 &&
+    if (four && use_tc && dm.head_dim == 128 && max_rows > kFewRows &&
         launch_attention_kv4_tc(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st)) {
-    } else if (four) launch_attention_kv4(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st);
+    } else if (four) launch_attention_kv4(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, max_rows, status, st);
     else launch_attention_tc_main(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st, layout_settled);
     // (the kernel in front signals its dependents when the list is settled)
     if (!whole) (dm.head_dim == 64 ? launch_combine<64> : launch_combine<128>)(bl, dm, o, lse, part_o, part_ml, n_sm, st, tiles, step, 1);

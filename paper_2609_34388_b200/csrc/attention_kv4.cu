@@ -1,16 +1,24 @@
 // Hybrid-mask paged attention over a pool in 4 bits, few query rows per kv head (mma.sync).
 //
-// Work items, masks and the combine kernel are those of attention.cu.  With x_j = m_j + s_j c_j for a row of K or V (kv4.cuh):
-//   score = s_K (q . (c_K - 8)) + (m_K + 8 s_K) sum(q)
-//   o     = sum_j (p_j s_Vj) (c_Vj - 8) + sum_j p_j (m_Vj + 8 s_Vj)
-// so the matrix instructions multiply codes, which bf16 holds exactly, and steps and minima enter in fp32: the scores are exact
-// up to fp32 sums, and the only rounding ahead of the result is that of p s_V to bf16 (2^-9 of each term, like p in the bf16
-// kernels).
+// Work items, masks and the combine kernel are those of attention.cu.  With x_j = m_j + s_j c_j for a row of K or V (kv4.cuh)
+//   score = s_K (q . c_K) + m_K sum(q),      o = sum_j (p_j s_Vj) c_Vj + sum_j p_j m_Vj
+// the matrix instructions multiply codes, which are exact, and steps and minima enter in fp32.  Both products are taken transposed,
+// S^T = K Q^T and O^T = V^T P^T, since there are fewer rows (the 8 columns of a product) than tokens or values (its 16 rows): one
+// token of four or five query heads fills half a product, not a quarter, and every lane needs the step and minimum of two tokens
+// only, not of four.  P^T turns from accumulators to operand by one movmatrix per eight tokens.
 //
-// One producer warp streams the item's blocks of 64 tokens, one bulk copy per page and head, into a ring; eight consumer warps
-// take 16 query rows each and share the blocks among themselves where there are fewer row tiles than warps.  The codes are
-// laid out such that a lane reads its part of a B operand with one 16-byte access and nothing goes through registers of other
-// lanes; the values of a row then stand at positions of the contraction that are permuted, and Q is loaded in the same order.
+// Single rows are bound by the bytes of the cache, if only the instructions that unpack the codes are few.  The operands are fp16,
+// and a code masked out of its word in the lowest 8 bits of a half IS an fp16 number, a subnormal one: c 2^-24 or 16 c 2^-24.  So
+// eight codes cost one shift and four ANDs, where bf16 takes three shifts, four masks with an exponent and four subtractions
+// (694 instructions for a page of 16 tokens, %OLD%).  What belongs to the 16 is divided out of Q and of the result.  Q is scaled by a power
+// of two for all rows of a warp, and the steps of V, as factors of P, by another that follows the largest of them; so a score
+// is off by 2^-30 of the largest row's scores at most, and p s_V by 2^-12 of itself.
+//
+// A warp is alone with its pages: it requests them itself (one bulk copy per page and head, into a ring of its own), every
+// kWarps-th of the item's, and runs ahead of itself into the next item.  The warps' results are merged at the end of an item.
+#include <cuda_fp16.h>
+#include <type_traits>
+
 #include "kernels.h"
 #include "kv4.cuh"
 
@@ -18,23 +26,25 @@ namespace recg {
 
 namespace {
 
-constexpr int kBlockTokens = 64;
-constexpr int kPagesPerBlock = kBlockTokens / kPageSize;
-constexpr int kConsumers = 8;
-constexpr int kThreads = (kConsumers + 1) * 32;
+constexpr int kSlots = 4;              // pages that a warp has on their way
 constexpr uint32_t kSpin = 1u << 22;
 constexpr float kNoRef = -1e30f;       // reference maximum of a row that has seen no token yet
 constexpr float kHeadroom = 8.f;       // a row's reference maximum moves when it is outgrown by more than 2^8
+constexpr float kLift = 7.f;           // probabilities stand as 2^7 p: with steps below 1 at most 2^15
 
-template <int D>
-struct Smem {
+// NT: groups of eight query rows
+template <int D, int NT>
+struct Shape {
+  static constexpr int kWarps = NT == 1 ? 16 : 12;
+  static constexpr int kThreads = kWarps * 32;
   static constexpr int kBlock = kv4_block_bytes(D);
-  static constexpr int kStage = kPagesPerBlock * kBlock;
-  static constexpr int kMergeFloats = (D / 2 + 4) * 32;                     // per warp: o, reference maxima, sums
-  static constexpr int kMerge = kConsumers * kMergeFloats * 4;
-  static constexpr int kStages = 16;
-  static constexpr int kBars = kStages * kStage + kMerge;
-  static constexpr int kTotal = kBars + 2 * kStages * 8;
+  static constexpr int kRing = kWarps * kSlots * kBlock;
+  static constexpr int kRowPad = D + 4;                            // floats from row to row of a merged part
+  static constexpr int kRows = 8 * NT;
+  static constexpr int kMerge = kWarps * kRows * kRowPad * 4;      // [warp][row][value]; values D and D + 1: reference maximum, sum
+  static constexpr int kBars = kRing + kMerge;
+  static constexpr int kTotal = kBars + kWarps * kSlots * 8;
+  static_assert(kTotal <= 227 * 1024, "shared memory budget");
 };
 
 struct Params {
@@ -57,8 +67,21 @@ struct Params {
   int* status;
 };
 
-__device__ __forceinline__ void consumer_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-
+// D(16x8, f32) += A(16x16, f16, row) * B(16x8, f16, col)
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return reinterpret_cast<const uint32_t&>(h);
+}
 template <int N>
 __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
   if constexpr (N == 4) {
@@ -69,340 +92,383 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
     w[0] = t.x; w[1] = t.y;
   }
 }
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, 1) attention_kv4_kernel(Params P) {
-  using SM = Smem<D>;
-  constexpr int kStages = SM::kStages;
+template <int D, int NT>
+__global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kernel(Params P) {
+  using SH = Shape<D, NT>;
   constexpr int NW = D / 32;             // words of codes a lane holds of a token (K) or token pair (V)
+  constexpr int W = SH::kWarps;
   extern __shared__ __align__(128) uint8_t smem[];
-  uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + SM::kBars);
-  uint64_t* empty_bar = full_bar + kStages;
-  float* merge = reinterpret_cast<float*>(smem + kStages * SM::kStage);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(&full_bar[s], 1);
-      mbar_init(&empty_bar[s], kConsumers);
-    }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + SH::kBars) + warp * kSlots;
+  uint8_t* ring = smem + warp * kSlots * SH::kBlock;
+  float* merge = reinterpret_cast<float*>(smem + SH::kRing);
+  if (lane == 0) {
+    for (int s = 0; s < kSlots; ++s) mbar_init(&full[s], 1);
     fence_barrier_init();
   }
-  __syncthreads();
+  __syncwarp();
   griddep_wait();
   griddep_launch();
 
-  // the CTA walks two ranges of the item list one after the other (see the layout kernel)
+  // the CTA walks two ranges of the item list one after the other (see the layout kernel); rows beyond SH::kRows of a tile take
+  // further turns over its pages
   const int4 r4 = *reinterpret_cast<const int4*>(P.cta_off + 4 * blockIdx.x);
-  const int range_n0 = r4.y - r4.x;
-  const int item_end = range_n0 + (r4.w - r4.z);
+  const int range_n0 = r4.y - r4.x, item_end = range_n0 + (r4.w - r4.z);
   auto item_at = [&](int i) { return i < range_n0 ? r4.x + i : r4.z + (i - range_n0); };
-  uint32_t it = 0;  // running block counter, identical in producer and consumers
-  bool aborted = false;
+  auto turns_of = [&](int ntok) { return (ntok * P.group + SH::kRows - 1) / SH::kRows; };
+  auto first_page = [&](const AttnItem& w) { return w.blk_begin * 4 + warp; };
+  auto end_page = [&](const AttnItem& w) { return min(w.blk_end * 4, (w.kv_len + kPageSize - 1) / kPageSize); };
 
-  if (warp == kConsumers) {
-    // ------------------------------ producer ------------------------------
-    for (int item = 0; item < item_end && !aborted; ++item) {
-      const AttnItem w = P.items[item_at(item)];
-      const int n_req_pages = (w.kv_len + kPageSize - 1) / kPageSize;
-      const int* pt = P.page_table + (size_t)w.req * P.pt_stride;
-      // lanes 0..3 each own one page of the block; ids are fetched one block ahead of their use
-      auto fetch_page = [&](int n) -> int {
-        const int lp = n * kPagesPerBlock + lane;
-        return lane < kPagesPerBlock && n < w.blk_end && lp < n_req_pages ? __ldg(pt + lp) : -1;
-      };
-      int pg_next = fetch_page(w.blk_begin);
-      for (int n = w.blk_begin; n < w.blk_end; ++n, ++it) {
-        const int s = it % kStages;
-        int my_pg = pg_next;
-        pg_next = fetch_page(n + 1);
-        if (my_pg >= P.n_pages) {
-          set_status(P.status, DEV_BAD_INDEX);
-          my_pg = -1;
-        }
-        if (!mbar_wait(&empty_bar[s], ((it / kStages) & 1) ^ 1, kSpin)) {
-          set_status(P.status, DEV_TIMEOUT_EMPTY);
-          aborted = true;
-          break;
-        }
-        const unsigned valid = __ballot_sync(0xffffffffu, my_pg >= 0);
-        if (lane == 0) {
-          if (valid == 0) mbar_arrive(&full_bar[s]);
-          else mbar_arrive_expect_tx(&full_bar[s], __popc(valid) * SM::kBlock);
-        }
-        __syncwarp();
-        if (my_pg >= 0)
-          bulk_g2s(smem + s * SM::kStage + lane * SM::kBlock, P.pool + kv4_block_base(P.n_pages, P.n_kv, D, P.layer, my_pg, w.kv_head),
-                   SM::kBlock, &full_bar[s]);
-        __syncwarp();
+  // ---- what the warp requests next: a page of (item, turn), its id already on its way ----
+  int f_item = -1, f_page = 0, f_first = 0, f_end = 0, f_turns = 0, f_head = 0, f_id = 0;
+  const int* f_table = nullptr;
+  auto advance = [&]() {
+    f_page += W;
+    if (f_page >= f_end) {
+      if (--f_turns > 0 && f_first < f_end) {
+        f_page = f_first;
+      } else {
+        do {
+          if (++f_item >= item_end) return;
+          const AttnItem w = P.items[item_at(f_item)];
+          f_page = f_first = first_page(w);
+          f_end = end_page(w);
+          f_turns = turns_of(w.ntok);
+          f_head = w.kv_head;
+          f_table = P.page_table + (size_t)w.req * P.pt_stride;
+        } while (f_page >= f_end);
       }
     }
-    if (aborted && lane == 0)         // let copies already in flight land before the CTA may exit
-      for (int s = 0; s < kStages; ++s)
-        for (uint32_t i = 0; i < (1u << 14); ++i) {
-          if (mbar_try_wait(&full_bar[s], 0) || mbar_try_wait(&full_bar[s], 1)) break;
-          __nanosleep(64);
-        }
-    return;
-  }
+    f_id = __ldg(f_table + f_page);
+  };
+  auto request = [&](int slot) {
+    if (f_item >= item_end) return;
+    if (lane == 0) {
+      if (f_id < 0 || f_id >= P.n_pages) {
+        set_status(P.status, DEV_BAD_INDEX);
+        mbar_arrive(&full[slot]);
+      } else {
+        mbar_arrive_expect_tx(&full[slot], SH::kBlock);
+        bulk_g2s(ring + slot * SH::kBlock, P.pool + kv4_block_base(P.n_pages, P.n_kv, D, P.layer, f_id, f_head), SH::kBlock, &full[slot]);
+      }
+    }
+    advance();
+  };
+  advance();
+  for (int s = 0; s < kSlots; ++s) request(s);
 
-  // ------------------------------ consumers ------------------------------
-  const int g = lane >> 2, t = lane & 3;
-
+  uint32_t count = 0;     // pages worked on so far
+  bool aborted = false;
   for (int item = 0; item < item_end; ++item) {
     const AttnItem w = P.items[item_at(item)];
-    const int R = w.ntok * P.group;
-    const int RW = (R + 15) >> 4, KW = kConsumers / RW;
-    const int rw = warp % RW, kw = warp / RW;
-    const bool active = kw < KW;
-
-    // Q fragments and visibility of this lane's two rows (g and g + 8 of the warp's 16).  Lane t holds the values
-    // [32 t, 32 t + 32) (d = 128) of a row, its word j of codes the values 8 j .. of these: k-step 2 j + u of the products
-    // takes the pairs 2 u and 2 u + 1 of word j.
-    uint32_t qf[D / 16][4];
-    float qsum[2];
-    int climit[2], vlo[2], vhi[2], row_tok[2], row_head[2];
-    bool rvalid[2];
+    const int R = w.ntok * P.group, n_turns = turns_of(w.ntok);
+    for (int turn = 0; turn < n_turns; ++turn) {
+      const int row0 = turn * SH::kRows;
+      // ---- Q as B operands: column g of row group nt.  Lane t holds the values [D / 4 t, D / 4 (t + 1)) of a row; k-step 2 j + u takes the
+      // pairs 2 u and 2 u + 1 of word j of codes, the second of which the K operand holds times 16 ----
+      uint32_t qf[NT][D / 16][2];
+      float qs[NT][2];                   // sums of the rows 2 t and 2 t + 1, times the scale of the scores
+      float factor;                      // what makes a product of this scaled Q and codes 2^-24 c a score
+      int climit[NT][2], vlo[NT][2], vhi[NT][2];
+      {
+        uint4 raw[NT][NW];
+        uint32_t top = 0;
 #pragma unroll
-    for (int hh = 0; hh < 2; ++hh) {
-      const int rho = rw * 16 + g + hh * 8;
-      rvalid[hh] = active && rho < R;
-      const int j = rho / P.group, hg = rho - j * P.group;
-      const int tok = w.tok0 + (rvalid[hh] ? j : 0);
-      row_tok[hh] = tok;
-      row_head[hh] = w.kv_head * P.group + hg;
-      climit[hh] = rvalid[hh] ? P.tok_climit[tok] : -1;
-      vlo[hh] = rvalid[hh] ? P.tok_lo[tok] : 0;
-      vhi[hh] = rvalid[hh] ? P.tok_hi[tok] : 0;
-      const uint4* src = reinterpret_cast<const uint4*>(P.q + ((size_t)tok * P.n_q + row_head[hh]) * D) + t * NW;
-      float sum = 0.f;
+        for (int nt = 0; nt < NT; ++nt) {
+          const int rho = row0 + nt * 8 + g, j = rho / P.group;
+          const bool there = rho < R;
+          const uint4* src = reinterpret_cast<const uint4*>(P.q + ((size_t)(w.tok0 + (there ? j : 0)) * P.n_q + w.kv_head * P.group + (there ? rho - j * P.group : 0)) * D) + t * NW;
+          float sum = 0.f;
 #pragma unroll
-      for (int j2 = 0; j2 < NW; ++j2) {
-        const uint4 v = rvalid[hh] ? __ldg(src + j2) : make_uint4(0, 0, 0, 0);
-        qf[2 * j2][hh] = v.x;
-        qf[2 * j2][hh + 2] = v.y;
-        qf[2 * j2 + 1][hh] = v.z;
-        qf[2 * j2 + 1][hh + 2] = v.w;
-        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+          for (int k = 0; k < NW; ++k) {
+            raw[nt][k] = there ? __ldg(src + k) : make_uint4(0, 0, 0, 0);
+            const uint32_t u[4] = {raw[nt][k].x, raw[nt][k].y, raw[nt][k].z, raw[nt][k].w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += __uint_as_float(u[i] << 16) + __uint_as_float(u[i] & 0xffff0000u);
-      }
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      qsum[hh] = sum + __shfl_xor_sync(0xffffffffu, sum, 2);
-    }
-
-    float o[D / 8][4];
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float ref[2] = {kNoRef, kNoRef};     // reference maximum (powers of two), the same in the four lanes of a row
-    float l[2] = {0.f, 0.f};             // this lane's part of the row's sum of probabilities
-    float om[2] = {0.f, 0.f};            // ... and of the part of o that all its values share: sum p (m + 8 s)
-
-    for (int n = w.blk_begin; n < w.blk_end; ++n, ++it) {
-      const int s = it % kStages;
-      if (!aborted && !mbar_wait(&full_bar[s], (it / kStages) & 1, kSpin)) {
-        set_status(P.status, DEV_TIMEOUT_FULL);
-        aborted = true;
-      }
-      if (!aborted && active && ((n - w.blk_begin) % KW) == kw) {
-        const int n_pg = min(kPagesPerBlock, (w.kv_len - n * kBlockTokens + kPageSize - 1) / kPageSize);
-#pragma unroll 1
-        for (int p = 0; p < n_pg; ++p) {
-          const uint8_t* pg = smem + s * SM::kStage + p * SM::kBlock;
-          const int pos0 = n * kBlockTokens + p * kPageSize;
-          // ---- S = Q C_K^T over the page's 16 tokens: n-tile h holds tokens 8 h .. 8 h + 7 ----
-          float sc[2][4];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t word[NW];
-            load_words(word, pg + (g + 8 * h) * (D / 2) + t * (NW * 4));
-            sc[h][0] = sc[h][1] = sc[h][2] = sc[h][3] = 0.f;
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-              mma_bf16_16816(sc[h], qf[k], kv4_pair(word[k >> 1], 2 * (k & 1)), kv4_pair(word[k >> 1], 2 * (k & 1) + 1));
-          }
-          // ---- scores in powers of two; columns 8 h + 2 t + c, rows e >> 1 ----
-          float sk[2][2], mk[2][2], sv[2][2], mv[2][2];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint2 kp = *reinterpret_cast<const uint2*>(pg + kv4_k_pairs(D) + 4 * (8 * h + 2 * t));
-            const uint2 vp = *reinterpret_cast<const uint2*>(pg + kv4_v_pairs(D) + 4 * (8 * h + 2 * t));
-            const uint32_t kk[2] = {kp.x, kp.y}, vv[2] = {vp.x, vp.y};
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              sk[h][c] = kv4_step(kk[c]) * P.scale_log2;
-              mk[h][c] = fmaf(8.f, kv4_step(kk[c]), kv4_min(kk[c])) * P.scale_log2;
-              sv[h][c] = kv4_step(vv[c]);
-              mv[h][c] = fmaf(8.f, sv[h][c], kv4_min(vv[c]));
+            for (int i = 0; i < 4; ++i) {
+              sum += __uint_as_float(u[i] << 16) + __uint_as_float(u[i] & 0xffff0000u);
+              const uint32_t lo = u[i] & 0x7fffu, hi = (u[i] >> 16) & 0x7fffu;
+              top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));      // (a row that is not finite does not concern the others)
             }
           }
-          // (rows that do not exist carry a limit of -1 and are masked everywhere)
-          const bool need_mask = __any_sync(0xffffffffu, pos0 + kPageSize - 1 > min(climit[0], climit[1]));
-          unsigned see = 0xff;
-          if (need_mask) {
-            see = 0;
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            qs[nt][e] = __shfl_sync(0xffffffffu, sum, (2 * t + e) * 4) * P.scale_log2;
+            const int rv = row0 + nt * 8 + 2 * t + e, tok = w.tok0 + rv / P.group;
+            const bool is = rv < R;      // (a row that does not exist needs no mask: nobody reads it)
+            climit[nt][e] = is ? P.tok_climit[tok] : 0x7fffffff;
+            vlo[nt][e] = is ? P.tok_lo[tok] : 0;
+            vhi[nt][e] = is ? P.tok_hi[tok] : 0;
+          }
+        }
+        // the largest value of all rows goes to [2^8, 2^9) (as far as the exponent allows: a factor and its inverse are normal numbers)
+        const int e = max(-100, min(100, (int)(__reduce_max_sync(0xffffffffu, top) >> 7) - 127 - 8));
+        const float down = pow2(-e), down16 = pow2(-e - 4);
+        factor = pow2(e) * 16777216.f * P.scale_log2;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int k = 0; k < NW; ++k) {
+            const uint4 v = raw[nt][k];
+            qf[nt][2 * k][0] = pack_f16(__uint_as_float(v.x << 16) * down, __uint_as_float(v.x & 0xffff0000u) * down);
+            qf[nt][2 * k][1] = pack_f16(__uint_as_float(v.y << 16) * down16, __uint_as_float(v.y & 0xffff0000u) * down16);
+            qf[nt][2 * k + 1][0] = pack_f16(__uint_as_float(v.z << 16) * down, __uint_as_float(v.z & 0xffff0000u) * down);
+            qf[nt][2 * k + 1][1] = pack_f16(__uint_as_float(v.w << 16) * down16, __uint_as_float(v.w & 0xffff0000u) * down16);
+          }
+      }
+
+      float o[NT][D / 16][4];              // O^T: rows (values) i, columns 2 t and 2 t + 1; see the writer for which values
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
+      // per row (columns 2 t, 2 t + 1; the same in all lanes of a column): reference maximum in powers of two; this lane's part of the
+      // sum of probabilities and of sum p m
+      float ref[NT][2], l[NT][2], om[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        ref[nt][0] = ref[nt][1] = kNoRef;
+        l[nt][0] = l[nt][1] = om[nt][0] = om[nt][1] = 0.f;
+      }
+      float s_top = 0.f, s_inv = 0.f;      // steps of V are below s_top (a power of two), and P holds p s_V 2^7 / s_top
+
+      int lim = 0x7fffffff;                // the position up to which every row of the warp sees everything
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) lim = min(lim, min(climit[nt][0], climit[nt][1]));
+      lim = __reduce_min_sync(0xffffffffu, lim);
+      const int p_end = end_page(w);
+
+      for (int p = first_page(w); p < p_end; p += W, ++count) {
+        const int slot = count % kSlots;
+        if (!aborted && !mbar_wait(&full[slot], (count / kSlots) & 1, kSpin)) {
+          set_status(P.status, DEV_TIMEOUT_FULL);
+          aborted = true;
+        }
+        const uint8_t* pg = ring + slot * SH::kBlock;
+        const int pos0 = p * kPageSize;
+        auto work = [&](auto masked) {
+          constexpr bool MASK = decltype(masked)::value;
+          // ---- S^T = C_K Q^T: rows g and g + 8 are the page's tokens ----
+          float sc[NT][4];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+          {
+            uint32_t k0[NW], k1[NW];
+            load_words(k0, pg + g * (D / 2) + t * (NW * 4));
+            load_words(k1, pg + (g + 8) * (D / 2) + t * (NW * 4));
+#pragma unroll
+            for (int j = 0; j < NW; ++j) {
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const uint32_t w0 = u ? k0[j] >> 8 : k0[j], w1 = u ? k1[j] >> 8 : k1[j];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+                  mma_f16(sc[nt], w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qf[nt][2 * j + u][0], qf[nt][2 * j + u][1]);
+              }
+            }
+          }
+          float sk[2], mk[2], sv[2], mv[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t kp = *reinterpret_cast<const uint32_t*>(pg + kv4_k_pairs(D) + 4 * (8 * h + g));
+            const uint32_t vp = *reinterpret_cast<const uint32_t*>(pg + kv4_v_pairs(D) + 4 * (8 * h + g));
+            sk[h] = kv4_step(kp) * factor;
+            mk[h] = kv4_min(kp);
+            sv[h] = kv4_step(vp);
+            mv[h] = kv4_min(vp);
+          }
+          bool see[NT][4];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int pos = pos0 + g + 8 * (e >> 1), c = e & 1;
+              see[nt][e] = !MASK || pos <= climit[nt][c] || (pos >= vlo[nt][c] && pos < vhi[nt][c]);
+            }
+          // (a token behind the request's end is seen by no row: its step may be anything)
+          if (MASK) {
+            const int kv_len = w.kv_len;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int pos = pos0 + 8 * h + 2 * t + (e & 1), hh = e >> 1;
-                if (pos <= climit[hh] || (pos >= vlo[hh] && pos < vhi[hh])) see |= 1u << (4 * h + e);
-              }
+              if (pos0 + g + 8 * h >= kv_len) sv[h] = mv[h] = 0.f;
           }
-          float pr[2][4];
+          float pr[NT][4];
           auto scores = [&]() {
             float top = -INFINITY;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                float y = fmaf(sc[h][e], sk[h][e & 1], fmaf(mk[h][e & 1], qsum[e >> 1], -ref[e >> 1]));
-                if (need_mask && !((see >> (4 * h + e)) & 1u)) y = -INFINITY;
-                pr[h][e] = y;
+                float y = fmaf(sc[nt][e], sk[e >> 1], fmaf(mk[e >> 1], qs[nt][e & 1], kLift - ref[nt][e & 1]));
+                if (MASK && !see[nt][e]) y = -INFINITY;
+                pr[nt][e] = y;
                 top = fmaxf(top, y);
               }
             return top;
           };
-          if (__any_sync(0xffffffffu, scores() > kHeadroom)) {
-            // some row's reference maximum moves, and what has been summed up is scaled to it
+          if (__any_sync(0xffffffffu, scores() > kHeadroom + kLift || fmaxf(sv[0], sv[1]) >= s_top)) {
+            // some row's reference maximum moves, or the scale of the steps does: what has been summed up is scaled to the new ones
+            const float v = fmaxf(sv[0], sv[1]);
+            const uint32_t top = __reduce_max_sync(0xffffffffu, v > 0.f ? __float_as_uint(v) : 0u);      // (NaN does not take part)
+            const float next_top = fmaxf(s_top, pow2(max(-100, (int)(top >> 23) - 127 + 1)));
+            const float fs = s_top / next_top;
+            s_top = next_top;
+            s_inv = 1.f / next_top;
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-              float z = -INFINITY;
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int h = 0; h < 2; ++h)
+              for (int c = 0; c < 2; ++c) {
+                float z = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                  if ((see >> (4 * h + 2 * hh + c)) & 1u) z = fmaxf(z, fmaf(sc[h][2 * hh + c], sk[h][c], mk[h][c] * qsum[hh]));
-              z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 1));
-              z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 2));
-              const float next = fmaxf(ref[hh], z), f = exp2f(ref[hh] - next);
-              ref[hh] = next;
-              l[hh] *= f;
-              om[hh] *= f;
+                for (int h = 0; h < 2; ++h)
+                  if (see[nt][2 * h + c]) z = fmaxf(z, fmaf(sc[nt][2 * h + c], sk[h], mk[h] * qs[nt][c]));
 #pragma unroll
-              for (int i = 0; i < D / 8; ++i) {
-                o[i][2 * hh] *= f;
-                o[i][2 * hh + 1] *= f;
+                for (int x = 4; x < 32; x <<= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, x));
+                // (it moves where it is outgrown by anything: the other rows' probabilities stay the same)
+                const float next = z > ref[nt][c] + kHeadroom || ref[nt][c] == kNoRef ? fmaxf(ref[nt][c], z) : ref[nt][c];
+                const float f = exp2f(ref[nt][c] - next);
+                ref[nt][c] = next;
+                l[nt][c] *= f;
+                om[nt][c] *= f;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                  o[nt][i][c] *= f * fs;
+                  o[nt][i][2 + c] *= f * fs;
+                }
               }
-            }
             scores();
           }
-          // ---- probabilities; O += (P s_V) C_V ----
+          // ---- probabilities; O^T += C_V^T (P s_V)^T ----
+          const float svs[2] = {sv[0] * s_inv, sv[1] * s_inv};
+          uint32_t b[NT][2];
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int nt = 0; nt < NT; ++nt) {
+            float ps[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float p_ = exp2f(pr[h][e]);
-              l[e >> 1] += p_;
-              float ps = p_ * sv[h][e & 1], pm = p_ * mv[h][e & 1];
-              if (need_mask && !((see >> (4 * h + e)) & 1u)) ps = pm = 0.f;      // (the step of a token that nobody wrote may be NaN)
-              om[e >> 1] += pm;
-              pr[h][e] = ps;
+              const float p_ = exp2f(pr[nt][e]);
+              l[nt][e & 1] += p_;
+              ps[e] = p_ * svs[e >> 1];
+              float pm = p_ * mv[e >> 1];
+              if (MASK && !see[nt][e]) ps[e] = pm = 0.f;
+              om[nt][e & 1] += pm;
             }
-          const uint32_t a[4] = {pack_bf16(pr[0][0], pr[0][1]), pack_bf16(pr[0][2], pr[0][3]), pack_bf16(pr[1][0], pr[1][1]),
-                                 pack_bf16(pr[1][2], pr[1][3])};
+            b[nt][0] = transpose8x8(pack_f16(ps[0], ps[1]));
+            b[nt][1] = transpose8x8(pack_f16(ps[2], ps[3]));
+          }
           uint32_t v0[NW], v1[NW];
           load_words(v0, pg + kv4_v_codes(D) + t * D + g * (D / 8));
           load_words(v1, pg + kv4_v_codes(D) + (t + 4) * D + g * (D / 8));
 #pragma unroll
-          for (int nt = 0; nt < D / 8; ++nt) mma_bf16_16816(o[nt], a, kv4_pair(v0[nt >> 2], nt & 3), kv4_pair(v1[nt >> 2], nt & 3));
-        }
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&empty_bar[s]);
-    }
-
+          for (int j = 0; j < NW; ++j)
 #pragma unroll
-    for (int hh = 0; hh < 2; ++hh) {
-      l[hh] += __shfl_xor_sync(0xffffffffu, l[hh], 1);
-      l[hh] += __shfl_xor_sync(0xffffffffu, l[hh], 2);
-      om[hh] += __shfl_xor_sync(0xffffffffu, om[hh], 1);
-      om[hh] += __shfl_xor_sync(0xffffffffu, om[hh], 2);
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t w0 = u ? v0[j] >> 8 : v0[j], w1 = u ? v1[j] >> 8 : v1[j];
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        o[i][2 * hh] += om[hh];
-        o[i][2 * hh + 1] += om[hh];
-      }
-    }
-
-    // ---- merge the warps that share a row tile ----
-    if (KW > 1) {
-      float* mine = merge + warp * SM::kMergeFloats;
-      if (active && kw > 0) {
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) mine[(i * 4 + e) * 32 + lane] = o[i][e];
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          mine[(D / 2 + hh) * 32 + lane] = ref[hh];
-          mine[(D / 2 + 2 + hh) * 32 + lane] = l[hh];
-        }
-      }
-      consumer_bar();
-      if (active && kw == 0)
-        for (int k2 = 1; k2 < KW; ++k2) {
-          const float* oth = merge + (k2 * RW + rw) * SM::kMergeFloats;
-#pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            const float ro = oth[(D / 2 + hh) * 32 + lane], lo = oth[(D / 2 + 2 + hh) * 32 + lane];
-            const float next = fmaxf(ref[hh], ro), fa = exp2f(ref[hh] - next), fb = exp2f(ro - next);
-            ref[hh] = next;
-            l[hh] = l[hh] * fa + lo * fb;
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i) {
-              o[i][2 * hh] = o[i][2 * hh] * fa + oth[(i * 4 + 2 * hh) * 32 + lane] * fb;
-              o[i][2 * hh + 1] = o[i][2 * hh + 1] * fa + oth[(i * 4 + 2 * hh + 1) * 32 + lane] * fb;
+              for (int nt = 0; nt < NT; ++nt)
+                mma_f16(o[nt][2 * j + u], w0 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x000f000fu, w1 & 0x00f000f0u, b[nt][0], b[nt][1]);
             }
+        };
+        if (!aborted) {
+          if (pos0 + kPageSize - 1 > lim) work(std::true_type{});
+          else work(std::false_type{});
+        }
+        __syncwarp();
+        if (!aborted) request(slot);
+      }
+
+      // ---- the warps' parts meet: row (column 2 t + c of group nt), the D / 8 values of g that this lane holds ----
+      constexpr float k1 = 16777216.f, k16 = 1048576.f;      // 2^24 and 2^20
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float ls = l[nt][c], ms = om[nt][c];
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) {
+            ls += __shfl_xor_sync(0xffffffffu, ls, x);
+            ms += __shfl_xor_sync(0xffffffffu, ms, x);
+          }
+          float* row = merge + (warp * SH::kRows + nt * 8 + 2 * t + c) * SH::kRowPad;
+          // tile 2 w + u: its row g is value 8 (w / 2) + 4 u + (w & 1) of the D / 8 of g, its row g + 8 the value two further, times 16
+#pragma unroll
+          for (int x = 0; x < NW / 2; ++x)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const float (&e)[4] = o[nt][4 * x + u];          // word 2 x: even values
+              const float (&f)[4] = o[nt][4 * x + 2 + u];      // word 2 x + 1: odd values
+              *reinterpret_cast<float4*>(row + g * (D / 8) + 8 * x + 4 * u) =
+                  make_float4(fmaf(e[c] * k1, s_top, ms), fmaf(f[c] * k1, s_top, ms), fmaf(e[2 + c] * k16, s_top, ms), fmaf(f[2 + c] * k16, s_top, ms));
+            }
+          if (g == 0) {
+            row[D] = ref[nt][c] - kLift;
+            row[D + 1] = ls;
           }
         }
-      consumer_bar();  // scratch may be rewritten by the next item only after everyone has read it
-    }
-
-    // ---- write out: n-tile 4 w + i holds the values 8 (w / 2) + 2 i + (w & 1) of the D / 8 that column 2 t (+ 1) stands for ----
-    if (active && kw == 0 && !aborted) {
+      __syncthreads();
+      // a warp takes every kWarps-th row, a lane D / 32 consecutive values of it
+      const int rows = min(SH::kRows, R - row0);
+      for (int rr = warp; rr < rows; rr += W) {
+        float m_all = lane < W ? merge[(lane * SH::kRows + rr) * SH::kRowPad + D] : kNoRef;
+        const float m_mine = m_all, l_mine = lane < W ? merge[(lane * SH::kRows + rr) * SH::kRowPad + D + 1] : 0.f;
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        if (!rvalid[hh]) continue;
-        const int rho = rw * 16 + g + hh * 8;
+        for (int x = 16; x; x >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, x));
+        const float f_mine = exp2f(m_mine - m_all);
+        float l_all = f_mine * l_mine;
+#pragma unroll
+        for (int x = 16; x; x >>= 1) l_all += __shfl_xor_sync(0xffffffffu, l_all, x);
+        constexpr int E = D / 32;
+        float acc[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < W; ++k) {
+          const float f = __shfl_sync(0xffffffffu, f_mine, k);
+          const float* src = merge + (k * SH::kRows + rr) * SH::kRowPad + lane * E;
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e] = fmaf(f, src[e], acc[e]);
+        }
+        const int rho = row0 + rr, j = rho / P.group;
         if (w.part < 0) {
-          const float inv = l[hh] > 0.f ? 1.f / l[hh] : 0.f;
-          __nv_bfloat16* dst = P.o + ((size_t)row_tok[hh] * P.n_q + row_head[hh]) * D + t * (D / 4);
+          const size_t row = (size_t)(w.tok0 + j) * P.n_q + w.kv_head * P.group + rho - j * P.group;
+          const float inv = l_all > 0.f ? 1.f / l_all : 0.f * l_all;
+          uint32_t* dst = reinterpret_cast<uint32_t*>(P.o + row * D + lane * E);
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int x = 0; x < NW / 2; ++x) {
-              uint32_t out[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) out[i] = pack_bf16(o[8 * x + i][2 * hh + c] * inv, o[8 * x + 4 + i][2 * hh + c] * inv);
-              *reinterpret_cast<uint4*>(dst + c * (D / 8) + 8 * x) = make_uint4(out[0], out[1], out[2], out[3]);
-            }
-          if (P.lse && t == 0) P.lse[(size_t)row_tok[hh] * P.n_q + row_head[hh]] = log_sum_exp(ref[hh], l[hh]);
+          for (int e = 0; e < E / 2; ++e) dst[e] = pack_bf16(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+          if (P.lse && lane == 0) P.lse[row] = log_sum_exp(m_all, l_all);
         } else {
-          float* dst = P.part_o + ((size_t)w.part * 128 + rho) * D + t * (D / 4);
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int x = 0; x < NW / 2; ++x)
-#pragma unroll
-              for (int i = 0; i < 4; i += 2)
-                *reinterpret_cast<float4*>(dst + c * (D / 8) + 8 * x + 2 * i) =
-                    make_float4(o[8 * x + i][2 * hh + c], o[8 * x + 4 + i][2 * hh + c], o[8 * x + i + 1][2 * hh + c], o[8 * x + 5 + i][2 * hh + c]);
-          if (t == 0) *reinterpret_cast<float2*>(P.part_ml + ((size_t)w.part * 128 + rho) * 2) = make_float2(ref[hh], l[hh]);
+          float* dst = P.part_o + ((size_t)w.part * 128 + rho) * D + lane * E;
+          if constexpr (E == 4) *reinterpret_cast<float4*>(dst) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+          else *reinterpret_cast<float2*>(dst) = make_float2(acc[0], acc[1]);
+          if (lane == 0) *reinterpret_cast<float2*>(P.part_ml + ((size_t)w.part * 128 + rho) * 2) = make_float2(m_all, l_all);
         }
       }
+      __syncthreads();      // the parts may be overwritten
     }
   }
+  if (aborted && lane == 0)         // let copies already in flight land before the CTA may exit
+    for (int s = 0; s < kSlots; ++s)
+      for (uint32_t i = 0; i < (1u << 14); ++i) {
+        if (mbar_try_wait(&full[s], 0) || mbar_try_wait(&full[s], 1)) break;
+        __nanosleep(64);
+      }
+}
+
+template <int D, int NT>
+void launch_rows(const Params& P, int n_sm, cudaStream_t st) {
+  static bool configured[kMaxDevices] = {false};
+  if (first_use_on_device(configured))
+    cudaFuncSetAttribute(attention_kv4_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D, NT>::kTotal);
+  launch_pdl(attention_kv4_kernel<D, NT>, dim3(n_sm), dim3(Shape<D, NT>::kThreads), Shape<D, NT>::kTotal, st, P);
 }
 
 }  // namespace
 
 void launch_attention_kv4(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
-                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status, cudaStream_t st) {
-  static bool configured[kMaxDevices] = {false};
-  if (first_use_on_device(configured)) {
-    cudaFuncSetAttribute(attention_kv4_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<64>::kTotal);
-    cudaFuncSetAttribute(attention_kv4_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<128>::kTotal);
-  }
+                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int max_rows, int* status, cudaStream_t st) {
   Params P;
   P.items = bl.items;
   P.cta_off = bl.cta_off;
@@ -424,8 +490,8 @@ void launch_attention_kv4(const BatchLayout& bl, const Dims& dm, int layer, cons
   P.part_o = part_o;
   P.part_ml = part_ml;
   P.status = status;
-  if (dm.head_dim == 64) launch_pdl(attention_kv4_kernel<64>, dim3(n_sm), dim3(kThreads), Smem<64>::kTotal, st, P);
-  else launch_pdl(attention_kv4_kernel<128>, dim3(n_sm), dim3(kThreads), Smem<128>::kTotal, st, P);
+  if (dm.head_dim == 64) (max_rows <= 8 ? launch_rows<64, 1> : launch_rows<64, 2>)(P, n_sm, st);
+  else (max_rows <= 8 ? launch_rows<128, 1> : launch_rows<128, 2>)(P, n_sm, st);
 }
 
 }  // namespace recg

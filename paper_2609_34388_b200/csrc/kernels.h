@@ -219,13 +219,13 @@ bool launch_gemm_chain(void* s, const ChainOp* ops, int n_ops, int M, const Chai
 void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, const void* kv_pool,
                       int64_t n_pages, float* part_o, float* part_ml, int tok_per_tile, int n_sm, int* status,
                       cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, bool four = false,
-                      float* lse = nullptr);
+                      float* lse = nullptr, int max_rows = 128);
 void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse,
                               const void* kv_pool, int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status,
                               cudaStream_t st, bool layout_settled);
-// the same over a pool in 4 bits
+// the same over a pool in 4 bits; max_rows: the largest number of query rows (new tokens times query heads of a kv head) of a row tile
 void launch_attention_kv4(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
-                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status, cudaStream_t st);
+                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int max_rows, int* status, cudaStream_t st);
 // ... on the tcgen05 tensor cores (head_dim 128); false: not launched (no tensor map over q)
 bool launch_attention_kv4_tc(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
                              int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status, cudaStream_t st);

@@ -58,6 +58,7 @@ struct recg_ctx {
   bool layout_valid = false;
   bool layout_has_pages = false;
   bool layout_whole = false;     // no attention tile was cut: no combine kernel
+  int layout_rows = 128;         // query rows of its largest row tile (128: the lengths are on the device)
   int layout_tiles = 0;          // its row tiles, all kv heads (0: the lengths are on the device)
   // An attention kernel has been enqueued behind the last layout kernel.  The first one waits for its predecessors before it
   // reads the work list, and no thread of it signals its dependents before that wait: whatever runs behind it finds the list
@@ -370,6 +371,9 @@ recg_status upload_and_layout(recg_ctx* ctx, const recg_batch* b, bool need_page
       ctx->h_rows[r] = request_rows(b, r);
       tiles += (ctx->h_rows[r] + ctx->tok_per_tile - 1) / ctx->tok_per_tile;
     }
+    int most = 0;
+    for (int r = 0; r < b->n_req; ++r) most = std::max(most, std::min(ctx->h_rows[r], ctx->tok_per_tile));
+    ctx->layout_rows = most * (ctx->dm.n_q / ctx->dm.n_kv);
     tiles *= ctx->dm.n_kv;
     ctx->layout_tiles = tiles < (1 << 20) ? (int)tiles : 1 << 20;
     ctx->layout_whole = attention_whole_tiles(b->n_req, b->ctx_len, ctx->h_rows.data(), ctx->dm.n_kv, ctx->tok_per_tile, ctx->target_items);
@@ -775,6 +779,7 @@ recg_status recg_step_device(recg_ctx* ctx, const recg_device_batch* b, recg_log
   launch_pack_device(device_round(ctx, b), ctx->d_desc, ctx->d_dyn, ctx->d_status, ctx->stream);
   ctx->layout_whole = false;           // (the lengths are on the device)
   ctx->layout_tiles = 0;
+  ctx->layout_rows = 128;
   launch_layout(bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, false, b->kv_pool_pages, ctx->d_status, false, ctx->d_desc, nullptr, ctx->stream);
   ctx->list_settled = false;
   ctx->small_desc.n = 0;
@@ -948,7 +953,7 @@ static recg_status attention(recg_ctx* ctx, const recg_batch* batch, int32_t lay
   if (s != RECG_OK) return s;
   launch_attention(ctx->bl, ctx->dm, layer, q, o, ctx->last_pool, ctx->last_pool_pages, ctx->part_o, ctx->part_ml,
                    ctx->tok_per_tile, ctx->n_sm, ctx->d_status, ctx->stream, !(ctx->cfg.flags & RECG_FLAG_SIMT_ATTENTION),
-                   ctx->list_settled, ctx->layout_whole, ctx->layout_tiles, false, four_bits(ctx), lse);
+                   ctx->list_settled, ctx->layout_whole, ctx->layout_tiles, false, four_bits(ctx), lse, ctx->layout_rows);
   CU(cudaGetLastError());
   ctx->list_settled = true;
   return RECG_OK;

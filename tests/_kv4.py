@@ -60,9 +60,12 @@ def visible(L, v, b, corr=(), bc=0):
 
 
 def attention_bounds(q, k_codes, v_codes, see):
-    """How far kernels may be from `attention` (o before its own rounding, and lse): p times a step is rounded to bf16 once
-    (2^-8 of every term p s |c - 8|), everything else is fp32: a score's sum of exact products takes eight steps in an accumulator
-    that drops what is below 2^-22 of its largest term, and 2^x and its argument are good to 2^-21 of the exponents."""
+    """How far kernels may be from `attention` (o before its own rounding, and lse).
+
+    o: both kernels round to fp16, half a step being 2^-11.  One multiplies p s, rounded, with the code c: 2^-11 of every term p s c.
+    The other rounds p and m + s c: 2 x 2^-11 of every term p |m + s c|.  Everything else is fp32: a score's sum of exact products takes
+    eight or nine steps in an accumulator that drops what is below 2^-22 of its largest term, 2^x and its argument are good to 2^-21 of the
+    exponents, and sums over tokens to 2^-17."""
     (ck, sk, mk), (cv, sv, mv) = k_codes, v_codes
     n, nq, d = q.shape
     g = nq // ck.shape[1]
@@ -76,9 +79,10 @@ def attention_bounds(q, k_codes, v_codes, see):
         top = z.max(-1, keepdims=True)
         p = np.exp(z - top)
         p /= p.sum(-1, keepdims=True)
-        coded = p @ np.where(see.any(0)[:, None], sv[:, kh] * np.abs(cv[:, kh] - 8), 0.0)
-        rest = p @ np.where(see.any(0)[:, None], np.abs(mv[:, kh] + 8 * sv[:, kh]), 0.0)
-        o_err[:, h] = 2.0 ** -8 * coded + (2.0 ** -17 + 4 * score)[:, None] * (coded + rest)
+        some = see.any(0)[:, None]
+        coded, held = p @ np.where(some, sv[:, kh] * cv[:, kh], 0.0), p @ np.where(some, np.abs(mv[:, kh] + sv[:, kh] * cv[:, kh]), 0.0)
+        low = p @ np.where(some, np.abs(mv[:, kh]), 0.0)
+        o_err[:, h] = 2.0 ** -11 * np.maximum(coded, 2 * held) + (2.0 ** -17 + 4 * score)[:, None] * (coded + low)
         lse_err[:, h] = score + 2.0 ** -20 * (1 + np.abs(top[:, 0]) + math.log(see.shape[1]))
     return o_err, lse_err
 
