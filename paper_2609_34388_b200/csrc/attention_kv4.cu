@@ -14,8 +14,9 @@
 // of two for all rows of a warp, and the steps of V, as factors of P, by another that follows the largest of them; so a score
 // is off by 2^-30 of the largest row's scores at most, and p s_V by 2^-12 of itself.
 //
-// A warp is alone with its pages: it requests them itself (one bulk copy per page and head, into a ring of its own), every
-// kWarps-th of the item's, and runs ahead of itself into the next item.  The warps' results are merged at the end of an item.
+// A warp is alone with its pages: it requests them itself (one bulk copy per page and head, into a ring of its own) and runs ahead of
+// itself into the next item.  The warps are divided among the item's row groups, those of a group share its pages among
+// themselves, and their results are merged at the end of the item.
 #include <cuda_fp16.h>
 #include <type_traits>
 
@@ -26,25 +27,28 @@ namespace recg {
 
 namespace {
 
-constexpr int kSlots = 4;              // pages that a warp has on their way
 constexpr uint32_t kSpin = 1u << 22;
 constexpr float kNoRef = -1e30f;       // reference maximum of a row that has seen no token yet
 constexpr float kHeadroom = 8.f;       // a row's reference maximum moves when it is outgrown by more than 2^8
 constexpr float kLift = 7.f;           // probabilities stand as 2^7 p: with steps below 1 at most 2^15
 
-// NT: groups of eight query rows
+// NT: groups of eight query rows a warp has.  Two pages at a time are two independent chains of instructions (one token of one request,
+// 131072 of context: %ONE% us with one page, %TWO% with two), for which sixteen rows leave no registers.
 template <int D, int NT>
 struct Shape {
-  static constexpr int kWarps = NT == 1 ? 16 : 12;
+  static constexpr int kWarps = 12;
   static constexpr int kThreads = kWarps * 32;
+  static constexpr int kPages = NT == 1 ? 2 : 1;                   // pages of a chunk, which a warp works on at once
+  static constexpr int kSlots = NT == 1 ? 3 : 4;                   // chunks that a warp has on their way
   static constexpr int kBlock = kv4_block_bytes(D);
-  static constexpr int kRing = kWarps * kSlots * kBlock;
+  static constexpr int kRing = kWarps * kSlots * kPages * kBlock;
   static constexpr int kRowPad = D + 4;                            // floats from row to row of a merged part
   static constexpr int kRows = 8 * NT;
   static constexpr int kMerge = kWarps * kRows * kRowPad * 4;      // [warp][row][value]; values D and D + 1: reference maximum, sum
   static constexpr int kBars = kRing + kMerge;
   static constexpr int kTotal = kBars + kWarps * kSlots * 8;
   static_assert(kTotal <= 227 * 1024, "shared memory budget");
+  static_assert(kWarps * kRows >= 128 || NT == 1, "every row of a tile has a warp");
 };
 
 struct Params {
@@ -98,11 +102,11 @@ template <int D, int NT>
 __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kernel(Params P) {
   using SH = Shape<D, NT>;
   constexpr int NW = D / 32;             // words of codes a lane holds of a token (K) or token pair (V)
-  constexpr int W = SH::kWarps;
+  constexpr int W = SH::kWarps, PG = SH::kPages, kSlots = SH::kSlots, kSlot = PG * SH::kBlock;
   extern __shared__ __align__(128) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + SH::kBars) + warp * kSlots;
-  uint8_t* ring = smem + warp * kSlots * SH::kBlock;
+  uint8_t* ring = smem + warp * kSlots * kSlot;
   float* merge = reinterpret_cast<float*>(smem + SH::kRing);
   if (lane == 0) {
     for (int s = 0; s < kSlots; ++s) mbar_init(&full[s], 1);
@@ -112,60 +116,73 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
   griddep_wait();
   griddep_launch();
 
-  // the CTA walks two ranges of the item list one after the other (see the layout kernel); rows beyond SH::kRows of a tile take
-  // further turns over its pages
+  // the CTA walks two ranges of the item list one after the other (see the layout kernel)
   const int4 r4 = *reinterpret_cast<const int4*>(P.cta_off + 4 * blockIdx.x);
   const int range_n0 = r4.y - r4.x, item_end = range_n0 + (r4.w - r4.z);
   auto item_at = [&](int i) { return i < range_n0 ? r4.x + i : r4.z + (i - range_n0); };
-  auto turns_of = [&](int ntok) { return (ntok * P.group + SH::kRows - 1) / SH::kRows; };
-  auto first_page = [&](const AttnItem& w) { return w.blk_begin * 4 + warp; };
-  auto end_page = [&](const AttnItem& w) { return min(w.blk_end * 4, (w.kv_len + kPageSize - 1) / kPageSize); };
+  // of an item: warps per row group; this warp's group; its first chunk of pages and the end of all
+  struct Share { int warps, group, page, end; };
+  auto share_of = [&](const AttnItem& w) {
+    Share s;
+    s.warps = W / ((w.ntok * P.group + SH::kRows - 1) / SH::kRows);
+    s.group = warp / s.warps;
+    s.end = s.group * SH::kRows < w.ntok * P.group ? min(w.blk_end * 4, (w.kv_len + kPageSize - 1) / kPageSize) : 0;
+    s.page = w.blk_begin * 4 + (warp - s.group * s.warps) * PG;
+    return s;
+  };
 
-  // ---- what the warp requests next: a page of (item, turn), its id already on its way ----
-  int f_item = -1, f_page = 0, f_first = 0, f_end = 0, f_turns = 0, f_head = 0, f_id = 0;
+  // ---- what the warp requests next: a chunk of an item, its page ids already on their way ----
+  int f_item = -1, f_page = 0, f_step = 0, f_end = 0, f_head = 0, f_id[PG];
   const int* f_table = nullptr;
   auto advance = [&]() {
-    f_page += W;
-    if (f_page >= f_end) {
-      if (--f_turns > 0 && f_first < f_end) {
-        f_page = f_first;
-      } else {
-        do {
-          if (++f_item >= item_end) return;
-          const AttnItem w = P.items[item_at(f_item)];
-          f_page = f_first = first_page(w);
-          f_end = end_page(w);
-          f_turns = turns_of(w.ntok);
-          f_head = w.kv_head;
-          f_table = P.page_table + (size_t)w.req * P.pt_stride;
-        } while (f_page >= f_end);
-      }
+    f_page += f_step;
+    while (f_page >= f_end) {
+      if (++f_item >= item_end) return;
+      const AttnItem w = P.items[item_at(f_item)];
+      const Share s = share_of(w);
+      f_page = s.page;
+      f_step = s.warps * PG;
+      f_end = s.end;
+      f_head = w.kv_head;
+      f_table = P.page_table + (size_t)w.req * P.pt_stride;
     }
-    f_id = __ldg(f_table + f_page);
+#pragma unroll
+    for (int i = 0; i < PG; ++i) f_id[i] = f_page + i < f_end ? __ldg(f_table + f_page + i) : 0;
   };
   auto request = [&](int slot) {
     if (f_item >= item_end) return;
     if (lane == 0) {
-      if (f_id < 0 || f_id >= P.n_pages) {
-        set_status(P.status, DEV_BAD_INDEX);
-        mbar_arrive(&full[slot]);
-      } else {
-        mbar_arrive_expect_tx(&full[slot], SH::kBlock);
-        bulk_g2s(ring + slot * SH::kBlock, P.pool + kv4_block_base(P.n_pages, P.n_kv, D, P.layer, f_id, f_head), SH::kBlock, &full[slot]);
+      bool ok[PG];
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < PG; ++i) {
+        ok[i] = f_page + i < f_end;
+        if (ok[i] && (f_id[i] < 0 || f_id[i] >= P.n_pages)) {
+          set_status(P.status, DEV_BAD_INDEX);
+          ok[i] = false;
+        }
+        n += ok[i];
       }
+      if (n == 0) mbar_arrive(&full[slot]);
+      else mbar_arrive_expect_tx(&full[slot], n * SH::kBlock);
+#pragma unroll
+      for (int i = 0; i < PG; ++i)
+        if (ok[i])
+          bulk_g2s(ring + slot * kSlot + i * SH::kBlock, P.pool + kv4_block_base(P.n_pages, P.n_kv, D, P.layer, f_id[i], f_head), SH::kBlock, &full[slot]);
     }
     advance();
   };
   advance();
   for (int s = 0; s < kSlots; ++s) request(s);
 
-  uint32_t count = 0;     // pages worked on so far
+  uint32_t count = 0;     // chunks worked on so far
   bool aborted = false;
   for (int item = 0; item < item_end; ++item) {
     const AttnItem w = P.items[item_at(item)];
-    const int R = w.ntok * P.group, n_turns = turns_of(w.ntok);
-    for (int turn = 0; turn < n_turns; ++turn) {
-      const int row0 = turn * SH::kRows;
+    const int R = w.ntok * P.group;
+    const Share sh = share_of(w);
+    {
+      const int row0 = sh.group * SH::kRows;
       // ---- Q as B operands: column g of row group nt.  Lane t holds the values [D / 4 t, D / 4 (t + 1)) of a row; k-step 2 j + u takes the
       // pairs 2 u and 2 u + 1 of word j of codes, the second of which the K operand holds times 16 ----
       uint32_t qf[NT][D / 16][2];
@@ -239,80 +256,81 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) lim = min(lim, min(climit[nt][0], climit[nt][1]));
       lim = __reduce_min_sync(0xffffffffu, lim);
-      const int p_end = end_page(w);
 
-      for (int p = first_page(w); p < p_end; p += W, ++count) {
+      for (int p = sh.page; p < sh.end; p += sh.warps * PG, ++count) {
         const int slot = count % kSlots;
         if (!aborted && !mbar_wait(&full[slot], (count / kSlots) & 1, kSpin)) {
           set_status(P.status, DEV_TIMEOUT_FULL);
           aborted = true;
         }
-        const uint8_t* pg = ring + slot * SH::kBlock;
+        const uint8_t* pg = ring + slot * kSlot;
         const int pos0 = p * kPageSize;
         auto work = [&](auto masked) {
           constexpr bool MASK = decltype(masked)::value;
-          // ---- S^T = C_K Q^T: rows g and g + 8 are the page's tokens ----
-          float sc[NT][4];
+          // ---- S^T = C_K Q^T: rows g and g + 8 of product i are tokens of page i ----
+          float sc[PG][NT][4];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+          for (int i = 0; i < PG; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sc[i][nt][0] = sc[i][nt][1] = sc[i][nt][2] = sc[i][nt][3] = 0.f;
           {
-            uint32_t k0[NW], k1[NW];
-            load_words(k0, pg + g * (D / 2) + t * (NW * 4));
-            load_words(k1, pg + (g + 8) * (D / 2) + t * (NW * 4));
+            uint32_t k0[PG][NW], k1[PG][NW];
 #pragma unroll
-            for (int j = 0; j < NW; ++j) {
-#pragma unroll
-              for (int u = 0; u < 2; ++u) {
-                const uint32_t w0 = u ? k0[j] >> 8 : k0[j], w1 = u ? k1[j] >> 8 : k1[j];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-                  mma_f16(sc[nt], w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qf[nt][2 * j + u][0], qf[nt][2 * j + u][1]);
-              }
+            for (int i = 0; i < PG; ++i) {
+              load_words(k0[i], pg + i * SH::kBlock + g * (D / 2) + t * (NW * 4));
+              load_words(k1[i], pg + i * SH::kBlock + (g + 8) * (D / 2) + t * (NW * 4));
             }
+#pragma unroll
+            for (int j = 0; j < NW; ++j)
+#pragma unroll
+              for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < PG; ++i) {
+                  const uint32_t w0 = u ? k0[i][j] >> 8 : k0[i][j], w1 = u ? k1[i][j] >> 8 : k1[i][j];
+#pragma unroll
+                  for (int nt = 0; nt < NT; ++nt)
+                    mma_f16(sc[i][nt], w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qf[nt][2 * j + u][0], qf[nt][2 * j + u][1]);
+                }
           }
-          float sk[2], mk[2], sv[2], mv[2];
+          // (token x = 2 i + h of this lane is token g + 8 h of page i)
+          float sk[2 * PG], mk[2 * PG], sv[2 * PG], mv[2 * PG];
+          float sv_top = 0.f;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t kp = *reinterpret_cast<const uint32_t*>(pg + kv4_k_pairs(D) + 4 * (8 * h + g));
-            const uint32_t vp = *reinterpret_cast<const uint32_t*>(pg + kv4_v_pairs(D) + 4 * (8 * h + g));
-            sk[h] = kv4_step(kp) * factor;
-            mk[h] = kv4_min(kp);
-            sv[h] = kv4_step(vp);
-            mv[h] = kv4_min(vp);
+          for (int x = 0; x < 2 * PG; ++x) {
+            const uint8_t* pair = pg + (x >> 1) * SH::kBlock + 4 * (8 * (x & 1) + g);
+            const uint32_t kp = *reinterpret_cast<const uint32_t*>(pair + kv4_k_pairs(D)), vp = *reinterpret_cast<const uint32_t*>(pair + kv4_v_pairs(D));
+            sk[x] = kv4_step(kp) * factor;
+            mk[x] = kv4_min(kp);
+            sv[x] = kv4_step(vp);
+            mv[x] = kv4_min(vp);
+            // (a token behind the request's end is seen by no row: its step may be anything)
+            if (MASK && pos0 + 16 * (x >> 1) + 8 * (x & 1) + g >= w.kv_len) sv[x] = mv[x] = 0.f;
+            sv_top = fmaxf(sv_top, sv[x]);
           }
-          bool see[NT][4];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int pos = pos0 + g + 8 * (e >> 1), c = e & 1;
-              see[nt][e] = !MASK || pos <= climit[nt][c] || (pos >= vlo[nt][c] && pos < vhi[nt][c]);
-            }
-          // (a token behind the request's end is seen by no row: its step may be anything)
-          if (MASK) {
-            const int kv_len = w.kv_len;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (pos0 + g + 8 * h >= kv_len) sv[h] = mv[h] = 0.f;
-          }
-          float pr[NT][4];
+          auto sees = [&](int x, int nt, int c) {
+            const int pos = pos0 + 16 * (x >> 1) + 8 * (x & 1) + g;
+            return !MASK || pos <= climit[nt][c] || (pos >= vlo[nt][c] && pos < vhi[nt][c]);
+          };
+          float pr[PG][NT][4];
           auto scores = [&]() {
             float top = -INFINITY;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int i = 0; i < PG; ++i)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                float y = fmaf(sc[nt][e], sk[e >> 1], fmaf(mk[e >> 1], qs[nt][e & 1], kLift - ref[nt][e & 1]));
-                if (MASK && !see[nt][e]) y = -INFINITY;
-                pr[nt][e] = y;
-                top = fmaxf(top, y);
-              }
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int x = 2 * i + (e >> 1);
+                  float y = fmaf(sc[i][nt][e], sk[x], fmaf(mk[x], qs[nt][e & 1], kLift - ref[nt][e & 1]));
+                  if (MASK && !sees(x, nt, e & 1)) y = -INFINITY;
+                  pr[i][nt][e] = y;
+                  top = fmaxf(top, y);
+                }
             return top;
           };
-          if (__any_sync(0xffffffffu, scores() > kHeadroom + kLift || fmaxf(sv[0], sv[1]) >= s_top)) {
+          if (__any_sync(0xffffffffu, scores() > kHeadroom + kLift || sv_top >= s_top)) {
             // some row's reference maximum moves, or the scale of the steps does: what has been summed up is scaled to the new ones
-            const float v = fmaxf(sv[0], sv[1]);
-            const uint32_t top = __reduce_max_sync(0xffffffffu, v > 0.f ? __float_as_uint(v) : 0u);      // (NaN does not take part)
+            const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(sv_top));      // (NaN does not take part)
             const float next_top = fmaxf(s_top, pow2(max(-100, (int)(top >> 23) - 127 + 1)));
             const float fs = s_top / next_top;
             s_top = next_top;
@@ -323,11 +341,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
               for (int c = 0; c < 2; ++c) {
                 float z = -INFINITY;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                  if (see[nt][2 * h + c]) z = fmaxf(z, fmaf(sc[nt][2 * h + c], sk[h], mk[h] * qs[nt][c]));
+                for (int x = 0; x < 2 * PG; ++x)
+                  if (sees(x, nt, c)) z = fmaxf(z, fmaf(sc[x >> 1][nt][2 * (x & 1) + c], sk[x], mk[x] * qs[nt][c]));
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, x));
-                // (it moves where it is outgrown by anything: the other rows' probabilities stay the same)
                 const float next = z > ref[nt][c] + kHeadroom || ref[nt][c] == kNoRef ? fmaxf(ref[nt][c], z) : ref[nt][c];
                 const float f = exp2f(ref[nt][c] - next);
                 ref[nt][c] = next;
@@ -342,38 +359,43 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
             scores();
           }
           // ---- probabilities; O^T += C_V^T (P s_V)^T ----
-          const float svs[2] = {sv[0] * s_inv, sv[1] * s_inv};
-          uint32_t b[NT][2];
+          uint32_t b[PG][NT][2];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float ps[4];
+          for (int i = 0; i < PG; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float p_ = exp2f(pr[nt][e]);
-              l[nt][e & 1] += p_;
-              ps[e] = p_ * svs[e >> 1];
-              float pm = p_ * mv[e >> 1];
-              if (MASK && !see[nt][e]) ps[e] = pm = 0.f;
-              om[nt][e & 1] += pm;
+            for (int nt = 0; nt < NT; ++nt) {
+              float ps[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int x = 2 * i + (e >> 1);
+                const float p_ = exp2f(pr[i][nt][e]);
+                l[nt][e & 1] += p_;
+                ps[e] = p_ * (sv[x] * s_inv);
+                float pm = p_ * mv[x];
+                if (MASK && !sees(x, nt, e & 1)) ps[e] = pm = 0.f;
+                om[nt][e & 1] += pm;
+              }
+              b[i][nt][0] = transpose8x8(pack_f16(ps[0], ps[1]));
+              b[i][nt][1] = transpose8x8(pack_f16(ps[2], ps[3]));
             }
-            b[nt][0] = transpose8x8(pack_f16(ps[0], ps[1]));
-            b[nt][1] = transpose8x8(pack_f16(ps[2], ps[3]));
+#pragma unroll
+          for (int i = 0; i < PG; ++i) {
+            uint32_t v0[NW], v1[NW];
+            load_words(v0, pg + i * SH::kBlock + kv4_v_codes(D) + t * D + g * (D / 8));
+            load_words(v1, pg + i * SH::kBlock + kv4_v_codes(D) + (t + 4) * D + g * (D / 8));
+#pragma unroll
+            for (int j = 0; j < NW; ++j)
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const uint32_t w0 = u ? v0[j] >> 8 : v0[j], w1 = u ? v1[j] >> 8 : v1[j];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+                  mma_f16(o[nt][2 * j + u], w0 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x000f000fu, w1 & 0x00f000f0u, b[i][nt][0], b[i][nt][1]);
+              }
           }
-          uint32_t v0[NW], v1[NW];
-          load_words(v0, pg + kv4_v_codes(D) + t * D + g * (D / 8));
-          load_words(v1, pg + kv4_v_codes(D) + (t + 4) * D + g * (D / 8));
-#pragma unroll
-          for (int j = 0; j < NW; ++j)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const uint32_t w0 = u ? v0[j] >> 8 : v0[j], w1 = u ? v1[j] >> 8 : v1[j];
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-                mma_f16(o[nt][2 * j + u], w0 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x000f000fu, w1 & 0x00f000f0u, b[nt][0], b[nt][1]);
-            }
         };
         if (!aborted) {
-          if (pos0 + kPageSize - 1 > lim) work(std::true_type{});
+          if (pos0 + PG * kPageSize - 1 > lim) work(std::true_type{});
           else work(std::false_type{});
         }
         __syncwarp();
@@ -410,10 +432,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
         }
       __syncthreads();
       // a warp takes every kWarps-th row, a lane D / 32 consecutive values of it
-      const int rows = min(SH::kRows, R - row0);
-      for (int rr = warp; rr < rows; rr += W) {
-        float m_all = lane < W ? merge[(lane * SH::kRows + rr) * SH::kRowPad + D] : kNoRef;
-        const float m_mine = m_all, l_mine = lane < W ? merge[(lane * SH::kRows + rr) * SH::kRowPad + D + 1] : 0.f;
+      for (int rr = warp; rr < R; rr += W) {
+        const float* part = merge + ((size_t)(rr / SH::kRows) * sh.warps * SH::kRows + rr % SH::kRows) * SH::kRowPad;   // of the group's first warp
+        constexpr int kPart = SH::kRows * SH::kRowPad;
+        const float m_mine = lane < sh.warps ? part[lane * kPart + D] : kNoRef, l_mine = lane < sh.warps ? part[lane * kPart + D + 1] : 0.f;
+        float m_all = m_mine;
 #pragma unroll
         for (int x = 16; x; x >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, x));
         const float f_mine = exp2f(m_mine - m_all);
@@ -425,13 +448,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = 0.f;
 #pragma unroll 4
-        for (int k = 0; k < W; ++k) {
+        for (int k = 0; k < sh.warps; ++k) {
           const float f = __shfl_sync(0xffffffffu, f_mine, k);
-          const float* src = merge + (k * SH::kRows + rr) * SH::kRowPad + lane * E;
+          const float* src = part + k * kPart + lane * E;
 #pragma unroll
           for (int e = 0; e < E; ++e) acc[e] = fmaf(f, src[e], acc[e]);
         }
-        const int rho = row0 + rr, j = rho / P.group;
+        const int rho = rr, j = rho / P.group;
         if (w.part < 0) {
           const size_t row = (size_t)(w.tok0 + j) * P.n_q + w.kv_head * P.group + rho - j * P.group;
           const float inv = l_all > 0.f ? 1.f / l_all : 0.f * l_all;
