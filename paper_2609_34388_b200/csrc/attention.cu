@@ -560,7 +560,7 @@ void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const vo
   if (four || (use_tc && dm.head_dim == 128)) {
     if (four && use_tc && dm.head_dim == 128 && max_rows > kFewRows &&
         launch_attention_kv4_tc(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st)) {
-    } else if (four) launch_attention_kv4(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, max_rows, status, st);
+    } else if (four) launch_attention_kv4(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, max_rows, status, st, layout_settled);
     else launch_attention_tc_main(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st, layout_settled);
     // (the kernel in front signals its dependents when the list is settled)
     if (!whole) (dm.head_dim == 64 ? launch_combine<64> : launch_combine<128>)(bl, dm, o, lse, part_o, part_ml, n_sm, st, tiles, step, 1);

@@ -14,8 +14,9 @@
 // of two for all rows of a warp, and the steps of V, as factors of P, by another that follows the largest of them; so a score
 // is off by 2^-30 of the largest row's scores at most, and p s_V by 2^-12 of itself.
 //
-// A warp is alone with its pages: it requests them itself (one bulk copy per page and head, into a ring of its own) and runs ahead of
-// itself into the next item.  The warps are divided among the item's row groups, those of a group share its pages among
+// A warp is alone with its pages: it requests them itself, 16 bytes a lane into a ring of its own, and runs ahead of itself into the
+// next item.  (One bulk copy per page and head and a barrier per slot: the one lane that issues them took 850 clocks for every 2100
+// of work.)  The warps are divided among the item's row groups, those of a group share its pages among
 // themselves, and their results are merged at the end of the item.
 #include <cuda_fp16.h>
 #include <type_traits>
@@ -27,7 +28,6 @@ namespace recg {
 
 namespace {
 
-constexpr uint32_t kSpin = 1u << 22;
 constexpr float kNoRef = -1e30f;       // reference maximum of a row that has seen no token yet
 constexpr float kHeadroom = 8.f;       // a row's reference maximum moves when it is outgrown by more than 2^8
 constexpr float kLift = 7.f;           // probabilities stand as 2^7 p: with steps below 1 at most 2^15
@@ -45,9 +45,10 @@ struct Shape {
   static constexpr int kRowPad = D + 4;                            // floats from row to row of a merged part
   static constexpr int kRows = 8 * NT;
   static constexpr int kMerge = kWarps * kRows * kRowPad * 4;      // [warp][row][value]; values D and D + 1: reference maximum, sum
-  static constexpr int kBars = kRing + kMerge;
-  static constexpr int kTotal = kBars + kWarps * kSlots * 8;
-  static_assert(kTotal <= 227 * 1024, "shared memory budget");
+  static constexpr int kItemsOff = kRing + kMerge;
+  static constexpr int kItems = 32;                                // items of the CTA whose descriptors are kept on chip
+  static constexpr int kTotal = kItemsOff + kItems * (int)sizeof(AttnItem);
+  static_assert(kBlock % 16 == 0 && kTotal <= 227 * 1024, "shared memory budget");
   static_assert(kWarps * kRows >= 128 || NT == 1, "every row of a tile has a warp");
 };
 
@@ -64,11 +65,12 @@ struct Params {
   float* lse;         // may be null
   const uint8_t* pool;
   int64_t n_pages;
-  int layer, n_q, n_kv, group;
+  int layer, n_q, n_kv, group, inv_group;      // inv_group: (rho * inv_group) >> 16 is rho / group for the rows of a tile
   float scale_log2;   // log2(e) / sqrt(d)
   float* part_o;      // [part][128][D]
   float* part_ml;     // [part][128][2]
   int* status;
+  int early_desc;     // the work list is settled: it may be read before the wait for the kernel in front of this one
 };
 
 // D(16x8, f32) += A(16x16, f16, row) * B(16x8, f16, col)
@@ -85,6 +87,9 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return reinterpret_cast<const uint32_t&>(h);
+}
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
@@ -105,138 +110,170 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
   constexpr int W = SH::kWarps, PG = SH::kPages, kSlots = SH::kSlots, kSlot = PG * SH::kBlock;
   extern __shared__ __align__(128) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + SH::kBars) + warp * kSlots;
   uint8_t* ring = smem + warp * kSlots * kSlot;
   float* merge = reinterpret_cast<float*>(smem + SH::kRing);
-  if (lane == 0) {
-    for (int s = 0; s < kSlots; ++s) mbar_init(&full[s], 1);
-    fence_barrier_init();
-  }
-  __syncwarp();
-  griddep_wait();
-  griddep_launch();
+  // (where the work list is settled all reads of it, and of page ids, overlap the end of the kernel in front)
+  if (!P.early_desc) griddep_wait();
 
   // the CTA walks two ranges of the item list one after the other (see the layout kernel)
   const int4 r4 = *reinterpret_cast<const int4*>(P.cta_off + 4 * blockIdx.x);
   const int range_n0 = r4.y - r4.x, item_end = range_n0 + (r4.w - r4.z);
   auto item_at = [&](int i) { return i < range_n0 ? r4.x + i : r4.z + (i - range_n0); };
+  static_assert(sizeof(AttnItem) == 32, "two 16-byte pieces");
+  uint4* kept = reinterpret_cast<uint4*>(smem + SH::kItemsOff);
+  for (int i = threadIdx.x; i < 2 * min(item_end, SH::kItems); i += SH::kThreads)
+    kept[i] = reinterpret_cast<const uint4*>(P.items + item_at(i >> 1))[i & 1];
+  __syncthreads();
+  auto item_of = [&](int i) { return i < SH::kItems ? reinterpret_cast<const AttnItem*>(kept)[i] : P.items[item_at(i)]; };
   // of an item: warps per row group; this warp's group; its first chunk of pages and the end of all
   struct Share { int warps, group, page, end; };
   auto share_of = [&](const AttnItem& w) {
     Share s;
-    s.warps = W / ((w.ntok * P.group + SH::kRows - 1) / SH::kRows);
-    s.group = warp / s.warps;
+    if (NT == 1) {                       // (one group)
+      s.warps = W;
+      s.group = 0;
+    } else {
+      s.warps = W / ((w.ntok * P.group + SH::kRows - 1) / SH::kRows);
+      s.group = warp / s.warps;
+    }
     s.end = s.group * SH::kRows < w.ntok * P.group ? min(w.blk_end * 4, (w.kv_len + kPageSize - 1) / kPageSize) : 0;
     s.page = w.blk_begin * 4 + (warp - s.group * s.warps) * PG;
     return s;
   };
 
-  // ---- what the warp requests next: a chunk of an item, its page ids already on their way ----
-  int f_item = -1, f_page = 0, f_step = 0, f_end = 0, f_head = 0, f_id[PG];
+  // ---- what the warp requests next: a chunk of an item.  Page ids are fetched 32 at a time, a lane one of them; a page's address is one
+  // multiplication away from its id (with the general formula for a block's place a request took 100 instructions a page, as many as the
+  // work on it leaves to the other warps of the scheduler) ----
+  int f_item = -1, f_page = 0, f_step = 0, f_end = 0, f_used = 0, f_ids = 0;
   const int* f_table = nullptr;
-  auto advance = [&]() {
-    f_page += f_step;
-    while (f_page >= f_end) {
-      if (++f_item >= item_end) return;
-      const AttnItem w = P.items[item_at(f_item)];
+  const uint8_t* f_base = nullptr;       // this lane's 16 bytes of the head's block in page 0 of the layer
+  const unsigned page_bytes = (unsigned)P.n_kv * SH::kBlock, n_pages = (unsigned)min(P.n_pages, (int64_t)0x7fffffff);
+  const uint32_t ring_at = smem_u32(ring) + lane * 16;
+  auto load_ids = [&]() {
+    f_used = 0;
+    const int page = f_page + (lane / PG) * f_step + lane % PG;
+    f_ids = page < f_end ? __ldg(f_table + page) : 0;
+  };
+  auto next_item = [&]() {
+    do {
+      if (++f_item >= item_end) {
+        f_end = -1;
+        return;
+      }
+      const AttnItem w = item_of(f_item);
       const Share s = share_of(w);
       f_page = s.page;
       f_step = s.warps * PG;
       f_end = s.end;
-      f_head = w.kv_head;
       f_table = P.page_table + (size_t)w.req * P.pt_stride;
-    }
-#pragma unroll
-    for (int i = 0; i < PG; ++i) f_id[i] = f_page + i < f_end ? __ldg(f_table + f_page + i) : 0;
+      f_base = P.pool + kv4_block_base(P.n_pages, P.n_kv, D, P.layer, 0, w.kv_head) + lane * 16;
+    } while (f_page >= f_end);
+    load_ids();
   };
-  auto request = [&](int slot) {
-    if (f_item >= item_end) return;
-    if (lane == 0) {
-      bool ok[PG];
-      int n = 0;
+  auto request = [&](uint32_t slot_at) {        // one group of copies per call, be it empty
+    if (f_end >= 0) {
 #pragma unroll
       for (int i = 0; i < PG; ++i) {
-        ok[i] = f_page + i < f_end;
-        if (ok[i] && (f_id[i] < 0 || f_id[i] >= P.n_pages)) {
+        const unsigned id = __shfl_sync(0xffffffffu, f_ids, f_used + i);
+        if (PG > 1 && i > 0 && f_page + i >= f_end) continue;
+        if (id >= n_pages) {
           set_status(P.status, DEV_BAD_INDEX);
-          ok[i] = false;
+          continue;
         }
-        n += ok[i];
-      }
-      if (n == 0) mbar_arrive(&full[slot]);
-      else mbar_arrive_expect_tx(&full[slot], n * SH::kBlock);
+        const uint8_t* src = f_base + (uint64_t)id * page_bytes;
+        const uint32_t dst = ring_at + slot_at + i * SH::kBlock;
 #pragma unroll
-      for (int i = 0; i < PG; ++i)
-        if (ok[i])
-          bulk_g2s(ring + slot * kSlot + i * SH::kBlock, P.pool + kv4_block_base(P.n_pages, P.n_kv, D, P.layer, f_id[i], f_head), SH::kBlock, &full[slot]);
+        for (int x = 0; x < SH::kBlock / 512; ++x) copy_async16(dst + x * 512, src + x * 512);
+        if (lane < SH::kBlock % 512 / 16) copy_async16(dst + SH::kBlock / 512 * 512, src + SH::kBlock / 512 * 512);
+      }
+      f_page += f_step;
+      f_used += PG;
+      if (f_page >= f_end) next_item();
+      else if (f_used >= 32) load_ids();
     }
-    advance();
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  advance();
-  for (int s = 0; s < kSlots; ++s) request(s);
+  next_item();
+  if (P.early_desc) griddep_wait();
+  griddep_launch();
 
-  uint32_t count = 0;     // chunks worked on so far
-  bool aborted = false;
+  // The rows of a warp's group in an item, read ahead of their use: column g of row group nt, of which lane t holds the values
+  // [D / 4 t, D / 4 (t + 1)); and what the rows 2 t and 2 t + 1 see
+  uint4 raw[NT][NW];
+  int climit[NT][2], vlo[NT][2], vhi[NT][2];
+  auto load_rows = [&](const AttnItem& w) {
+    const int R = w.ntok * P.group, row0 = share_of(w).group * SH::kRows;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int rho = row0 + nt * 8 + g, j = (rho * P.inv_group) >> 16;
+      const bool there = rho < R;
+      const uint4* src = reinterpret_cast<const uint4*>(P.q + ((size_t)(w.tok0 + (there ? j : 0)) * P.n_q + w.kv_head * P.group + (there ? rho - j * P.group : 0)) * D) + t * NW;
+#pragma unroll
+      for (int k = 0; k < NW; ++k) raw[nt][k] = there ? __ldg(src + k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int rv = row0 + nt * 8 + 2 * t + e, tok = w.tok0 + ((rv * P.inv_group) >> 16);
+        const bool is = rv < R;      // (a row that does not exist needs no mask: nobody reads it)
+        climit[nt][e] = is ? P.tok_climit[tok] : 0x7fffffff;
+        vlo[nt][e] = is ? P.tok_lo[tok] : 0;
+        vhi[nt][e] = is ? P.tok_hi[tok] : 0;
+      }
+    }
+  };
+  if (item_end > 0) load_rows(item_of(0));
+  for (int s = 0; s < kSlots; ++s) request(s * kSlot);
+
+  uint32_t slot_at = 0;   // the slot of the next chunk
   for (int item = 0; item < item_end; ++item) {
-    const AttnItem w = P.items[item_at(item)];
+    const AttnItem w = item_of(item);
     const int R = w.ntok * P.group;
     const Share sh = share_of(w);
+    // ---- Q as B operands: k-step 2 j + u takes the pairs 2 u and 2 u + 1 of word j of codes, the second of which the K operand holds
+    // times 16 ----
+    uint32_t qf[NT][D / 16][2];
+    float qs[NT][2];                     // sums of the rows 2 t and 2 t + 1, times the scale of the scores
+    float factor;                        // what makes a product of this scaled Q and codes 2^-24 c a score
+    int lim = 0x7fffffff;                // the position up to which every row of the warp sees everything
     {
-      const int row0 = sh.group * SH::kRows;
-      // ---- Q as B operands: column g of row group nt.  Lane t holds the values [D / 4 t, D / 4 (t + 1)) of a row; k-step 2 j + u takes the
-      // pairs 2 u and 2 u + 1 of word j of codes, the second of which the K operand holds times 16 ----
-      uint32_t qf[NT][D / 16][2];
-      float qs[NT][2];                   // sums of the rows 2 t and 2 t + 1, times the scale of the scores
-      float factor;                      // what makes a product of this scaled Q and codes 2^-24 c a score
-      int climit[NT][2], vlo[NT][2], vhi[NT][2];
-      {
-        uint4 raw[NT][NW];
-        uint32_t top = 0;
+      uint32_t top = 0;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const int rho = row0 + nt * 8 + g, j = rho / P.group;
-          const bool there = rho < R;
-          const uint4* src = reinterpret_cast<const uint4*>(P.q + ((size_t)(w.tok0 + (there ? j : 0)) * P.n_q + w.kv_head * P.group + (there ? rho - j * P.group : 0)) * D) + t * NW;
-          float sum = 0.f;
+      for (int nt = 0; nt < NT; ++nt) {
+        float sum = 0.f;
 #pragma unroll
-          for (int k = 0; k < NW; ++k) {
-            raw[nt][k] = there ? __ldg(src + k) : make_uint4(0, 0, 0, 0);
-            const uint32_t u[4] = {raw[nt][k].x, raw[nt][k].y, raw[nt][k].z, raw[nt][k].w};
+        for (int k = 0; k < NW; ++k) {
+          const uint32_t u[4] = {raw[nt][k].x, raw[nt][k].y, raw[nt][k].z, raw[nt][k].w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              sum += __uint_as_float(u[i] << 16) + __uint_as_float(u[i] & 0xffff0000u);
-              const uint32_t lo = u[i] & 0x7fffu, hi = (u[i] >> 16) & 0x7fffu;
-              top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));      // (a row that is not finite does not concern the others)
-            }
-          }
-          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            qs[nt][e] = __shfl_sync(0xffffffffu, sum, (2 * t + e) * 4) * P.scale_log2;
-            const int rv = row0 + nt * 8 + 2 * t + e, tok = w.tok0 + rv / P.group;
-            const bool is = rv < R;      // (a row that does not exist needs no mask: nobody reads it)
-            climit[nt][e] = is ? P.tok_climit[tok] : 0x7fffffff;
-            vlo[nt][e] = is ? P.tok_lo[tok] : 0;
-            vhi[nt][e] = is ? P.tok_hi[tok] : 0;
+          for (int i = 0; i < 4; ++i) {
+            sum += __uint_as_float(u[i] << 16) + __uint_as_float(u[i] & 0xffff0000u);
+            const uint32_t lo = u[i] & 0x7fffu, hi = (u[i] >> 16) & 0x7fffu;
+            top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));      // (a row that is not finite does not concern the others)
           }
         }
-        // the largest value of all rows goes to [2^8, 2^9) (as far as the exponent allows: a factor and its inverse are normal numbers)
-        const int e = max(-100, min(100, (int)(__reduce_max_sync(0xffffffffu, top) >> 7) - 127 - 8));
-        const float down = pow2(-e), down16 = pow2(-e - 4);
-        factor = pow2(e) * 16777216.f * P.scale_log2;
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int k = 0; k < NW; ++k) {
-            const uint4 v = raw[nt][k];
-            qf[nt][2 * k][0] = pack_f16(__uint_as_float(v.x << 16) * down, __uint_as_float(v.x & 0xffff0000u) * down);
-            qf[nt][2 * k][1] = pack_f16(__uint_as_float(v.y << 16) * down16, __uint_as_float(v.y & 0xffff0000u) * down16);
-            qf[nt][2 * k + 1][0] = pack_f16(__uint_as_float(v.z << 16) * down, __uint_as_float(v.z & 0xffff0000u) * down);
-            qf[nt][2 * k + 1][1] = pack_f16(__uint_as_float(v.w << 16) * down16, __uint_as_float(v.w & 0xffff0000u) * down16);
-          }
+        for (int e = 0; e < 2; ++e) {
+          qs[nt][e] = __shfl_sync(0xffffffffu, sum, (2 * t + e) * 4) * P.scale_log2;
+          lim = min(lim, climit[nt][e]);
+        }
       }
-
+      lim = __reduce_min_sync(0xffffffffu, lim);
+      // the largest value of all rows goes to [2^8, 2^9) (as far as the exponent allows: a factor and its inverse are normal numbers)
+      const int e = max(-100, min(100, (int)(__reduce_max_sync(0xffffffffu, top) >> 7) - 127 - 8));
+      const float down = pow2(-e), down16 = pow2(-e - 4);
+      factor = pow2(e) * 16777216.f * P.scale_log2;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < NW; ++k) {
+          const uint4 v = raw[nt][k];
+          qf[nt][2 * k][0] = pack_f16(__uint_as_float(v.x << 16) * down, __uint_as_float(v.x & 0xffff0000u) * down);
+          qf[nt][2 * k][1] = pack_f16(__uint_as_float(v.y << 16) * down16, __uint_as_float(v.y & 0xffff0000u) * down16);
+          qf[nt][2 * k + 1][0] = pack_f16(__uint_as_float(v.z << 16) * down, __uint_as_float(v.z & 0xffff0000u) * down);
+          qf[nt][2 * k + 1][1] = pack_f16(__uint_as_float(v.w << 16) * down16, __uint_as_float(v.w & 0xffff0000u) * down16);
+        }
+    }
+    {
       float o[NT][D / 16][4];              // O^T: rows (values) i, columns 2 t and 2 t + 1; see the writer for which values
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -252,18 +289,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
       }
       float s_top = 0.f, s_inv = 0.f;      // steps of V are below s_top (a power of two), and P holds p s_V 2^7 / s_top
 
-      int lim = 0x7fffffff;                // the position up to which every row of the warp sees everything
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) lim = min(lim, min(climit[nt][0], climit[nt][1]));
-      lim = __reduce_min_sync(0xffffffffu, lim);
-
-      for (int p = sh.page; p < sh.end; p += sh.warps * PG, ++count) {
-        const int slot = count % kSlots;
-        if (!aborted && !mbar_wait(&full[slot], (count / kSlots) & 1, kSpin)) {
-          set_status(P.status, DEV_TIMEOUT_FULL);
-          aborted = true;
-        }
-        const uint8_t* pg = ring + slot * kSlot;
+      for (int p = sh.page; p < sh.end; p += sh.warps * PG) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 1) : "memory");
+        __syncwarp();
+        const uint8_t* pg = ring + slot_at;
         const int pos0 = p * kPageSize;
         auto work = [&](auto masked) {
           constexpr bool MASK = decltype(masked)::value;
@@ -394,14 +423,15 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
               }
           }
         };
-        if (!aborted) {
-          if (pos0 + PG * kPageSize - 1 > lim) work(std::true_type{});
-          else work(std::false_type{});
-        }
+        if (pos0 + PG * kPageSize - 1 > lim) work(std::true_type{});
+        else work(std::false_type{});
         __syncwarp();
-        if (!aborted) request(slot);
+        request(slot_at);
+        slot_at = slot_at == (kSlots - 1) * kSlot ? 0 : slot_at + kSlot;
       }
 
+      if (item + 1 < item_end) load_rows(item_of(item + 1));
+      __syncthreads();      // (the parts of the item before have been read)
       // ---- the warps' parts meet: row (column 2 t + c of group nt), the D / 8 values of g that this lane holds ----
       constexpr float k1 = 16777216.f, k16 = 1048576.f;      // 2^24 and 2^20
 #pragma unroll
@@ -469,15 +499,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
           if (lane == 0) *reinterpret_cast<float2*>(P.part_ml + ((size_t)w.part * 128 + rho) * 2) = make_float2(m_all, l_all);
         }
       }
-      __syncthreads();      // the parts may be overwritten
     }
   }
-  if (aborted && lane == 0)         // let copies already in flight land before the CTA may exit
-    for (int s = 0; s < kSlots; ++s)
-      for (uint32_t i = 0; i < (1u << 14); ++i) {
-        if (mbar_try_wait(&full[s], 0) || mbar_try_wait(&full[s], 1)) break;
-        __nanosleep(64);
-      }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 template <int D, int NT>
@@ -491,7 +515,7 @@ void launch_rows(const Params& P, int n_sm, cudaStream_t st) {
 }  // namespace
 
 void launch_attention_kv4(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
-                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int max_rows, int* status, cudaStream_t st) {
+                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int max_rows, int* status, cudaStream_t st, bool list_settled) {
   Params P;
   P.items = bl.items;
   P.cta_off = bl.cta_off;
@@ -509,10 +533,12 @@ void launch_attention_kv4(const BatchLayout& bl, const Dims& dm, int layer, cons
   P.n_q = dm.n_q;
   P.n_kv = dm.n_kv;
   P.group = dm.n_q / dm.n_kv;
+  P.inv_group = 65536 / P.group + 1;
   P.scale_log2 = 1.4426950408889634f / sqrtf((float)dm.head_dim);
   P.part_o = part_o;
   P.part_ml = part_ml;
   P.status = status;
+  P.early_desc = list_settled ? 1 : 0;
   if (dm.head_dim == 64) (max_rows <= 8 ? launch_rows<64, 1> : launch_rows<64, 2>)(P, n_sm, st);
   else (max_rows <= 8 ? launch_rows<128, 1> : launch_rows<128, 2>)(P, n_sm, st);
 }

@@ -225,7 +225,8 @@ void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, 
                               cudaStream_t st, bool layout_settled);
 // the same over a pool in 4 bits; max_rows: the largest number of query rows (new tokens times query heads of a kv head) of a row tile
 void launch_attention_kv4(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
-                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int max_rows, int* status, cudaStream_t st);
+                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int max_rows, int* status, cudaStream_t st,
+                          bool list_settled);
 // ... on the tcgen05 tensor cores (head_dim 128); false: not launched (no tensor map over q)
 bool launch_attention_kv4_tc(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
                              int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status, cudaStream_t st);
