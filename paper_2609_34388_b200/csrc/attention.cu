@@ -552,8 +552,11 @@ size_t attention_smem_bytes(int head_dim) {
   return head_dim == 64 ? AttnSmem<64>::kTotal : AttnSmem<128>::kTotal;
 }
 
-// (rule to be measured)
-constexpr int kFewRows = 16;
+// Attention over a 4-bit pool, head_dim 128: row tiles of at most this many query rows take the mma.sync kernel, which unpacks fewer codes per
+// byte than the tensor cores want as operands but needs eight columns of products for eight rows.  Sixteen requests of 512 to 8192 tokens, 4, 8,
+// 12 and 32 rows a kv head: 25.5, 26.3, 50.6 and 68.3 us with mma.sync, 48.8, 48.9, 49.3 and 50.3 with tcgen05; one request of 4096: 8.7, 9.1,
+// 14.7, 17.3 and 13.7, 14.2, 14.3, 14.5.
+constexpr int kFewRows = 8;
 void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, const void* kv_pool,
                       int64_t n_pages, float* part_o, float* part_ml, int tok_per_tile, int n_sm, int* status,
                       cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, bool four, float* lse, int max_rows) {
