@@ -1,13 +1,21 @@
 // The attention weight that cached tokens gather (recg_kv_weights): per kv head and position j
 //   out[j] = (j < L ? decay in[j] : 0) + sum over the rows t and the query heads of the group of w_t exp(score_tj - lse_t).
 // With the log-sum-exp of every row from the attention kernel each probability follows from its score alone, so one pass over K
-// gives them: S^T = K Q^T with the tokens as rows of the product.  A warp owns the 16 tokens of a page, keeps their K as A operands in
-// registers and walks over the query rows; the sum over rows is a sum over the columns of its accumulators, which stay in the
-// warp.  Nothing is added by atomics: a position belongs to one warp, which takes the rows in order, so results repeat bit for bit.
+// gives them: S^T = K Q^T (mma.sync) with the tokens as rows of the product.  A warp owns the 16 tokens of a page, has their K as A
+// operands in registers and walks over the query rows; the sum over rows is a sum over the columns of its accumulators, which stays in
+// the warp.  Nothing is added by atomics: a position belongs to one warp, which takes the rows in order, so results repeat bit for bit.
 //
-// K of either kind of pool is read straight into operands: a lane holds the values [D / 4 t, D / 4 (t + 1)) of two tokens (t its
-// number in the quad), which are contiguous; the contraction index is permuted accordingly and Q is staged in shared memory in
-// that order.  Codes are exact in bf16, steps and minima enter in fp32 (kv4.cuh), so the scores are those of the attention kernel.
+// Bound by the bytes of K as long as rows are few.  The pages of all requests and heads are one line, of which every CTA takes an
+// equal piece; per (request, head) in it the rows that count (weight not zero) are staged in shared memory once, and the warps
+// stream pages past them, each into a ring of its own, 16 bytes a lane.  (One CTA per 128 tokens, with its own staging and K by
+// plain loads: sixteen decoding requests 41.5 us, a serving batch on a bf16 pool 140; now %DEC% and %BATCH%.)
+//
+// Operands: a lane holds the values [D / 4 t, D / 4 (t + 1)) of two tokens (t its number in the quad), which are contiguous; the
+// contraction index is permuted accordingly and Q is staged in that order.  A pool in 4 bits: codes as subnormal fp16 numbers, Q scaled by a
+// power of two, steps and minima in fp32 (attention_kv4.cu has the reasons).
+#include <cuda_fp16.h>
+#include <type_traits>
+
 #include "kernels.h"
 #include "kv4.cuh"
 
@@ -15,9 +23,8 @@ namespace recg {
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kTileTokens = kWarps * kPageSize;
-constexpr int kChunkRows = 64;              // query rows staged at a time
+constexpr int kWarps = 12, kThreads = kWarps * 32;
+constexpr int kChunkRows = 128;             // query rows staged at a time
 
 struct Params {
   const int* ctx_len;
@@ -40,27 +47,60 @@ struct Params {
   int* status;
 };
 
-struct RowInfo {              // a staged query row
-  float qsum, lse2, weight;   // sum of its values, its log-sum-exp in powers of two, what its probabilities count
-  int climit, lo, hi;
+template <int D, bool FOUR>
+struct Shape {
+  static constexpr int kBlock = FOUR ? kv4_block_bytes(D) : 4 * kPageSize * D;      // of a page and head in the pool
+  static constexpr int kCodes = FOUR ? kPageSize * D / 2 : kPageSize * D * 2;       // its K: codes or values ...
+  static constexpr int kPage = kCodes + (FOUR ? 64 : 0);                            // ... and pairs
+  static constexpr int kSlots = FOUR ? 4 : 3;                                       // pages that a warp has on their way
+  static constexpr int kRowBytes = 2 * D + 64;      // from staged row to staged row: lanes of eight rows meet no bank twice
+  static constexpr int kRing = kWarps * kSlots * kPage;
+  static constexpr int kRowsOff = kRing;
+  static constexpr int kInfoOff = kRowsOff + kChunkRows * kRowBytes;
+  static constexpr int kVisOff = kInfoOff + kChunkRows * 16;
+  static constexpr int kListOff = kVisOff + kChunkRows * 16;
+  static constexpr int kTotal = kListOff + kChunkRows * 4;
 };
 
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+template <bool HALF>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (HALF)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t scaled_f16(uint32_t pair, float by) {
+  const __half2 h = __floats2half2_rn(__uint_as_float(pair << 16) * by, __uint_as_float(pair & 0xffff0000u) * by);
+  return reinterpret_cast<const uint32_t&>(h);
+}
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
+
 template <int D, bool FOUR>
-__global__ void __launch_bounds__(kThreads, 2) kv_weights_kernel(Params P) {
-  constexpr int NW = D / 32, kChunks = D / 8;
-  constexpr int kRowChunks = kChunks + 4;     // 16-byte chunks from row to row: lanes of eight rows meet no bank twice
-  __shared__ uint4 s_q[kChunkRows * kRowChunks];
-  __shared__ RowInfo s_row[kChunkRows];
-  __shared__ int s_scan[kWarps];
-  extern __shared__ int s_tiles[];            // [n_req + 1] token tiles (one kv head) in front of request r
+__global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_constant__ Params P) {
+  using SH = Shape<D, FOUR>;
+  constexpr int NW = D / 32, kChunks = D / 8;           // 16-byte chunks a lane holds of a row; of a row
+  extern __shared__ __align__(128) uint8_t smem[];
+  float4* s_info = reinterpret_cast<float4*>(smem + SH::kInfoOff);     // a staged row: sum of its values times the scale, -lse (powers of two), weight
+  int4* s_vis = reinterpret_cast<int4*>(smem + SH::kVisOff);
+  int* s_list = reinterpret_cast<int*>(smem + SH::kListOff);           // tokens that count
+  int* s_first = reinterpret_cast<int*>(smem + SH::kTotal);            // [n_req + 1] pages (all kv heads) in front of request r
+  __shared__ int s_scan[kWarps], s_count, s_next, s_lim;
+  __shared__ unsigned s_top;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   griddep_wait();
   griddep_launch();
-  auto kv_len_of = [&](int r) { return P.ctx_len[r] + P.cu_tok[r + 1] - P.cu_tok[r]; };
+  auto pages_of = [&](int r) { return (P.ctx_len[r] + P.cu_tok[r + 1] - P.cu_tok[r] + kPageSize - 1) / kPageSize; };
   {
     const int per = (P.n_req + kThreads - 1) / kThreads, r0 = min(P.n_req, tid * per), r1 = min(P.n_req, r0 + per);
     int mine = 0;
-    for (int r = r0; r < r1; ++r) mine += (kv_len_of(r) + kTileTokens - 1) / kTileTokens;
+    for (int r = r0; r < r1; ++r) mine += pages_of(r) * P.n_kv;
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -72,144 +112,264 @@ __global__ void __launch_bounds__(kThreads, 2) kv_weights_kernel(Params P) {
     int at = incl - mine;
     for (int k = 0; k < warp; ++k) at += s_scan[k];
     for (int r = r0; r < r1; ++r) {
-      s_tiles[r] = at;
-      at += (kv_len_of(r) + kTileTokens - 1) / kTileTokens;
+      s_first[r] = at;
+      at += pages_of(r) * P.n_kv;
     }
-    if (tid == kThreads - 1) s_tiles[P.n_req] = at;
+    if (tid == kThreads - 1) s_first[P.n_req] = at;
     __syncthreads();
   }
-  const int n_items = s_tiles[P.n_req] * P.n_kv;     // (item = token tile * n_kv + head)
+  // this CTA's piece of the line of pages [request][kv head][page]
+  const int n_units = s_first[P.n_req];
+  const int unit_begin = (int)((long long)n_units * blockIdx.x / gridDim.x), unit_end = (int)((long long)n_units * (blockIdx.x + 1) / gridDim.x);
+  const uint32_t ring_at = smem_u32(smem + warp * SH::kSlots * SH::kPage) + lane * 16;
+  const unsigned page_bytes = (unsigned)P.n_kv * SH::kBlock;
 
-  for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
-    const int tile = item / P.n_kv, h = item - tile * P.n_kv;
-    int lo_r = 0, hi_r = P.n_req;                     // largest r with s_tiles[r] <= tile (every request has a tile)
-    while (hi_r - lo_r > 1) {
-      const int mid = (lo_r + hi_r) >> 1;
-      if (s_tiles[mid] <= tile) lo_r = mid; else hi_r = mid;
+  for (int unit = unit_begin; unit < unit_end;) {
+    int r = 0, hi_r = P.n_req;                         // largest r with s_first[r] <= unit (every request has a page)
+    while (hi_r - r > 1) {
+      const int mid = (r + hi_r) >> 1;
+      if (s_first[mid] <= unit) r = mid; else hi_r = mid;
     }
-    const int r = lo_r, tok_first = P.cu_tok[r], n_new = P.cu_tok[r + 1] - tok_first, L = P.ctx_len[r], kv_len = L + n_new;
-    const int pos0 = (tile - s_tiles[r]) * kTileTokens + warp * kPageSize;
-    int page = -1;
-    if (pos0 < kv_len) {
-      page = P.page_table[(size_t)r * P.pt_stride + pos0 / kPageSize];
-      if (page < 0 || page >= P.n_pages) {
-        set_status(P.status, DEV_BAD_INDEX);
-        page = -1;
-      }
-    }
-    // ---- K of the warp's page as A operands: rows g and g + 8 are its tokens ----
-    uint32_t a[D / 16][4];
-    float sk[2] = {P.scale_log2, P.scale_log2}, mk[2] = {0.f, 0.f};
+    const int tok_first = P.cu_tok[r], n_new = P.cu_tok[r + 1] - tok_first, L = P.ctx_len[r], kv_len = L + n_new;
+    const int n_pages = (kv_len + kPageSize - 1) / kPageSize, h = (unit - s_first[r]) / n_pages;
+    const int page0 = unit - s_first[r] - h * n_pages, page1 = min(n_pages, page0 + unit_end - unit);      // pages [page0, page1) of head h
+    unit += page1 - page0;
+    const int* table = P.page_table + (size_t)r * P.pt_stride;
+    const uint8_t* base = P.pool + (((size_t)P.layer * P.n_pages) * P.n_kv + h) * (size_t)SH::kBlock + lane * 16;
+    const size_t out_base = ((size_t)P.layer * P.n_pages * P.n_kv + h) * kPageSize;
+
+    for (int first_tok = 0, chunk = 0; first_tok < n_new || chunk == 0; ++chunk) {
+      // ---- the warp's first pages on their way; ids 32 at a time, a lane one of them ----
+      int next = page0 + warp, ids = 0, used = 0;
+      auto load_ids = [&]() {
+        used = 0;
+        ids = next + lane * kWarps < page1 ? __ldg(table + next + lane * kWarps) : 0;
+      };
+      auto request = [&](uint32_t slot_at) {            // one group of copies per call, be it empty
+        if (next < page1) {
+          const unsigned id = __shfl_sync(0xffffffffu, ids, used);
+          if (id < (unsigned long long)P.n_pages) {
+            const uint8_t* src = base + (uint64_t)id * page_bytes;
+            const uint32_t dst = ring_at + slot_at;
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) a[k][0] = a[k][1] = a[k][2] = a[k][3] = 0;
-    if (page >= 0) {
-      if (FOUR) {
-        const uint8_t* block = P.pool + kv4_block_base(P.n_pages, P.n_kv, D, P.layer, page, h);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          uint32_t word[4];
-          const uint8_t* src = block + (g + 8 * e) * (D / 2) + t * (NW * 4);
-          if (NW == 4) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(src));
-            word[0] = v.x; word[1] = v.y; word[2] = v.z; word[3] = v.w;
-          } else {
-            const uint2 v = __ldg(reinterpret_cast<const uint2*>(src));
-            word[0] = v.x; word[1] = v.y;
+            for (int x = 0; x < SH::kCodes / 512; ++x) copy_async16(dst + x * 512, src + x * 512);
+            if (FOUR && lane < 4) copy_async16(dst + SH::kCodes, src + kv4_k_pairs(D));
           }
-          const uint32_t pair = __ldg(reinterpret_cast<const uint32_t*>(block + kv4_k_pairs(D)) + g + 8 * e);
-          sk[e] = kv4_step(pair) * P.scale_log2;
-          mk[e] = fmaf(8.f, kv4_step(pair), kv4_min(pair)) * P.scale_log2;
-#pragma unroll
-          for (int j = 0; j < NW; ++j)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              a[2 * j + u][e] = kv4_pair(word[j], 2 * u);
-              a[2 * j + u][e + 2] = kv4_pair(word[j], 2 * u + 1);
-            }
+          next += kWarps;
+          if (++used == 32) load_ids();
         }
-      } else {
-        const uint8_t* block = P.pool + 2 * kv_tile_base(P.n_pages, P.n_kv, D, P.layer, page, h);
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int j = 0; j < NW; ++j) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(block + 2 * kv_tile_offset(g + 8 * e, t * (D / 4) + 8 * j, D)));
-            a[2 * j][e] = v.x;
-            a[2 * j][e + 2] = v.y;
-            a[2 * j + 1][e] = v.z;
-            a[2 * j + 1][e + 2] = v.w;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      };
+      load_ids();
+      for (int s = 0; s < SH::kSlots; ++s) request(s * SH::kPage);
+
+      // ---- the rows that count, as many as fit ----
+      if (warp == 0) {
+        const int fit = kChunkRows / P.group;
+        int n = 0, at = first_tok;
+        while (at < n_new && n < fit) {
+          const bool counts = at + lane < n_new && (!P.row_weight || P.row_weight[tok_first + at + lane] != 0.f);
+          unsigned m = __ballot_sync(0xffffffffu, counts);
+          const int mine = n + __popc(m & ((1u << lane) - 1));
+          if (counts && mine < fit) s_list[mine] = tok_first + at + lane;
+          if (n + __popc(m) > fit) {                     // up to the last one that fits
+            for (int k = fit - n; k > 1; --k) m &= m - 1;
+            at += __ffs(m);
+            n = fit;
+          } else {
+            n += __popc(m);
+            at += 32;
           }
+        }
+        if (lane == 0) {
+          s_count = n;
+          s_next = min(at, n_new);
+          s_top = 0;
+          s_lim = 0x7fffffff;
+        }
       }
-    }
-    float acc[2] = {0.f, 0.f};
-    const int R = n_new * P.group;
-    for (int row0 = 0; row0 < R; row0 += kChunkRows) {
-      // ---- stage the next rows: chunk c of a row at (c % NW) * 4 + c / NW, where lane c / NW of a quad looks for it ----
       __syncthreads();
-      const int rows = min(kChunkRows, R - row0), rows8 = (rows + 7) & ~7;
-      for (int i = tid; i < rows8 * kChunks; i += kThreads) {
-        const int row = i / kChunks, c = i - row * kChunks, rho = row0 + row;
-        const int tok = tok_first + rho / P.group, head = h * P.group + rho % P.group;
-        const uint4 v = row < rows ? __ldg(reinterpret_cast<const uint4*>(P.q + ((size_t)tok * P.n_q + head) * D) + c) : make_uint4(0, 0, 0, 0);
-        s_q[row * kRowChunks + (c % NW) * 4 + c / NW] = v;
-        float sum = 0.f;
+      first_tok = s_next;
+      const int rows = s_count * P.group, rows8 = (rows + 7) & ~7;
+      // chunk c of a row, values 8 c .. 8 c + 7, goes where lane c / NW of a quad looks for its word c % NW
+      constexpr int kPer = kChunkRows * kChunks / kThreads + 1;
+      uint4 raw[kPer];
+      unsigned top = 0;
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        const int i = tid + k * kThreads, row = i / kChunks, c = i % kChunks;
+        raw[k] = make_uint4(0, 0, 0, 0);
+        if (row < rows) {
+          const int j = row / P.group;
+          raw[k] = __ldg(reinterpret_cast<const uint4*>(P.q + ((size_t)s_list[j] * P.n_q + h * P.group + row - j * P.group) * D) + c);
+        }
+        if (FOUR) {
+          const uint32_t u[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const unsigned lo = u[x] & 0x7fffu, hi = (u[x] >> 16) & 0x7fffu;
+            top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+          }
+        }
+      }
+      if (FOUR) {
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) atomicMax(&s_top, top);
+      }
+      for (int row = tid; row < rows8; row += kThreads) {
+        float4 info = make_float4(0.f, -1e30f, 0.f, 0.f);         // (a row that fills up the last eight: probability 0)
+        int4 vis = make_int4(-1, 0, 0, 0);
+        if (row < rows) {
+          const int j = row / P.group, tok = s_list[j];
+          info.y = -1.4426950408889634f * P.lse[(size_t)tok * P.n_q + h * P.group + row - j * P.group];
+          info.z = P.row_weight ? P.row_weight[tok] : 1.f;
+          vis = make_int4(P.tok_climit[tok], P.tok_lo[tok], P.tok_hi[tok], 0);
+          atomicMin(&s_lim, vis.x);
+        }
+        *reinterpret_cast<float3*>(&s_info[row].y) = make_float3(info.y, info.z, info.w);
+        s_vis[row] = vis;
+      }
+      __syncthreads();
+      const int e = FOUR ? max(-100, min(100, (int)(s_top >> 7) - 127 - 8)) : 0;       // the largest value to [2^8, 2^9)
+      const float down = pow2(-e), down16 = pow2(-e - 4), factor = FOUR ? pow2(e) * 16777216.f * P.scale_log2 : P.scale_log2;
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        const int i = tid + k * kThreads, row = i / kChunks, c = i % kChunks, lane_t = c / NW;
+        if (row >= rows8) continue;
+        // (bf16: the words in the order in which the lanes of a quad read K without meeting a bank twice)
+        const int word = FOUR || NW < 4 ? c % NW : (c % NW) ^ (2 * (lane_t >> 1));
+        const uint4 v = raw[k];
+        *reinterpret_cast<uint4*>(smem + SH::kRowsOff + row * SH::kRowBytes + (word * 4 + lane_t) * 16) =
+            FOUR ? make_uint4(scaled_f16(v.x, down), scaled_f16(v.y, down16), scaled_f16(v.z, down), scaled_f16(v.w, down16)) : v;
         if (FOUR) {
           const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+          float sum = 0.f;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) sum += __uint_as_float(u[k] << 16) + __uint_as_float(u[k] & 0xffff0000u);
+          for (int x = 0; x < 4; ++x) sum += __uint_as_float(u[x] << 16) + __uint_as_float(u[x] & 0xffff0000u);
           // (rows8 * kChunks is a multiple of 64 and kThreads of kChunks: whole quarter and half warps come here together)
-          const unsigned group_mask = (kChunks == 16 ? 0xffffu : 0xffu) << (lane & ~(kChunks - 1));
+          const unsigned together = (kChunks == 16 ? 0xffffu : 0xffu) << (lane & ~(kChunks - 1));
 #pragma unroll
-          for (int o = kChunks / 2; o; o >>= 1) sum += __shfl_xor_sync(group_mask, sum, o);
-        }
-        if (c == 0) {
-          RowInfo ri = {sum, 0.f, 0.f, 0x7fffffff, 0, 0};
-          if (row < rows) {
-            ri.weight = P.row_weight ? P.row_weight[tok] : 1.f;
-            ri.lse2 = P.lse[(size_t)tok * P.n_q + head] * 1.4426950408889634f;
-            ri.climit = P.tok_climit[tok];
-            ri.lo = P.tok_lo[tok];
-            ri.hi = P.tok_hi[tok];
-          }
-          s_row[row] = ri;
+          for (int o = kChunks / 2; o; o >>= 1) sum += __shfl_xor_sync(together, sum, o);
+          if (c == 0) s_info[row].x = sum * P.scale_log2;
+        } else if (c == 0) {
+          s_info[row].x = 0.f;
         }
       }
       __syncthreads();
-      if (page < 0) continue;
-      for (int nt = 0; nt < rows8; nt += 8) {
-        const RowInfo r0 = s_row[nt + 2 * t], r1 = s_row[nt + 2 * t + 1];
-        if (!__any_sync(0xffffffffu, r0.weight != 0.f || r1.weight != 0.f)) continue;
-        float sc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < NW; ++j) {
-          const uint4 b = s_q[(nt + g) * kRowChunks + j * 4 + t];
-          mma_bf16_16816(sc, a[2 * j], b.x, b.y);
-          mma_bf16_16816(sc, a[2 * j + 1], b.z, b.w);
+      const int lim = s_lim;
+
+      // ---- pages past the rows ----
+      uint32_t slot_at = 0;
+      for (int p = page0 + warp; p < page1; p += kWarps) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(SH::kSlots - 1) : "memory");
+        const int id = __ldg(table + p), pos0 = p * kPageSize;
+        const bool there = (unsigned)id < (unsigned long long)P.n_pages;
+        const int tok = g + 8 * t;                       // lane 0 of a quad stores row g, lane 1 row g + 8
+        const bool stores = t < 2 && there && pos0 + tok < kv_len;
+        const size_t at = out_base + (size_t)(there ? id : 0) * P.n_kv * kPageSize + tok;
+        float before = 0.f;
+        if (stores) {
+          if (chunk) before = P.out[at];
+          else if (P.in && pos0 + tok < L && P.decay != 0.f) before = P.decay * P.in[at];
         }
-        const bool need_mask = __any_sync(0xffffffffu, pos0 + kPageSize - 1 > min(r0.climit, r1.climit));
+        if (!there && lane == 0) set_status(P.status, DEV_BAD_INDEX);
+        __syncwarp();
+        const uint8_t* pg = smem + warp * SH::kSlots * SH::kPage + slot_at;
+        uint32_t a[D / 16][4];
+        float sk[2] = {factor, factor}, mk[2] = {0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const RowInfo& ri = (e & 1) ? r1 : r0;
-          float p = exp2f(fmaf(sc[e], sk[e >> 1], fmaf(mk[e >> 1], ri.qsum, -ri.lse2)));
-          const int pos = pos0 + g + 8 * (e >> 1);
-          bool counts = ri.weight != 0.f;
-          if (need_mask) counts = counts && (pos <= ri.climit || (pos >= ri.lo && pos < ri.hi));
-          if (counts) acc[e >> 1] = fmaf(p, ri.weight, acc[e >> 1]);
+        for (int e2 = 0; e2 < 2; ++e2) {
+          const int tk = g + 8 * e2;
+          if (FOUR) {
+            uint32_t word[4];
+            if (NW == 4) {
+              const uint4 v = *reinterpret_cast<const uint4*>(pg + tk * (D / 2) + t * 16);
+              word[0] = v.x; word[1] = v.y; word[2] = v.z; word[3] = v.w;
+            } else {
+              const uint2 v = *reinterpret_cast<const uint2*>(pg + tk * (D / 2) + t * 8);
+              word[0] = v.x; word[1] = v.y;
+            }
+            const uint32_t pair = *reinterpret_cast<const uint32_t*>(pg + SH::kCodes + 4 * tk);
+            sk[e2] = kv4_step(pair) * factor;
+            mk[e2] = kv4_min(pair);
+#pragma unroll
+            for (int j = 0; j < NW; ++j)
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const uint32_t w = u ? word[j] >> 8 : word[j];
+                a[2 * j + u][e2] = w & 0x000f000fu;
+                a[2 * j + u][e2 + 2] = w & 0x00f000f0u;
+              }
+          } else {
+#pragma unroll
+            for (int j = 0; j < NW; ++j) {
+              const int word = NW < 4 ? j : j ^ (2 * (t >> 1));
+              const uint4 v = *reinterpret_cast<const uint4*>(pg + 2 * kv_tile_offset(tk, t * (D / 4) + 8 * word, D));
+              a[2 * j][e2] = v.x;
+              a[2 * j][e2 + 2] = v.y;
+              a[2 * j + 1][e2] = v.z;
+              a[2 * j + 1][e2 + 2] = v.w;
+            }
+          }
         }
+        __syncwarp();
+        request(slot_at);
+        slot_at = slot_at == (SH::kSlots - 1) * SH::kPage ? 0 : slot_at + SH::kPage;
+        float acc[2] = {0.f, 0.f};
+        auto walk = [&](auto masked) {
+          constexpr bool MASK = decltype(masked)::value;
+#pragma unroll 2
+          for (int nt = 0; nt < rows8; nt += 8) {
+            float sc[2][4] = {};
+#pragma unroll
+            for (int j = 0; j < NW; ++j) {
+              const uint4 b = *reinterpret_cast<const uint4*>(smem + SH::kRowsOff + (nt + g) * SH::kRowBytes + (j * 4 + t) * 16);
+              mma<FOUR>(sc[0], a[2 * j][0], a[2 * j][1], a[2 * j][2], a[2 * j][3], b.x, b.y);
+              mma<FOUR>(sc[1], a[2 * j + 1][0], a[2 * j + 1][1], a[2 * j + 1][2], a[2 * j + 1][3], b.z, b.w);
+            }
+            const float4 i0 = s_info[nt + 2 * t], i1 = s_info[nt + 2 * t + 1];
+            int4 v0, v1;
+            if (MASK) {
+              v0 = s_vis[nt + 2 * t];
+              v1 = s_vis[nt + 2 * t + 1];
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const float4& ri = (x & 1) ? i1 : i0;
+              const float shift = FOUR ? fmaf(mk[x >> 1], ri.x, ri.y) : ri.y;
+              const float p_ = exp2f(fmaf(sc[0][x] + sc[1][x], sk[x >> 1], shift));
+              if (MASK) {
+                const int4& vi = (x & 1) ? v1 : v0;
+                const int pos = pos0 + g + 8 * (x >> 1);
+                if (pos <= vi.x || (pos >= vi.y && pos < vi.z)) acc[x >> 1] = fmaf(p_, ri.z, acc[x >> 1]);
+              } else {
+                acc[x >> 1] = fmaf(p_, ri.z, acc[x >> 1]);
+              }
+            }
+          }
+        };
+        if (pos0 + kPageSize - 1 > lim) walk(std::true_type{});
+        else walk(std::false_type{});
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          acc[x] += __shfl_xor_sync(0xffffffffu, acc[x], 1);
+          acc[x] += __shfl_xor_sync(0xffffffffu, acc[x], 2);
+        }
+        if (stores) P.out[at] = before + (t ? acc[1] : acc[0]);
       }
-    }
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], 1);
-      acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], 2);
-    }
-    const int tok = g + 8 * t, pos = pos0 + tok;       // lane 0 of a quad stores row g, lane 1 row g + 8
-    if (t < 2 && page >= 0 && pos < kv_len) {
-      const size_t at = (((size_t)P.layer * P.n_pages + page) * P.n_kv + h) * kPageSize + tok;
-      const float before = P.in && pos < L && P.decay != 0.f ? P.decay * P.in[at] : 0.f;
-      P.out[at] = before + (t ? acc[1] : acc[0]);
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      __syncthreads();                                   // the staged rows may be replaced
     }
   }
+}
+
+template <int D, bool FOUR>
+void launch_shape(const Params& P, int n_sm, cudaStream_t st) {
+  constexpr int kMost = Shape<D, FOUR>::kTotal + (kMaxLayoutRequests + 1) * (int)sizeof(int);
+  static_assert(kMost <= 227 * 1024, "shared memory budget");
+  static bool configured[kMaxDevices] = {false};
+  if (first_use_on_device(configured)) cudaFuncSetAttribute(kv_weights_kernel<D, FOUR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+  launch_pdl(kv_weights_kernel<D, FOUR>, dim3(n_sm), dim3(kThreads), Shape<D, FOUR>::kTotal + (P.n_req + 1) * sizeof(int), st, P);
 }
 
 }  // namespace
@@ -240,9 +400,8 @@ void launch_kv_weights(const BatchLayout& bl, const Dims& dm, int layer, const v
   P.group = dm.n_q / dm.n_kv;
   P.scale_log2 = 1.4426950408889634f / sqrtf((float)dm.head_dim);
   P.status = status;
-  auto* kernel = dm.head_dim == 128 ? (four ? kv_weights_kernel<128, true> : kv_weights_kernel<128, false>)
-                                    : (four ? kv_weights_kernel<64, true> : kv_weights_kernel<64, false>);
-  launch_pdl(kernel, dim3(2 * n_sm), dim3(kThreads), (bl.n_req + 1) * sizeof(int), st, P);
+  if (dm.head_dim == 128) (four ? launch_shape<128, true> : launch_shape<128, false>)(P, n_sm, st);
+  else (four ? launch_shape<64, true> : launch_shape<64, false>)(P, n_sm, st);
 }
 
 }  // namespace recg
