@@ -10,9 +10,9 @@
 // stream pages past them, each into a ring of its own, 16 bytes a lane.  (One CTA per 128 tokens, with its own staging and K by
 // plain loads: sixteen decoding requests 41.5 us, a serving batch on a bf16 pool 140; now %DEC% and %BATCH%.)
 //
-// Operands: a lane holds the values [D / 4 t, D / 4 (t + 1)) of two tokens (t its number in the quad), which are contiguous; the
-// contraction index is permuted accordingly and Q is staged in that order.  A pool in 4 bits: codes as subnormal fp16 numbers, Q scaled by a
-// power of two, steps and minima in fp32 (attention_kv4.cu has the reasons).
+// Operands.  A bf16 pool: its tiles are what ldmatrix takes.  A pool in 4 bits: a lane holds the values [D / 4 t, D / 4 (t + 1)) of two
+// tokens (t its number in the quad), the contraction index is permuted accordingly; codes as subnormal fp16 numbers, Q scaled by a power of
+// two, steps and minima in fp32 (attention_kv4.cu has the reasons).  Q is staged in the order in which a lane takes two k-steps at once.
 #include <cuda_fp16.h>
 #include <type_traits>
 
@@ -65,16 +65,18 @@ struct Shape {
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-template <bool HALF>
-__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+// d (+)= a b; FIRST: the accumulator starts from zero
+template <bool HALF, bool FIRST>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  const float c0 = FIRST ? 0.f : d[0], c1 = FIRST ? 0.f : d[1], c2 = FIRST ? 0.f : d[2], c3 = FIRST ? 0.f : d[3];
   if (HALF)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 __device__ __forceinline__ uint32_t scaled_f16(uint32_t pair, float by) {
   const __half2 h = __floats2half2_rn(__uint_as_float(pair << 16) * by, __uint_as_float(pair & 0xffff0000u) * by);
@@ -191,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
       __syncthreads();
       first_tok = s_next;
       const int rows = s_count * P.group, rows8 = (rows + 7) & ~7;
-      // chunk c of a row, values 8 c .. 8 c + 7, goes where lane c / NW of a quad looks for its word c % NW
+      // (chunk c of a row: its values 8 c .. 8 c + 7)
       constexpr int kPer = kChunkRows * kChunks / kThreads + 1;
       uint4 raw[kPer];
       unsigned top = 0;
@@ -234,13 +236,22 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
       const float down = pow2(-e), down16 = pow2(-e - 4), factor = FOUR ? pow2(e) * 16777216.f * P.scale_log2 : P.scale_log2;
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
-        const int i = tid + k * kThreads, row = i / kChunks, c = i % kChunks, lane_t = c / NW;
+        const int i = tid + k * kThreads, row = i / kChunks, c = i % kChunks;
         if (row >= rows8) continue;
-        // (bf16: the words in the order in which the lanes of a quad read K without meeting a bank twice)
-        const int word = FOUR || NW < 4 ? c % NW : (c % NW) ^ (2 * (lane_t >> 1));
         const uint4 v = raw[k];
-        *reinterpret_cast<uint4*>(smem + SH::kRowsOff + row * SH::kRowBytes + (word * 4 + lane_t) * 16) =
-            FOUR ? make_uint4(scaled_f16(v.x, down), scaled_f16(v.y, down16), scaled_f16(v.z, down), scaled_f16(v.w, down16)) : v;
+        uint8_t* at = smem + SH::kRowsOff + row * SH::kRowBytes;
+        if (FOUR) {
+          // where lane c / NW of a quad looks for its word c % NW
+          *reinterpret_cast<uint4*>(at + ((c % NW) * 4 + c / NW) * 16) =
+              make_uint4(scaled_f16(v.x, down), scaled_f16(v.y, down16), scaled_f16(v.z, down), scaled_f16(v.w, down16));
+        } else {
+          // pair i of the chunk belongs to lane i of a quad, which takes the pairs of four chunks at once: two k-steps
+          uint32_t* to = reinterpret_cast<uint32_t*>(at + (c >> 2) * 64) + (c & 3);
+          to[0] = v.x;
+          to[4] = v.y;
+          to[8] = v.z;
+          to[12] = v.w;
+        }
         if (FOUR) {
           const uint32_t u[4] = {v.x, v.y, v.z, v.w};
           float sum = 0.f;
@@ -300,17 +311,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
                 a[2 * j + u][e2] = w & 0x000f000fu;
                 a[2 * j + u][e2 + 2] = w & 0x00f000f0u;
               }
-          } else {
-#pragma unroll
-            for (int j = 0; j < NW; ++j) {
-              const int word = NW < 4 ? j : j ^ (2 * (t >> 1));
-              const uint4 v = *reinterpret_cast<const uint4*>(pg + 2 * kv_tile_offset(tk, t * (D / 4) + 8 * word, D));
-              a[2 * j][e2] = v.x;
-              a[2 * j][e2 + 2] = v.y;
-              a[2 * j + 1][e2] = v.z;
-              a[2 * j + 1][e2 + 2] = v.w;
-            }
           }
+        }
+        if (!FOUR) {           // matrices: tokens 0..7 and 8..15 of values 16 k .., then of 16 k + 8 ..
+          const uint32_t tk = lane & 15, half = lane >> 4, pg_at = smem_u32(pg);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            ldmatrix_x4(a[k][0], a[k][1], a[k][2], a[k][3], pg_at + 2 * kv_tile_offset(tk, 16 * k + 8 * half, D));
         }
         __syncwarp();
         request(slot_at);
@@ -320,12 +327,17 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
           constexpr bool MASK = decltype(masked)::value;
 #pragma unroll 2
           for (int nt = 0; nt < rows8; nt += 8) {
-            float sc[2][4] = {};
+            float sc[2][4];
 #pragma unroll
             for (int j = 0; j < NW; ++j) {
               const uint4 b = *reinterpret_cast<const uint4*>(smem + SH::kRowsOff + (nt + g) * SH::kRowBytes + (j * 4 + t) * 16);
-              mma<FOUR>(sc[0], a[2 * j][0], a[2 * j][1], a[2 * j][2], a[2 * j][3], b.x, b.y);
-              mma<FOUR>(sc[1], a[2 * j + 1][0], a[2 * j + 1][1], a[2 * j + 1][2], a[2 * j + 1][3], b.z, b.w);
+              if (j == 0) {
+                mma<FOUR, true>(sc[0], a[0], b.x, b.y);
+                mma<FOUR, true>(sc[1], a[1], b.z, b.w);
+              } else {
+                mma<FOUR, false>(sc[0], a[2 * j], b.x, b.y);
+                mma<FOUR, false>(sc[1], a[2 * j + 1], b.z, b.w);
+              }
             }
             const float4 i0 = s_info[nt + 2 * t], i1 = s_info[nt + 2 * t + 1];
             int4 v0, v1;
