@@ -31,9 +31,12 @@ struct Params {
   const int* cu_tok;
   const int* page_table;
   int pt_stride, n_req;
+  const int* tok_req;
   const int* tok_climit;
   const int* tok_lo;
   const int* tok_hi;
+  const int* dyn;
+  int n_tok;
   const __nv_bfloat16* q;
   const float* lse;
   const float* row_weight;    // null: one each
@@ -51,7 +54,9 @@ template <int D, bool FOUR>
 struct Shape {
   static constexpr int kBlock = FOUR ? kv4_block_bytes(D) : 4 * kPageSize * D;      // of a page and head in the pool
   static constexpr int kCodes = FOUR ? kPageSize * D / 2 : kPageSize * D * 2;       // its K: codes or values ...
-  static constexpr int kPage = kCodes + (FOUR ? 64 : 0);                            // ... and pairs
+  static constexpr int kWeights = kCodes + (FOUR ? 64 : 0);                         // ... and pairs; the weights so far;
+  static constexpr int kId = kWeights + 64;                                         // the page's id
+  static constexpr int kPage = kId + 16;
   static constexpr int kSlots = FOUR ? 4 : 3;                                       // pages that a warp has on their way
   static constexpr int kRowBytes = 2 * D + 64;      // from staged row to staged row: lanes of eight rows meet no bank twice
   static constexpr int kRing = kWarps * kSlots * kPage;
@@ -60,6 +65,7 @@ struct Shape {
   static constexpr int kVisOff = kInfoOff + kChunkRows * 16;
   static constexpr int kListOff = kVisOff + kChunkRows * 16;
   static constexpr int kTotal = kListOff + kChunkRows * 4;
+  static_assert(kPage % 16 == 0 && kTotal % 16 == 0, "16-byte pieces");
 };
 
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
@@ -92,55 +98,85 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
   float4* s_info = reinterpret_cast<float4*>(smem + SH::kInfoOff);     // a staged row: sum of its values times the scale, -lse (powers of two), weight
   int4* s_vis = reinterpret_cast<int4*>(smem + SH::kVisOff);
   int* s_list = reinterpret_cast<int*>(smem + SH::kListOff);           // tokens that count
-  int* s_first = reinterpret_cast<int*>(smem + SH::kTotal);            // [n_req + 1] pages (all kv heads) in front of request r
-  __shared__ int s_scan[kWarps], s_count, s_next, s_lim;
+  int* s_cost = reinterpret_cast<int*>(smem + SH::kTotal);             // [n_req] cost of a page and head of request r
+  long long* s_first = reinterpret_cast<long long*>(smem);             // [n_req + 1] cost in front of request r (where rings and rows are later)
+  __shared__ long long s_scan[kWarps];
+  __shared__ int s_count, s_next, s_lim;
   __shared__ unsigned s_top;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   griddep_wait();
   griddep_launch();
+  // The line of pages [request][kv head][page], each as long as it takes: kPageCost for K and as much again for eight rows that count.
+  // (With pages of one length the CTAs of requests with few rows waited for the others: a serving batch on a bf16 pool 86 us.)
+  constexpr int kPageCost = 3;
+  const int n_tok = P.dyn ? P.dyn[0] : P.n_tok;
+  for (int r = tid; r < P.n_req; r += kThreads) s_cost[r] = 0;
+  __syncthreads();
+  for (int x = tid; x < n_tok; x += kThreads)
+    if (!P.row_weight || P.row_weight[x] != 0.f) atomicAdd(&s_cost[P.tok_req[x]], 1);
+  __syncthreads();
   auto pages_of = [&](int r) { return (P.ctx_len[r] + P.cu_tok[r + 1] - P.cu_tok[r] + kPageSize - 1) / kPageSize; };
   {
     const int per = (P.n_req + kThreads - 1) / kThreads, r0 = min(P.n_req, tid * per), r1 = min(P.n_req, r0 + per);
-    int mine = 0;
-    for (int r = r0; r < r1; ++r) mine += pages_of(r) * P.n_kv;
-    int incl = mine;
+    long long mine = 0;
+    for (int r = r0; r < r1; ++r) {
+      const int cost = kPageCost + (s_cost[r] * P.group + 7) / 8;
+      s_cost[r] = cost;
+      s_first[r] = mine;
+      mine += (long long)pages_of(r) * P.n_kv * cost;
+    }
+    long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, incl, o);
+      const long long y = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += y;
     }
     if (lane == 31) s_scan[warp] = incl;
     __syncthreads();
-    int at = incl - mine;
+    long long at = incl - mine;
     for (int k = 0; k < warp; ++k) at += s_scan[k];
-    for (int r = r0; r < r1; ++r) {
-      s_first[r] = at;
-      at += pages_of(r) * P.n_kv;
-    }
-    if (tid == kThreads - 1) s_first[P.n_req] = at;
+    for (int r = r0; r < r1; ++r) s_first[r] += at;
+    if (tid == kThreads - 1) s_first[P.n_req] = at + mine;
     __syncthreads();
   }
-  // this CTA's piece of the line of pages [request][kv head][page]
-  const int n_units = s_first[P.n_req];
-  const int unit_begin = (int)((long long)n_units * blockIdx.x / gridDim.x), unit_end = (int)((long long)n_units * (blockIdx.x + 1) / gridDim.x);
+  // this CTA's piece of it: the pages that begin there
+  const long long total = s_first[P.n_req], piece = (total + gridDim.x - 1) / gridDim.x;
+  const long long begin = piece * blockIdx.x, end = min(total, begin + piece);
   const uint32_t ring_at = smem_u32(smem + warp * SH::kSlots * SH::kPage) + lane * 16;
   const unsigned page_bytes = (unsigned)P.n_kv * SH::kBlock;
 
-  for (int unit = unit_begin; unit < unit_end;) {
-    int r = 0, hi_r = P.n_req;                         // largest r with s_first[r] <= unit (every request has a page)
+  int r = 0, unit = 0;                                 // request and (head, page) of it the piece goes on with
+  long long first = 0;                                 // cost in front of the request
+  if (begin < end) {
+    int hi_r = P.n_req;                                // largest r with s_first[r] <= begin (every request has a page)
     while (hi_r - r > 1) {
       const int mid = (r + hi_r) >> 1;
-      if (s_first[mid] <= unit) r = mid; else hi_r = mid;
+      if (s_first[mid] <= begin) r = mid; else hi_r = mid;
     }
+    first = s_first[r];
+    unit = (int)((begin - first + s_cost[r] - 1) / s_cost[r]);
+  }
+  __syncthreads();
+  while (begin < end && r < P.n_req && first < end) {
     const int tok_first = P.cu_tok[r], n_new = P.cu_tok[r + 1] - tok_first, L = P.ctx_len[r], kv_len = L + n_new;
-    const int n_pages = (kv_len + kPageSize - 1) / kPageSize, h = (unit - s_first[r]) / n_pages;
-    const int page0 = unit - s_first[r] - h * n_pages, page1 = min(n_pages, page0 + unit_end - unit);      // pages [page0, page1) of head h
+    const int n_pages = (kv_len + kPageSize - 1) / kPageSize;
+    const int unit_end = (int)min((long long)n_pages * P.n_kv, (end - first + s_cost[r] - 1) / s_cost[r]);
+    if (unit >= unit_end) {
+      first += (long long)n_pages * P.n_kv * s_cost[r];
+      ++r;
+      unit = 0;
+      continue;
+    }
+    const int h = unit / n_pages, page0 = unit - h * n_pages, page1 = min(n_pages, page0 + unit_end - unit);      // pages [page0, page1) of head h
     unit += page1 - page0;
     const int* table = P.page_table + (size_t)r * P.pt_stride;
     const uint8_t* base = P.pool + (((size_t)P.layer * P.n_pages) * P.n_kv + h) * (size_t)SH::kBlock + lane * 16;
     const size_t out_base = ((size_t)P.layer * P.n_pages * P.n_kv + h) * kPageSize;
 
     for (int first_tok = 0, chunk = 0; first_tok < n_new || chunk == 0; ++chunk) {
+      // what the weights are added to: those so far, or what the chunk of rows before this one left
+      const float* old = chunk ? P.out + out_base : (P.in && P.decay != 0.f ? P.in + out_base : nullptr);
+      const float keep = chunk ? 1.f : P.decay;
       // ---- the warp's first pages on their way; ids 32 at a time, a lane one of them ----
       int next = page0 + warp, ids = 0, used = 0;
       auto load_ids = [&]() {
@@ -156,7 +192,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
 #pragma unroll
             for (int x = 0; x < SH::kCodes / 512; ++x) copy_async16(dst + x * 512, src + x * 512);
             if (FOUR && lane < 4) copy_async16(dst + SH::kCodes, src + kv4_k_pairs(D));
+            if (old && lane < 4) copy_async16(dst + SH::kWeights, old + (size_t)id * P.n_kv * kPageSize + lane * 4);
+          } else {
+            set_status(P.status, DEV_BAD_INDEX);
           }
+          if (lane == 0) *reinterpret_cast<unsigned*>(smem + warp * SH::kSlots * SH::kPage + slot_at + SH::kId) = id;
           next += kWarps;
           if (++used == 32) load_ids();
         }
@@ -273,19 +313,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
       uint32_t slot_at = 0;
       for (int p = page0 + warp; p < page1; p += kWarps) {
         asm volatile("cp.async.wait_group %0;" ::"n"(SH::kSlots - 1) : "memory");
-        const int id = __ldg(table + p), pos0 = p * kPageSize;
-        const bool there = (unsigned)id < (unsigned long long)P.n_pages;
-        const int tok = g + 8 * t;                       // lane 0 of a quad stores row g, lane 1 row g + 8
-        const bool stores = t < 2 && there && pos0 + tok < kv_len;
-        const size_t at = out_base + (size_t)(there ? id : 0) * P.n_kv * kPageSize + tok;
-        float before = 0.f;
-        if (stores) {
-          if (chunk) before = P.out[at];
-          else if (P.in && pos0 + tok < L && P.decay != 0.f) before = P.decay * P.in[at];
-        }
-        if (!there && lane == 0) set_status(P.status, DEV_BAD_INDEX);
         __syncwarp();
         const uint8_t* pg = smem + warp * SH::kSlots * SH::kPage + slot_at;
+        const int pos0 = p * kPageSize;
+        const unsigned id = *reinterpret_cast<const unsigned*>(pg + SH::kId);
+        const int tok = g + 8 * t;                       // lane 0 of a quad stores row g, lane 1 row g + 8
+        const bool stores = t < 2 && id < (unsigned long long)P.n_pages && pos0 + tok < kv_len;
+        float before = 0.f;
+        if (old && stores && (chunk || pos0 + tok < L)) before = keep * reinterpret_cast<const float*>(pg + SH::kWeights)[tok];
         uint32_t a[D / 16][4];
         float sk[2] = {factor, factor}, mk[2] = {0.f, 0.f};
 #pragma unroll
@@ -367,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
           acc[x] += __shfl_xor_sync(0xffffffffu, acc[x], 1);
           acc[x] += __shfl_xor_sync(0xffffffffu, acc[x], 2);
         }
-        if (stores) P.out[at] = before + (t ? acc[1] : acc[0]);
+        if (stores) P.out[out_base + (size_t)id * P.n_kv * kPageSize + tok] = before + (t ? acc[1] : acc[0]);
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
       __syncthreads();                                   // the staged rows may be replaced
@@ -377,11 +412,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
 
 template <int D, bool FOUR>
 void launch_shape(const Params& P, int n_sm, cudaStream_t st) {
-  constexpr int kMost = Shape<D, FOUR>::kTotal + (kMaxLayoutRequests + 1) * (int)sizeof(int);
+  constexpr int kMost = Shape<D, FOUR>::kTotal + kMaxLayoutRequests * (int)sizeof(int);
+  static_assert(Shape<D, FOUR>::kTotal >= (kMaxLayoutRequests + 1) * (int)sizeof(long long), "the sums fit where rings and rows are");
   static_assert(kMost <= 227 * 1024, "shared memory budget");
   static bool configured[kMaxDevices] = {false};
   if (first_use_on_device(configured)) cudaFuncSetAttribute(kv_weights_kernel<D, FOUR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-  launch_pdl(kv_weights_kernel<D, FOUR>, dim3(n_sm), dim3(kThreads), Shape<D, FOUR>::kTotal + (P.n_req + 1) * sizeof(int), st, P);
+  launch_pdl(kv_weights_kernel<D, FOUR>, dim3(n_sm), dim3(kThreads), Shape<D, FOUR>::kTotal + P.n_req * sizeof(int), st, P);
 }
 
 }  // namespace
@@ -395,6 +431,9 @@ void launch_kv_weights(const BatchLayout& bl, const Dims& dm, int layer, const v
   P.page_table = bl.page_table;
   P.pt_stride = bl.pt_stride;
   P.n_req = bl.n_req;
+  P.tok_req = bl.tok_req;
+  P.dyn = bl.dyn;
+  P.n_tok = bl.n_tok;
   P.tok_climit = bl.tok_climit;
   P.tok_lo = bl.tok_lo;
   P.tok_hi = bl.tok_hi;
