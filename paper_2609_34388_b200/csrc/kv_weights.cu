@@ -23,7 +23,6 @@ namespace recg {
 
 namespace {
 
-constexpr int kWarps = 12, kThreads = kWarps * 32;
 constexpr int kChunkRows = 128;             // query rows staged at a time
 
 struct Params {
@@ -31,12 +30,10 @@ struct Params {
   const int* cu_tok;
   const int* page_table;
   int pt_stride, n_req;
-  const int* tok_req;
+  const int* verify_len;
   const int* tok_climit;
   const int* tok_lo;
   const int* tok_hi;
-  const int* dyn;
-  int n_tok;
   const __nv_bfloat16* q;
   const float* lse;
   const float* row_weight;    // null: one each
@@ -52,12 +49,13 @@ struct Params {
 
 template <int D, bool FOUR>
 struct Shape {
+  static constexpr int kWarps = 16, kThreads = kWarps * 32;
   static constexpr int kBlock = FOUR ? kv4_block_bytes(D) : 4 * kPageSize * D;      // of a page and head in the pool
   static constexpr int kCodes = FOUR ? kPageSize * D / 2 : kPageSize * D * 2;       // its K: codes or values ...
   static constexpr int kWeights = kCodes + (FOUR ? 64 : 0);                         // ... and pairs; the weights so far;
   static constexpr int kId = kWeights + 64;                                         // the page's id
   static constexpr int kPage = kId + 16;
-  static constexpr int kSlots = FOUR ? 4 : 3;                                       // pages that a warp has on their way
+  static constexpr int kSlots = FOUR ? 4 : 2;                                       // pages that a warp has on their way
   static constexpr int kRowBytes = 2 * D + 64;      // from staged row to staged row: lanes of eight rows meet no bank twice
   static constexpr int kRing = kWarps * kSlots * kPage;
   static constexpr int kRowsOff = kRing;
@@ -91,8 +89,9 @@ __device__ __forceinline__ uint32_t scaled_f16(uint32_t pair, float by) {
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
 
 template <int D, bool FOUR>
-__global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_constant__ Params P) {
+__global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel(const __grid_constant__ Params P) {
   using SH = Shape<D, FOUR>;
+  constexpr int kWarps = SH::kWarps, kThreads = SH::kThreads;
   constexpr int NW = D / 32, kChunks = D / 8;           // 16-byte chunks a lane holds of a row; of a row
   extern __shared__ __align__(128) uint8_t smem[];
   float4* s_info = reinterpret_cast<float4*>(smem + SH::kInfoOff);     // a staged row: sum of its values times the scale, -lse (powers of two), weight
@@ -106,24 +105,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   griddep_wait();
   griddep_launch();
-  // The line of pages [request][kv head][page], each as long as it takes: kPageCost for K and as much again for eight rows that count.
-  // (With pages of one length the CTAs of requests with few rows waited for the others: a serving batch on a bf16 pool 86 us.)
+  // The line of pages [request][kv head][page], each as long as it takes: kPageCost for K and one for eight rows.  (With pages of one
+  // length the CTAs of requests with few rows waited for the others: a serving batch on a bf16 pool 86 us, 61 with this.)  Where rows are
+  // weighted the verify rows are taken to be the ones that count.
   constexpr int kPageCost = 3;
-  const int n_tok = P.dyn ? P.dyn[0] : P.n_tok;
-  for (int r = tid; r < P.n_req; r += kThreads) s_cost[r] = 0;
-  __syncthreads();
-  for (int x = tid; x < n_tok; x += kThreads)
-    if (!P.row_weight || P.row_weight[x] != 0.f) atomicAdd(&s_cost[P.tok_req[x]], 1);
-  __syncthreads();
-  auto pages_of = [&](int r) { return (P.ctx_len[r] + P.cu_tok[r + 1] - P.cu_tok[r] + kPageSize - 1) / kPageSize; };
+  const int per = (P.n_req + kThreads - 1) / kThreads, my_r0 = min(P.n_req, tid * per), my_r1 = min(P.n_req, my_r0 + per);
   {
-    const int per = (P.n_req + kThreads - 1) / kThreads, r0 = min(P.n_req, tid * per), r1 = min(P.n_req, r0 + per);
     long long mine = 0;
-    for (int r = r0; r < r1; ++r) {
-      const int cost = kPageCost + (s_cost[r] * P.group + 7) / 8;
+    for (int r = my_r0; r < my_r1; ++r) {
+      const int n_new = P.cu_tok[r + 1] - P.cu_tok[r], verify = P.verify_len[r];
+      const int cost = kPageCost + ((P.row_weight && verify > 0 ? verify : n_new) * P.group + 7) / 8;
       s_cost[r] = cost;
       s_first[r] = mine;
-      mine += (long long)pages_of(r) * P.n_kv * cost;
+      mine += (long long)((P.ctx_len[r] + n_new + kPageSize - 1) / kPageSize * P.n_kv) * cost;
     }
     long long incl = mine;
 #pragma unroll
@@ -135,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
     __syncthreads();
     long long at = incl - mine;
     for (int k = 0; k < warp; ++k) at += s_scan[k];
-    for (int r = r0; r < r1; ++r) s_first[r] += at;
+    for (int r = my_r0; r < my_r1; ++r) s_first[r] += at;
     if (tid == kThreads - 1) s_first[P.n_req] = at + mine;
     __syncthreads();
   }
@@ -143,7 +137,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
   const long long total = s_first[P.n_req], piece = (total + gridDim.x - 1) / gridDim.x;
   const long long begin = piece * blockIdx.x, end = min(total, begin + piece);
   const uint32_t ring_at = smem_u32(smem + warp * SH::kSlots * SH::kPage) + lane * 16;
-  const unsigned page_bytes = (unsigned)P.n_kv * SH::kBlock;
+  const unsigned page_bytes = (unsigned)P.n_kv * SH::kBlock, weight_bytes = (unsigned)P.n_kv * kPageSize * 4;
+  const unsigned pool_pages = (unsigned)min(P.n_pages, (int64_t)0x7fffffff);
 
   int r = 0, unit = 0;                                 // request and (head, page) of it the piece goes on with
   long long first = 0;                                 // cost in front of the request
@@ -172,12 +167,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
     const int* table = P.page_table + (size_t)r * P.pt_stride;
     const uint8_t* base = P.pool + (((size_t)P.layer * P.n_pages) * P.n_kv + h) * (size_t)SH::kBlock + lane * 16;
     const size_t out_base = ((size_t)P.layer * P.n_pages * P.n_kv + h) * kPageSize;
+    uint8_t* out_at = reinterpret_cast<uint8_t*>(P.out + out_base + g + 8 * (t & 1));
 
     for (int first_tok = 0, chunk = 0; first_tok < n_new || chunk == 0; ++chunk) {
       // what the weights are added to: those so far, or what the chunk of rows before this one left
-      const float* old = chunk ? P.out + out_base : (P.in && P.decay != 0.f ? P.in + out_base : nullptr);
+      const uint8_t* old = reinterpret_cast<const uint8_t*>(chunk ? P.out : (P.decay != 0.f ? P.in : nullptr));
+      if (old) old += out_base * 4 + (lane & 3) * 16;
       const float keep = chunk ? 1.f : P.decay;
-      // ---- the warp's first pages on their way; ids 32 at a time, a lane one of them ----
+      // ---- the warp's pages on their way; ids 32 at a time, a lane one of them ----
       int next = page0 + warp, ids = 0, used = 0;
       auto load_ids = [&]() {
         used = 0;
@@ -186,24 +183,25 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
       auto request = [&](uint32_t slot_at) {            // one group of copies per call, be it empty
         if (next < page1) {
           const unsigned id = __shfl_sync(0xffffffffu, ids, used);
-          if (id < (unsigned long long)P.n_pages) {
+          const uint32_t dst = ring_at + slot_at;
+          if (id < pool_pages) {
             const uint8_t* src = base + (uint64_t)id * page_bytes;
-            const uint32_t dst = ring_at + slot_at;
 #pragma unroll
             for (int x = 0; x < SH::kCodes / 512; ++x) copy_async16(dst + x * 512, src + x * 512);
-            if (FOUR && lane < 4) copy_async16(dst + SH::kCodes, src + kv4_k_pairs(D));
-            if (old && lane < 4) copy_async16(dst + SH::kWeights, old + (size_t)id * P.n_kv * kPageSize + lane * 4);
+            if (lane < 4) {
+              if (FOUR) copy_async16(dst + SH::kCodes, src + kv4_k_pairs(D));
+              if (old) copy_async16(dst + SH::kWeights, old + (uint64_t)id * weight_bytes);
+            }
           } else {
             set_status(P.status, DEV_BAD_INDEX);
           }
-          if (lane == 0) *reinterpret_cast<unsigned*>(smem + warp * SH::kSlots * SH::kPage + slot_at + SH::kId) = id;
+          if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + SH::kId), "r"(id) : "memory");
           next += kWarps;
           if (++used == 32) load_ids();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
       load_ids();
-      for (int s = 0; s < SH::kSlots; ++s) request(s * SH::kPage);
 
       // ---- the rows that count, as many as fit ----
       if (warp == 0) {
@@ -236,7 +234,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
       // (chunk c of a row: its values 8 c .. 8 c + 7)
       constexpr int kPer = kChunkRows * kChunks / kThreads + 1;
       uint4 raw[kPer];
-      unsigned top = 0;
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
         const int i = tid + k * kThreads, row = i / kChunks, c = i % kChunks;
@@ -245,7 +242,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
           const int j = row / P.group;
           raw[k] = __ldg(reinterpret_cast<const uint4*>(P.q + ((size_t)s_list[j] * P.n_q + h * P.group + row - j * P.group) * D) + c);
         }
-        if (FOUR) {
+      }
+      for (int s = 0; s < SH::kSlots; ++s) request(s * SH::kPage);
+      unsigned top = 0;
+      if (FOUR)
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
           const uint32_t u[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
@@ -253,7 +255,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
             top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
           }
         }
-      }
       if (FOUR) {
         top = __reduce_max_sync(0xffffffffu, top);
         if (lane == 0) atomicMax(&s_top, top);
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
         const int pos0 = p * kPageSize;
         const unsigned id = *reinterpret_cast<const unsigned*>(pg + SH::kId);
         const int tok = g + 8 * t;                       // lane 0 of a quad stores row g, lane 1 row g + 8
-        const bool stores = t < 2 && id < (unsigned long long)P.n_pages && pos0 + tok < kv_len;
+        const bool stores = t < 2 && id < pool_pages && pos0 + tok < kv_len;
         float before = 0.f;
         if (old && stores && (chunk || pos0 + tok < L)) before = keep * reinterpret_cast<const float*>(pg + SH::kWeights)[tok];
         uint32_t a[D / 16][4];
@@ -402,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_kernel(const __grid_co
           acc[x] += __shfl_xor_sync(0xffffffffu, acc[x], 1);
           acc[x] += __shfl_xor_sync(0xffffffffu, acc[x], 2);
         }
-        if (stores) P.out[out_base + (size_t)id * P.n_kv * kPageSize + tok] = before + (t ? acc[1] : acc[0]);
+        if (stores) *reinterpret_cast<float*>(out_at + (uint64_t)id * weight_bytes) = before + (t ? acc[1] : acc[0]);
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
       __syncthreads();                                   // the staged rows may be replaced
@@ -417,7 +418,7 @@ void launch_shape(const Params& P, int n_sm, cudaStream_t st) {
   static_assert(kMost <= 227 * 1024, "shared memory budget");
   static bool configured[kMaxDevices] = {false};
   if (first_use_on_device(configured)) cudaFuncSetAttribute(kv_weights_kernel<D, FOUR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-  launch_pdl(kv_weights_kernel<D, FOUR>, dim3(n_sm), dim3(kThreads), Shape<D, FOUR>::kTotal + P.n_req * sizeof(int), st, P);
+  launch_pdl(kv_weights_kernel<D, FOUR>, dim3(n_sm), dim3(Shape<D, FOUR>::kThreads), Shape<D, FOUR>::kTotal + P.n_req * sizeof(int), st, P);
 }
 
 }  // namespace
@@ -431,9 +432,7 @@ void launch_kv_weights(const BatchLayout& bl, const Dims& dm, int layer, const v
   P.page_table = bl.page_table;
   P.pt_stride = bl.pt_stride;
   P.n_req = bl.n_req;
-  P.tok_req = bl.tok_req;
-  P.dyn = bl.dyn;
-  P.n_tok = bl.n_tok;
+  P.verify_len = bl.verify_len;
   P.tok_climit = bl.tok_climit;
   P.tok_lo = bl.tok_lo;
   P.tok_hi = bl.tok_hi;
