@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
         float acc[2] = {0.f, 0.f};
         auto walk = [&](auto masked) {
           constexpr bool MASK = decltype(masked)::value;
-#pragma unroll 2
+#pragma unroll 1
           for (int nt = 0; nt < rows8; nt += 8) {
             float sc[2][4];
 #pragma unroll
