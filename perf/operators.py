@@ -341,7 +341,7 @@ def run(s):
         keep = torch.empty((case["layers"], len(plan["ctx"]), nkv, int(s["budget"].max())), dtype=torch.int32, device="cuda")
         s["ctx"].recg_kv_select(s["eviction"], keep)
         s["ctx"].recg_kv_compact(s["eviction"], keep)
-        return keep, s["w_out"], [s["ctx"].recg_kv_rows(s["kept"], layer) for layer in range(case["layers"])]
+        return keep, s["w_out"], [s["ctx"].recg_kv_rows(None if layer else s["kept"], layer) for layer in range(case["layers"])]
     L = int(plan["ctx"].max())
     slot, pos = _slots(s["table"], L), torch.arange(L, device="cuda")
     page, off = slot.clamp(min=0) // PAGE, slot.clamp(min=0) % PAGE
