@@ -41,65 +41,74 @@ __device__ __forceinline__ uint32_t kv4_pair(uint32_t word, int i) {
 __device__ __forceinline__ float kv4_step(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float kv4_min(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {       // of bf16 pairs; NaN stays
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// Which of its neighbours a value on the border between two codes (or next to it) goes to: r the bits of the code tried, e = a - r s,
+// |e| at least half a step.  On the border to the even one, or, where a = x - lo was rounded onto it, to where the difference lies.
+__device__ __forceinline__ uint32_t kv4_settle(uint32_t r, float e, float half, float x, float lo, float a) {
+  const int toward = e > 0.f ? 1 : -1;
+  if (fabsf(e) > half) return r + toward;
+  if (fabsf(e) < half) return r;
+  const float back = __fsub_rn(a, x), err = __fsub_rn(__fsub_rn(x, __fsub_rn(a, back)), __fadd_rn(lo, back));      // (x - lo) - a
+  return (err == 0.f ? (r & 1u) != 0 : (err > 0.f) == (toward > 0)) ? r + toward : r;
+}
 // Eight values of a row, whose other values the LANES threads around this one (consecutive lanes of a warp, aligned) hold:
 // their word of codes; *pair receives the row's {s, m}.
 template <int LANES>
 __device__ __forceinline__ uint32_t kv4_quantise(const uint4& raw, uint32_t* pair) {
   const uint32_t in[4] = {raw.x, raw.y, raw.z, raw.w};
-  float x[8];
-  bool bad = false;
+  // {max x, max -x} of the row as a bf16 pair
+  const uint32_t up = max2_nan(max2_nan(in[0], in[1]), max2_nan(in[2], in[3]));
+  const uint32_t down = max2_nan(max2_nan(in[0] ^ 0x80008000u, in[1] ^ 0x80008000u), max2_nan(in[2] ^ 0x80008000u, in[3] ^ 0x80008000u));
+  uint32_t top = max2_nan(__byte_perm(up, down, 0x5410), __byte_perm(up, down, 0x7632));
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(in[i] << 16);
-    x[2 * i + 1] = __uint_as_float(in[i] & 0xffff0000u);
-    bad |= (in[i] & 0x7f80u) == 0x7f80u || (in[i] & 0x7f800000u) == 0x7f800000u;
-  }
-  float lo = x[0], hi = x[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) {
-    lo = fminf(lo, x[i]);
-    hi = fmaxf(hi, x[i]);
-  }
-#pragma unroll
-  for (int o = LANES / 2; o; o >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
-  }
-  const __nv_bfloat16 step = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
+  for (int o = LANES / 2; o; o >>= 1) top = max2_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float hi = __uint_as_float(top << 16), lo = __uint_as_float((top & 0xffff0000u) ^ 0x80000000u);
+  // the quotient by 15, correctly rounded: the reciprocal is, and one step of the remainder follows
+  const float span = __fsub_rn(hi, lo), first = __fmul_rn(span, 1.f / 15.f);
+  const __nv_bfloat16 step = __float2bfloat16_rn(__fmaf_rn(__fmaf_rn(-first, 15.f, span), 1.f / 15.f, first));
   uint32_t sb = __bfloat16_as_ushort(step);
-  if (bad || (sb & 0x7f80u) == 0x7f80u) sb = 0x7fc0u;
+  if ((sb & 0x7f80u) == 0x7f80u) sb = 0x7fc0u;          // a value, or the range, is not finite
   else if ((sb & 0x7f80u) < 0x0400u) sb = 0;            // (a step below 2^-119, whose half may be no normal number: the row is its minimum)
   *pair = sb | (__float_as_uint(lo) & 0xffff0000u);
   const float s = __uint_as_float(sb << 16);
   if (!(s > 0.f)) return 0;
-  const float inv = __frcp_rn(s), half = .5f * s;
+  // 2^23 + 2^22 added to a number below 2^22 rounds it to a whole one, which then stands in the low bits (conversion instructions run at an
+  // eighth of the rate).  r is the quotient rounded, or next to it; the remainder e = a - r s is exact and says whether: it is as long as the
+  // reciprocal is good to 2^-19.  Every code is a nibble of the word: a sum of bits << shift, less that of the bits of 0.
+  constexpr float kWhole = 12582912.f;
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  const float half = .5f * s;
+  const float2 lo2 = make_float2(-lo, -lo), inv2 = make_float2(inv, inv), whole2 = make_float2(kWhole, kWhole), minus2 = make_float2(-kWhole, -kWhole),
+               s2 = make_float2(-s, -s);
   uint32_t word = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    // r is the quotient rounded, or next to it; the remainder a - r s is exact and says which
-    const float a = __fsub_rn(x[i], lo);
-    float r = rintf(a * inv);
-    const float e = __fmaf_rn(-r, s, a);
-    if (e > half) r += 1.f;
-    else if (e < -half) r -= 1.f;
-    else if (fabsf(e) == half) {                        // on the border, or a was rounded onto it
-      const float low = e > 0.f ? r : r - 1.f;
-      const double at = (double)x[i] - (double)lo, border = ((double)low + .5) * (double)s;
-      r = at > border ? low + 1.f : (at < border ? low : 2.f * rintf(.5f * (low + .5f)));
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = make_float2(__uint_as_float(in[i] << 16), __uint_as_float(in[i] & 0xffff0000u)), a = add2(x, lo2), q = fma2(a, inv2, whole2),
+                 e = fma2(add2(q, minus2), s2, a);
+    uint32_t r0 = __float_as_uint(q.x), r1 = __float_as_uint(q.y);
+    if (fmaxf(fabsf(e.x), fabsf(e.y)) >= half) {
+      r0 = kv4_settle(r0, e.x, half, x.x, lo, a.x);
+      r1 = kv4_settle(r1, e.y, half, x.y, lo, a.y);
     }
-    const uint32_t c = (uint32_t)fminf(fmaxf(r, 0.f), 15.f);
-    word |= c << (4 * (i >> 1) + 16 * (i & 1));
+    word += (r0 << (4 * i)) + (r1 << (4 * i + 16));
   }
-  return word;
+  constexpr uint32_t kZero = 0x4b400000u;               // the bits of kWhole
+  return word - (kZero + (kZero << 4) + (kZero << 8) + (kZero << 12) + (kZero << 16) + (kZero << 20) + (kZero << 24) + (kZero << 28));
 }
 // the eight bf16 values that a word stands for
 __device__ __forceinline__ uint4 kv4_values(uint32_t word, uint32_t pair) {
   const float s = kv4_step(pair), m = kv4_min(pair);
   uint32_t out[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    out[i] = pack_bf16(__fmaf_rn(s, (float)((word >> (4 * i)) & 15u), m), __fmaf_rn(s, (float)((word >> (4 * i + 16)) & 15u), m));
+  for (int i = 0; i < 4; ++i) {       // (2^23 + c is 0x4b000000 | c)
+    const float lo = __uint_as_float(((word >> (4 * i)) & 15u) | 0x4b000000u) - 8388608.f, hi = __uint_as_float(((word >> (4 * i + 16)) & 15u) | 0x4b000000u) - 8388608.f;
+    out[i] = pack_bf16(__fmaf_rn(s, lo, m), __fmaf_rn(s, hi, m));
+  }
   return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
