@@ -13,6 +13,7 @@ from typing import Dict, Optional
 import numpy as np
 import torch
 
+_CUDA = torch.device("cuda")
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librecg.so")
 
@@ -387,13 +388,14 @@ class Context:
         return k, v
 
     def _kv_rows_args(self, batch: Optional[Batch], k: torch.Tensor, v: torch.Tensor):
-        want = (self._n_tok(batch), self.cfg.n_kv_heads, self.cfg.head_dim)
-        for t in (k, v):
-            if t.dtype != torch.bfloat16 or not t.is_cuda or t.shape != want or t.stride()[1:] != (want[2], 1):
-                raise ValueError(f"k and v must be CUDA bf16 {list(want)} with contiguous rows")
-        if k.stride(0) != v.stride(0) and want[0] > 1:
+        n, strides = self._n_tok(batch), k.stride()
+        want = (n, self.cfg.n_kv_heads, self.cfg.head_dim)
+        if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16 or not k.is_cuda or not v.is_cuda or k.shape != want or \
+                v.shape != want or strides[1:] != (want[2], 1) or v.stride()[1:] != (want[2], 1):
+            raise ValueError(f"k and v must be CUDA bf16 {list(want)} with contiguous rows")
+        if n > 1 and strides[0] != v.stride(0):
             raise ValueError("the rows of k and v must be equally far apart")
-        return C.byref(batch.c) if batch is not None else None, k.data_ptr(), v.data_ptr(), k.stride(0) if want[0] > 1 else 0
+        return C.byref(batch.c) if batch is not None else None, k.data_ptr(), v.data_ptr(), strides[0] if n > 1 else 0
 
     def _n_tok(self, batch: Optional[Batch]) -> int:
         """Rows of the batch, or of the one that an operation was given last."""
@@ -409,8 +411,12 @@ class Context:
     def recg_kv_rows(self, batch: Optional[Batch], layer: int, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
         """The K and V rows of the batch as the pool holds them, into k and v or into new tensors."""
         if k is None or v is None:
-            k = torch.empty((self._n_tok(batch), self.cfg.n_kv_heads, self.cfg.head_dim), dtype=torch.bfloat16, device="cuda")
-            v = torch.empty_like(k)
+            # (one allocation for both; what was just made needs no checks)
+            n, heads, d = self._n_tok(batch), self.cfg.n_kv_heads, self.cfg.head_dim
+            kv = torch.empty((2, n, heads, d), dtype=torch.bfloat16, device=_CUDA)
+            at = kv.data_ptr()
+            self._check(lib().recg_kv_rows(self.h, C.byref(batch.c) if batch is not None else None, layer, at, at + 2 * n * heads * d, 0))
+            return kv[0], kv[1]
         b, kp, vp, stride = self._kv_rows_args(batch, k, v)
         self._check(lib().recg_kv_rows(self.h, b, layer, kp, vp, stride))
         return k, v
