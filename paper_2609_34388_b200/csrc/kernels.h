@@ -81,8 +81,9 @@ struct SmallDesc {
 // whole: no tile is cut (attention_whole_tiles), and no combine kernel has to follow the attention kernel.
 // tokens: the per-token arrays as well (else launch_embed follows, which fills them).
 // desc (may be null): the descriptor to be written to desc_dev, where bl points.
+// list: the work list (else the per-token arrays only, and the list may follow by itself).
 void launch_layout(const BatchLayout& bl, const Dims& dm, int tok_per_tile, int n_ctas, bool whole, int64_t n_pages,
-                   int* status, bool tokens, int* desc_dev, const SmallDesc* desc, cudaStream_t st);
+                   int* status, bool tokens, int* desc_dev, const SmallDesc* desc, cudaStream_t st, bool list = true);
 // HOST arrays [n_req]; rows: rows per request
 bool attention_whole_tiles(int n_req, const int* ctx_len, const int* rows, int n_kv, int tok_per_tile, int n_ctas);
 // the layout kernel keeps five ints per request in shared memory: requests per step are bounded by this
@@ -285,7 +286,7 @@ struct EvictDesc {
   const int* page_table;   // [n_req][pt_stride]
   const int* dst_table;    // [n_req][dst_stride], or null: in place
 };
-void launch_kv_select(const EvictDesc& E, const float* weights, int64_t n_pages, int n_kv, int n_layers, int* keep, int keep_stride,
+void launch_kv_select(EvictDesc E, const float* weights, int64_t n_pages, int n_kv, int n_layers, int max_pages, int* keep, int keep_stride,
                       cudaStream_t st);
 void launch_kv_compact(EvictDesc E, const Dims& dm, void* pool, float* weights, int64_t n_pages, bool four, int n_layers, int max_keep,
                        const int* keep, int keep_stride, int* status, cudaStream_t st);

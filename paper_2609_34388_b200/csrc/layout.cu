@@ -114,7 +114,7 @@ __device__ __forceinline__ TokenPos layout_token(const BatchLayout& bl, int r, i
 }
 
 __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, int n_kv, int mask_id, int tok_per_tile,
-                                                                int n_ctas, int whole, int64_t n_pages, int* status, int* desc_dev,
+                                                                int n_ctas, int whole, int list, int64_t n_pages, int* status, int* desc_dev,
                                                                 const __grid_constant__ SmallDesc desc) {
   extern __shared__ int sm[];
   const int C = bl.n_req;
@@ -150,6 +150,7 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, 
   }
 
   // ---- attention work list ----
+  if (!list) return;
   for (int r = tid; r < C; r += kLayoutThreads) {
     ctx[r] = bl.ctx_len[r];
     vis[r] = bl.verify_len[r];
@@ -551,7 +552,7 @@ bool attention_whole_tiles(int n_req, const int* ctx_len, const int* rows, int n
 }
 
 void launch_layout(const BatchLayout& bl, const Dims& dm, int tok_per_tile, int n_ctas, bool whole, int64_t n_pages,
-                   int* status, bool tokens, int* desc_dev, const SmallDesc* desc, cudaStream_t st) {
+                   int* status, bool tokens, int* desc_dev, const SmallDesc* desc, cudaStream_t st, bool list) {
   static const SmallDesc none{};
   const size_t smem = layout_smem_bytes(bl.n_req, n_ctas);
   static bool configured[kMaxDevices] = {false};
@@ -559,7 +560,7 @@ void launch_layout(const BatchLayout& bl, const Dims& dm, int tok_per_tile, int 
     cudaFuncSetAttribute(layout_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)layout_smem_bytes(kMaxLayoutRequests, 1024));
   const int token_ctas = tokens ? (bl.n_tok + kLayoutThreads - 1) / kLayoutThreads : 0;
   launch_pdl(layout_kernel, dim3(1 + token_ctas), dim3(kLayoutThreads), smem, st, bl, dm.n_kv, dm.mask_id, tok_per_tile, n_ctas,
-             whole ? 1 : 0, n_pages, status, desc_dev, desc ? *desc : none);
+             whole ? 1 : 0, list ? 1 : 0, n_pages, status, desc_dev, desc ? *desc : none);
 }
 
 void launch_embed(const BatchLayout& bl, const Dims& dm, const void* embed, float* h, const void* gain, void* x, float* ss,

@@ -57,6 +57,7 @@ struct recg_ctx {
   BatchLayout bl{};
   bool layout_valid = false;
   bool layout_has_pages = false;
+  bool list_pending = false;     // its work list has not been built: only operations on rows have asked for the batch so far
   bool layout_whole = false;     // no attention tile was cut: no combine kernel
   int layout_rows = 128;         // query rows of its largest row tile (128: the lengths are on the device)
   int layout_tiles = 0;          // its row tiles, all kv heads (0: the lengths are on the device)
@@ -347,7 +348,8 @@ void embed_tokens(recg_ctx* ctx, int64_t n_pages) {
                ctx->small_desc.n ? &ctx->small_desc : nullptr, ctx->stream);
 }
 
-recg_status upload_and_layout(recg_ctx* ctx, const recg_batch* b, bool need_pages, bool need_tokens = true, bool forward = false) {
+recg_status upload_and_layout(recg_ctx* ctx, const recg_batch* b, bool need_pages, bool need_tokens = true, bool forward = false,
+                              bool list = true) {
   int T = 0, Tv = 0;
   ctx->layout_valid = false;
   recg_status s = pack_batch(ctx, b, need_pages, need_tokens, &T, &Tv);
@@ -378,8 +380,9 @@ recg_status upload_and_layout(recg_ctx* ctx, const recg_batch* b, bool need_page
     ctx->layout_tiles = tiles < (1 << 20) ? (int)tiles : 1 << 20;
     ctx->layout_whole = attention_whole_tiles(b->n_req, b->ctx_len, ctx->h_rows.data(), ctx->dm.n_kv, ctx->tok_per_tile, ctx->target_items);
     launch_layout(ctx->bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, ctx->layout_whole, n_pages, ctx->d_status,
-                  !forward, ctx->d_desc, small ? &ctx->small_desc : nullptr, ctx->stream);
+                  !forward, ctx->d_desc, small ? &ctx->small_desc : nullptr, ctx->stream, list);
     ctx->list_settled = false;
+    ctx->list_pending = !list;
     if (forward) embed_tokens(ctx, n_pages);
   }
   CU(cudaGetLastError());
@@ -782,6 +785,7 @@ recg_status recg_step_device(recg_ctx* ctx, const recg_device_batch* b, recg_log
   ctx->layout_rows = 128;
   launch_layout(bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, false, b->kv_pool_pages, ctx->d_status, false, ctx->d_desc, nullptr, ctx->stream);
   ctx->list_settled = false;
+  ctx->list_pending = false;
   ctx->small_desc.n = 0;
   embed_tokens(ctx, b->kv_pool_pages);
   CU(cudaGetLastError());
@@ -932,16 +936,24 @@ recg_status recg_policy_step(recg_ctx* ctx, const recg_policy_state* state, cons
 }
 
 // The batch of a standalone operation on the pool: the one given, or the one laid out last.
-static recg_status operation_batch(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const char* who) {
+// list: it needs the attention work list too.
+static recg_status operation_batch(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const char* who, bool list = true) {
   if (layer < 0 || (ctx->cfg.n_layers > 0 && layer >= ctx->cfg.n_layers))
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": layer out of range");
   if (batch) {
-    recg_status s = upload_and_layout(ctx, batch, true, false);
+    recg_status s = upload_and_layout(ctx, batch, true, false, false, list);
     if (s == RECG_OK) ctx->logits_valid = false;
     return s;
   }
   if (!ctx->layout_valid || !ctx->layout_has_pages || !ctx->last_pool)
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": no batch given and none with a KV pool laid out before");
+  if (list && ctx->list_pending) {
+    // (the descriptor is in device memory by now)
+    launch_layout(ctx->bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, ctx->layout_whole, ctx->last_pool_pages, ctx->d_status, false,
+                  ctx->d_desc, nullptr, ctx->stream);
+    CU(cudaGetLastError());
+    ctx->list_settled = ctx->list_pending = false;
+  }
   return RECG_OK;
 }
 
@@ -1002,7 +1014,9 @@ static recg_status kv_rows(recg_ctx* ctx, bool write, const recg_batch* batch, i
   if (row_stride == 0) row_stride = width;
   if (row_stride < width || row_stride > INT32_MAX || row_stride % 8 || !aligned16(k, v))
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": rows must be 16-byte aligned and at least n_kv_heads * head_dim elements apart");
-  recg_status s = operation_batch(ctx, batch, layer, who);
+  // (Rows that are read are rarely followed by attention of the same batch, and one CTA builds its work list: 35 us for 21500 rows of four
+  // requests.  Rows that are appended usually are.)
+  recg_status s = operation_batch(ctx, batch, layer, who, write);
   if (s != RECG_OK) return s;
   launch_kv_rows(write, four_bits(ctx), ctx->bl, ctx->last_pool, ctx->last_pool_pages, layer, ctx->dm, k, v, row_stride, ctx->stream);
   CU(cudaGetLastError());
@@ -1020,7 +1034,7 @@ recg_status recg_kv_weights(recg_ctx* ctx, const recg_batch* batch, int32_t laye
   if (!ctx || !q || !lse || !weights_out) return RECG_ERR_INVALID_ARG;
   if (!(decay >= 0.f && decay <= 3e38f)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: decay must be a finite number >= 0");
   if (!aligned16(q, q)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: q must be 16-byte aligned");
-  recg_status s = operation_batch(ctx, batch, layer, "recg_kv_weights");
+  recg_status s = operation_batch(ctx, batch, layer, "recg_kv_weights", false);
   if (s != RECG_OK) return s;
   if (!aligned16(ctx->last_pool, ctx->last_pool)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: the KV pool must be 16-byte aligned");
   launch_kv_weights(ctx->bl, ctx->dm, layer, q, lse, row_weight, decay, weights_in, weights_out, ctx->last_pool, ctx->last_pool_pages,
@@ -1031,7 +1045,7 @@ recg_status recg_kv_weights(recg_ctx* ctx, const recg_batch* batch, int32_t laye
 
 // Validates an eviction and leaves its descriptor [ctx_len | kept | page table | destination table] on the device.
 static recg_status evict_batch(recg_ctx* ctx, const recg_eviction* e, int32_t keep_stride, bool moves, const char* who, EvictDesc* out,
-                               int* max_keep) {
+                               int* max_keep, int* max_pages) {
   const std::string name(who);
   if (!e || e->n_req <= 0 || !e->ctx_len || !e->budget || !e->page_table || e->kv_pool_pages <= 0)
     return fail(ctx, RECG_ERR_INVALID_ARG, name + ": null array, n_req <= 0 or no pages");
@@ -1056,7 +1070,7 @@ static recg_status evict_batch(recg_ctx* ctx, const recg_eviction* e, int32_t ke
       std::fill(ctx->h_page_seen.begin(), ctx->h_page_seen.end(), 0);
     }
   }
-  *max_keep = 0;
+  *max_keep = *max_pages = 0;
   for (int r = 0; r < C; ++r) {
     const int L = e->ctx_len[r], b = e->budget[r];
     if (L < 0 || b < 0) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": negative ctx_len or budget");
@@ -1065,6 +1079,7 @@ static recg_status evict_batch(recg_ctx* ctx, const recg_eviction* e, int32_t ke
     const int kept = L < b ? L : b;
     if (kept > *max_keep) *max_keep = kept;
     const long long need = ((long long)L + kPageSize - 1) / kPageSize, dst_need = (kept + kPageSize - 1) / kPageSize;
+    if (need > *max_pages && need <= e->page_table_stride) *max_pages = (int)need;
     if (need > e->page_table_stride || (other && dst_need > e->dst_stride))
       return fail(ctx, RECG_ERR_CAPACITY, name + ": a page table row does not cover its positions");
     d[r] = L;
@@ -1112,18 +1127,18 @@ recg_status recg_kv_select(recg_ctx* ctx, const recg_eviction* e, int32_t* keep,
   if (!ctx || !keep) return RECG_ERR_INVALID_ARG;
   if (e && !e->weights) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_select: weights is null");
   EvictDesc E;
-  int max_keep = 0;
-  recg_status s = evict_batch(ctx, e, keep_stride, false, "recg_kv_select", &E, &max_keep);
+  int max_keep = 0, max_pages = 0;
+  recg_status s = evict_batch(ctx, e, keep_stride, false, "recg_kv_select", &E, &max_keep, &max_pages);
   if (s != RECG_OK) return s;
-  launch_kv_select(E, e->weights, e->kv_pool_pages, ctx->dm.n_kv, e->layer_end - e->layer_begin, keep, keep_stride, ctx->stream);
+  launch_kv_select(E, e->weights, e->kv_pool_pages, ctx->dm.n_kv, e->layer_end - e->layer_begin, max_pages, keep, keep_stride, ctx->stream);
   CU(cudaGetLastError());
   return RECG_OK;
 }
 recg_status recg_kv_compact(recg_ctx* ctx, const recg_eviction* e, const int32_t* keep, int32_t keep_stride) {
   if (!ctx || !keep) return RECG_ERR_INVALID_ARG;
   EvictDesc E;
-  int max_keep = 0;
-  recg_status s = evict_batch(ctx, e, keep_stride, true, "recg_kv_compact", &E, &max_keep);
+  int max_keep = 0, max_pages = 0;
+  recg_status s = evict_batch(ctx, e, keep_stride, true, "recg_kv_compact", &E, &max_keep, &max_pages);
   if (s != RECG_OK) return s;
   launch_kv_compact(E, ctx->dm, e->kv_pool, e->weights, e->kv_pool_pages, four_bits(ctx), e->layer_end - e->layer_begin, max_keep, keep,
                     keep_stride, ctx->d_status, ctx->stream);

@@ -161,3 +161,38 @@ def test_refusals():
     ctx.recg_attention(batch, 0, q, torch.empty_like(q), lse)
     ctx.recg_sync()
     ctx.recg_free()
+
+
+@pytest.mark.parametrize("flags", [0] + FLAGS)
+def test_operations_on_rows_and_attention_of_one_batch_in_any_order(flags):
+    """Reading rows lays the batch out without attention's work list, which an attention without a batch then has to build."""
+    desc = synth.fixed_descriptor([700, 33, 0], [5, 1, 40], [4, 0, 3], seed=3)
+    T = desc.n_tokens
+    ctx = binding.Context(binding.make_config(shape_of(B8), 3, T, desc.page_table.shape[1], flags))
+    pool = binding.alloc_kv_pool(ctx, desc.n_pages)
+    for r, n in enumerate(desc.ctx_len + desc.rows):
+        k, v = synth.kv_values(int(n), 8, 128, seed=r)
+        ctx.recg_kv_write(pool, desc.n_pages, 0, desc.page_table[r], 0, k.cuda(), v.cuda())
+    batch = binding.Batch(desc.ctx_len, desc.verify_len, desc.block_size, None, desc.page_table, pool, desc.n_pages)
+    q = synth.queries(T, 32, 128, seed=8).cuda()
+    want, lse = torch.empty_like(q), torch.empty((T, 32), device="cuda")
+    ctx.recg_attention(batch, 0, q, want, lse)
+    w_want = torch.zeros((2, desc.n_pages, 8, 16), device="cuda")
+    ctx.recg_kv_weights(None, 0, q, lse, None, w_want)
+    other = binding.Batch([3], [2], [0], None, desc.page_table[:1], pool, desc.n_pages)
+    ctx.recg_attention(other, 0, q, torch.empty_like(q))                # another batch's list stands in the workspace now
+    rows = ctx.recg_kv_rows(batch, 0)
+    got, got_lse = torch.empty_like(q), torch.empty_like(lse)
+    ctx.recg_attention(None, 0, q, got, got_lse)
+    assert torch.equal(got, want) and torch.equal(got_lse, lse)
+    ctx.recg_attention(other, 0, q, torch.empty_like(q))
+    w = torch.zeros_like(w_want)
+    ctx.recg_kv_weights(batch, 0, q, lse, None, w)
+    ctx.recg_kv_append(None, 0, *rows)
+    got.zero_()
+    ctx.recg_attention(None, 0, q, got)
+    assert torch.equal(w, w_want)
+    if not flags:
+        assert torch.equal(got, want)                                  # (in 4 bits rows that come back are other values)
+    ctx.recg_sync()
+    ctx.recg_free()

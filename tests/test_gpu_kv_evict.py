@@ -149,6 +149,7 @@ def draw_weights(n_layers, n_pages, nkv, seed, kind):
 @pytest.mark.parametrize("reqs,sink,recent", [
     ([(0, 5), (1, 1), (16, 4), (17, 16), (100, 7), (333, 300), (64, 64), (50, 80)], 0, 0),
     ([(100, 5), (101, 6), (333, 300), (3, 9)], 4, 1), ([(9000, 1234), (8192, 64), (8193, 8192)], 4, 60), ([(40000, 39999)], 16, 0),
+    ([(100000, 70001), (31, 30)], 4, 16), ([(300000, 1000)], 3, 50),
     ([(500, 20), (20, 20)], 0, 20)])
 def test_choice(kind, reqs, sink, recent):
     nkv = 2
