@@ -62,7 +62,8 @@ enum {
   RECG_FLAG_KV_4BIT = 64,    /* the KV pool holds 4 bits a value, about a quarter of the bytes: every kv head's K row and V row
                                 of a token is 16 levels from its smallest value m in steps of s = bf16((max - m) / 15), each
                                 value taken to the nearest (ties to the even level); a row with a value that is not finite
-                                reads back as NaN.  recg_kv_pool_bytes() and everything that takes the pool follow it   */
+                                reads back as NaN.  recg_kv_pool_bytes() and everything that takes the pool follow it, steps too
+                                (RECG_FLAG_CHAIN has no effect with it)                            */
   RECG_FLAG_DEBUG_CHECKS = 8 /* guard bands behind every workspace region, checked by recg_sync() (RECG_ERR_INTERNAL
                                 if a kernel wrote past the end of one), and a host check that no page which receives
                                 new rows is named by two requests (RECG_ERR_INVALID_ARG)          */
@@ -301,6 +302,18 @@ typedef struct {
   int32_t layer_begin, layer_end;
 } recg_eviction;
 recg_status recg_kv_select(recg_ctx *ctx, const recg_eviction *eviction, int32_t *keep, int32_t keep_stride);
+/*
+ * Eviction around whole steps.
+ * recg_kv_track(): from now on every layer of a step (recg_step, recg_step_device) adds the weight that its verify rows give to the
+ *   cached tokens into `weights`, as recg_kv_weights() with weights_in = weights_out = weights and row_weight 1 for verify and 0 for all
+ *   other rows.  The array is for the pool of the steps' batches; 16-byte aligned; NULL: no longer.  (A rejected draft has given its
+ *   weight, as the rows behind it have.)
+ * recg_kv_shift(): shift[r] tokens (HOST [n_req]) of request r have been evicted: the rotary positions of its rows in the steps from now on
+ *   are those of a context longer by as much.  Requests from n_req on are not shifted; n_req = 0: none is.  recg_next_round() leaves it as
+ *   it is.  Refused while the stream is being captured.
+ */
+recg_status recg_kv_track(recg_ctx *ctx, float *weights, float decay);
+recg_status recg_kv_shift(recg_ctx *ctx, int32_t n_req, const int32_t *shift);
 recg_status recg_kv_compact(recg_ctx *ctx, const recg_eviction *eviction, const int32_t *keep, int32_t keep_stride);
 
 /*

@@ -123,6 +123,8 @@ def lib() -> C.CDLL:
         L.recg_kv_weights.argtypes = [C.c_void_p, C.POINTER(recg_batch), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
                                       C.c_void_p, C.c_void_p]
         L.recg_kv_select.argtypes = [C.c_void_p, C.POINTER(recg_eviction), C.c_void_p, C.c_int32]
+        L.recg_kv_track.argtypes = [C.c_void_p, C.c_void_p, C.c_float]
+        L.recg_kv_shift.argtypes = [C.c_void_p, C.c_int32, C.c_void_p]
         L.recg_kv_compact.argtypes = L.recg_kv_select.argtypes
         L.recg_linear.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         L.recg_debug_buffer.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_void_p), C.POINTER(C.c_int32),
@@ -145,7 +147,8 @@ def lib() -> C.CDLL:
         L.recg_debug_map_cache_selftest.argtypes = [C.c_int32, C.POINTER(C.c_int32)]
         L.recg_debug_map_cache_selftest.restype = C.c_int32
         for f in ("recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write", "recg_kv_read",
-                  "recg_attention_lse", "recg_kv_append", "recg_kv_rows", "recg_kv_weights", "recg_kv_select", "recg_kv_compact",
+                  "recg_attention_lse", "recg_kv_append", "recg_kv_rows", "recg_kv_weights", "recg_kv_select", "recg_kv_compact", "recg_kv_track",
+           "recg_kv_shift",
            "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_timing_enable", "recg_timing_read",
                   "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
                   "recg_step_device", "recg_next_round"):
@@ -155,7 +158,8 @@ def lib() -> C.CDLL:
 
 
 EXPORTS = ("recg_kv_pool_bytes", "recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write",
-           "recg_attention_lse", "recg_kv_read", "recg_kv_append", "recg_kv_rows", "recg_kv_weights", "recg_kv_select", "recg_kv_compact",
+           "recg_attention_lse", "recg_kv_read", "recg_kv_append", "recg_kv_rows", "recg_kv_weights", "recg_kv_select", "recg_kv_compact", "recg_kv_track",
+           "recg_kv_shift",
            "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_last_error",
            "recg_timing_enable", "recg_timing_read", "recg_row_stats_static", "recg_row_stats_static_error",
            "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
@@ -458,6 +462,16 @@ class Context:
     def recg_kv_compact(self, ev: Eviction, keep: torch.Tensor):
         """Moves K, V and weights of the positions in keep to the front of the request's pages, or to the destination pages."""
         self._check(lib().recg_kv_compact(self.h, *self._keep_args(ev, keep)))
+
+    def recg_kv_track(self, weights: Optional[torch.Tensor], decay: float = 1.0):
+        """Steps add the weight that their verify rows give to the cached tokens into `weights` (None: no longer)."""
+        self._check(lib().recg_kv_track(self.h, self._floats("weights", weights), float(decay)))
+        self._track = weights                          # (the steps write to it)
+
+    def recg_kv_shift(self, shift):
+        """shift [n_req]: tokens that have been evicted from each request (empty: none)."""
+        a = _i32(shift)
+        self._check(lib().recg_kv_shift(self.h, a.size, _ptr(a) if a.size else None))
 
     def recg_linear(self, x: torch.Tensor, w: torch.Tensor, out_dtype=torch.float32) -> torch.Tensor:
         M, K = x.shape

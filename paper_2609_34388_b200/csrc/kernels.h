@@ -44,6 +44,8 @@ struct BatchLayout {
   // per token, written by the layout kernel
   int* tok_id;
   int* tok_req;
+  const int* pos_shift;   // [C] tokens of the request that an eviction has taken out (null: none): rotary positions lie behind them
+  float* tok_weight;      // 1 for verify rows, 0 for all others
   int* tok_pos;     // rotary position (a branch token: the position its branch hypothesises)
   int* tok_slot;    // page*16 + offset of cache position L + (row within the request)
   int* tok_climit;  // sees every cache position <= climit ...
@@ -273,6 +275,9 @@ void launch_kv4_io(bool write, void* pool, int64_t n_pages, int layer, const Dim
 void launch_kv_rows(bool write, bool four, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, void* k,
                     void* v, int64_t row_stride, cudaStream_t st);
 
+// The rows of a round that the QKV projection has left in a bf16 staging pool (row t in slot t of it) into a pool in 4 bits
+void launch_kv_stage(const BatchLayout& bl, const void* stage, int stage_pages, void* pool, int64_t n_pages, int layer, const Dims& dm,
+                     cudaStream_t st);
 // Attention weight gathered by the cached tokens of the batch laid out last; row_weight and in may be null
 void launch_kv_weights(const BatchLayout& bl, const Dims& dm, int layer, const void* q, const float* lse, const float* row_weight,
                        float decay, const float* in, float* out, const void* pool, int64_t n_pages, bool four, int n_sm, int* status,

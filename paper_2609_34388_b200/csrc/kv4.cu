@@ -66,7 +66,8 @@ __global__ void __launch_bounds__(kThreads) kv4_io_kernel(uint8_t* pool, int64_t
 }
 
 // The rows of a batch, row t to or from slot tok_slot[t]; rows row_stride elements apart.  FOUR: a pool in 4 bits.
-template <int D, bool FOUR, bool WRITE>
+// STAGED: row t of k and v lies in slot t of a bf16 pool of row_stride pages (v is not used).
+template <int D, bool FOUR, bool WRITE, bool STAGED>
 __global__ void __launch_bounds__(kThreads) kv_rows_kernel(uint8_t* pool, int64_t n_pages, int layer, int n_kv, const int* __restrict__ tok_slot,
                                                            int n_tok, const int* dyn, uint8_t* k, uint8_t* v, int64_t row_stride) {
   constexpr int kLanes = D / 8;
@@ -74,7 +75,9 @@ __global__ void __launch_bounds__(kThreads) kv_rows_kernel(uint8_t* pool, int64_
   const int64_t unit = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes;
   const int j = threadIdx.x % kLanes;
   const int t = (int)(unit / n_kv), h = (int)(unit - (int64_t)t * n_kv);
-  const size_t at = ((size_t)t * row_stride + (size_t)h * D + 8 * j) * 2;
+  const size_t at = STAGED ? 2 * (kv_tile_base(row_stride, n_kv, D, 0, t / kPageSize, h) + kv_tile_offset(t % kPageSize, 8 * j, D))
+                           : ((size_t)t * row_stride + (size_t)h * D + 8 * j) * 2;
+  if (STAGED) v = k + 2 * kv_tile_elems(D);
   griddep_wait();
   if (dyn) n_tok = dyn[0];
   const int slot = t < n_tok ? tok_slot[t] : -1;
@@ -121,8 +124,8 @@ using IoKernel = void (*)(uint8_t*, int64_t, int, int, const IoPages, int, int, 
 using RowsKernel = void (*)(uint8_t*, int64_t, int, int, const int*, int, const int*, uint8_t*, uint8_t*, int64_t);
 template <int D>
 RowsKernel rows_kernel(bool four, bool write) {
-  if (four) return write ? kv_rows_kernel<D, true, true> : kv_rows_kernel<D, true, false>;
-  return write ? kv_rows_kernel<D, false, true> : kv_rows_kernel<D, false, false>;
+  if (four) return write ? kv_rows_kernel<D, true, true, false> : kv_rows_kernel<D, true, false, false>;
+  return write ? kv_rows_kernel<D, false, true, false> : kv_rows_kernel<D, false, false, false>;
 }
 
 }  // namespace
@@ -157,6 +160,15 @@ void launch_kv_rows(bool write, bool four, const BatchLayout& bl, void* pool, in
   RowsKernel kernel = dm.head_dim == 128 ? rows_kernel<128>(four, write) : rows_kernel<64>(four, write);
   launch_pdl(kernel, grid, dim3(kThreads), 0, st, static_cast<uint8_t*>(pool), n_pages, layer, dm.n_kv, (const int*)bl.tok_slot,
              bl.n_tok, bl.dyn, static_cast<uint8_t*>(k), static_cast<uint8_t*>(v), row_stride);
+}
+
+void launch_kv_stage(const BatchLayout& bl, const void* stage, int stage_pages, void* pool, int64_t n_pages, int layer, const Dims& dm,
+                     cudaStream_t st) {
+  const int64_t threads = (int64_t)bl.n_tok * dm.n_kv * (dm.head_dim / 8);
+  RowsKernel kernel = dm.head_dim == 128 ? kv_rows_kernel<128, true, true, true> : kv_rows_kernel<64, true, true, true>;
+  uint8_t* from = const_cast<uint8_t*>(static_cast<const uint8_t*>(stage));
+  launch_pdl(kernel, dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, static_cast<uint8_t*>(pool), n_pages, layer,
+             dm.n_kv, (const int*)bl.tok_slot, bl.n_tok, bl.dyn, from, from, (int64_t)stage_pages);
 }
 
 }  // namespace recg

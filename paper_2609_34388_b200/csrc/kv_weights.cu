@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
       const int cost = kPageCost + ((P.row_weight && verify > 0 ? verify : n_new) * P.group + 7) / 8;
       s_cost[r] = cost;
       s_first[r] = mine;
-      mine += (long long)((P.ctx_len[r] + n_new + kPageSize - 1) / kPageSize * P.n_kv) * cost;
+      // (a device-resident round that was refused has no rows, and lengths that may be anything)
+      if (n_new > 0) mine += (long long)((P.ctx_len[r] + n_new + kPageSize - 1) / kPageSize * P.n_kv) * cost;
     }
     long long incl = mine;
 #pragma unroll
@@ -143,7 +144,7 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
   int r = 0, unit = 0;                                 // request and (head, page) of it the piece goes on with
   long long first = 0;                                 // cost in front of the request
   if (begin < end) {
-    int hi_r = P.n_req;                                // largest r with s_first[r] <= begin (every request has a page)
+    int hi_r = P.n_req;                                // largest r with s_first[r] <= begin
     while (hi_r - r > 1) {
       const int mid = (r + hi_r) >> 1;
       if (s_first[mid] <= begin) r = mid; else hi_r = mid;
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
   __syncthreads();
   while (begin < end && r < P.n_req && first < end) {
     const int tok_first = P.cu_tok[r], n_new = P.cu_tok[r + 1] - tok_first, L = P.ctx_len[r], kv_len = L + n_new;
-    const int n_pages = (kv_len + kPageSize - 1) / kPageSize;
+    const int n_pages = n_new > 0 ? (kv_len + kPageSize - 1) / kPageSize : 0;
     const int unit_end = (int)min((long long)n_pages * P.n_kv, (end - first + s_cost[r] - 1) / s_cost[r]);
     if (unit >= unit_end) {
       first += (long long)n_pages * P.n_kv * s_cost[r];

@@ -99,6 +99,8 @@ __device__ __forceinline__ TokenPos layout_token(const BatchLayout& bl, int r, i
     lo = first;
     hi = q == 0 ? first + 1 : first + span;
   }
+  if (bl.pos_shift) pos += bl.pos_shift[r];
+  bl.tok_weight[t] = j < v ? 1.f : 0.f;
   bl.tok_req[t] = r;
   bl.tok_pos[t] = pos;
   bl.tok_id[t] = id;

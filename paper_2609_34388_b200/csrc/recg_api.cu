@@ -96,6 +96,14 @@ struct recg_ctx {
   std::vector<int> h_rows;
   SmallDesc small_desc{};        // the descriptor laid out last, where it is small enough to travel with the launches (n > 0)
   std::vector<int> h_page_owner;   // debug checks: which request names a page
+  // RECG_FLAG_KV_4BIT: the QKV projection writes a round's rows to a bf16 pool of their own, row t in slot t, from where they are coded
+  void* stage = nullptr;
+  int stage_pages = 0;
+  int* d_stage_slot = nullptr;
+  int* d_pos_shift = nullptr;      // recg_kv_shift()
+  float* lse = nullptr;            // recg_kv_track(): of a layer's attention
+  float* track = nullptr;          // the caller's weights (null: off)
+  float track_decay = 1.f;
   int* d_evict = nullptr;          // eviction: the descriptor uploaded last, and on the host
   std::vector<int> h_evict;
   std::vector<int> h_page_seen;    // eviction: per page the call (times two, plus one where it is a destination) that named it last
@@ -135,6 +143,8 @@ recg_status fail(recg_ctx* c, recg_status s, const std::string& msg) {
       return fail(ctx, RECG_ERR_CUDA, std::string(#call) + ": " + cudaGetErrorString(e__));         \
   } while (0)
 
+bool four_bits(const recg_ctx* ctx) { return ctx->cfg.flags & RECG_FLAG_KV_4BIT; }
+
 size_t carve(recg_ctx* c, DeviceArena& A) {
   const recg_config& g = c->cfg;
   const size_t Cm = g.max_requests, Tm = g.max_tokens, Pm = g.max_pages_per_request;
@@ -157,6 +167,8 @@ size_t carve(recg_ctx* c, DeviceArena& A) {
   bl.cta_off = A.take<int>(4 * (c->target_items + 1));
   bl.counts = A.take<int>(4);
   c->d_evict = A.take<int>(2 * Cm + 2 * Cm * Pm);
+  c->d_pos_shift = A.take<int>(Cm);
+  bl.tok_weight = A.take<float>(Tm);
   c->d_status = A.take<int>(1);
   c->d_dyn = A.take<int>(4);
   c->d_policy = A.take<int>(8 + 8 + 64 + RECG_POLICY_MAX_BLOCKS * RECG_POLICY_MAX_BINS * RECG_POLICY_MAX_BLOCKS * 2);
@@ -194,6 +206,12 @@ size_t carve(recg_ctx* c, DeviceArena& A) {
     c->x = A.take<__nv_bfloat16>(Tm * d.hidden);
     c->ss = A.take<float>(Tm * (size_t)(d.hidden / 64 + 1));   // a column tile is at least 64 wide
     c->act = A.take<__nv_bfloat16>(Tm * d.ffn);
+    c->lse = A.take<float>(Tm * d.n_q);
+    if (four_bits(c)) {
+      c->stage_pages = (int)((Tm + kPageSize - 1) / kPageSize);
+      c->stage = A.take<__nv_bfloat16>((size_t)c->stage_pages * d.n_kv * 2 * kv_tile_elems(d.head_dim));
+      c->d_stage_slot = A.take<int>(Tm);
+    }
     const size_t esz = (g.flags & RECG_FLAG_LOGITS_BF16) ? 2 : 4;
     c->logits = A.take<uint8_t>(Tm * (size_t)d.vocab * esz);
   }
@@ -206,8 +224,6 @@ size_t carve(recg_ctx* c, DeviceArena& A) {
   }
   return A.used + 256;
 }
-
-bool four_bits(const recg_ctx* ctx) { return ctx->cfg.flags & RECG_FLAG_KV_4BIT; }
 
 // Rows of request r: verify tokens, continuation masks and the correction branches (replacement + masks each).
 static inline int request_rows(const recg_batch* b, int r) {
@@ -443,8 +459,6 @@ recg_status recg_init(recg_ctx** out, const recg_config* cfg, const recg_weights
   if (g.hidden % 64 || g.ffn % 64 || g.vocab % 16 || ((g.n_q_heads + 2 * g.n_kv_heads) * g.head_dim) % 128)
     return fail(ctx, RECG_ERR_SHAPE, "recg_init: hidden and ffn must be multiples of 64, vocab of 16, qkv width of 128");
   if (g.mask_token_id >= g.vocab) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_init: mask_token_id outside the vocabulary");
-  if (w && (g.flags & RECG_FLAG_KV_4BIT))
-    return fail(ctx, RECG_ERR_INVALID_ARG, "recg_init: RECG_FLAG_KV_4BIT is for contexts without weights");
   if (w && g.n_layers > 0 &&
       (!w->embed || !w->final_norm || !w->lm_head || !w->attn_norm || !w->wqkv || !w->wo || !w->ffn_norm ||
        !w->w_gate_up || !w->w_down))
@@ -512,6 +526,18 @@ recg_status recg_init(recg_ctx** out, const recg_config* cfg, const recg_weights
     ctx->h_vout = nullptr;   // fall back to one copy per output array
   }
   cudaMemsetAsync(ctx->d_status, 0, sizeof(int), ctx->stream);
+  if (ctx->d_stage_slot) {
+    ctx->h_desc.resize(g.max_tokens);
+    for (int t = 0; t < g.max_tokens; ++t) ctx->h_desc[t] = t;
+    if (cudaMemcpyAsync(ctx->d_stage_slot, ctx->h_desc.data(), g.max_tokens * sizeof(int), cudaMemcpyHostToDevice, ctx->stream) != cudaSuccess ||
+        cudaStreamSynchronize(ctx->stream) != cudaSuccess) {
+      if (ctx->h_vout) cudaFreeHost(ctx->h_vout);
+      cudaFree(ctx->arena.base);
+      delete ctx;
+      ctx = nullptr;
+      return fail(ctx, RECG_ERR_CUDA, "recg_init: cannot upload the staging slots");
+    }
+  }
   ctx->tc_state = tc_state_create(n_sm);
   if ((g.flags & RECG_FLAG_CHAIN) && w && g.head_dim == 128 && !(g.flags & RECG_FLAG_SIMT_GEMM)) {
     ctx->chain_state = chain_state_create(n_sm);
@@ -596,7 +622,9 @@ static recg_status run_forward(recg_ctx* ctx, void* kv_pool, int64_t kv_pool_pag
   cudaStream_t st = ctx->stream;
   // (RECG_FLAG_CHAIN: steps of at most 128 rows run the projections between two attention calls as one persistent kernel)
   cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-  const bool chain = ctx->chain_state && !bl.dyn && T <= 128 && d.n_layers > 0 && (d.n_q * d.head_dim) % 64 == 0 &&
+  // (not with a staged or observed K/V: the chain has the next layer's QKV projection inside)
+  const bool four = four_bits(ctx);
+  const bool chain = ctx->chain_state && !four && !ctx->track && !bl.dyn && T <= 128 && d.n_layers > 0 && (d.n_q * d.head_dim) % 64 == 0 &&
                      d.hidden % 128 == 0 && d.ffn % 64 == 0 &&
                      cudaStreamIsCapturing(st, &cap) == cudaSuccess && cap == cudaStreamCaptureStatusNone;
   const bool fold = folds_norm(ctx);
@@ -635,18 +663,26 @@ static recg_status run_forward(recg_ctx* ctx, void* kv_pool, int64_t kv_pool_pag
     normed(a);
     a.w = ctx->wqkv[l]; a.out = ctx->q;
     a.M = T; a.N = (d.n_q + 2 * d.n_kv) * d.head_dim; a.epi = EPI_QKV_ROPE;
-    a.tok_pos = bl.tok_pos; a.tok_slot = bl.tok_slot; a.kv_pool = kv_pool; a.n_pages = kv_pool_pages;
-    a.layer = l; a.n_q = d.n_q; a.n_kv = d.n_kv; a.head_dim = d.head_dim; a.rope_cs = ctx->rope_cs;
+    a.tok_pos = bl.tok_pos;
+    a.tok_slot = four ? ctx->d_stage_slot : bl.tok_slot;
+    a.kv_pool = four ? ctx->stage : kv_pool;
+    a.n_pages = four ? ctx->stage_pages : kv_pool_pages;
+    a.layer = four ? 0 : l; a.n_q = d.n_q; a.n_kv = d.n_kv; a.head_dim = d.head_dim; a.rope_cs = ctx->rope_cs;
     if ((s = run_gemm(ctx, a)) != RECG_OK) return s;
-    ctx->mark(2, 1);
+    if (four) launch_kv_stage(bl, ctx->stage, ctx->stage_pages, kv_pool, kv_pool_pages, l, d, st);
+    ctx->mark(2, four ? 2 : 1);
     }
     // (the first layer's attention kernel may be resident while the work list is still being built: idle lanes of a projection
     // signal its dependents before the projection has waited)
     launch_attention(bl, d, l, ctx->q, ctx->o, kv_pool, kv_pool_pages, ctx->part_o, ctx->part_ml, ctx->tok_per_tile, ctx->n_sm,
-                     ctx->d_status, st, !(ctx->cfg.flags & RECG_FLAG_SIMT_ATTENTION), ctx->list_settled, ctx->layout_whole, ctx->layout_tiles, true);
+                     ctx->d_status, st, !(ctx->cfg.flags & RECG_FLAG_SIMT_ATTENTION), ctx->list_settled, ctx->layout_whole, ctx->layout_tiles, true, four,
+                     ctx->track ? ctx->lse : nullptr, ctx->layout_rows);
+    if (ctx->track)
+      launch_kv_weights(bl, d, l, ctx->q, ctx->lse, bl.tok_weight, ctx->track_decay, ctx->track, ctx->track, kv_pool, kv_pool_pages, four,
+                        ctx->n_sm, ctx->d_status, st);
     CU(cudaGetLastError());
     ctx->list_settled = true;
-    ctx->mark(3, ctx->layout_whole ? 1 : 2);
+    ctx->mark(3, (ctx->layout_whole ? 1 : 2) + (ctx->track ? 1 : 0));
     if (chain) {
       const bool last = l + 1 == d.n_layers;
       const int slots_h = d.hidden / 128;      // sum-of-squares slots a residual op of the chain fills
@@ -731,6 +767,8 @@ static recg_status check_device_batch(recg_ctx* ctx, const recg_device_batch* b,
   if (!b || b->n_req <= 0 || !b->ctx_len || !b->verify_len || !b->block_size || !b->verify_tokens || !b->page_table ||
       !b->kv_pool || b->kv_pool_pages <= 0)
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": null array, n_req <= 0 or no KV pool");
+  if (four_bits(ctx) && (reinterpret_cast<uintptr_t>(b->kv_pool) & 15))
+    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": kv_pool must be 16-byte aligned");
   if (b->n_req > ctx->cfg.max_requests) return fail(ctx, RECG_ERR_CAPACITY, std::string(who) + ": n_req exceeds max_requests");
   if (b->max_verify < 1 || b->max_verify > ctx->cfg.max_tokens)
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": max_verify must be 1 .. max_tokens");
@@ -1121,6 +1159,34 @@ static recg_status evict_batch(recg_ctx* ctx, const recg_eviction* e, int32_t ke
   const int* at = ctx->d_evict;
   *out = EvictDesc{C, e->n_sink, e->n_recent, e->layer_begin, e->page_table_stride, other ? e->dst_stride : 0, 1, at, at + C, at + 2 * C,
                    other ? at + 2 * C + (size_t)C * e->page_table_stride : nullptr};
+  return RECG_OK;
+}
+recg_status recg_kv_track(recg_ctx* ctx, float* weights, float decay) {
+  if (!ctx) return RECG_ERR_INVALID_ARG;
+  if (!ctx->has_weights) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_track: the context was created without weights");
+  if (!aligned16(weights, weights)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_track: weights must be 16-byte aligned");
+  if (!(decay >= 0.f && decay <= 3e38f)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_track: decay must be a finite number >= 0");
+  ctx->track = weights;
+  ctx->track_decay = decay;
+  return RECG_OK;
+}
+recg_status recg_kv_shift(recg_ctx* ctx, int32_t n_req, const int32_t* shift) {
+  if (!ctx) return RECG_ERR_INVALID_ARG;
+  if (n_req < 0 || (n_req > 0 && !shift)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_shift: negative n_req or null array");
+  if (n_req > ctx->cfg.max_requests) return fail(ctx, RECG_ERR_CAPACITY, "recg_kv_shift: n_req exceeds max_requests");
+  if (n_req == 0) {
+    ctx->bl.pos_shift = nullptr;
+    return RECG_OK;
+  }
+  for (int r = 0; r < n_req; ++r)
+    if (shift[r] < 0 || shift[r] > (1 << 30)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_shift: a shift must be 0 .. 2^30");
+  cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+  CU(cudaStreamIsCapturing(ctx->stream, &cap));
+  if (cap != cudaStreamCaptureStatusNone) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_shift: not while the stream is being captured");
+  std::vector<int> h(ctx->cfg.max_requests, 0);      // (a larger batch: its further requests are not shifted)
+  memcpy(h.data(), shift, n_req * sizeof(int));
+  CU(cudaMemcpyAsync(ctx->d_pos_shift, h.data(), h.size() * sizeof(int), cudaMemcpyHostToDevice, ctx->stream));
+  ctx->bl.pos_shift = ctx->d_pos_shift;
   return RECG_OK;
 }
 recg_status recg_kv_select(recg_ctx* ctx, const recg_eviction* e, int32_t* keep, int32_t keep_stride) {
