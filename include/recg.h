@@ -266,8 +266,10 @@ recg_status recg_kv_rows(recg_ctx *ctx, const recg_batch *batch, int32_t layer, 
  *   q [T, n_q_heads, head_dim] bf16 and lse [T, n_q_heads] as recg_attention_lse() had and gave them; row_weight float32 [T] or
  *   NULL (1 each; 0 leaves a row out: mask rows, drafts that verification rejected); decay >= 0; all DEVICE.
  * weights_in, weights_out: DEVICE float32 [n_layers, kv_pool_pages, n_kv_heads, 16], entry (layer, page, head, offset) for the
- * token in that slot; they may be the same array.  weights_in == NULL: nothing gathered so far.  Entries of other slots are left as they are.
- * batch == NULL: the batch laid out last.
+ * token in that slot; they may be the same array.  weights_in == NULL: nothing gathered so far.  16-byte aligned, as the pool has to be.
+ *   Entries of other slots are left as they are.
+ * batch == NULL: the batch laid out last.  A page that the batch names twice is refused: requests that share pages gather in a call
+ * each, one after the other (of a device-resident round, whose page table is on the device, the caller sees to that).
  */
 recg_status recg_kv_weights(recg_ctx *ctx, const recg_batch *batch, int32_t layer, const void *q, const float *lse,
                             const float *row_weight, float decay, const float *weights_in, float *weights_out);
@@ -306,7 +308,7 @@ recg_status recg_kv_select(recg_ctx *ctx, const recg_eviction *eviction, int32_t
  * Eviction around whole steps.
  * recg_kv_track(): from now on every layer of a step (recg_step, recg_step_device) adds the weight that its verify rows give to the
  *   cached tokens into `weights`, as recg_kv_weights() with weights_in = weights_out = weights and row_weight 1 for verify and 0 for all
- *   other rows.  The array is for the pool of the steps' batches; 16-byte aligned; NULL: no longer.  (A rejected draft has given its
+ *   other rows.  The array is for the pool of the steps' batches; 16-byte aligned, as that is; NULL: no longer.  (A rejected draft has given its
  *   weight, as the rows behind it have.)
  * recg_kv_shift(): shift[r] tokens (HOST [n_req]) of request r have been evicted: the rotary positions of its rows in the steps from now on
  *   are those of a context longer by as much.  Requests from n_req on are not shifted; n_req = 0: none is.  recg_next_round() leaves it as

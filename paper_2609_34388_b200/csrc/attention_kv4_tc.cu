@@ -7,7 +7,7 @@
 // two fp16 numbers.  (K as m + s c rounded to 16 bits would leave the log-sum-exp of a few tokens good to 1e-4 only; steps applied
 // in fp32 behind the product have to be broadcast to every row's thread, and that alone took more of the shared memory's
 // bandwidth than all operands: 325 us instead of 193 us for 1001 rows over 6000 tokens of 40 / 8 heads.)  V stands as m + s c
-// rounded once, and P as fp16 too: 2^-12 of each term, a sixteenth of the rounding of the result.
+// rounded once, and P as fp16 too: 2^-11 of each term by either, a quarter of the rounding of the result together.
 //
 // Range.  fp16 has five bits of exponent, so everything is scaled by powers of two: a query row by its own largest value, K and V
 // of 32 tokens by theirs, in steps of 2^8.  The scale of a row of Q and of 32 tokens of K is one factor of the score.  The scale of V
@@ -20,7 +20,7 @@
 //   warps 4-7  turn a raw stage into the operand K (K-major) and warps 8-11 into V (MN-major), 32 tokens a warp: 16 tokens x 128 values
 //              in 128-byte-swizzled atoms as the tensor core reads them.  Every lane turns words of eight codes into 16-byte stores;
 //              the words of a lane are taken in an order in which no two lanes of a store meet a bank.  Warps 4-7 also turn the
-//              rows of Q, one a thread.  (One warpgroup for both had a chain of latencies longer than a stage: 272 us.)
+//              rows of Q, one a thread.  (One warpgroup for both had a chain of latencies longer than a stage: 272 us, where two took 201 at the time.)
 //   warp 1     one elected lane issues S = Q K^T (two stages ahead) and per softmax group O_g += P_g V_g (P from TMEM)
 //   warps 12-15 and 16-19  two softmax groups: group g takes tokens [64 g, 64 g + 64) of every stage, one thread one query row, its
 //              own O accumulator and running (reference maximum, sum); merged at the end of an item.

@@ -3,7 +3,7 @@
 // A row x (one token, one kv head, K or V; d values) is held as d codes c of 4 bits, a minimum m and a step s:
 //   m = min x,  s = bf16((max x - m) / 15),  c = nearest whole number to (x - m) / s, ties to even (0 where s is 0)
 // and stands for m + s c.  m is one of the bf16 inputs, hence exact in 16 bits; s rounded to bf16 moves the largest value by at
-// most 15 s 2^-9 = 0.03 s, a sixteenth of what rounding to codes does.  One pair (s, m) per row, not per 32 or 64 values: the
+// most 15 s 2^-8 = 0.06 s, an eighth of what rounding to codes does.  One pair (s, m) per row, not per 32 or 64 values: the
 // products q.(m + s c) = s (q.c) + m sum(q) and sum_j p_j (m_j + s_j c_j) then need the pairs outside of the matrix products
 // only, whose operands, the codes, are exact.  A row with a value that is not finite (or whose range overflows) gets s = NaN.
 //
@@ -29,14 +29,6 @@ __host__ __device__ __forceinline__ size_t kv4_block_base(int64_t n_pages, int n
 __host__ __device__ __forceinline__ int kv4_k_word(int tok, int j, int d) { return tok * (d >> 1) + 4 * j; }
 __host__ __device__ __forceinline__ int kv4_v_word(int tok, int j, int odd, int d) { return kv4_v_codes(d) + (tok >> 1) * d + 8 * j + 4 * odd; }
 
-// Pair i of a word of codes as two bf16 values c - 8 (exact: 128 + c is 0x4300 | c, and 136 is subtracted).  Centred, because sums
-// of products with values of one sign grow and lose low bits in the accumulators of the matrix units.
-__device__ __forceinline__ uint32_t kv4_pair(uint32_t word, int i) {
-  const uint32_t x = ((word >> (4 * i)) & 0x000f000fu) | 0x43004300u;
-  const __nv_bfloat162 off = __halves2bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308));   // 136
-  const __nv_bfloat162 r = __hsub2(reinterpret_cast<const __nv_bfloat162&>(x), off);
-  return reinterpret_cast<const uint32_t&>(r);
-}
 // {s, m} of a row
 __device__ __forceinline__ float kv4_step(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float kv4_min(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }

@@ -8,7 +8,7 @@
 // Bound by the bytes of K as long as rows are few.  The pages of all requests and heads are one line, of which every CTA takes an
 // equal piece; per (request, head) in it the rows that count (weight not zero) are staged in shared memory once, and the warps
 // stream pages past them, each into a ring of its own, 16 bytes a lane.  (One CTA per 128 tokens, with its own staging and K by
-// plain loads: sixteen decoding requests 41.5 us, a serving batch on a bf16 pool 140; now %DEC% and %BATCH%.)
+// plain loads: sixteen decoding requests 41.5 us, a serving batch on a bf16 pool 140; now 25.6 and 57.6.)
 //
 // Operands.  A bf16 pool: its tiles are what ldmatrix takes.  A pool in 4 bits: a lane holds the values [D / 4 t, D / 4 (t + 1)) of two
 // tokens (t its number in the quad), the contraction index is permuted accordingly; codes as subnormal fp16 numbers, Q scaled by a power of

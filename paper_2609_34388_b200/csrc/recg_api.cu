@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cstdio>
 #include <cstring>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -106,8 +107,9 @@ struct recg_ctx {
   float track_decay = 1.f;
   int* d_evict = nullptr;          // eviction: the descriptor uploaded last, and on the host
   std::vector<int> h_evict;
-  std::vector<int> h_page_seen;    // eviction: per page the call (times two, plus one where it is a destination) that named it last
-  int evict_calls = 0;
+  std::vector<int> h_page_seen;    // per page the set of pages (a number) that it was put into last
+  int page_set = 0;
+  int pages_shared = -1;           // whether the batch laid out last names a page twice (-1: not looked at yet)
   // optional per-class timing
   bool timing = false;
   std::vector<cudaEvent_t> ev_pool;
@@ -223,6 +225,22 @@ size_t carve(recg_ctx* c, DeviceArena& A) {
     A.guard = was;
   }
   return A.used + 256;
+}
+
+bool aligned16(const void* a, const void* b) { return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15) == 0; }
+
+// Pages that a call has named: a new set of them, and whether one is in it already.
+void new_pages(recg_ctx* ctx) {
+  if (++ctx->page_set != INT32_MAX) return;
+  ctx->page_set = 1;
+  std::fill(ctx->h_page_seen.begin(), ctx->h_page_seen.end(), 0);
+}
+bool page_seen(recg_ctx* ctx, int page) {
+  std::vector<int>& seen = ctx->h_page_seen;
+  if ((size_t)page >= seen.size()) seen.resize((size_t)page + 1, 0);
+  const bool before = seen[page] == ctx->page_set;
+  seen[page] = ctx->page_set;
+  return before;
 }
 
 // Rows of request r: verify tokens, continuation masks and the correction branches (replacement + masks each).
@@ -399,6 +417,7 @@ recg_status upload_and_layout(recg_ctx* ctx, const recg_batch* b, bool need_page
                   !forward, ctx->d_desc, small ? &ctx->small_desc : nullptr, ctx->stream, list);
     ctx->list_settled = false;
     ctx->list_pending = !list;
+    ctx->pages_shared = -1;
     if (forward) embed_tokens(ctx, n_pages);
   }
   CU(cudaGetLastError());
@@ -406,6 +425,28 @@ recg_status upload_and_layout(recg_ctx* ctx, const recg_batch* b, bool need_page
   ctx->layout_has_pages = b->page_table != nullptr;
   ctx->last_pool = b->kv_pool;
   ctx->last_pool_pages = b->kv_pool_pages;
+  return RECG_OK;
+}
+
+// Whether the weights of the batch laid out last can be gathered: a slot that two requests see would get one of two sums.  (Of a
+// device-resident round the page table is on the device, where nothing looks for this.)
+recg_status gathers(recg_ctx* ctx, const char* who) {
+  if (!aligned16(ctx->last_pool, ctx->last_pool)) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": the KV pool must be 16-byte aligned");
+  if (ctx->bl.dyn) return RECG_OK;
+  if (ctx->pages_shared < 0) {
+    const int C = ctx->bl.n_req, stride = ctx->bl.pt_stride;
+    const int* table = ctx->h_desc.data() + ctx->h_desc.size() - (size_t)C * stride;
+    int shared = 0;
+    try {
+      new_pages(ctx);
+      for (int r = 0; r < C && !shared; ++r)
+        for (int i = 0; i < (ctx->h_desc[r] + ctx->h_rows[r] + kPageSize - 1) / kPageSize; ++i) shared |= page_seen(ctx, table[(size_t)r * stride + i]);
+    } catch (const std::bad_alloc&) {
+      return fail(ctx, RECG_ERR_CAPACITY, std::string(who) + ": out of host memory");
+    }
+    ctx->pages_shared = shared;
+  }
+  if (ctx->pages_shared) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": a page is named twice, whose weights would be one of two sums");
   return RECG_OK;
 }
 
@@ -758,6 +799,7 @@ recg_status recg_step(recg_ctx* ctx, const recg_batch* batch, recg_logits* logit
   ctx->logits_valid = false;
   ctx->mark(-1);
   recg_status s = upload_and_layout(ctx, batch, true, true, true);
+  if (s == RECG_OK && ctx->track) s = gathers(ctx, "recg_step");
   if (s != RECG_OK) return s;
   return run_forward(ctx, batch->kv_pool, batch->kv_pool_pages, 0, logits);
 }
@@ -767,7 +809,7 @@ static recg_status check_device_batch(recg_ctx* ctx, const recg_device_batch* b,
   if (!b || b->n_req <= 0 || !b->ctx_len || !b->verify_len || !b->block_size || !b->verify_tokens || !b->page_table ||
       !b->kv_pool || b->kv_pool_pages <= 0)
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": null array, n_req <= 0 or no KV pool");
-  if (four_bits(ctx) && (reinterpret_cast<uintptr_t>(b->kv_pool) & 15))
+  if ((four_bits(ctx) || ctx->track) && !aligned16(b->kv_pool, b->kv_pool))
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": kv_pool must be 16-byte aligned");
   if (b->n_req > ctx->cfg.max_requests) return fail(ctx, RECG_ERR_CAPACITY, std::string(who) + ": n_req exceeds max_requests");
   if (b->max_verify < 1 || b->max_verify > ctx->cfg.max_tokens)
@@ -986,16 +1028,18 @@ static recg_status operation_batch(recg_ctx* ctx, const recg_batch* batch, int32
   if (!ctx->layout_valid || !ctx->layout_has_pages || !ctx->last_pool)
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": no batch given and none with a KV pool laid out before");
   if (list && ctx->list_pending) {
-    // (the descriptor is in device memory by now)
+    // (the descriptor is in device memory by now; a captured launch builds nothing yet, so the list stays pending)
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    CU(cudaStreamIsCapturing(ctx->stream, &cap));
     launch_layout(ctx->bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, ctx->layout_whole, ctx->last_pool_pages, ctx->d_status, false,
                   ctx->d_desc, nullptr, ctx->stream);
     CU(cudaGetLastError());
-    ctx->list_settled = ctx->list_pending = false;
+    ctx->list_settled = false;
+    ctx->list_pending = cap != cudaStreamCaptureStatusNone;
   }
   return RECG_OK;
 }
 
-static bool aligned16(const void* a, const void* b) { return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15) == 0; }
 
 static recg_status attention(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, void* o, float* lse, const char* who) {
   if (four_bits(ctx) && !aligned16(q, o)) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": q and o must be 16-byte aligned");
@@ -1027,7 +1071,7 @@ static recg_status kv_io(recg_ctx* ctx, bool write, void* pool, int64_t n_pool_p
   if (four_bits(ctx) && (!aligned16(k, v) || !aligned16(pool, pool)))
     return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_*: k, v and the pool must be 16-byte aligned");
   if (n_pos == 0) return RECG_OK;
-  if ((pos0 + n_pos - 1) / kPageSize >= n_table) return fail(ctx, RECG_ERR_CAPACITY, "recg_kv_*: positions beyond the page table row");
+  if (((int64_t)pos0 + n_pos - 1) / kPageSize >= n_table) return fail(ctx, RECG_ERR_CAPACITY, "recg_kv_*: positions beyond the page table row");
   for (int i = pos0 / kPageSize; i <= (pos0 + n_pos - 1) / kPageSize; ++i)
     if (row[i] < 0 || row[i] >= n_pool_pages) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_*: page id outside the pool");
   (four_bits(ctx) ? launch_kv4_io : launch_kv_io)(write, pool, n_pool_pages, layer, ctx->dm, row, pos0, n_pos, k, v, ctx->stream);
@@ -1056,6 +1100,7 @@ static recg_status kv_rows(recg_ctx* ctx, bool write, const recg_batch* batch, i
   // requests.  Rows that are appended usually are.)
   recg_status s = operation_batch(ctx, batch, layer, who, write);
   if (s != RECG_OK) return s;
+  if (!aligned16(ctx->last_pool, ctx->last_pool)) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": the KV pool must be 16-byte aligned");
   launch_kv_rows(write, four_bits(ctx), ctx->bl, ctx->last_pool, ctx->last_pool_pages, layer, ctx->dm, k, v, row_stride, ctx->stream);
   CU(cudaGetLastError());
   return RECG_OK;
@@ -1071,10 +1116,11 @@ recg_status recg_kv_weights(recg_ctx* ctx, const recg_batch* batch, int32_t laye
                             const float* row_weight, float decay, const float* weights_in, float* weights_out) {
   if (!ctx || !q || !lse || !weights_out) return RECG_ERR_INVALID_ARG;
   if (!(decay >= 0.f && decay <= 3e38f)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: decay must be a finite number >= 0");
-  if (!aligned16(q, q)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: q must be 16-byte aligned");
+  if (!aligned16(q, q) || !aligned16(weights_in, weights_out))
+    return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: q, weights_in and weights_out must be 16-byte aligned");
   recg_status s = operation_batch(ctx, batch, layer, "recg_kv_weights", false);
   if (s != RECG_OK) return s;
-  if (!aligned16(ctx->last_pool, ctx->last_pool)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: the KV pool must be 16-byte aligned");
+  if ((s = gathers(ctx, "recg_kv_weights")) != RECG_OK) return s;
   launch_kv_weights(ctx->bl, ctx->dm, layer, q, lse, row_weight, decay, weights_in, weights_out, ctx->last_pool, ctx->last_pool_pages,
                     four_bits(ctx), ctx->n_sm, ctx->d_status, ctx->stream);
   CU(cudaGetLastError());
@@ -1101,13 +1147,7 @@ static recg_status evict_batch(recg_ctx* ctx, const recg_eviction* e, int32_t ke
     return fail(ctx, RECG_ERR_INVALID_ARG, name + ": the KV pool is null or not 16-byte aligned");
   if (reinterpret_cast<uintptr_t>(e->weights) & 15) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": weights must be 16-byte aligned");
   std::vector<int> d(2 * (size_t)C + (size_t)C * (e->page_table_stride + (other ? e->dst_stride : 0)));
-  if (moves) {
-    if (ctx->h_page_seen.size() < (size_t)e->kv_pool_pages) ctx->h_page_seen.resize((size_t)e->kv_pool_pages, 0);
-    if (++ctx->evict_calls > 0x3ffffff0) {
-      ctx->evict_calls = 1;
-      std::fill(ctx->h_page_seen.begin(), ctx->h_page_seen.end(), 0);
-    }
-  }
+  if (moves) new_pages(ctx);
   *max_keep = *max_pages = 0;
   for (int r = 0; r < C; ++r) {
     const int L = e->ctx_len[r], b = e->budget[r];
@@ -1128,10 +1168,8 @@ static recg_status evict_batch(recg_ctx* ctx, const recg_eviction* e, int32_t ke
       if (i >= need) continue;
       if (pt[i] < 0 || pt[i] >= e->kv_pool_pages) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": page id outside the pool");
       if (!moves) continue;
-      int& seen = ctx->h_page_seen[pt[i]];
       // (requests may share source pages where nothing is written to them)
-      if (!other && seen >> 1 == ctx->evict_calls) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": in place, a page is named twice");
-      seen = ctx->evict_calls << 1;
+      if (page_seen(ctx, pt[i]) && !other) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": in place, a page is named twice");
     }
   }
   if (other)
@@ -1142,9 +1180,7 @@ static recg_status evict_batch(recg_ctx* ctx, const recg_eviction* e, int32_t ke
         if (i >= (d[C + r] + kPageSize - 1) / kPageSize) continue;
         if (pt[i] < 0 || pt[i] >= e->kv_pool_pages) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": page id outside the pool");
         if (!moves) continue;
-        int& seen = ctx->h_page_seen[pt[i]];
-        if (seen >> 1 == ctx->evict_calls) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": a destination page is named twice or is a source");
-        seen = ctx->evict_calls << 1;
+        if (page_seen(ctx, pt[i])) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": a destination page is named twice or is a source");
       }
     }
   if (keep_stride < *max_keep || keep_stride <= 0) return fail(ctx, RECG_ERR_CAPACITY, name + ": keep_stride is below the positions that stay");
@@ -1183,9 +1219,9 @@ recg_status recg_kv_shift(recg_ctx* ctx, int32_t n_req, const int32_t* shift) {
   cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
   CU(cudaStreamIsCapturing(ctx->stream, &cap));
   if (cap != cudaStreamCaptureStatusNone) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_shift: not while the stream is being captured");
-  std::vector<int> h(ctx->cfg.max_requests, 0);      // (a larger batch: its further requests are not shifted)
-  memcpy(h.data(), shift, n_req * sizeof(int));
-  CU(cudaMemcpyAsync(ctx->d_pos_shift, h.data(), h.size() * sizeof(int), cudaMemcpyHostToDevice, ctx->stream));
+  int h[kMaxLayoutRequests];                         // (a larger batch: its further requests are not shifted)
+  std::fill(std::copy(shift, shift + n_req, h), h + ctx->cfg.max_requests, 0);
+  CU(cudaMemcpyAsync(ctx->d_pos_shift, h, ctx->cfg.max_requests * sizeof(int), cudaMemcpyHostToDevice, ctx->stream));
   ctx->bl.pos_shift = ctx->d_pos_shift;
   return RECG_OK;
 }
@@ -1194,7 +1230,12 @@ recg_status recg_kv_select(recg_ctx* ctx, const recg_eviction* e, int32_t* keep,
   if (e && !e->weights) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_select: weights is null");
   EvictDesc E;
   int max_keep = 0, max_pages = 0;
-  recg_status s = evict_batch(ctx, e, keep_stride, false, "recg_kv_select", &E, &max_keep, &max_pages);
+  recg_status s;
+  try {
+    s = evict_batch(ctx, e, keep_stride, false, "recg_kv_select", &E, &max_keep, &max_pages);
+  } catch (const std::bad_alloc&) {
+    return fail(ctx, RECG_ERR_CAPACITY, "recg_kv_select: out of host memory");
+  }
   if (s != RECG_OK) return s;
   launch_kv_select(E, e->weights, e->kv_pool_pages, ctx->dm.n_kv, e->layer_end - e->layer_begin, max_pages, keep, keep_stride, ctx->stream);
   CU(cudaGetLastError());
@@ -1204,7 +1245,12 @@ recg_status recg_kv_compact(recg_ctx* ctx, const recg_eviction* e, const int32_t
   if (!ctx || !keep) return RECG_ERR_INVALID_ARG;
   EvictDesc E;
   int max_keep = 0, max_pages = 0;
-  recg_status s = evict_batch(ctx, e, keep_stride, true, "recg_kv_compact", &E, &max_keep, &max_pages);
+  recg_status s;
+  try {
+    s = evict_batch(ctx, e, keep_stride, true, "recg_kv_compact", &E, &max_keep, &max_pages);
+  } catch (const std::bad_alloc&) {
+    return fail(ctx, RECG_ERR_CAPACITY, "recg_kv_compact: out of host memory");
+  }
   if (s != RECG_OK) return s;
   launch_kv_compact(E, ctx->dm, e->kv_pool, e->weights, e->kv_pool_pages, four_bits(ctx), e->layer_end - e->layer_begin, max_keep, keep,
                     keep_stride, ctx->d_status, ctx->stream);

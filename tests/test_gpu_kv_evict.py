@@ -303,3 +303,77 @@ def test_refusals():
     assert binding.lib().recg_kv_weights(ctx.h, C.byref(batch.c), 0, q.data_ptr() + 2, lse.data_ptr(), None, 1.0, None, w.data_ptr()) == 1
     ctx.recg_sync()
     ctx.recg_free()
+
+
+@pytest.mark.parametrize("flags", POOLS)
+def test_calls_that_would_collide_or_be_misaligned_are_refused(flags):
+    ctx = make(TINY, 4, 8, 2, flags)
+    pool = binding.alloc_kv_pool(ctx, 16)
+    w = torch.zeros((2 * 16 * 2 * 16 + 4,), device="cuda")
+    q, lse = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 4), device="cuda")
+    even, odd = w[:-4], w[1:-3]
+    table = np.array([[0, 1, 2, 3], [4, 5, 6, 7]])
+    batch = binding.Batch([40, 50], [1, 1], [0, 0], None, table, pool, 16)
+    lib = binding.lib()
+    for src, dst in ((odd, even), (even, odd), (None, odd)):
+        assert lib.recg_kv_weights(ctx.h, C.byref(batch.c), 0, q.data_ptr(), lse.data_ptr(), None, 1.0,
+                                   None if src is None else src.data_ptr(), dst.data_ptr()) == 1
+        assert b"16-byte" in lib.recg_last_error(ctx.h)
+    out = even.view(2, 16, 2, 16)
+    for bad in (np.array([[0, 1, 2, 3], [0, 5, 6, 7]]), np.array([[0, 1, 2, 3], [4, 5, 4, 7]])):
+        shared = binding.Batch([40, 50], [1, 1], [0, 0], None, bad, pool, 16)
+        for given in (shared, None):                                   # (the second: laid out by the call that was refused)
+            with pytest.raises(binding.RecgError, match="named twice"):
+                ctx.recg_kv_weights(given, 0, q, lse, None, out)
+    ctx.recg_kv_weights(binding.Batch([40, 33], [1, 1], [0, 0], None, np.array([[0, 1, 2, 3], [4, 5, 6, 0]]), pool, 16), 0, q, lse, None, out)
+    ctx.recg_kv_weights(batch, 0, q, lse, None, out)                   # (a page behind the last position is nobody's)
+    rows = torch.zeros((2, 2, 64), dtype=torch.bfloat16, device="cuda")
+    off = binding.Batch([3], [2], [0], None, np.arange(4)[None], pool.view(torch.uint8)[2:] if flags else pool[1:], 15)
+    with pytest.raises(binding.RecgError, match="16-byte"):
+        ctx.recg_kv_append(off, 0, rows, rows)
+    with pytest.raises(binding.RecgError, match="beyond"):             # pos0 + n_pos passes 31 bits
+        ctx._check(lib.recg_kv_read(ctx.h, pool.data_ptr(), 16, 0, table.astype(np.int32)[0].ctypes.data, 4, 2 ** 31 - 1, 2,
+                                    rows.data_ptr(), rows.data_ptr()))
+    ctx.recg_sync()
+    ctx.recg_free()
+
+
+@pytest.mark.parametrize("flags", POOLS)
+def test_attention_captured_before_its_work_list_was_built(flags):
+    """A batch that only rows were read of has no work list; the one that a captured attention builds is there after a replay only."""
+    nq, nkv, d = B8
+    desc = synth.fixed_descriptor([300, 20], [3, 1], [2, 0], seed=3)
+    T = desc.n_tokens
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ctx = make(B8, desc.page_table.shape[1], T, 2, flags)
+        pool = binding.alloc_kv_pool(ctx, desc.n_pages)
+        for r, n in enumerate(desc.ctx_len + desc.rows):
+            k, v = synth.kv_values(int(n), nkv, d, seed=r)
+            ctx.recg_kv_write(pool, desc.n_pages, 0, desc.page_table[r], 0, k.cuda(), v.cuda())
+        batch = binding.Batch(desc.ctx_len, desc.verify_len, desc.block_size, None, desc.page_table, pool, desc.n_pages)
+        other = binding.Batch([3], [2], [0], None, desc.page_table[:1], pool, desc.n_pages)
+        q = synth.queries(T, nq, d, seed=8).cuda()
+        want, got, again, spare = (torch.zeros_like(q) for _ in range(4))
+        w_want, w_got = (torch.zeros((2, desc.n_pages, nkv, 16), device="cuda") for _ in range(2))
+        lse = torch.empty((T, nq), device="cuda")
+        ctx.recg_attention(batch, 0, q, want, lse)
+        ctx.recg_kv_weights(None, 0, q, lse, None, w_want)
+        ctx.recg_attention(other, 0, q, spare)
+        ctx.recg_kv_rows(batch, 0)
+        ctx.recg_sync()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            ctx.recg_attention(None, 0, q, got, lse)
+            ctx.recg_kv_weights(None, 0, q, lse, None, w_got)
+        ctx.recg_attention(None, 0, q, again)                          # the graph has not run yet
+        torch.cuda.synchronize()
+        assert torch.equal(again, want) and not got.any()
+        for _ in range(2):
+            got.zero_(), w_got.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got, want) and torch.equal(w_got, w_want)
+        del graph
+        ctx.recg_sync()
+        ctx.recg_free()

@@ -49,7 +49,7 @@ def check(ctx, shape, ocfg, W64, lg, pool, n_pages, table, L, v, b, ys, shift=No
             for got, full in zip(held[l], pair):
                 new = full[L[r] + n:]
                 # a row within TOL of the largest: its ends move by that, so its step by 2 TOL / 15, and 7.5 steps are half its range;
-                # the step and the value read are rounded to bf16 (2^-9 each, 15 steps at most)
+                # the step and the value read are rounded to bf16 (2^-8 each, of 15 steps and of the value)
                 span = new.max(-1, keepdims=True) - new.min(-1, keepdims=True)
                 err = 3 * TOL * np.abs(new).max() + span / 30 + 2.0 ** -8 * (span + np.abs(new))
                 assert (np.abs(got[L[r]:] - new) <= (err if four else 2 * TOL * np.abs(new).max())).all(), (l, r)
