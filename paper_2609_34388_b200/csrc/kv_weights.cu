@@ -6,9 +6,10 @@
 // the warp.  Nothing is added by atomics: a position belongs to one warp, which takes the rows in order, so results repeat bit for bit.
 //
 // Bound by the bytes of K as long as rows are few.  The pages of all requests and heads are one line, of which every CTA takes an
-// equal piece; per (request, head) in it the rows that count (weight not zero) are staged in shared memory once, and the warps
-// stream pages past them, each into a ring of its own, 16 bytes a lane.  (One CTA per 128 tokens, with its own staging and K by
-// plain loads: sixteen decoding requests 41.5 us, a serving batch on a bf16 pool 140; now 25.6 and 57.6.)
+// equal piece.  The rows that count (weight not zero) of as many (request, head) pairs of the piece as fit are staged in shared memory
+// together, and the warps stream the pairs' pages past them in one go, each into a ring of its own, 16 bytes a lane.  (Pair by pair, each
+// with its staging and its barriers: sixteen decoding requests 25.5 us, a serving batch on a bf16 pool 57.8; now 19.0 and 47.2.  One CTA per 128
+// tokens, with its own staging and K by plain loads: 41.5 and 140.)
 //
 // Operands.  A bf16 pool: its tiles are what ldmatrix takes.  A pool in 4 bits: a lane holds the values [D / 4 t, D / 4 (t + 1)) of two
 // tokens (t its number in the quad), the contraction index is permuted accordingly; codes as subnormal fp16 numbers, Q scaled by a power of
@@ -62,7 +63,7 @@ struct Shape {
   static constexpr int kInfoOff = kRowsOff + kChunkRows * kRowBytes;
   static constexpr int kVisOff = kInfoOff + kChunkRows * 16;
   static constexpr int kListOff = kVisOff + kChunkRows * 16;
-  static constexpr int kTotal = kListOff + kChunkRows * 4;
+  static constexpr int kTotal = kListOff + kChunkRows * 8;
   static_assert(kPage % 16 == 0 && kTotal % 16 == 0, "16-byte pieces");
 };
 
@@ -96,12 +97,15 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
   extern __shared__ __align__(128) uint8_t smem[];
   float4* s_info = reinterpret_cast<float4*>(smem + SH::kInfoOff);     // a staged row: sum of its values times the scale, -lse (powers of two), weight
   int4* s_vis = reinterpret_cast<int4*>(smem + SH::kVisOff);
-  int* s_list = reinterpret_cast<int*>(smem + SH::kListOff);           // tokens that count
+  int2* s_src = reinterpret_cast<int2*>(smem + SH::kListOff);          // a staged row: its place in lse (-1: fills up an eight); row of the batch | segment << 20
   int* s_cost = reinterpret_cast<int*>(smem + SH::kTotal);             // [n_req] cost of a page and head of request r
   long long* s_first = reinterpret_cast<long long*>(smem);             // [n_req + 1] cost in front of request r (where rings and rows are later)
   __shared__ long long s_scan[kWarps];
-  __shared__ int s_count, s_next, s_lim;
-  __shared__ unsigned s_top;
+  // segments, (request, head) pairs whose rows are staged together
+  __shared__ int s_req[kWarps], s_head[kWarps], s_page0[kWarps], s_pages[kWarps], s_tok0[kWarps], s_new[kWarps], s_ctx[kWarps];
+  __shared__ int s_cum[kWarps], s_row0[kWarps], s_rows8[kWarps], s_count[kWarps], s_next[kWarps], s_lim[kWarps];
+  __shared__ unsigned s_top[kWarps];
+  __shared__ long long s_ahead[kWarps];                                // cost in front of what follows the segment
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   griddep_wait();
   griddep_launch();
@@ -138,60 +142,127 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
   const long long total = s_first[P.n_req], piece = (total + gridDim.x - 1) / gridDim.x;
   const long long begin = piece * blockIdx.x, end = min(total, begin + piece);
   const uint32_t ring_at = smem_u32(smem + warp * SH::kSlots * SH::kPage) + lane * 16;
-  const unsigned page_bytes = (unsigned)P.n_kv * SH::kBlock, weight_bytes = (unsigned)P.n_kv * kPageSize * 4;
   const unsigned pool_pages = (unsigned)min(P.n_pages, (int64_t)0x7fffffff);
 
-  int r = 0, unit = 0;                                 // request and (head, page) of it the piece goes on with
-  long long first = 0;                                 // cost in front of the request
+  const size_t out_layer = (size_t)P.layer * P.n_pages * P.n_kv * kPageSize;
+  const uint8_t* base = P.pool + (size_t)P.layer * P.n_pages * P.n_kv * SH::kBlock + lane * 16;
+  float* out_at = P.out + out_layer + g + 8 * (t & 1);
+
+  int pair = 0;                                        // (request, head) the piece begins in, and the cost in front of it
+  long long ahead = 0;
   if (begin < end) {
-    int hi_r = P.n_req;                                // largest r with s_first[r] <= begin
+    int r = 0, hi_r = P.n_req;                         // largest r with s_first[r] <= begin: it has pages
     while (hi_r - r > 1) {
       const int mid = (r + hi_r) >> 1;
       if (s_first[mid] <= begin) r = mid; else hi_r = mid;
     }
-    first = s_first[r];
-    unit = (int)((begin - first + s_cost[r] - 1) / s_cost[r]);
+    const long long one = (s_first[r + 1] - s_first[r]) / P.n_kv;
+    const int h = (int)((begin - s_first[r]) / one);
+    pair = r * P.n_kv + h;
+    ahead = s_first[r] + h * one;
   }
   __syncthreads();
-  while (begin < end && r < P.n_req && first < end) {
-    const int tok_first = P.cu_tok[r], n_new = P.cu_tok[r + 1] - tok_first, L = P.ctx_len[r], kv_len = L + n_new;
-    const int n_pages = n_new > 0 ? (kv_len + kPageSize - 1) / kPageSize : 0;
-    const int unit_end = (int)min((long long)n_pages * P.n_kv, (end - first + s_cost[r] - 1) / s_cost[r]);
-    if (unit >= unit_end) {
-      first += (long long)n_pages * P.n_kv * s_cost[r];
-      ++r;
-      unit = 0;
-      continue;
+  const int n_pairs = P.n_req * P.n_kv;
+  while (begin < end && pair < n_pairs && ahead < end) {
+    // ---- the next segments: a lane one of them ----
+    if (warp == 0) {
+      const int q = pair + lane, r = q < n_pairs ? q / P.n_kv : 0;
+      int first_tok = 0, n_new = 0, L = 0, n_pages = 0;
+      if (lane < kWarps && q < n_pairs) {
+        first_tok = P.cu_tok[r];
+        n_new = P.cu_tok[r + 1] - first_tok;
+        L = P.ctx_len[r];
+        if (n_new > 0) n_pages = (L + n_new + kPageSize - 1) / kPageSize;
+      }
+      const int cost = s_cost[r];
+      const long long mine = (long long)n_pages * cost;
+      long long upto = mine;
+#pragma unroll
+      for (int o = 1; o < kWarps; o <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+      }
+      upto += ahead;
+      const long long from = upto - mine;
+      const int lo = begin > from ? (int)min((long long)n_pages, (begin - from + cost - 1) / cost) : 0;
+      const int hi = from < end ? (int)min((long long)n_pages, (end - from + cost - 1) / cost) : 0;
+      if (lane < kWarps) {
+        s_req[lane] = r;
+        s_head[lane] = q - r * P.n_kv;
+        s_page0[lane] = lo;
+        s_pages[lane] = max(0, hi - lo);
+        s_tok0[lane] = first_tok;
+        s_new[lane] = n_new;
+        s_ctx[lane] = L;
+        s_ahead[lane] = upto;
+        s_count[lane] = hi > lo ? n_new : 0;
+        s_lim[lane] = 0x7fffffff;
+        s_top[lane] = 0;
+      }
     }
-    const int h = unit / n_pages, page0 = unit - h * n_pages, page1 = min(n_pages, page0 + unit_end - unit);      // pages [page0, page1) of head h
-    unit += page1 - page0;
-    const int* table = P.page_table + (size_t)r * P.pt_stride;
-    const uint8_t* base = P.pool + (((size_t)P.layer * P.n_pages) * P.n_kv + h) * (size_t)SH::kBlock + lane * 16;
-    const size_t out_base = ((size_t)P.layer * P.n_pages * P.n_kv + h) * kPageSize;
-    uint8_t* out_at = reinterpret_cast<uint8_t*>(P.out + out_base + g + 8 * (t & 1));
+    __syncthreads();
+    // ---- how many rows of each count; those whose rows fit are taken together (or one, in pieces) ----
+    if (P.row_weight) {
+      const int first_tok = s_tok0[warp], n_new = s_count[warp];
+      int n = 0;
+      for (int at = lane; at < n_new; at += 32) n += P.row_weight[first_tok + at] != 0.f;
+      n = __reduce_add_sync(0xffffffffu, n);
+      __syncwarp();
+      if (lane == 0) s_count[warp] = n;
+      __syncthreads();
+    }
+    int cum, nseg, total, row0;                          // (row0: of the warp's segment)
+    {
+      const int rows_of = lane < kWarps ? (s_count[lane] * P.group + 7) & ~7 : 0, pages = lane < kWarps ? s_pages[lane] : 0;
+      int rows_to = rows_of, pages_to = pages;
+#pragma unroll
+      for (int o = 1; o < kWarps; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, rows_to, o), z = __shfl_up_sync(0xffffffffu, pages_to, o);
+        if (lane >= o) {
+          rows_to += y;
+          pages_to += z;
+        }
+      }
+      const unsigned fit = __ballot_sync(0xffffffffu, lane < kWarps && rows_to <= kChunkRows);
+      nseg = max(1, __ffs(~fit) - 1);
+      total = __shfl_sync(0xffffffffu, pages_to, nseg - 1);
+      cum = lane < nseg ? pages_to - pages : 0x7fffffff;
+      row0 = __shfl_sync(0xffffffffu, rows_to - rows_of, warp);
+      if (warp == 0 && lane < nseg) {
+        s_cum[lane] = cum;
+        s_row0[lane] = rows_to - rows_of;
+      }
+    }
+    const bool whole = nseg > 1 || (s_count[0] * P.group + 7) / 8 * 8 <= kChunkRows;
 
-    for (int first_tok = 0, chunk = 0; first_tok < n_new || chunk == 0; ++chunk) {
+    for (int first_tok = 0, chunk = 0;; ++chunk) {
       // what the weights are added to: those so far, or what the chunk of rows before this one left
       const uint8_t* old = reinterpret_cast<const uint8_t*>(chunk ? P.out : (P.decay != 0.f ? P.in : nullptr));
-      if (old) old += out_base * 4 + (lane & 3) * 16;
+      if (old) old += out_layer * 4 + (lane & 3) * 16;
       const float keep = chunk ? 1.f : P.decay;
-      // ---- the warp's pages on their way; ids 32 at a time, a lane one of them ----
-      int next = page0 + warp, ids = 0, used = 0;
+      // ---- the warp's pages on their way; ids 32 at a time, a lane one of them (and its head) ----
+      int next = warp, ids = 0, heads = 0, used = 0;
       auto load_ids = [&]() {
         used = 0;
-        ids = next + lane * kWarps < page1 ? __ldg(table + next + lane * kWarps) : 0;
+        const int at = next + lane * kWarps;
+        int k = 0;
+        for (int x = 1; x < nseg; ++x) k += at >= __shfl_sync(0xffffffffu, cum, x);
+        const int from = __shfl_sync(0xffffffffu, cum, k);
+        heads = s_head[k];
+        ids = at < total ? __ldg(P.page_table + (size_t)s_req[k] * P.pt_stride + s_page0[k] + at - from) : 0;
       };
       auto request = [&](uint32_t slot_at) {            // one group of copies per call, be it empty
-        if (next < page1) {
-          const unsigned id = __shfl_sync(0xffffffffu, ids, used);
+        if (next < total) {
+          const unsigned id = __shfl_sync(0xffffffffu, ids, used), head = __shfl_sync(0xffffffffu, heads, used);
           const uint32_t dst = ring_at + slot_at;
           if (id < pool_pages) {
-            const uint8_t* src = base + (uint64_t)id * page_bytes;
+            const uint64_t block = (uint64_t)id * (unsigned)P.n_kv + head;
+            const uint8_t* src = base + block * SH::kBlock;
 #pragma unroll
             for (int x = 0; x < SH::kCodes / 512; ++x) copy_async16(dst + x * 512, src + x * 512);
             if (lane < 4) {
               if (FOUR) copy_async16(dst + SH::kCodes, src + kv4_k_pairs(D));
-              if (old) copy_async16(dst + SH::kWeights, old + (uint64_t)id * weight_bytes);
+              if (old) copy_async16(dst + SH::kWeights, old + block * (kPageSize * 4));
             }
           } else {
             set_status(P.status, DEV_BAD_INDEX);
@@ -203,16 +274,19 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
         asm volatile("cp.async.commit_group;" ::: "memory");
       };
       load_ids();
+      for (int x = 0; x < SH::kSlots; ++x) request(x * SH::kPage);
 
-      // ---- the rows that count, as many as fit ----
-      if (warp == 0) {
-        const int fit = kChunkRows / P.group;
+      // ---- the rows that count, as many as fit: a warp those of a segment ----
+      if (warp < nseg) {
+        const int fit = kChunkRows / P.group, tok0 = s_tok0[warp], n_new = s_pages[warp] ? s_new[warp] : 0, h = s_head[warp];
+        int2* src = s_src + row0;
         int n = 0, at = first_tok;
         while (at < n_new && n < fit) {
-          const bool counts = at + lane < n_new && (!P.row_weight || P.row_weight[tok_first + at + lane] != 0.f);
+          const bool counts = at + lane < n_new && (!P.row_weight || P.row_weight[tok0 + at + lane] != 0.f);
           unsigned m = __ballot_sync(0xffffffffu, counts);
-          const int mine = n + __popc(m & ((1u << lane) - 1));
-          if (counts && mine < fit) s_list[mine] = tok_first + at + lane;
+          const int mine = n + __popc(m & ((1u << lane) - 1)), tok = tok0 + at + lane;
+          if (counts && mine < fit)
+            for (int x = 0; x < P.group; ++x) src[mine * P.group + x] = make_int2(tok * P.n_q + h * P.group + x, tok | warp << 20);
           if (n + __popc(m) > fit) {                     // up to the last one that fits
             for (int k = fit - n; k > 1; --k) m &= m - 1;
             at += __ffs(m);
@@ -222,16 +296,16 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
             at += 32;
           }
         }
+        const int rows = n * P.group, rows8 = (rows + 7) & ~7;
+        if (lane < rows8 - rows) src[rows + lane] = make_int2(-1, warp << 20);
         if (lane == 0) {
-          s_count = n;
-          s_next = min(at, n_new);
-          s_top = 0;
-          s_lim = 0x7fffffff;
+          s_rows8[warp] = rows8;
+          s_next[warp] = min(at, n_new);
         }
       }
       __syncthreads();
-      first_tok = s_next;
-      const int rows = s_count * P.group, rows8 = (rows + 7) & ~7;
+      first_tok = s_next[0];
+      const int staged = s_row0[nseg - 1] + s_rows8[nseg - 1];
       // (chunk c of a row: its values 8 c .. 8 c + 7)
       constexpr int kPer = kChunkRows * kChunks / kThreads + 1;
       uint4 raw[kPer];
@@ -239,50 +313,52 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
       for (int k = 0; k < kPer; ++k) {
         const int i = tid + k * kThreads, row = i / kChunks, c = i % kChunks;
         raw[k] = make_uint4(0, 0, 0, 0);
-        if (row < rows) {
-          const int j = row / P.group;
-          raw[k] = __ldg(reinterpret_cast<const uint4*>(P.q + ((size_t)s_list[j] * P.n_q + h * P.group + row - j * P.group) * D) + c);
+        if (row < staged) {
+          const int at = s_src[row].x;
+          if (at >= 0) raw[k] = __ldg(reinterpret_cast<const uint4*>(P.q + (size_t)at * D) + c);
         }
       }
-      for (int s = 0; s < SH::kSlots; ++s) request(s * SH::kPage);
-      unsigned top = 0;
       if (FOUR)
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
+          // (the rows of a warp are neighbours within eight, hence of one segment)
+          const int row = (tid + k * kThreads) / kChunks;
+          if (__all_sync(0xffffffffu, row >= staged)) break;
+          unsigned top = 0;
           const uint32_t u[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             const unsigned lo = u[x] & 0x7fffu, hi = (u[x] >> 16) & 0x7fffu;
             top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
           }
+          top = __reduce_max_sync(0xffffffffu, top);
+          if (lane == 0) atomicMax(&s_top[s_src[row].y >> 20], top);
         }
-      if (FOUR) {
-        top = __reduce_max_sync(0xffffffffu, top);
-        if (lane == 0) atomicMax(&s_top, top);
-      }
-      for (int row = tid; row < rows8; row += kThreads) {
+      for (int row = tid; row < staged; row += kThreads) {
+        const int2 from = s_src[row];
         float4 info = make_float4(0.f, -1e30f, 0.f, 0.f);         // (a row that fills up the last eight: probability 0)
         int4 vis = make_int4(-1, 0, 0, 0);
-        if (row < rows) {
-          const int j = row / P.group, tok = s_list[j];
-          info.y = -1.4426950408889634f * P.lse[(size_t)tok * P.n_q + h * P.group + row - j * P.group];
+        if (from.x >= 0) {
+          const int tok = from.y & 0xfffff;
+          info.y = -1.4426950408889634f * P.lse[from.x];
           info.z = P.row_weight ? P.row_weight[tok] : 1.f;
           vis = make_int4(P.tok_climit[tok], P.tok_lo[tok], P.tok_hi[tok], 0);
-          atomicMin(&s_lim, vis.x);
+          atomicMin(&s_lim[from.y >> 20], vis.x);
         }
         *reinterpret_cast<float3*>(&s_info[row].y) = make_float3(info.y, info.z, info.w);
         s_vis[row] = vis;
       }
       __syncthreads();
-      const int e = FOUR ? max(-100, min(100, (int)(s_top >> 7) - 127 - 8)) : 0;       // the largest value to [2^8, 2^9)
-      const float down = pow2(-e), down16 = pow2(-e - 4), factor = FOUR ? pow2(e) * 16777216.f * P.scale_log2 : P.scale_log2;
+      auto scale_of = [&](int k) { return FOUR ? max(-100, min(100, (int)(s_top[k] >> 7) - 127 - 8)) : 0; };       // the largest value to [2^8, 2^9)
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
         const int i = tid + k * kThreads, row = i / kChunks, c = i % kChunks;
-        if (row >= rows8) continue;
+        if (row >= staged) continue;
         const uint4 v = raw[k];
         uint8_t* at = smem + SH::kRowsOff + row * SH::kRowBytes;
         if (FOUR) {
+          const int e = scale_of(s_src[row].y >> 20);
+          const float down = pow2(-e), down16 = pow2(-e - 4);
           // where lane c / NW of a quad looks for its word c % NW
           *reinterpret_cast<uint4*>(at + ((c % NW) * 4 + c / NW) * 16) =
               make_uint4(scaled_f16(v.x, down), scaled_f16(v.y, down16), scaled_f16(v.z, down), scaled_f16(v.w, down16));
@@ -299,7 +375,7 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
           float sum = 0.f;
 #pragma unroll
           for (int x = 0; x < 4; ++x) sum += __uint_as_float(u[x] << 16) + __uint_as_float(u[x] & 0xffff0000u);
-          // (rows8 * kChunks is a multiple of 64 and kThreads of kChunks: whole quarter and half warps come here together)
+          // (staged * kChunks is a multiple of 64 and kThreads of kChunks: whole quarter and half warps come here together)
           const unsigned together = (kChunks == 16 ? 0xffffu : 0xffu) << (lane & ~(kChunks - 1));
 #pragma unroll
           for (int o = kChunks / 2; o; o >>= 1) sum += __shfl_xor_sync(together, sum, o);
@@ -309,11 +385,30 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
         }
       }
       __syncthreads();
-      const int lim = s_lim;
 
       // ---- pages past the rows ----
       uint32_t slot_at = 0;
-      for (int p = page0 + warp; p < page1; p += kWarps) {
+      int seg_end = 0, to_page = 0, L = 0, kv_len = 0, h = 0, lim = 0, rows8 = 0;
+      float factor = 0.f;
+      const uint8_t* rows_at = smem + SH::kRowsOff;      // of the segment
+      const float4* info_at = s_info;
+      const int4* vis_at = s_vis;
+      for (int i = warp; i < total; i += kWarps) {
+        if (i >= seg_end) {
+          const int k = 31 - __clz(__ballot_sync(0xffffffffu, cum <= i)), seg_row0 = s_row0[k];
+          to_page = s_page0[k] - s_cum[k];
+          seg_end = s_cum[k] + s_pages[k];
+          L = s_ctx[k];
+          kv_len = L + s_new[k];
+          h = s_head[k];
+          lim = s_lim[k];
+          rows8 = s_rows8[k];
+          factor = FOUR ? pow2(scale_of(k)) * 16777216.f * P.scale_log2 : P.scale_log2;
+          rows_at = smem + SH::kRowsOff + seg_row0 * SH::kRowBytes;
+          info_at = s_info + seg_row0;
+          vis_at = s_vis + seg_row0;
+        }
+        const int p = i + to_page;
         asm volatile("cp.async.wait_group %0;" ::"n"(SH::kSlots - 1) : "memory");
         __syncwarp();
         const uint8_t* pg = smem + warp * SH::kSlots * SH::kPage + slot_at;
@@ -367,7 +462,7 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
             float sc[2][4];
 #pragma unroll
             for (int j = 0; j < NW; ++j) {
-              const uint4 b = *reinterpret_cast<const uint4*>(smem + SH::kRowsOff + (nt + g) * SH::kRowBytes + (j * 4 + t) * 16);
+              const uint4 b = *reinterpret_cast<const uint4*>(rows_at + (nt + g) * SH::kRowBytes + (j * 4 + t) * 16);
               if (j == 0) {
                 mma<FOUR, true>(sc[0], a[0], b.x, b.y);
                 mma<FOUR, true>(sc[1], a[1], b.z, b.w);
@@ -376,11 +471,11 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
                 mma<FOUR, false>(sc[1], a[2 * j + 1], b.z, b.w);
               }
             }
-            const float4 i0 = s_info[nt + 2 * t], i1 = s_info[nt + 2 * t + 1];
+            const float4 i0 = info_at[nt + 2 * t], i1 = info_at[nt + 2 * t + 1];
             int4 v0, v1;
             if (MASK) {
-              v0 = s_vis[nt + 2 * t];
-              v1 = s_vis[nt + 2 * t + 1];
+              v0 = vis_at[nt + 2 * t];
+              v1 = vis_at[nt + 2 * t + 1];
             }
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
@@ -404,11 +499,20 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
           acc[x] += __shfl_xor_sync(0xffffffffu, acc[x], 1);
           acc[x] += __shfl_xor_sync(0xffffffffu, acc[x], 2);
         }
-        if (stores) *reinterpret_cast<float*>(out_at + (uint64_t)id * weight_bytes) = before + (t ? acc[1] : acc[0]);
+        if (stores) out_at[((uint64_t)id * (unsigned)P.n_kv + h) * kPageSize] = before + (t ? acc[1] : acc[0]);
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");
+      const bool more = first_tok < s_new[0] && !whole;
       __syncthreads();                                   // the staged rows may be replaced
+      if (!more) break;
+      if (tid == 0) {
+        s_lim[0] = 0x7fffffff;
+        s_top[0] = 0;
+      }
     }
+    pair += nseg;
+    ahead = s_ahead[nseg - 1];
+    __syncthreads();
   }
 }
 
