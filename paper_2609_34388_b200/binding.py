@@ -311,6 +311,7 @@ class Context:
         self.cfg = cfg
         self._last_rows = self._last_pages = 0
         self._keep = weights
+        self._track = None
         self.h = C.c_void_p()
         wptr = None
         if weights is not None:
@@ -340,6 +341,7 @@ class Context:
         """Returns a torch view [T, vocab] of the library-owned logits (valid until the next step)."""
         lg = recg_logits()
         self._n_tok(batch)
+        self._track_fits(self._last_pages)
         self._check(lib().recg_step(self.h, C.byref(batch.c), C.byref(lg)))
         return lg
 
@@ -468,6 +470,10 @@ class Context:
         self._check(lib().recg_kv_track(self.h, self._floats("weights", weights), float(decay)))
         self._track = weights                          # (the steps write to it)
 
+    def _track_fits(self, pages: int):
+        if self._track is not None and self._track.numel() != max(self.cfg.n_layers, 1) * pages * self.cfg.n_kv_heads * 16:
+            raise ValueError("the weights that are gathered must be [n_layers, pages, n_kv_heads, 16] of the batch's pool")
+
     def recg_kv_shift(self, shift):
         """shift [n_req]: tokens that have been evicted from each request (empty: none)."""
         a = _i32(shift)
@@ -510,6 +516,7 @@ class Context:
     def recg_step_device(self, batch: "DeviceBatch"):
         lg = recg_logits()
         self._last_rows, self._last_pages = self.cfg.max_tokens, int(batch.c.kv_pool_pages)
+        self._track_fits(self._last_pages)
         self._check(lib().recg_step_device(self.h, C.byref(batch.c), C.byref(lg)))
         return lg
 

@@ -224,5 +224,12 @@ def test_refusals():
     with pytest.raises(RuntimeError):
         bare = binding.Context(binding.make_config(shape, 2, 32, 8, FOUR))
         bare.recg_kv_track(w)
+    ctx.recg_kv_track(w)
+    with pytest.raises(ValueError, match="batch's pool"):              # weights of another pool
+        ctx.recg_step(binding.Batch([0], [1], [0], [3], np.zeros((1, 1)), binding.alloc_kv_pool(ctx, 9), 9))
+    for pages in ([[0, 1], [0, 2]], [[0, 0], [1, 2]]):                 # a page that two requests name, or one twice
+        with pytest.raises(binding.RecgError, match="named twice"):
+            ctx.recg_step(binding.Batch([16, 16], [1, 1], [0, 0], [3, 4], np.array(pages), pool, 8))
+    ctx.recg_step(binding.Batch([16, 16], [1, 1], [0, 0], [3, 4], np.array([[0, 3], [1, 2]]), pool, 8))
     ctx.recg_sync()
     ctx.recg_free()
