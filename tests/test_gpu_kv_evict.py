@@ -100,6 +100,19 @@ def test_gathered_weight_of_long_contexts_branches_and_groups(heads, reqs, corr,
     weights_case(heads, reqs, seed=21, flags=flags, corr=corr, decay=1.0)
 
 
+@pytest.mark.parametrize("flags", POOLS)
+@pytest.mark.parametrize("heads", [TINY, B8, B14])
+def test_gathered_weight_of_many_requests(heads, flags):
+    """Many short requests, whose rows are staged together, and among them some whose rows alone do not fit."""
+    g = np.random.default_rng(5)
+    reqs = [(int(g.integers(0, 90)), int(g.integers(1, 6)), int(g.integers(0, 4))) for _ in range(120)]
+    for r, n in ((0, 70), (17, 33), (18, 140), (60, 26), (119, 65)):
+        reqs[r] = (reqs[r][0], n, 3)
+    reqs[80] = (4000, 2, 0)
+    weights_case(heads, reqs, seed=31, flags=flags)
+    weights_case(heads, reqs[:40], seed=32, flags=flags, row_weight=None, decay=0.5)
+
+
 def test_weights_add_up_to_the_rows():
     """Every counted row hands out its weight once per query head: what a kv head's positions gather sums to rows x group."""
     desc = synth.fixed_descriptor([777], [9], [4], seed=3)
