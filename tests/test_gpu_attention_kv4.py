@@ -99,6 +99,13 @@ def test_branches(heads, flags):
     run_case(heads, [(100, 8, 8), (0, 5, 4), (1030, 16, 7), (31, 2, 0)], seed=31, flags=flags, corr=[(1, 6), (4,), (3, 15), (1,)])
 
 
+@pytest.mark.parametrize("heads,n,rows", [(B8, 700, (1, 0)), (B8, 260, (3, 1)), (TINY, 900, (2, 0)), (B14, 150, (1, 2))])
+def test_many_short_requests(heads, n, rows):
+    """More work items than a CTA keeps descriptors of on chip."""
+    g = np.random.default_rng(9)
+    run_case(heads, [(int(x), *rows) for x in g.integers(0, 100, n)], seed=61)
+
+
 @pytest.mark.parametrize("flags", FLAGS)
 def test_sharp_scores_and_keys_off_centre(flags):
     """Scores whose maximum moves through the context, and keys that all lie far from zero (their common part only shifts the scores)."""
