@@ -6,7 +6,7 @@
 // is exact up to fp32 sums: the second term is one more step of 16 of the contraction, in which both factors stand as sums of
 // two fp16 numbers.  (K as m + s c rounded to 16 bits would leave the log-sum-exp of a few tokens good to 1e-4 only; steps applied
 // in fp32 behind the product have to be broadcast to every row's thread, and that alone took more of the shared memory's
-// bandwidth than all operands: 325 us instead of 193 us for 1001 rows over 6000 tokens of 40 / 8 heads.)  V stands as m + s c
+// bandwidth than all operands: 325 us instead of 192 us for 1001 rows over 6000 tokens of 40 / 8 heads.)  V stands as m + s c
 // rounded once, and P as fp16 too: 2^-11 of each term by either, a quarter of the rounding of the result together.
 //
 // Range.  fp16 has five bits of exponent, so everything is scaled by powers of two: a query row by its own largest value, K and V
@@ -413,7 +413,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
         const uint8_t* src = raw + r * (D / 2) + q * 16;
         uint8_t* dst = smem + kOffK + s * kOperand + wq * 8192 + (q >> 1) * 1024 + r * 128;
         uint4 next = *reinterpret_cast<const uint4*>(src);
-#pragma unroll 1
+        // (two units at a time in K and V: 187.0 us instead of 189.5 for one; all four, whose code is twice as long, as slow as one)
+#pragma unroll 2
         for (int u = 0; u < 4; ++u) {
           const uint4 v = (q & 2) ? make_uint4(next.z, next.w, next.x, next.y) : next;
           if (u < 3) next = *reinterpret_cast<const uint4*>(src + ((u + 1) >> 1) * kBlock + ((u + 1) & 1) * (4 * D));
@@ -492,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
         const uint8_t* src = raw + kv4_v_codes(D) + r * D + g * 16;
         uint8_t* dst = smem + kOffV + s * kOperand + wq * 8192 + (g >> 2) * 1024 + 2 * r * 128;
         uint4 next = *reinterpret_cast<const uint4*>(src);
-#pragma unroll 1
+#pragma unroll 2
         for (int u = 0; u < 4; ++u) {
           const uint4 v = (g & 4) ? make_uint4(next.z, next.w, next.x, next.y) : next;
           if (u < 3) next = *reinterpret_cast<const uint4*>(src + ((u + 1) >> 1) * kBlock + ((u + 1) & 1) * (4 * D));

@@ -4,6 +4,9 @@
 // Nothing is computed that counts, so the bytes bound it: 4 d in, d + 8 out per position and head (K and V) to write, the reverse
 // to read.  The d / 8 lanes that share a row take eight values of it each, one 16-byte access, and reduce minimum and maximum by
 // shuffles; each makes one word of codes.
+#include <algorithm>
+#include <cstring>
+
 #include "kernels.h"
 #include "kv4.cuh"
 
@@ -12,24 +15,27 @@ namespace recg {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kIoPages = 896;        // page ids that travel with a launch: 3.5 of the 4 KB of kernel parameters
+// Page ids travel with a launch: 3.5 KB of kernel parameters, or 16 of the 32 KB that there are for longer ranges.  (16001 positions in two
+// launches of 3.5 KB, written and read: 41.8 us; in one: 37.6.)
+constexpr int kFewPages = 896, kManyPages = 4000;
+template <int N>
 struct IoPages {
   int first;                         // logical page of ids[0]
-  int ids[kIoPages];
+  int ids[N];
 };
 
 // Positions [pos0, pos0 + n_pos) of a request; k, v [n_pos][n_kv][D].  Two positions of a token pair (2 p, 2 p + 1) and one head
 // are 2 D / 8 consecutive lanes, so that a word of V, which holds both, is put together by one shuffle.
-template <int D, bool WRITE>
+template <int D, bool WRITE, int N>
 __global__ void __launch_bounds__(kThreads) kv4_io_kernel(uint8_t* pool, int64_t n_pages, int layer, int n_kv,
-                                                          const __grid_constant__ IoPages pages, int pos0, int n_pos,
+                                                          const __grid_constant__ IoPages<N> pages, int pos0, int n_pos,
                                                           uint4* __restrict__ k, uint4* __restrict__ v) {
   constexpr int kLanes = D / 8;
   griddep_launch();
-  const int unit = (int)((blockIdx.x * (unsigned)kThreads + threadIdx.x) / (2 * kLanes));
+  const unsigned unit = blockIdx.x * (kThreads / (2 * kLanes)) + threadIdx.x / (2 * kLanes);
   const int half = (threadIdx.x / kLanes) & 1, j = threadIdx.x % kLanes;
   const int first_pair = pos0 >> 1, n_pairs = ((pos0 + n_pos - 1) >> 1) - first_pair + 1;
-  const int pair = unit / n_kv, h = unit - pair * n_kv;
+  const int pair = (int)(unit / (unsigned)n_kv), h = (int)(unit - (unsigned)pair * (unsigned)n_kv);
   const int pos = 2 * (first_pair + pair) + half, i = pos - pos0;
   const bool mine = pair < n_pairs && i >= 0 && i < n_pos;
   const int tok = pos & (kPageSize - 1);
@@ -72,9 +78,9 @@ __global__ void __launch_bounds__(kThreads) kv_rows_kernel(uint8_t* pool, int64_
                                                            int n_tok, const int* dyn, uint8_t* k, uint8_t* v, int64_t row_stride) {
   constexpr int kLanes = D / 8;
   griddep_launch();
-  const int64_t unit = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes;
+  const unsigned unit = blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;      // (a row and head: below 2^20 n_kv)
   const int j = threadIdx.x % kLanes;
-  const int t = (int)(unit / n_kv), h = (int)(unit - (int64_t)t * n_kv);
+  const int t = (int)(unit / (unsigned)n_kv), h = (int)(unit - (unsigned)t * (unsigned)n_kv);
   const size_t at = STAGED ? 2 * (kv_tile_base(row_stride, n_kv, D, 0, t / kPageSize, h) + kv_tile_offset(t % kPageSize, 8 * j, D))
                            : ((size_t)t * row_stride + (size_t)h * D + 8 * j) * 2;
   if (STAGED) v = k + 2 * kv_tile_elems(D);
@@ -120,12 +126,29 @@ __global__ void __launch_bounds__(kThreads) kv_rows_kernel(uint8_t* pool, int64_
   }
 }
 
-using IoKernel = void (*)(uint8_t*, int64_t, int, int, const IoPages, int, int, uint4*, uint4*);
+template <int N>
+using IoKernel = void (*)(uint8_t*, int64_t, int, int, const IoPages<N>, int, int, uint4*, uint4*);
 using RowsKernel = void (*)(uint8_t*, int64_t, int, int, const int*, int, const int*, uint8_t*, uint8_t*, int64_t);
 template <int D>
 RowsKernel rows_kernel(bool four, bool write) {
   if (four) return write ? kv_rows_kernel<D, true, true, false> : kv_rows_kernel<D, true, false, false>;
   return write ? kv_rows_kernel<D, false, true, false> : kv_rows_kernel<D, false, false, false>;
+}
+
+// As many of the positions as N page ids cover (whole pairs: a page is even); returns how many.
+template <int N>
+int launch_io(bool write, void* pool, int64_t n_pages, int layer, const Dims& dm, const int* page_row, int pos0, int n_pos, uint4* k, uint4* v,
+              cudaStream_t st) {
+  IoPages<N> pg;
+  pg.first = pos0 / kPageSize;
+  const int n = (int)std::min<int64_t>(n_pos, (int64_t)(pg.first + N) * kPageSize - pos0), last = (pos0 + n - 1) / kPageSize;
+  memcpy(pg.ids, page_row + pg.first, (last - pg.first + 1) * sizeof(int));
+  const size_t pairs = ((pos0 + n - 1) >> 1) - (pos0 >> 1) + 1, threads = pairs * dm.n_kv * (dm.head_dim / 4);
+  IoKernel<N> kernel = dm.head_dim == 128 ? (write ? kv4_io_kernel<128, true, N> : kv4_io_kernel<128, false, N>)
+                                          : (write ? kv4_io_kernel<64, true, N> : kv4_io_kernel<64, false, N>);
+  launch_pdl(kernel, dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, static_cast<uint8_t*>(pool), n_pages, layer,
+             dm.n_kv, pg, pos0, n, k, v);
+  return n;
 }
 
 }  // namespace
@@ -134,18 +157,10 @@ void launch_kv4_io(bool write, void* pool, int64_t n_pages, int layer, const Dim
                    void* k, void* v, cudaStream_t st) {
   uint4 *kp = static_cast<uint4*>(k), *vp = static_cast<uint4*>(v);
   const size_t row = (size_t)dm.n_kv * (dm.head_dim / 8);
-  IoPages pg;
   while (n_pos > 0) {
-    pg.first = pos0 / kPageSize;
-    int n = (pg.first + kIoPages) * kPageSize - pos0;          // positions that the launch's page ids cover (whole pairs: a page is even)
-    if (n > n_pos) n = n_pos;
-    const int last = (pos0 + n - 1) / kPageSize;
-    for (int i = pg.first; i <= last; ++i) pg.ids[i - pg.first] = page_row[i];
-    const size_t pairs = ((pos0 + n - 1) >> 1) - (pos0 >> 1) + 1, threads = pairs * dm.n_kv * (dm.head_dim / 4);
-    const dim3 grid((unsigned)((threads + kThreads - 1) / kThreads));
-    IoKernel kernel = dm.head_dim == 128 ? (write ? kv4_io_kernel<128, true> : kv4_io_kernel<128, false>)
-                                         : (write ? kv4_io_kernel<64, true> : kv4_io_kernel<64, false>);
-    launch_pdl(kernel, grid, dim3(kThreads), 0, st, static_cast<uint8_t*>(pool), n_pages, layer, dm.n_kv, pg, pos0, n, kp, vp);
+    const bool few = (pos0 + n_pos - 1) / kPageSize - pos0 / kPageSize < kFewPages;
+    const int n = few ? launch_io<kFewPages>(write, pool, n_pages, layer, dm, page_row, pos0, n_pos, kp, vp, st)
+                      : launch_io<kManyPages>(write, pool, n_pages, layer, dm, page_row, pos0, n_pos, kp, vp, st);
     pos0 += n;
     n_pos -= n;
     kp += n * row;

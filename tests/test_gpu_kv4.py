@@ -55,6 +55,20 @@ def test_positions_round_trip(head_dim, n_kv, pos0, n_pos):
     ctx.recg_free()
 
 
+@pytest.mark.parametrize("pos0,n_pos", [(9, 14336 - 9), (9, 14336), (9, 64000 - 9), (9, 64000), (15, 130000)])
+def test_long_ranges(pos0, n_pos):
+    """Ranges that take as many page ids as a launch carries, one more, and several launches."""
+    pt, n_pages = synth.page_tables([pos0], [n_pos + 1], 16, seed=3, spare_pages=3)
+    ctx = make(1, 64, pt.shape[1])
+    pool = binding.alloc_kv_pool(ctx, n_pages)
+    k, v = synth.kv_values(n_pos, 1, 64, seed=7, device="cuda")
+    ctx.recg_kv_write(pool, n_pages, 1, pt[0], pos0, k, v)
+    kb, vb = ctx.recg_kv_read(pool, n_pages, 1, pt[0], pos0, n_pos)
+    assert torch.equal(kb.cpu(), _kv4.values_bf16(k)) and torch.equal(vb.cpu(), _kv4.values_bf16(v))
+    ctx.recg_sync()
+    ctx.recg_free()
+
+
 def special_rows(d):
     """Rows on the format's borders, [rows, d] bf16."""
     bf = lambda t: torch.as_tensor(t, dtype=torch.float64).float().bfloat16()
