@@ -54,7 +54,8 @@ struct AttnParams {
 
 __device__ __forceinline__ void consumer_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-template <int D>
+// (LSE, here and in the kernels below: the log-sum-exp is wanted.  Asked at run time it took 0.2 us a call from those that do not want it.)
+template <int D, bool LSE>
 __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P) {
   using SM = AttnSmem<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -347,7 +348,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P
 #pragma unroll
           for (int i = 0; i < D / 8; ++i)
             dst[i * 4 + q4] = pack_bf16(o[i][2 * hh] * inv, o[i][2 * hh + 1] * inv);
-          if (P.lse && q4 == 0) P.lse[(size_t)qrow_tok[hh] * P.n_q + qrow_head[hh]] = log_sum_exp(m_run[hh], l_run[hh]);
+          if (LSE && q4 == 0) P.lse[(size_t)qrow_tok[hh] * P.n_q + qrow_head[hh]] = log_sum_exp(m_run[hh], l_run[hh]);
         } else {
           float2* dst = reinterpret_cast<float2*>(P.part_o + ((size_t)w.part * 128 + rho) * D);
 #pragma unroll
@@ -373,7 +374,7 @@ enum CombineMode { kManyTiles, kSplitRows, kDeepRows };
 // p, so that one read and a few shuffles give all weights of up to 32 parts, and the rows of the first kRows parts are on
 // their way at the same time.  Attention and combine kernel of a layer together, one request of 18 parts per row: 19.5 us with
 // four parts fetched at a time, each with its own pair, 16.1 with six and one read for all pairs; 13.9 now, with four warps a row.
-template <int D, CombineMode MODE>
+template <int D, CombineMode MODE, bool LSE>
 __global__ void __launch_bounds__(512, MODE == kDeepRows ? 1 : 2) attention_combine_kernel(const AttnTile* __restrict__ tiles,
                                                                 const int* __restrict__ counts, int n_q, int group,
                                                                 const float* __restrict__ part_o,
@@ -468,7 +469,7 @@ __global__ void __launch_bounds__(512, MODE == kDeepRows ? 1 : 2) attention_comb
       const int j = rho / group, hg = rho % group;
       const size_t row = (size_t)(tl.tok0 + j) * n_q + tl.kv_head * group + hg;
       __nv_bfloat16* dst = o + row * D + lane * E;
-      if (lse && lane == 0) lse[row] = log_sum_exp(m, l);
+      if (LSE && lane == 0) lse[row] = log_sum_exp(m, l);
       if constexpr (E == 4) {
         uint2 pk;
         pk.x = pack_bf16(acc[0] * inv, acc[1] * inv);
@@ -499,17 +500,18 @@ int combine_split(int tiles, int n_sm, bool step) {
 }
 bool few_tiles(int tiles, int n_sm) { return tiles > 0 && tiles * 16 <= 2 * n_sm; }
 unsigned combine_ctas(int tiles, int log_s, int n_sm) { return few_tiles(tiles, n_sm) ? (unsigned)tiles << (3 + log_s) : 4u * n_sm; }
-template <int D>
+template <int D, bool LSE>
 auto combine_kernel(int tiles, int log_s, int n_sm) {
-  return log_s ? attention_combine_kernel<D, kSplitRows>
-               : (few_tiles(tiles, n_sm) ? attention_combine_kernel<D, kDeepRows> : attention_combine_kernel<D, kManyTiles>);
+  return log_s ? attention_combine_kernel<D, kSplitRows, LSE>
+               : (few_tiles(tiles, n_sm) ? attention_combine_kernel<D, kDeepRows, LSE> : attention_combine_kernel<D, kManyTiles, LSE>);
 }
 
 template <int D>
 void launch_combine(const BatchLayout& bl, const Dims& dm, void* o, float* lse, const float* part_o, const float* part_ml, int n_sm,
                     cudaStream_t st, int tiles, bool step, int list_settled) {
   const int log_s = combine_split(tiles, n_sm, step);
-  launch_pdl(combine_kernel<D>(tiles, log_s, n_sm), dim3(combine_ctas(tiles, log_s, n_sm)), dim3(512), 0, st, (const AttnTile*)bl.tiles,
+  auto* kernel = lse ? combine_kernel<D, true>(tiles, log_s, n_sm) : combine_kernel<D, false>(tiles, log_s, n_sm);
+  launch_pdl(kernel, dim3(combine_ctas(tiles, log_s, n_sm)), dim3(512), 0, st, (const AttnTile*)bl.tiles,
              (const int*)bl.counts, dm.n_q, dm.n_q / dm.n_kv, part_o, part_ml, static_cast<__nv_bfloat16*>(o), lse, list_settled, log_s);
 }
 
@@ -519,7 +521,8 @@ void launch_attention_t(const BatchLayout& bl, const Dims& dm, int layer, const 
                         cudaStream_t st, bool whole, int tiles, bool step) {
   static bool configured[kMaxDevices] = {false};
   if (first_use_on_device(configured))
-    cudaFuncSetAttribute(attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnSmem<D>::kTotal);
+    for (auto* kernel : {attention_kernel<D, false>, attention_kernel<D, true>})
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnSmem<D>::kTotal);
 
   AttnParams P;
   P.items = bl.items;
@@ -542,7 +545,7 @@ void launch_attention_t(const BatchLayout& bl, const Dims& dm, int layer, const 
   P.part_o = part_o;
   P.part_ml = part_ml;
   P.status = status;
-  launch_pdl(attention_kernel<D>, dim3(n_sm), dim3(kAttnThreads), AttnSmem<D>::kTotal, st, P);
+  launch_pdl(lse ? attention_kernel<D, true> : attention_kernel<D, false>, dim3(n_sm), dim3(kAttnThreads), AttnSmem<D>::kTotal, st, P);
   if (!whole) launch_combine<D>(bl, dm, o, lse, part_o, part_ml, n_sm, st, tiles, step, 0);
 }
 

@@ -104,6 +104,8 @@ __device__ __forceinline__ int col_token(int c) { return c; }
 __device__ __forceinline__ void softmax_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 
+// LSE: the log-sum-exp of the rows is wanted
+template <bool LSE>
 __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_constant__ CUtensorMap qmap, TcAttnParams P) {
   extern __shared__ __align__(1024) uint8_t smem[];
   if (smem_u32(smem) & 1023u) {          // the swizzled operand layouts need a 1 KB aligned base
@@ -597,7 +599,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             __syncwarp();
           }
         }
-        if (P.lse && g == 0 && rvalid && w.part < 0)
+        if (LSE && g == 0 && rvalid && w.part < 0)
           P.lse[(size_t)(w.tok0 + j) * P.n_q + w.kv_head * P.group + hg] = log_sum_exp(m_all, l_all);
         if (g == 0 && rvalid && w.part >= 0) {
           P.part_ml[((size_t)w.part * 128 + row) * 2 + 0] = m_all;
@@ -690,7 +692,8 @@ void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, 
                               cudaStream_t st, bool layout_settled) {
   static bool configured[kMaxDevices] = {false};
   if (first_use_on_device(configured))
-    cudaFuncSetAttribute(attention_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    for (auto* kernel : {attention_tc_kernel<false>, attention_tc_kernel<true>})
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
 
   TcAttnParams P;
   P.items = bl.items;
@@ -721,7 +724,7 @@ void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, 
     if (status) cudaMemcpyAsync(status, &code, sizeof(int), cudaMemcpyHostToDevice, st);
     return;
   }
-  launch_pdl(attention_tc_kernel, dim3(n_sm), dim3(kThreads), kSmemBytes, st, qmap, P);
+  launch_pdl(lse ? attention_tc_kernel<true> : attention_tc_kernel<false>, dim3(n_sm), dim3(kThreads), kSmemBytes, st, qmap, P);
 }
 
 }  // namespace recg

@@ -168,9 +168,6 @@ size_t carve(recg_ctx* c, DeviceArena& A) {
   bl.tiles = A.take<AttnTile>(max_tiles);
   bl.cta_off = A.take<int>(4 * (c->target_items + 1));
   bl.counts = A.take<int>(4);
-  c->d_evict = A.take<int>(2 * Cm + 2 * Cm * Pm);
-  c->d_pos_shift = A.take<int>(Cm);
-  bl.tok_weight = A.take<float>(Tm);
   c->d_status = A.take<int>(1);
   c->d_dyn = A.take<int>(4);
   c->d_policy = A.take<int>(8 + 8 + 64 + RECG_POLICY_MAX_BLOCKS * RECG_POLICY_MAX_BINS * RECG_POLICY_MAX_BLOCKS * 2);
@@ -208,15 +205,18 @@ size_t carve(recg_ctx* c, DeviceArena& A) {
     c->x = A.take<__nv_bfloat16>(Tm * d.hidden);
     c->ss = A.take<float>(Tm * (size_t)(d.hidden / 64 + 1));   // a column tile is at least 64 wide
     c->act = A.take<__nv_bfloat16>(Tm * d.ffn);
+    const size_t esz = (g.flags & RECG_FLAG_LOGITS_BF16) ? 2 : 4;
+    c->logits = A.take<uint8_t>(Tm * (size_t)d.vocab * esz);
     c->lse = A.take<float>(Tm * d.n_q);
     if (four_bits(c)) {
       c->stage_pages = (int)((Tm + kPageSize - 1) / kPageSize);
       c->stage = A.take<__nv_bfloat16>((size_t)c->stage_pages * d.n_kv * 2 * kv_tile_elems(d.head_dim));
       c->d_stage_slot = A.take<int>(Tm);
     }
-    const size_t esz = (g.flags & RECG_FLAG_LOGITS_BF16) ? 2 : 4;
-    c->logits = A.take<uint8_t>(Tm * (size_t)d.vocab * esz);
   }
+  c->d_evict = A.take<int>(2 * Cm + 2 * Cm * Pm);
+  c->d_pos_shift = A.take<int>(Cm);
+  bl.tok_weight = A.take<float>(Tm);
   if (A.guard) {
     c->n_guards = (int)A.guards.size();
     const bool was = A.guard;
