@@ -312,7 +312,8 @@ recg_status recg_kv_select(recg_ctx *ctx, const recg_eviction *eviction, int32_t
  *   weight, as the rows behind it have.)
  * recg_kv_shift(): shift[r] tokens (HOST [n_req]) of request r have been evicted: the rotary positions of its rows in the steps from now on
  *   are those of a context longer by as much.  Requests from n_req on are not shifted; n_req = 0: none is.  recg_next_round() leaves it as
- *   it is.  Refused while the stream is being captured.
+ *   it is.  Refused while the stream is being captured; a step that was captured after a first call (with n_req > 0) follows later ones,
+ *   one captured before does not.
  */
 recg_status recg_kv_track(recg_ctx *ctx, float *weights, float decay);
 recg_status recg_kv_shift(recg_ctx *ctx, int32_t n_req, const int32_t *shift);

@@ -1210,19 +1210,16 @@ recg_status recg_kv_shift(recg_ctx* ctx, int32_t n_req, const int32_t* shift) {
   if (!ctx) return RECG_ERR_INVALID_ARG;
   if (n_req < 0 || (n_req > 0 && !shift)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_shift: negative n_req or null array");
   if (n_req > ctx->cfg.max_requests) return fail(ctx, RECG_ERR_CAPACITY, "recg_kv_shift: n_req exceeds max_requests");
-  if (n_req == 0) {
-    ctx->bl.pos_shift = nullptr;
-    return RECG_OK;
-  }
   for (int r = 0; r < n_req; ++r)
     if (shift[r] < 0 || shift[r] > (1 << 30)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_shift: a shift must be 0 .. 2^30");
   cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
   CU(cudaStreamIsCapturing(ctx->stream, &cap));
   if (cap != cudaStreamCaptureStatusNone) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_shift: not while the stream is being captured");
+  if (n_req == 0 && !ctx->bl.pos_shift) return RECG_OK;
   int h[kMaxLayoutRequests];                         // (a larger batch: its further requests are not shifted)
   std::fill(std::copy(shift, shift + n_req, h), h + ctx->cfg.max_requests, 0);
   CU(cudaMemcpyAsync(ctx->d_pos_shift, h, ctx->cfg.max_requests * sizeof(int), cudaMemcpyHostToDevice, ctx->stream));
-  ctx->bl.pos_shift = ctx->d_pos_shift;
+  ctx->bl.pos_shift = n_req ? ctx->d_pos_shift : nullptr;      // (zeros are uploaded all the same: a captured step may read them)
   return RECG_OK;
 }
 recg_status recg_kv_select(recg_ctx* ctx, const recg_eviction* e, int32_t* keep, int32_t keep_stride) {

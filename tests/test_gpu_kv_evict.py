@@ -390,3 +390,31 @@ def test_attention_captured_before_its_work_list_was_built(flags):
         del graph
         ctx.recg_sync()
         ctx.recg_free()
+
+
+def test_eviction_and_shift_are_refused_while_captured():
+    """They copy host arrays; what lies around them in the capture is not harmed."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ctx = make(TINY, 4, 8, 2, binding.FLAG_KV_4BIT)
+        pool = binding.alloc_kv_pool(ctx, 8)
+        w = torch.rand((2, 8, 2, 16), device="cuda")
+        keep = torch.zeros((1, 2, 2, 10), dtype=torch.int32, device="cuda")
+        ev = binding.Eviction([40, 50], [10, 10], np.arange(8).reshape(2, 4), pool, 8, w)
+        rows = torch.randn((2, 2, 64), device="cuda").bfloat16()
+        ctx.recg_kv_append(binding.Batch([40, 50], [1, 1], [0, 0], None, np.arange(8).reshape(2, 4), pool, 8), 0, rows, rows)
+        ctx.recg_sync()
+        graph = torch.cuda.CUDAGraph()
+        got = torch.zeros((2, 2, 2, 64), dtype=torch.bfloat16, device="cuda")
+        with torch.cuda.graph(graph, stream=stream):
+            for call in (lambda: ctx.recg_kv_select(ev, keep), lambda: ctx.recg_kv_compact(ev, keep), lambda: ctx.recg_kv_shift([1, 2])):
+                with pytest.raises(binding.RecgError, match="captured"):
+                    call()
+            ctx.recg_kv_rows(None, 0, got[0], got[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0].cpu(), _kv4.values_bf16(rows.cpu())) and torch.equal(got[0], got[1])
+        del graph
+        ctx.recg_kv_select(ev, keep)
+        ctx.recg_sync()
+        ctx.recg_free()
