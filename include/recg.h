@@ -259,6 +259,12 @@ recg_status recg_kv_append(recg_ctx *ctx, const recg_batch *batch, int32_t layer
 recg_status recg_kv_rows(recg_ctx *ctx, const recg_batch *batch, int32_t layer, void *k, void *v, int64_t row_stride);
 
 /*
+ * The batch that batch == NULL stands for in the operations on the pool: its rows (n_rows; of a device-resident round max_tokens, the rows it
+ * may have) and the pages of its pool.  Arrays that go with batch == NULL are for this many.  0 and 0: there is none, and such a call is refused.
+ */
+recg_status recg_layout_info(recg_ctx *ctx, int32_t *n_rows, int64_t *kv_pool_pages);
+
+/*
  * The attention weight that the cached tokens of a batch gather in one layer (what an eviction goes by).  Per request, kv head
  * and cache position j < L_r + n_r, in float32:
  *   weights_out[j] = (j < L_r ? decay * weights_in[j] : 0) + sum over the rows t of the request and the query heads that share the

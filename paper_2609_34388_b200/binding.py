@@ -126,6 +126,7 @@ def lib() -> C.CDLL:
         L.recg_kv_track.argtypes = [C.c_void_p, C.c_void_p, C.c_float]
         L.recg_kv_shift.argtypes = [C.c_void_p, C.c_int32, C.c_void_p]
         L.recg_kv_compact.argtypes = L.recg_kv_select.argtypes
+        L.recg_layout_info.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
         L.recg_linear.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         L.recg_debug_buffer.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_void_p), C.POINTER(C.c_int32),
                                         C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
@@ -148,7 +149,7 @@ def lib() -> C.CDLL:
         L.recg_debug_map_cache_selftest.restype = C.c_int32
         for f in ("recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write", "recg_kv_read",
                   "recg_attention_lse", "recg_kv_append", "recg_kv_rows", "recg_kv_weights", "recg_kv_select", "recg_kv_compact", "recg_kv_track",
-           "recg_kv_shift",
+           "recg_kv_shift", "recg_layout_info",
            "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_timing_enable", "recg_timing_read",
                   "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
                   "recg_step_device", "recg_next_round"):
@@ -159,7 +160,7 @@ def lib() -> C.CDLL:
 
 EXPORTS = ("recg_kv_pool_bytes", "recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write",
            "recg_attention_lse", "recg_kv_read", "recg_kv_append", "recg_kv_rows", "recg_kv_weights", "recg_kv_select", "recg_kv_compact", "recg_kv_track",
-           "recg_kv_shift",
+           "recg_kv_shift", "recg_layout_info",
            "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_last_error",
            "recg_timing_enable", "recg_timing_read", "recg_row_stats_static", "recg_row_stats_static_error",
            "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
@@ -309,7 +310,8 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("recg needs a CUDA device (there is no CPU fallback)")
         self.cfg = cfg
-        self._last_rows = self._last_pages = 0
+        self._rows, self._pages = C.c_int32(), C.c_int64()             # what recg_layout_info() writes
+        self._info = C.addressof(self._rows), C.addressof(self._pages)
         self._keep = weights
         self._track = None
         self.h = C.c_void_p()
@@ -340,8 +342,7 @@ class Context:
     def recg_step(self, batch: Batch):
         """Returns a torch view [T, vocab] of the library-owned logits (valid until the next step)."""
         lg = recg_logits()
-        self._n_tok(batch)
-        self._track_fits(self._last_pages)
+        self._track_fits(int(batch.c.kv_pool_pages))
         self._check(lib().recg_step(self.h, C.byref(batch.c), C.byref(lg)))
         return lg
 
@@ -370,11 +371,11 @@ class Context:
 
     def recg_attention(self, batch: Optional[Batch], layer: int, q: torch.Tensor, o: torch.Tensor, lse: Optional[torch.Tensor] = None):
         """lse (float32 [T, n_q_heads], optional) receives the log-sum-exp of every row's scores."""
-        n_tok = self._n_tok(batch)
         b = C.byref(batch.c) if batch is not None else None
         if lse is None:
             self._check(lib().recg_attention(self.h, b, layer, q.data_ptr(), o.data_ptr()))
             return
+        n_tok = self._n_tok(batch)
         if lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous() or lse.numel() != n_tok * self.cfg.n_q_heads:
             raise ValueError(f"lse must be contiguous CUDA float32 [{n_tok}, {self.cfg.n_q_heads}]")
         self._check(lib().recg_attention_lse(self.h, b, layer, q.data_ptr(), o.data_ptr(), lse.data_ptr()))
@@ -404,10 +405,14 @@ class Context:
         return C.byref(batch.c) if batch is not None else None, k.data_ptr(), v.data_ptr(), strides[0] if n > 1 else 0
 
     def _n_tok(self, batch: Optional[Batch]) -> int:
-        """Rows of the batch, or of the one that an operation was given last."""
-        if batch is not None:
-            self._last_rows, self._last_pages = batch.n_tok, int(batch.c.kv_pool_pages)
-        return self._last_rows
+        """Rows of the batch, or of the one that the library has laid out last (which calls lay one out, and which are refused before they
+        do, it alone knows)."""
+        return batch.n_tok if batch is not None else self._layout()[0]
+
+    def _layout(self):
+        """Rows and pool pages of the batch that None stands for."""
+        self._check(lib().recg_layout_info(self.h, *self._info))
+        return self._rows.value, self._pages.value
 
     def recg_kv_append(self, batch: Optional[Batch], layer: int, k: torch.Tensor, v: torch.Tensor):
         """k, v [T, n_kv_heads, head_dim]: rows of the batch (None: the one laid out last); rows may lie in a wider array."""
@@ -443,7 +448,8 @@ class Context:
             raise ValueError(f"q must be contiguous CUDA bf16 [{n}, {self.cfg.n_q_heads}, {self.cfg.head_dim}]")
         if weights_in is not None and weights_in.numel() != weights_out.numel():
             raise ValueError("weights_in and weights_out must have one shape")
-        if self._last_pages and weights_out.numel() != self.cfg.n_layers * self._last_pages * self.cfg.n_kv_heads * 16:
+        pages = int(batch.c.kv_pool_pages) if batch is not None else self._layout()[1]
+        if pages and weights_out.numel() != self.cfg.n_layers * pages * self.cfg.n_kv_heads * 16:
             raise ValueError("weights must be [n_layers, pages of the pool, n_kv_heads, 16]")
         self._check(lib().recg_kv_weights(self.h, C.byref(batch.c) if batch is not None else None, layer, q.data_ptr(),
                                           self._floats("lse", lse, n * self.cfg.n_q_heads), self._floats("row_weight", row_weight, n),
@@ -515,8 +521,7 @@ class Context:
 
     def recg_step_device(self, batch: "DeviceBatch"):
         lg = recg_logits()
-        self._last_rows, self._last_pages = self.cfg.max_tokens, int(batch.c.kv_pool_pages)
-        self._track_fits(self._last_pages)
+        self._track_fits(int(batch.c.kv_pool_pages))
         self._check(lib().recg_step_device(self.h, C.byref(batch.c), C.byref(lg)))
         return lg
 

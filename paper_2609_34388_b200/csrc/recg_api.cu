@@ -1015,6 +1015,18 @@ recg_status recg_policy_step(recg_ctx* ctx, const recg_policy_state* state, cons
   return RECG_OK;
 }
 
+// Whether there is a batch that batch == NULL stands for.
+static bool has_batch(const recg_ctx* ctx) { return ctx->layout_valid && ctx->layout_has_pages && ctx->last_pool; }
+recg_status recg_layout_info(recg_ctx* ctx, int32_t* n_rows, int64_t* kv_pool_pages) {
+  if (!ctx || !n_rows || !kv_pool_pages) return RECG_ERR_INVALID_ARG;
+  *n_rows = has_batch(ctx) ? ctx->bl.n_tok : 0;
+  *kv_pool_pages = has_batch(ctx) ? ctx->last_pool_pages : 0;
+  return RECG_OK;
+}
+static recg_status no_batch(recg_ctx* ctx, const char* who) {
+  return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": no batch given and none with a KV pool laid out before");
+}
+
 // The batch of a standalone operation on the pool: the one given, or the one laid out last.
 // list: it needs the attention work list too.
 static recg_status operation_batch(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const char* who, bool list = true) {
@@ -1025,8 +1037,7 @@ static recg_status operation_batch(recg_ctx* ctx, const recg_batch* batch, int32
     if (s == RECG_OK) ctx->logits_valid = false;
     return s;
   }
-  if (!ctx->layout_valid || !ctx->layout_has_pages || !ctx->last_pool)
-    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": no batch given and none with a KV pool laid out before");
+  if (!has_batch(ctx)) return no_batch(ctx, who);
   if (list && ctx->list_pending) {
     // (the descriptor is in device memory by now; a captured launch builds nothing yet, so the list stays pending)
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
@@ -1091,7 +1102,9 @@ recg_status recg_kv_read(recg_ctx* ctx, const void* kv_pool, int64_t kv_pool_pag
 
 static recg_status kv_rows(recg_ctx* ctx, bool write, const recg_batch* batch, int32_t layer, void* k, void* v, int64_t row_stride,
                            const char* who) {
-  if (!ctx || !k || !v) return RECG_ERR_INVALID_ARG;
+  if (!ctx) return RECG_ERR_INVALID_ARG;
+  if (!batch && !has_batch(ctx)) return no_batch(ctx, who);       // (before the arrays: those for no rows are null)
+  if (!k || !v) return RECG_ERR_INVALID_ARG;
   const int64_t width = (int64_t)ctx->dm.n_kv * ctx->dm.head_dim;
   if (row_stride == 0) row_stride = width;
   if (row_stride < width || row_stride > INT32_MAX || row_stride % 8 || !aligned16(k, v))
