@@ -73,6 +73,8 @@ typedef struct recg_ctx recg_ctx;
 
 /* Model and capacity description; immutable after recg_init(). */
 typedef struct {
+  /* n_layers may be 0 for a context that only runs the standalone operations; those on a pool then take one of a single layer
+     (of the size for n_layers = 1) */
   int32_t n_layers, hidden, n_q_heads, n_kv_heads, head_dim, ffn, vocab;
   float rope_base;        /* rotary base; pairing is (i, i + head_dim/2)                         */
   float rms_eps;

@@ -432,6 +432,10 @@ class Context:
         self._check(lib().recg_kv_rows(self.h, b, layer, kp, vp, stride))
         return k, v
 
+    def _weights_size(self, pages: int) -> int:
+        """Elements of a pool's weights (a context without layers has a pool of one)."""
+        return max(self.cfg.n_layers, 1) * pages * self.cfg.n_kv_heads * 16
+
     def _floats(self, name: str, t: Optional[torch.Tensor], n: Optional[int] = None):
         if t is None:
             return None
@@ -449,7 +453,7 @@ class Context:
         if weights_in is not None and weights_in.numel() != weights_out.numel():
             raise ValueError("weights_in and weights_out must have one shape")
         pages = int(batch.c.kv_pool_pages) if batch is not None else self._layout()[1]
-        if pages and weights_out.numel() != self.cfg.n_layers * pages * self.cfg.n_kv_heads * 16:
+        if pages and weights_out.numel() != self._weights_size(pages):
             raise ValueError("weights must be [n_layers, pages of the pool, n_kv_heads, 16]")
         self._check(lib().recg_kv_weights(self.h, C.byref(batch.c) if batch is not None else None, layer, q.data_ptr(),
                                           self._floats("lse", lse, n * self.cfg.n_q_heads), self._floats("row_weight", row_weight, n),
@@ -459,7 +463,7 @@ class Context:
         want = (ev.layers[1] - ev.layers[0], ev.c.n_req, self.cfg.n_kv_heads)
         if keep.dtype != torch.int32 or not keep.is_cuda or not keep.is_contiguous() or keep.ndim != 4 or keep.shape[:3] != want:
             raise ValueError(f"keep must be contiguous CUDA int32 {list(want)} + [positions]")
-        if ev.weights is not None and ev.weights.numel() != self.cfg.n_layers * int(ev.c.kv_pool_pages) * self.cfg.n_kv_heads * 16:
+        if ev.weights is not None and ev.weights.numel() != self._weights_size(int(ev.c.kv_pool_pages)):
             raise ValueError("weights must be [n_layers, pages of the pool, n_kv_heads, 16]")
         return C.byref(ev.c), keep.data_ptr(), keep.shape[3]
 
@@ -477,7 +481,7 @@ class Context:
         self._track = weights                          # (the steps write to it)
 
     def _track_fits(self, pages: int):
-        if self._track is not None and self._track.numel() != max(self.cfg.n_layers, 1) * pages * self.cfg.n_kv_heads * 16:
+        if self._track is not None and self._track.numel() != self._weights_size(pages):
             raise ValueError("the weights that are gathered must be [n_layers, pages, n_kv_heads, 16] of the batch's pool")
 
     def recg_kv_shift(self, shift):

@@ -146,6 +146,8 @@ recg_status fail(recg_ctx* c, recg_status s, const std::string& msg) {
   } while (0)
 
 bool four_bits(const recg_ctx* ctx) { return ctx->cfg.flags & RECG_FLAG_KV_4BIT; }
+// Layers of a pool that operations are given (a context without layers runs them on a pool of one).
+int pool_layers(const recg_ctx* ctx) { return ctx->cfg.n_layers > 0 ? ctx->cfg.n_layers : 1; }
 
 size_t carve(recg_ctx* c, DeviceArena& A) {
   const recg_config& g = c->cfg;
@@ -1030,7 +1032,7 @@ static recg_status no_batch(recg_ctx* ctx, const char* who) {
 // The batch of a standalone operation on the pool: the one given, or the one laid out last.
 // list: it needs the attention work list too.
 static recg_status operation_batch(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const char* who, bool list = true) {
-  if (layer < 0 || (ctx->cfg.n_layers > 0 && layer >= ctx->cfg.n_layers))
+  if (layer < 0 || layer >= pool_layers(ctx))
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": layer out of range");
   if (batch) {
     recg_status s = upload_and_layout(ctx, batch, true, false, false, list);
@@ -1077,7 +1079,7 @@ static recg_status kv_io(recg_ctx* ctx, bool write, void* pool, int64_t n_pool_p
                          const int32_t* row, int32_t n_table, int32_t pos0, int32_t n_pos, void* k, void* v) {
   if (!ctx || !pool || !row || !k || !v) return RECG_ERR_INVALID_ARG;
   if (pos0 < 0 || n_pos < 0 || n_table <= 0 || n_table > ctx->cfg.max_pages_per_request || layer < 0 ||
-      (ctx->cfg.n_layers > 0 && layer >= ctx->cfg.n_layers) || n_pool_pages <= 0)
+      layer >= pool_layers(ctx) || n_pool_pages <= 0)
     return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_*: bad position range, layer or table length");
   if (four_bits(ctx) && (!aligned16(k, v) || !aligned16(pool, pool)))
     return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_*: k, v and the pool must be 16-byte aligned");
@@ -1148,7 +1150,7 @@ static recg_status evict_batch(recg_ctx* ctx, const recg_eviction* e, int32_t ke
     return fail(ctx, RECG_ERR_INVALID_ARG, name + ": null array, n_req <= 0 or no pages");
   const int C = e->n_req;
   if (C > ctx->cfg.max_requests) return fail(ctx, RECG_ERR_CAPACITY, name + ": n_req exceeds max_requests");
-  if (e->layer_begin < 0 || e->layer_end <= e->layer_begin || e->layer_end > (ctx->cfg.n_layers > 0 ? ctx->cfg.n_layers : 1) ||
+  if (e->layer_begin < 0 || e->layer_end <= e->layer_begin || e->layer_end > pool_layers(ctx) ||
       e->layer_end - e->layer_begin > 65535)
     return fail(ctx, RECG_ERR_INVALID_ARG, name + ": layer range");
   if (e->n_sink < 0 || e->n_recent < 0) return fail(ctx, RECG_ERR_INVALID_ARG, name + ": negative n_sink or n_recent");

@@ -1,0 +1,64 @@
+"""The pool's operations at the edges of what they are given: contexts without layers."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_34388_b200 import binding, synth
+from tests import _kv4
+
+pytestmark = pytest.mark.gpu
+
+POOLS = [0, binding.FLAG_KV_4BIT]
+
+
+def make(layers, flags, heads=(4, 2, 64), max_req=2, max_tokens=32, stride=4):
+    nq, nkv, d = heads
+    shape = synth.ModelShape(n_layers=layers, hidden=64, n_q_heads=nq, n_kv_heads=nkv, head_dim=d, ffn=64, vocab=64)
+    return binding.Context(binding.make_config(shape, max_req, max_tokens, stride, flags))
+
+
+@pytest.mark.parametrize("flags", POOLS)
+def test_a_context_without_layers_has_a_pool_of_one(flags):
+    ctx, one = make(0, flags), make(1, flags)
+    pool, table = binding.alloc_kv_pool(one, 4), np.arange(4)[None]
+    k = torch.randn((60, 2, 64), device="cuda").bfloat16()
+    held = _kv4.values_bf16(k) if flags else k.cpu()
+    ctx.recg_kv_write(pool, 4, 0, table[0], 0, k, k)
+    batch = binding.Batch([55], [5], [0], None, table, pool, 4)
+    q = torch.randn((5, 4, 64), device="cuda").bfloat16()
+    w = torch.zeros((1, 4, 2, 16), device="cuda")
+    lib, rows = binding.lib(), k[:5].clone()
+    o, lse, want, lse_want = torch.empty_like(q), torch.empty((5, 4), device="cuda"), torch.empty_like(q), torch.empty((5, 4), device="cuda")
+    one.recg_attention(batch, 0, q, want, lse_want)
+    # the second layer: refused by every operation, before anything is launched
+    calls = [lambda l: ctx.recg_kv_write(pool, 4, l, table[0], 0, k, k), lambda l: ctx.recg_kv_read(pool, 4, l, table[0], 0, 60),
+             lambda l: ctx.recg_kv_append(batch, l, rows, rows), lambda l: ctx.recg_kv_rows(batch, l), lambda l: ctx.recg_attention(batch, l, q, o, lse),
+             lambda l: ctx.recg_attention(batch, l, q, o), lambda l: ctx.recg_kv_weights(batch, l, q, lse_want, None, w)]
+    for call in calls:
+        for layer in (1, 2 ** 31 - 1, -1):
+            with pytest.raises(binding.RecgError, match="layer"):
+                call(layer)
+    # the first: as a context of one layer
+    ctx.recg_attention(batch, 0, q, o, lse)
+    assert torch.equal(o, want) and torch.equal(lse, lse_want)
+    for x in ctx.recg_kv_rows(batch, 0):
+        assert torch.equal(x.cpu(), held[55:])
+    ctx.recg_kv_weights(batch, 0, q, lse, None, w)
+    w_one = torch.zeros_like(w)
+    one.recg_kv_weights(batch, 0, q, lse, None, w_one)
+    assert torch.equal(w, w_one) and float(w.sum()) > 1
+    with pytest.raises(ValueError):
+        ctx.recg_kv_weights(batch, 0, q, lse, None, w.repeat(2, 1, 1, 1))
+    keep = torch.empty((1, 1, 2, 20), dtype=torch.int32, device="cuda")
+    ev = binding.Eviction([60], [20], table, pool, 4, w, 2, 3)
+    ctx.recg_kv_select(ev, keep)
+    ctx.recg_kv_compact(ev, keep)
+    got = ctx.recg_kv_read(pool, 4, 0, table[0], 0, 20)[0].cpu()
+    for h in range(2):
+        assert torch.equal(got[:, h], held[keep[0, 0, h].cpu().long(), h])
+    assert lib.recg_kv_select(ctx.h, C.byref(binding.Eviction([60], [20], table, pool, 4, w, layers=(0, 2)).c), keep.data_ptr(), 20) == 1
+    for c in (ctx, one):
+        c.recg_sync()
+        c.recg_free()
