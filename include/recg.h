@@ -295,7 +295,7 @@ recg_status recg_kv_weights(recg_ctx *ctx, const recg_batch *batch, int32_t laye
  * recg_kv_select() writes keep: DEVICE int32 [layer_end - layer_begin, n_req, n_kv_heads, keep_stride], the positions that stay in
  * ascending order, -1 behind the last.  kv_pool is not read.
  * recg_kv_compact() moves K, V and weight (weights may be NULL) of position keep[i] to position i.  keep may be any list of
- * positions below ctx_len, in place with keep[i] >= i; an entry that is not sets the device status word (recg_sync() returns
+ * positions below ctx_len (for a request that is not cut too), in place with keep[i] >= i; an entry that is not sets the device status word (recg_sync() returns
  * RECG_ERR_INTERNAL) and its position is left as it was.
  * Both copy the HOST arrays and do not synchronise; they are refused while the stream is being captured.
  */

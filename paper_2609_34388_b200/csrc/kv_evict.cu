@@ -280,7 +280,6 @@ __global__ void __launch_bounds__(kMoveThreads) kv_compact_kernel(EvictDesc E, u
   griddep_launch();
   const int L = E.ctx_len[r], n_keep = E.kept[r];
   const bool in_place = E.dst_table == nullptr;
-  if (in_place && n_keep >= L) return;
   const int* list = keep + (((size_t)blockIdx.z * E.n_req + r) * n_kv + h) * keep_stride;
   const int* src_pt = E.page_table + (size_t)r * E.pt_stride;
   const int* dst_pt = in_place ? src_pt : E.dst_table + (size_t)r * E.dst_stride;

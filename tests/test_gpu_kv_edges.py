@@ -62,3 +62,53 @@ def test_a_context_without_layers_has_a_pool_of_one(flags):
     for c in (ctx, one):
         c.recg_sync()
         c.recg_free()
+
+
+@pytest.mark.parametrize("flags", POOLS)
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_in_place_lists_of_requests_that_are_not_cut(flags, head_dim):
+    """keep may be any list with keep[i] >= i, also where as many positions stay as there are; an entry that is not one is reported."""
+    ctx = make(1, flags, heads=(4, 2, head_dim), stride=16)
+    n, table = [5, 200], np.arange(32).reshape(2, 16)
+    pool, w = binding.alloc_kv_pool(ctx, 32), torch.rand((1, 32, 2, 16), device="cuda")
+    before = w.clone()
+    rows = []
+    for r in range(2):
+        k, v = synth.kv_values(n[r], 2, head_dim, seed=r, device="cuda")
+        ctx.recg_kv_write(pool, 32, 0, table[r], 0, k, v)
+        rows.append([t.cpu() for t in ctx.recg_kv_read(pool, 32, 0, table[r], 0, n[r])])
+    g = np.random.default_rng(4)
+    lists = np.full((1, 2, 2, 200), -1, dtype=np.int32)
+    for h in range(2):
+        lists[0, 0, h, :5] = [1, 1, 3, 3, 4]
+        lists[0, 1, h] = [g.integers(i, 200) for i in range(200)]
+    lists[0, 1, 0, 30:180] = np.arange(30, 180)                      # whole pages that stay where they are, behind and before some that do not
+    keep = torch.from_numpy(lists).cuda()
+    ev = binding.Eviction(n, [5, 1000], table, pool, 32, w)
+    ctx.recg_kv_compact(ev, keep)
+    ctx.recg_sync()
+
+    def check(lists):
+        for r in range(2):
+            for got, had in zip(ctx.recg_kv_read(pool, 32, 0, table[r], 0, n[r]), rows[r]):
+                for h in range(2):
+                    assert torch.equal(got.cpu()[:, h], had[lists[0, r, h, :n[r]].astype(np.int64), h]), (r, h)
+            pos = np.arange(n[r])
+            for h in range(2):
+                src = lists[0, r, h, :n[r]]
+                assert torch.equal(w[0, table[r][pos // 16], h, pos % 16], before[0, table[r][src // 16], h, src % 16]), (r, h)
+
+    check(lists)
+    # the identity changes nothing
+    same = np.broadcast_to(np.arange(200, dtype=np.int32), (1, 2, 2, 200)).copy()
+    bytes_before = pool.view(torch.uint8).clone()
+    ctx.recg_kv_compact(ev, torch.from_numpy(same).cuda())
+    ctx.recg_sync()
+    assert torch.equal(pool.view(torch.uint8), bytes_before)
+    # entries that name no position, or one in front: reported, and their positions are left as they were
+    same[0, 0, 1, 4], same[0, 1, 0, 7], same[0, 1, 1, 199] = 5, 6, -1
+    ctx.recg_kv_compact(ev, torch.from_numpy(same).cuda())
+    with pytest.raises(binding.RecgError, match="out of range"):
+        ctx.recg_sync()
+    assert torch.equal(pool.view(torch.uint8), bytes_before)
+    ctx.recg_free()
