@@ -10,9 +10,12 @@
 // Single rows are bound by the bytes of the cache, if only the instructions that unpack the codes are few.  The operands are fp16,
 // and a code masked out of its word in the lowest 8 bits of a half IS an fp16 number, a subnormal one: c 2^-24 or 16 c 2^-24.  So
 // eight codes cost one shift and four ANDs, where bf16 takes three shifts, four masks with an exponent and four subtractions
-// (694 instructions for a page of 16 tokens: 99.5 us for one token over 131072 of context, 32 / 8 heads; now 34.3).  What belongs to the 16 is divided out of Q and of the result.  Q is scaled by a power
-// of two for all rows of a warp, and the steps of V, as factors of P, by another that follows the largest of them; so a score
-// is off by 2^-30 of the largest row's scores at most, and p s_V by 2^-11 of itself.
+// (694 instructions for a page of 16 tokens: 99.5 us for one token over 131072 of context, 32 / 8 heads; now 35.0).  What belongs to
+// the 16 is divided out of Q and of the result.  Rows of Q are scaled by a power of two, one for all rows of a warp unless they lie
+// far apart, and the steps of V, as factors of a row of P, by another that follows the largest step that the row sees.  So a value of
+// q is off by 2^-21 of the row's largest at most, and p s_V by 2^-11 of itself or, where that is more, by 2^-31 of the largest step.
+// (Rows with scales of their own, masks and large scores are a second form of the loop's body.  With one scale for whatever the
+// warp has at hand, a row was wrong by half where another one's V was 2^30 as large; it took 34.3 instead of 35.0 us.)
 //
 // A warp is alone with its pages: it requests them itself, 16 bytes a lane into a ring of its own, and runs ahead of itself into the
 // next item.  (One bulk copy per page and head and a barrier per slot: the one lane that issues them took 850 clocks for every 2100
@@ -31,6 +34,8 @@ namespace {
 constexpr float kNoRef = -1e30f;       // reference maximum of a row that has seen no token yet
 constexpr float kHeadroom = 8.f;       // a row's reference maximum moves when it is outgrown by more than 2^8
 constexpr float kLift = 7.f;           // probabilities stand as 2^7 p: with steps below 1 at most 2^15
+constexpr float kLarge = 512.f;        // scores (in powers of two) from which on the reference is subtracted exactly (see below)
+constexpr int kNear = 8;               // rows of Q whose largest values are within 2^8 of each other stand on one scale
 
 // NT: groups of eight query rows a warp has.  Two pages at a time are two independent chains of instructions (one token of one request,
 // 131072 of context: 41.9 us with one page, 40.3 with two, before the merge of parts got shorter), for which sixteen rows leave no registers.
@@ -44,7 +49,7 @@ struct Shape {
   static constexpr int kRing = kWarps * kSlots * kPages * kBlock;
   static constexpr int kRowPad = D + 4;                            // floats from row to row of a merged part
   static constexpr int kRows = 8 * NT;
-  static constexpr int kMerge = kWarps * kRows * kRowPad * 4;      // [warp][row][value]; values D and D + 1: reference maximum, sum
+  static constexpr int kMerge = kWarps * kRows * kRowPad * 4;      // [warp][row][value]; values D to D + 2: reference maximum, sum, scale of Q
   static constexpr int kItemsOff = kRing + kMerge;
   static constexpr int kItems = 32;                                // items of the CTA whose descriptors are kept on chip
   static constexpr int kTotal = kItemsOff + kItems * (int)sizeof(AttnItem);
@@ -102,6 +107,7 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
   }
 }
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
+__device__ __forceinline__ float inverse(float power) { return __int_as_float(0x7f000000 - __float_as_int(power)); }       // of 2^e
 
 template <int D, int NT>
 __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kernel(Params P) {
@@ -112,6 +118,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint8_t* ring = smem + warp * kSlots * kSlot;
   float* merge = reinterpret_cast<float*>(smem + SH::kRing);
+  // scale of a row of Q of this warp, relative to the scale of all (in shared memory: as a register more in the loop 35.5 us
+  // instead of 35.0 for one token over 131072 of context)
+  auto below = [&](int nt, int column) -> float& { return merge[(warp * SH::kRows + nt * 8 + column) * SH::kRowPad + D + 2]; };
   // (where the work list is settled all reads of it, and of page ids, overlap the end of the kernel in front)
   if (!P.early_desc) griddep_wait();
 
@@ -232,12 +241,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
     // times 16 ----
     uint32_t qf[NT][D / 16][2];
     float qs[NT][2];                     // sums of the rows 2 t and 2 t + 1, times the scale of the scores
-    float factor;                        // what makes a product of this scaled Q and codes 2^-24 c a score
+    float factor;                        // what makes a product of scaled Q and codes 2^-24 c a score
     int lim = 0x7fffffff;                // the position up to which every row of the warp sees everything
     {
-      uint32_t top = 0;
+      uint32_t top[NT];                  // largest value of this quarter of row g
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
+        top[nt] = 0;
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < NW; ++k) {
@@ -246,24 +256,41 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
           for (int i = 0; i < 4; ++i) {
             sum += __uint_as_float(u[i] << 16) + __uint_as_float(u[i] & 0xffff0000u);
             const uint32_t lo = u[i] & 0x7fffu, hi = (u[i] >> 16) & 0x7fffu;
-            top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));      // (a row that is not finite does not concern the others)
+            top[nt] = max(top[nt], max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));      // (a row that is not finite does not concern the others)
           }
         }
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          qs[nt][e] = __shfl_sync(0xffffffffu, sum, (2 * t + e) * 4) * P.scale_log2;
-          lim = min(lim, climit[nt][e]);
+        for (int c = 0; c < 2; ++c) {
+          qs[nt][c] = __shfl_sync(0xffffffffu, sum, (2 * t + c) * 4) * P.scale_log2;
+          lim = min(lim, climit[nt][c]);
         }
       }
       lim = __reduce_min_sync(0xffffffffu, lim);
-      // the largest value of all rows goes to [2^8, 2^9) (as far as the exponent allows: a factor and its inverse are normal numbers)
-      const int e = max(-100, min(100, (int)(__reduce_max_sync(0xffffffffu, top) >> 7) - 127 - 8));
-      const float down = pow2(-e), down16 = pow2(-e - 4);
-      factor = pow2(e) * 16777216.f * P.scale_log2;
+      // The largest value of all rows goes to [2^8, 2^9) (as far as the exponent allows: a factor and its inverse are normal numbers), or, where
+      // the quarters of rows that the lanes hold lie far apart, each row's own.
+      auto exponent = [](uint32_t largest) { return max(-100, min(100, (int)(largest >> 7) - 127 - 8)); };
+      int e_most = -100, e_least = 100;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt) {
+        e_most = max(e_most, exponent(top[nt]));
+        if (top[nt]) e_least = min(e_least, exponent(top[nt]));
+      }
+      e_most = __reduce_max_sync(0xffffffffu, e_most);
+      const bool far = __reduce_min_sync(0xffffffffu, e_least) + kNear < e_most;
+      factor = pow2(e_most) * 16777216.f * P.scale_log2;
+      if (far) lim = -1;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        int e = e_most;
+        if (far) {
+          uint32_t row = max(top[nt], __shfl_xor_sync(0xffffffffu, top[nt], 1));
+          row = max(row, __shfl_xor_sync(0xffffffffu, row, 2));
+          e = max(exponent(row), e_most - 126);
+        }
+        if (t == 0) below(nt, g) = pow2(e - e_most);
+        const float down = pow2(-e), down16 = pow2(-e - 4);
 #pragma unroll
         for (int k = 0; k < NW; ++k) {
           const uint4 v = raw[nt][k];
@@ -272,6 +299,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
           qf[nt][2 * k + 1][0] = pack_f16(__uint_as_float(v.z << 16) * down, __uint_as_float(v.z & 0xffff0000u) * down);
           qf[nt][2 * k + 1][1] = pack_f16(__uint_as_float(v.w << 16) * down16, __uint_as_float(v.w & 0xffff0000u) * down16);
         }
+      }
     }
     {
       float o[NT][D / 16][4];              // O^T: rows (values) i, columns 2 t and 2 t + 1; see the writer for which values
@@ -279,21 +307,27 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
-      // per row (columns 2 t, 2 t + 1; the same in all lanes of a column): reference maximum in powers of two; this lane's part of the
-      // sum of probabilities and of sum p m
+      // per row (columns 2 t, 2 t + 1; the same in all lanes of a column): reference maximum in powers of two, less kLift; this lane's
+      // part of the sum of probabilities and of sum p m
       float ref[NT][2], l[NT][2], om[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         ref[nt][0] = ref[nt][1] = kNoRef;
         l[nt][0] = l[nt][1] = om[nt][0] = om[nt][1] = 0.f;
       }
-      float s_top = 0.f, s_inv = 0.f;      // steps of V are below s_top (a power of two), and P holds p s_V 2^7 / s_top
+      // Per row: the steps of V that it has seen are below s_top (a power of two), and P holds p s_V 2^7 / s_top.  They are the same for all
+      // rows as long as all rows see everything; what a row does not see may be larger than what it does by more than fp16 holds.
+      // s_least: the least of this lane's
+      float s_top[NT][2], s_least = 0.f;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) s_top[nt][0] = s_top[nt][1] = 0.f;
 
       for (int p = sh.page; p < sh.end; p += sh.warps * PG) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 1) : "memory");
         __syncwarp();
         const uint8_t* pg = ring + slot_at;
         const int pos0 = p * kPageSize;
+        // Without MASK: every row sees everything, rows of Q stand on one scale and scores are not large (returns whether they turn out to be)
         auto work = [&](auto masked) {
           constexpr bool MASK = decltype(masked)::value;
           // ---- S^T = C_K Q^T: rows g and g + 8 of product i are tokens of page i ----
@@ -321,6 +355,19 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
                     mma_f16(sc[i][nt], w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u, qf[nt][2 * j + u][0], qf[nt][2 * j + u][1]);
                 }
           }
+          if (MASK && lim < 0) {               // (rows on scales of their own, or large scores)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const float by = below(nt, 2 * t + c);
+#pragma unroll
+                for (int i = 0; i < PG; ++i) {
+                  sc[i][nt][c] *= by;
+                  sc[i][nt][2 + c] *= by;
+                }
+              }
+          }
           // (token x = 2 i + h of this lane is token g + 8 h of page i)
           float sk[2 * PG], mk[2 * PG], sv[2 * PG], mv[2 * PG];
           float sv_top = 0.f;
@@ -340,6 +387,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
             const int pos = pos0 + 16 * (x >> 1) + 8 * (x & 1) + g;
             return !MASK || pos <= climit[nt][c] || (pos >= vlo[nt][c] && pos < vhi[nt][c]);
           };
+          // Score, and its distance from the reference.  Scores below kLarge: the reference joins the sum, whose terms are rounded as
+          // coarsely as it is; beyond, it is subtracted from the rounded score whose maximum it was.
+          auto score = [&](int x, int nt, int c) {
+            return fmaf(sc[x >> 1][nt][2 * (x & 1) + c], sk[x], __fmul_rn(mk[x], qs[nt][c]));
+          };
           float pr[PG][NT][4];
           auto scores = [&]() {
             float top = -INFINITY;
@@ -350,31 +402,48 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   const int x = 2 * i + (e >> 1);
-                  float y = fmaf(sc[i][nt][e], sk[x], fmaf(mk[x], qs[nt][e & 1], kLift - ref[nt][e & 1]));
-                  if (MASK && !sees(x, nt, e & 1)) y = -INFINITY;
+                  float y;
+                  if (MASK) y = sees(x, nt, e & 1) ? __fsub_rn(score(x, nt, e & 1), ref[nt][e & 1]) : -INFINITY;
+                  else y = fmaf(sc[i][nt][e], sk[x], fmaf(mk[x], qs[nt][e & 1], -ref[nt][e & 1]));
                   pr[i][nt][e] = y;
                   top = fmaxf(top, y);
                 }
             return top;
           };
-          if (__any_sync(0xffffffffu, scores() > kHeadroom + kLift || sv_top >= s_top)) {
-            // some row's reference maximum moves, or the scale of the steps does: what has been summed up is scaled to the new ones
-            const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(sv_top));      // (NaN does not take part)
-            const float next_top = fmaxf(s_top, pow2(max(-100, (int)(top >> 23) - 127 + 1)));
-            const float fs = s_top / next_top;
-            s_top = next_top;
-            s_inv = 1.f / next_top;
+          if (__any_sync(0xffffffffu, scores() > kHeadroom + kLift || sv_top >= s_least)) {
+            // some row's reference maximum moves, or its scale of the steps does: what has been summed up is scaled to the new ones
+            float z[NT][2], step[NT][2], large = 0.f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int c = 0; c < 2; ++c) {
-                float z = -INFINITY;
+                z[nt][c] = -INFINITY;
+                step[nt][c] = 0.f;
 #pragma unroll
                 for (int x = 0; x < 2 * PG; ++x)
-                  if (sees(x, nt, c)) z = fmaxf(z, fmaf(sc[x >> 1][nt][2 * (x & 1) + c], sk[x], mk[x] * qs[nt][c]));
+                  if (sees(x, nt, c)) {
+                    z[nt][c] = fmaxf(z[nt][c], score(x, nt, c));
+                    if (MASK) step[nt][c] = fmaxf(step[nt][c], sv[x]);      // (NaN does not take part)
+                  }
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, x));
-                const float next = z > ref[nt][c] + kHeadroom || ref[nt][c] == kNoRef ? fmaxf(ref[nt][c], z) : ref[nt][c];
+                for (int x = 4; x < 32; x <<= 1) {
+                  z[nt][c] = fmaxf(z[nt][c], __shfl_xor_sync(0xffffffffu, z[nt][c], x));
+                  if (MASK) step[nt][c] = fmaxf(step[nt][c], __shfl_xor_sync(0xffffffffu, step[nt][c], x));
+                }
+                if (!MASK) large = fmaxf(large, fabsf(z[nt][c]));
+              }
+            const float step_all = MASK ? 0.f : __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv_top)));
+            s_least = INFINITY;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const float next_top = fmaxf(s_top[nt][c], pow2(max(-100, (int)(__float_as_uint(MASK ? step[nt][c] : step_all) >> 23) - 127 + 1)));
+                const float fs = s_top[nt][c] * inverse(next_top);
+                s_top[nt][c] = next_top;
+                s_least = fminf(s_least, next_top);
+                const float to = z[nt][c] - kLift;
+                const float next = to > ref[nt][c] + kHeadroom || ref[nt][c] == kNoRef ? fmaxf(ref[nt][c], to) : ref[nt][c];
                 const float f = exp2f(ref[nt][c] - next);
                 ref[nt][c] = next;
                 l[nt][c] *= f;
@@ -386,6 +455,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
                 }
               }
             scores();
+            if (!MASK && __any_sync(0xffffffffu, large >= kLarge)) return true;
           }
           // ---- probabilities; O^T += C_V^T (P s_V)^T ----
           uint32_t b[PG][NT][2];
@@ -399,7 +469,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
                 const int x = 2 * i + (e >> 1);
                 const float p_ = exp2f(pr[i][nt][e]);
                 l[nt][e & 1] += p_;
-                ps[e] = p_ * (sv[x] * s_inv);
+                ps[e] = p_ * (sv[x] * inverse(MASK ? s_top[nt][e & 1] : s_top[0][0]));
                 float pm = p_ * mv[x];
                 if (MASK && !sees(x, nt, e & 1)) ps[e] = pm = 0.f;
                 om[nt][e & 1] += pm;
@@ -422,9 +492,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
                   mma_f16(o[nt][2 * j + u], w0 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x000f000fu, w1 & 0x00f000f0u, b[i][nt][0], b[i][nt][1]);
               }
           }
+          return false;
         };
+        if (pos0 + PG * kPageSize - 1 <= lim && work(std::false_type{})) lim = -1;      // (to the end of the item)
         if (pos0 + PG * kPageSize - 1 > lim) work(std::true_type{});
-        else work(std::false_type{});
         __syncwarp();
         request(slot_at);
         slot_at = slot_at == (kSlots - 1) * kSlot ? 0 : slot_at + kSlot;
@@ -453,10 +524,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv4_kerne
               const float (&e)[4] = o[nt][4 * x + u];          // word 2 x: even values
               const float (&f)[4] = o[nt][4 * x + 2 + u];      // word 2 x + 1: odd values
               *reinterpret_cast<float4*>(row + g * (D / 8) + 8 * x + 4 * u) =
-                  make_float4(fmaf(e[c] * k1, s_top, ms), fmaf(f[c] * k1, s_top, ms), fmaf(e[2 + c] * k16, s_top, ms), fmaf(f[2 + c] * k16, s_top, ms));
+                  make_float4(fmaf(e[c] * k1, s_top[nt][c], ms), fmaf(f[c] * k1, s_top[nt][c], ms), fmaf(e[2 + c] * k16, s_top[nt][c], ms),
+                              fmaf(f[2 + c] * k16, s_top[nt][c], ms));
             }
           if (g == 0) {
-            row[D] = ref[nt][c] - kLift;
+            row[D] = ref[nt][c];
             row[D + 1] = ls;
           }
         }

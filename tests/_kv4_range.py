@@ -10,10 +10,12 @@ many rows  (the tcgen05 kernel)
     K     s (c - 8), of a rounded s, and the second term of m + 8 s: (8 + 1 + 1) 2^-25 2^e a value (of sum |q|)
     Q     2^-25 2^e a value (of sum |s (c - 8)|), and 2^-25 2^e for the second term of its sum (of |m + 8 s|)
 few rows, and gathered weights
-    Q     the largest of all rows of a warp (of a request) in [2^8, 2^9) 2^e, half of the values divided by 16 besides: 2^-21 2^e a value
-    P s   stands as 2^7 p s / s_top, s_top a power of two above the largest step so far, at most twice the largest: 2^-11 p s, and 2^-32 s_top
-The largest are those of all tokens and rows that the kernel has at hand, whether the row in question sees them or not; the bounds take all of
-the request's.
+    Q     a row's largest, or one at most 2^8 as large (gathered weights: the request's), in [2^8, 2^9) 2^e, half of the values divided by
+          16 besides: 2^-21 2^e a value
+    P s   stands as 2^7 p s / s_top, s_top a power of two above the largest step that the row has seen so far, at most twice the largest:
+          2^-11 p s, and 2^-32 s_top
+The largest of many rows are those of all tokens that the kernel has at hand, whether the row in question sees them or not; the bounds take
+all of the request's.
 
 Everything else is fp32: a score's sum takes eight or nine steps in an accumulator that drops what is below 2^-22 of its largest term (2^-19
 of the terms' sum, which is taken with c - 8 by many rows and with c by few), 2^x and its argument are good to 2^-21, sums over tokens to 2^-17."""
@@ -34,7 +36,8 @@ def of_32(per_token):
 
 
 def score_bounds(q, ck, sk, mk, many, top_q):
-    """|error| of every score in nats, [n, L].  q [n, d] of a head; ck [L, d], sk and mk [L] of its kv head; top_q: largest |q| of the request."""
+    """|error| of every score in nats, [n, L].  q [n, d] of a head; ck [L, d], sk and mk [L] of its kv head; top_q: largest |q| on whose scale a
+    row stands (few rows), [n] or one for all."""
     d = q.shape[1]
     aq = np.abs(q)
     if many:
@@ -45,7 +48,7 @@ def score_bounds(q, ck, sk, mk, many, top_q):
     else:
         sc = sk[:, None] * ck
         size = aq @ sc.T + np.abs(q.sum(-1))[:, None] * np.abs(mk)[None]
-        lost = 2.0 ** -29 * 2.0 ** np.floor(np.log2(top_q)) * sc.sum(-1)[None]
+        lost = 2.0 ** -29 * 2.0 ** np.floor(np.log2(np.reshape(top_q, (-1, 1)))) * sc.sum(-1)[None]
     return (size * 2.0 ** -19 + lost) / np.sqrt(d) + 2.0 ** -21
 
 
@@ -65,7 +68,11 @@ def attention(q, k_codes, v_codes, see, many):
         p /= total
         x = m_v[:, None] + s_v[:, None] * cv[:, kh]
         o[:, h], lse[:, h] = p @ x, (top + np.log(total))[:, 0]
-        pd = p * np.where(see, score_bounds(q[:, h], ck[:, kh], s_k, m_k, many, np.abs(q).max()), 0.0)
+        off = np.where(see, score_bounds(q[:, h], ck[:, kh], s_k, m_k, many, np.minimum(np.abs(q).max(), 2.0 ** 8 * np.abs(q[:, h]).max(-1))), 0.0)
+        pd = p * off
+        # (where the largest score is ahead of all others by more than any two can be off, its position is all of the result)
+        second = np.sort(z, -1)[:, -2] if z.shape[1] > 1 else np.full(n, -np.inf)
+        pd_o = np.where((top[:, 0] - second > 2 * off.max(-1) + 30)[:, None], 0.0, pd)
         coded, held, low = p @ (s_v[:, None] * cv[:, kh]), p @ np.abs(x), p @ np.abs(m_v)[:, None]
         if many:
             ev = scale_exp(of_32(np.maximum(np.abs(m_v), np.abs(m_v + 15 * s_v))))
@@ -73,9 +80,9 @@ def attention(q, k_codes, v_codes, see, many):
             lost = np.sqrt(2) / total * (np.where(see, 2.0 ** -32 * 2.0 ** (ev.max() - ev), 0.0) @ np.abs(x)) + 17 * 2.0 ** -25 * p @ (2.0 ** ev)[:, None]
             rounded = 2 * 2.0 ** -11 * held
         else:
-            lost = see.sum(-1, keepdims=True) / total * 15 * 2.0 ** -32 * 2 * s_v.max()
+            lost = see.sum(-1, keepdims=True) / total * 15 * 2.0 ** -32 * 2 * np.where(see, s_v, 0.0).max(-1, keepdims=True)
             rounded = 2.0 ** -11 * coded
-        o_err[:, h] = rounded + lost + 2.0 ** -17 * (coded + low) + 1.1 * (pd @ np.abs(x) + np.abs(o[:, h]) * pd.sum(-1, keepdims=True))
+        o_err[:, h] = rounded + lost + 2.0 ** -17 * (coded + low) + 1.1 * (pd_o @ np.abs(x) + np.abs(o[:, h]) * pd_o.sum(-1, keepdims=True))
         lse_err[:, h] = 1.1 * pd.sum(-1) + 2.0 ** -20 * (1 + np.abs(top[:, 0]) + np.log(see.shape[1]))
     return o, lse, o_err, lse_err
 

@@ -40,7 +40,7 @@ def times(x, e, dim=0):
     return (x.double() * torch.from_numpy(2.0 ** np.asarray(e, dtype=np.float64)).view(shape)).bfloat16()
 
 
-def run(path, seed, k_of, v_of, q_of, corr=None, layer=1):
+def run(path, seed, k_of, v_of, q_of, corr=None, layer=1, weights=True):
     """k_of, v_of(r, x [L + n, nkv, d]) and q_of(q [T, nq, d]) change the inputs.  Returns the outputs' distances over their bounds."""
     (nq, nkv, d), reqs, flags, many = PATHS[path]
     L, v, b = (list(x) for x in zip(*reqs))
@@ -62,7 +62,8 @@ def run(path, seed, k_of, v_of, q_of, corr=None, layer=1):
     o, lse = torch.empty((T, nq, d), dtype=torch.bfloat16, device="cuda"), torch.empty((T, nq), device="cuda")
     ctx.recg_attention(batch, layer, q.cuda(), o, lse)
     w = torch.zeros((2, desc.n_pages, nkv, 16), device="cuda")
-    ctx.recg_kv_weights(None, layer, q.cuda(), lse, None, w)
+    if weights:
+        ctx.recg_kv_weights(None, layer, q.cuda(), lse, None, w)
     ctx.recg_sync()
     w = f64(w)
     t, worst = 0, [0.0, 0.0, 0.0]
@@ -73,7 +74,7 @@ def run(path, seed, k_of, v_of, q_of, corr=None, layer=1):
         kc, vc = _kv4.codes(ks[r]), _kv4.codes(vs[r])
         want, want_lse, o_err, lse_err = _kv4_range.attention(qr, kc, vc, see, many)
         pos = np.arange(L[r] + n)
-        gw, gw_err = _kv4_range.gathered(qr, kc, see, got_lse, np.ones(n))
+        gw, gw_err = _kv4_range.gathered(qr, kc, see, got_lse, np.ones(n)) if weights else (np.zeros((nkv, len(pos))),) * 2
         got_w = w[layer, desc.page_table[r][pos // 16], :, pos % 16].T
         over = (np.abs(got - want) / (o_err + 2.0 ** -8 * (np.abs(want) + o_err)), np.abs(got_lse - want_lse) / lse_err,
                 np.abs(got_w - gw) / (gw_err + 2.0 ** -22 * gw + 1e-30))
@@ -119,6 +120,17 @@ def test_queries(path):
     run(path, 7, lambda r, k: times(k, exponents("scattered", len(k), 3)), lambda r, v: times(v, exponents("by 32", len(v), 8)), scaled)
 
 
+@pytest.mark.parametrize("path,gap", [(p, g) for p in PATHS for g in (12, 24, 60) if g < 60 or not PATHS[p][3]])
+def test_queries_next_to_enormous_ones(path, gap):
+    """Every third row and every second head is 2^gap times as large, whose attention is one position (of many rows up to the scores of which
+    the attention over a bf16 pool makes sense too: it has them relative to a reference rounded as coarsely as they are)."""
+    def scaled(q):
+        large = (np.arange(len(q)) % 3 == 1)[:, None] | (np.arange(q.shape[1]) % 2 == 1)[None]
+        return (q.double() * torch.from_numpy(np.where(large, 2.0 ** gap, 1.0))[:, :, None]).bfloat16()
+
+    run(path, 10, lambda r, k: k, lambda r, v: v, scaled, weights=False)
+
+
 @pytest.mark.parametrize("gap", [8, 12])
 @pytest.mark.parametrize("path", PATHS)
 def test_large_values_that_hardly_count(path, gap):
@@ -139,8 +151,8 @@ def test_large_values_that_hardly_count(path, gap):
     run(path, 8, keys, lambda r, v: times(v, np.where(far(len(v)), gap, 0)), queries)
 
 
-@pytest.mark.parametrize("gap", [8, 12])
-@pytest.mark.parametrize("path", ["many rows", "row groups", "head_dim 64, row groups"])
+@pytest.mark.parametrize("path,gap", [(p, g) for p in ("many rows", "row groups", "head_dim 64, row groups") for g in (8, 12, 30, 100)
+                                      if p != "many rows" or g < 30])
 def test_large_values_that_others_see(path, gap):
     """The rows of a branch hold V of 2^gap and K of 2^3, which the rows outside of it do not see."""
     L, v, b = PATHS[path][1][0]
