@@ -8,12 +8,13 @@
 // Bound by the bytes of K as long as rows are few.  The pages of all requests and heads are one line, of which every CTA takes an
 // equal piece.  The rows that count (weight not zero) of as many (request, head) pairs of the piece as fit are staged in shared memory
 // together, and the warps stream the pairs' pages past them in one go, each into a ring of its own, 16 bytes a lane.  (Pair by pair, each
-// with its staging and its barriers: sixteen decoding requests 25.5 us, a serving batch on a bf16 pool 57.8; now 19.0 and 47.2.  One CTA per 128
+// with its staging and its barriers: sixteen decoding requests 25.5 us, a serving batch on a bf16 pool 57.8; now 18.9 and 47.1.  One CTA per 128
 // tokens, with its own staging and K by plain loads: 41.5 and 140.)
 //
 // Operands.  A bf16 pool: its tiles are what ldmatrix takes.  A pool in 4 bits: a lane holds the values [D / 4 t, D / 4 (t + 1)) of two
-// tokens (t its number in the quad), the contraction index is permuted accordingly; codes as subnormal fp16 numbers, Q scaled by a power of
-// two, steps and minima in fp32 (attention_kv4.cu has the reasons).  Q is staged in the order in which a lane takes two k-steps at once.
+// tokens (t its number in the quad), the contraction index is permuted accordingly; codes as subnormal fp16 numbers, a row of Q scaled by a
+// power of two of its own, steps and minima in fp32 (attention_kv4.cu has the reasons).  Q is staged in the order in which a lane takes
+// two k-steps at once.
 #include <cuda_fp16.h>
 #include <type_traits>
 
@@ -95,7 +96,8 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
   constexpr int kWarps = SH::kWarps, kThreads = SH::kThreads;
   constexpr int NW = D / 32, kChunks = D / 8;           // 16-byte chunks a lane holds of a row; of a row
   extern __shared__ __align__(128) uint8_t smem[];
-  float4* s_info = reinterpret_cast<float4*>(smem + SH::kInfoOff);     // a staged row: sum of its values times the scale, -lse (powers of two), weight
+  // a staged row: sum of its values times the scale, -lse (powers of two), weight, what makes a product of codes a score
+  float4* s_info = reinterpret_cast<float4*>(smem + SH::kInfoOff);
   int4* s_vis = reinterpret_cast<int4*>(smem + SH::kVisOff);
   int2* s_src = reinterpret_cast<int2*>(smem + SH::kListOff);          // a staged row: its place in lse (-1: fills up an eight); row of the batch | segment << 20
   int* s_cost = reinterpret_cast<int*>(smem + SH::kTotal);             // [n_req] cost of a page and head of request r
@@ -104,7 +106,6 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
   // segments, (request, head) pairs whose rows are staged together
   __shared__ int s_req[kWarps], s_head[kWarps], s_page0[kWarps], s_pages[kWarps], s_tok0[kWarps], s_new[kWarps], s_ctx[kWarps];
   __shared__ int s_cum[kWarps], s_row0[kWarps], s_rows8[kWarps], s_count[kWarps], s_next[kWarps], s_lim[kWarps];
-  __shared__ unsigned s_top[kWarps];
   __shared__ long long s_ahead[kWarps];                                // cost in front of what follows the segment
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   griddep_wait();
@@ -197,7 +198,6 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
         s_ahead[lane] = upto;
         s_count[lane] = hi > lo ? n_new : 0;
         s_lim[lane] = 0x7fffffff;
-        s_top[lane] = 0;
       }
     }
     __syncthreads();
@@ -318,46 +318,50 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
           if (at >= 0) raw[k] = __ldg(reinterpret_cast<const uint4*>(P.q + (size_t)at * D) + c);
         }
       }
-      if (FOUR)
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-          // (the rows of a warp are neighbours within eight, hence of one segment)
-          const int row = (tid + k * kThreads) / kChunks;
-          if (__all_sync(0xffffffffu, row >= staged)) break;
-          unsigned top = 0;
-          const uint32_t u[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const unsigned lo = u[x] & 0x7fffu, hi = (u[x] >> 16) & 0x7fffu;
-            top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-          }
-          top = __reduce_max_sync(0xffffffffu, top);
-          if (lane == 0) atomicMax(&s_top[s_src[row].y >> 20], top);
-        }
       for (int row = tid; row < staged; row += kThreads) {
         const int2 from = s_src[row];
-        float4 info = make_float4(0.f, -1e30f, 0.f, 0.f);         // (a row that fills up the last eight: probability 0)
+        float minus_lse = -1e30f, weight = 0.f;                   // (a row that fills up the last eight: probability 0)
         int4 vis = make_int4(-1, 0, 0, 0);
         if (from.x >= 0) {
           const int tok = from.y & 0xfffff;
-          info.y = -1.4426950408889634f * P.lse[from.x];
-          info.z = P.row_weight ? P.row_weight[tok] : 1.f;
+          minus_lse = -1.4426950408889634f * P.lse[from.x];
+          weight = P.row_weight ? P.row_weight[tok] : 1.f;
           vis = make_int4(P.tok_climit[tok], P.tok_lo[tok], P.tok_hi[tok], 0);
           atomicMin(&s_lim[from.y >> 20], vis.x);
         }
-        *reinterpret_cast<float3*>(&s_info[row].y) = make_float3(info.y, info.z, info.w);
+        s_info[row].y = minus_lse;
+        s_info[row].z = weight;
         s_vis[row] = vis;
       }
-      __syncthreads();
-      auto scale_of = [&](int k) { return FOUR ? max(-100, min(100, (int)(s_top[k] >> 7) - 127 - 8)) : 0; };       // the largest value to [2^8, 2^9)
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
         const int i = tid + k * kThreads, row = i / kChunks, c = i % kChunks;
         if (row >= staged) continue;
         const uint4 v = raw[k];
         uint8_t* at = smem + SH::kRowsOff + row * SH::kRowBytes;
+        // (staged * kChunks is a multiple of 64 and kThreads of kChunks: whole quarter and half warps come here together)
+        const unsigned together = (kChunks == 16 ? 0xffffu : 0xffu) << (lane & ~(kChunks - 1));
         if (FOUR) {
-          const int e = scale_of(s_src[row].y >> 20);
+          // the row's largest value goes to [2^8, 2^9) (as far as the exponent allows)
+          const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+          float sum = 0.f;
+          unsigned top = 0;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            sum += __uint_as_float(u[x] << 16) + __uint_as_float(u[x] & 0xffff0000u);
+            const unsigned lo = u[x] & 0x7fffu, hi = (u[x] >> 16) & 0x7fffu;
+            top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+          }
+#pragma unroll
+          for (int o = kChunks / 2; o; o >>= 1) {
+            sum += __shfl_xor_sync(together, sum, o);
+            top = max(top, __shfl_xor_sync(together, top, o));
+          }
+          const int e = max(-100, min(100, (int)(top >> 7) - 127 - 8));
+          if (c == 0) {
+            s_info[row].x = sum * P.scale_log2;
+            s_info[row].w = pow2(e) * 16777216.f * P.scale_log2;
+          }
           const float down = pow2(-e), down16 = pow2(-e - 4);
           // where lane c / NW of a quad looks for its word c % NW
           *reinterpret_cast<uint4*>(at + ((c % NW) * 4 + c / NW) * 16) =
@@ -370,26 +374,12 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
           to[8] = v.z;
           to[12] = v.w;
         }
-        if (FOUR) {
-          const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-          float sum = 0.f;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) sum += __uint_as_float(u[x] << 16) + __uint_as_float(u[x] & 0xffff0000u);
-          // (staged * kChunks is a multiple of 64 and kThreads of kChunks: whole quarter and half warps come here together)
-          const unsigned together = (kChunks == 16 ? 0xffffu : 0xffu) << (lane & ~(kChunks - 1));
-#pragma unroll
-          for (int o = kChunks / 2; o; o >>= 1) sum += __shfl_xor_sync(together, sum, o);
-          if (c == 0) s_info[row].x = sum * P.scale_log2;
-        } else if (c == 0) {
-          s_info[row].x = 0.f;
-        }
       }
       __syncthreads();
 
       // ---- pages past the rows ----
       uint32_t slot_at = 0;
       int seg_end = 0, to_page = 0, L = 0, kv_len = 0, h = 0, lim = 0, rows8 = 0;
-      float factor = 0.f;
       const uint8_t* rows_at = smem + SH::kRowsOff;      // of the segment
       const float4* info_at = s_info;
       const int4* vis_at = s_vis;
@@ -403,7 +393,6 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
           h = s_head[k];
           lim = s_lim[k];
           rows8 = s_rows8[k];
-          factor = FOUR ? pow2(scale_of(k)) * 16777216.f * P.scale_log2 : P.scale_log2;
           rows_at = smem + SH::kRowsOff + seg_row0 * SH::kRowBytes;
           info_at = s_info + seg_row0;
           vis_at = s_vis + seg_row0;
@@ -419,7 +408,7 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
         float before = 0.f;
         if (old && stores && (chunk || pos0 + tok < L)) before = keep * reinterpret_cast<const float*>(pg + SH::kWeights)[tok];
         uint32_t a[D / 16][4];
-        float sk[2] = {factor, factor}, mk[2] = {0.f, 0.f};
+        float sk[2] = {P.scale_log2, P.scale_log2}, mk[2] = {0.f, 0.f};
 #pragma unroll
         for (int e2 = 0; e2 < 2; ++e2) {
           const int tk = g + 8 * e2;
@@ -433,7 +422,7 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
               word[0] = v.x; word[1] = v.y;
             }
             const uint32_t pair = *reinterpret_cast<const uint32_t*>(pg + SH::kCodes + 4 * tk);
-            sk[e2] = kv4_step(pair) * factor;
+            sk[e2] = kv4_step(pair);
             mk[e2] = kv4_min(pair);
 #pragma unroll
             for (int j = 0; j < NW; ++j)
@@ -481,7 +470,7 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
             for (int x = 0; x < 4; ++x) {
               const float4& ri = (x & 1) ? i1 : i0;
               const float shift = FOUR ? fmaf(mk[x >> 1], ri.x, ri.y) : ri.y;
-              const float p_ = exp2f(fmaf(sc[0][x] + sc[1][x], sk[x >> 1], shift));
+              const float p_ = exp2f(fmaf(sc[0][x] + sc[1][x], FOUR ? sk[x >> 1] * ri.w : sk[x >> 1], shift));
               if (MASK) {
                 const int4& vi = (x & 1) ? v1 : v0;
                 const int pos = pos0 + g + 8 * (x >> 1);
@@ -505,10 +494,7 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
       const bool more = first_tok < s_new[0] && !whole;
       __syncthreads();                                   // the staged rows may be replaced
       if (!more) break;
-      if (tid == 0) {
-        s_lim[0] = 0x7fffffff;
-        s_top[0] = 0;
-      }
+      if (tid == 0) s_lim[0] = 0x7fffffff;
     }
     pair += nseg;
     ahead = s_ahead[nseg - 1];

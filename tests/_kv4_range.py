@@ -10,8 +10,8 @@ many rows  (the tcgen05 kernel)
     K     s (c - 8), of a rounded s, and the second term of m + 8 s: (8 + 1 + 1) 2^-25 2^e a value (of sum |q|)
     Q     2^-25 2^e a value (of sum |s (c - 8)|), and 2^-25 2^e for the second term of its sum (of |m + 8 s|)
 few rows, and gathered weights
-    Q     a row's largest, or one at most 2^8 as large (gathered weights: the request's), in [2^8, 2^9) 2^e, half of the values divided by
-          16 besides: 2^-21 2^e a value
+    Q     a row's largest, or (few rows) one at most 2^8 as large, in [2^8, 2^9) 2^e, half of the values divided by 16 besides: 2^-21 2^e
+          a value
     P s   stands as 2^7 p s / s_top, s_top a power of two above the largest step that the row has seen so far, at most twice the largest:
           2^-11 p s, and 2^-32 s_top
 The largest of many rows are those of all tokens that the kernel has at hand, whether the row in question sees them or not; the bounds take
@@ -97,8 +97,8 @@ def gathered(q, k_codes, see, lse, row_weight):
     for h in range(nq):
         kh = h // g
         z = q[:, h] @ (mk[:, kh] + sk[:, kh] * ck[:, kh]).T / np.sqrt(d)
-        off = score_bounds(q[:, h], ck[:, kh], sk[:, kh, 0], mk[:, kh, 0], False, np.abs(q).max()) + 2.0 ** -20 * (1 + np.abs(z) + np.abs(lse[:, h:h + 1]))
-        p = np.where(see, np.exp(z - lse[:, h:h + 1]) * row_weight[:, None], 0.0)
+        off = score_bounds(q[:, h], ck[:, kh], sk[:, kh, 0], mk[:, kh, 0], False, np.abs(q[:, h]).max(-1)) + 2.0 ** -20 * (1 + np.abs(z) + np.abs(lse[:, h:h + 1]))
+        p = np.exp(np.where(see, z - lse[:, h:h + 1], -np.inf)) * row_weight[:, None]
         out[kh] += p.sum(0)
         err[kh] += (p * (1.1 * np.where(see, off, 0.0) + n * g * 2.0 ** -23)).sum(0)
     return out, err
