@@ -9,10 +9,12 @@
 // bandwidth than all operands: 325 us instead of 192 us for 1001 rows over 6000 tokens of 40 / 8 heads.)  V stands as m + s c
 // rounded once, and P as fp16 too: 2^-11 of each term by either, a quarter of the rounding of the result together.
 //
-// Range.  fp16 has five bits of exponent, so everything is scaled by powers of two: a query row by its own largest value, K and V
-// of 32 tokens by theirs, in steps of 2^8.  The scale of a row of Q and of 32 tokens of K is one factor of the score.  The scale of V
-// joins the exponent of the probabilities, relative to the largest one so far (O is rescaled when that grows).  Values next to others
-// that are 2^25 times as large lose bits, as in any fp32 sum of both.
+// Range.  fp16 has five bits of exponent, so everything is scaled by powers of two, in steps of 2^8: a query row by its own largest
+// value, K and V of 32 tokens by theirs, or, where tokens lie 2^16 apart, each by its own (a row may see one and not the other).  The
+// scale of a row of Q and of 32 tokens of K is one factor of the score, that of a single token is applied to it.  The scale of V joins
+// the exponent of the probabilities, relative to the largest one that the row has seen (its O is rescaled when that grows); that of
+// a single token is applied to P.  So K and V lose at most what is 2^-20 of the largest of their 32 tokens where none lies below 2^-16 of
+// it, and P what is 2^-31 of the reference, 2^(e - e_j) times as much for a token whose V is on a scale 2^(e - e_j) below the row's.
 //
 // Per CTA (20 warps = 5 warpgroups, one CTA per SM, persistent over the work list), stages of 128 tokens:
 //   warp 0     streams the blocks of the pool (codes and pairs of a page and head: one bulk copy) into a ring of two raw stages, and
@@ -51,6 +53,7 @@ constexpr uint32_t kSpin = 1u << 22;             // polls of a wait
 constexpr int kTmemCols = 512;                   // two S buffers of 128 columns; O of group g at 256 + 128 g
 constexpr int kTmemO = 2 * kBT;
 constexpr float kNoRef = -1e30f;       // reference maximum of a row that has seen no token yet
+constexpr int kNoScale = -1000;        // scale of its O
 constexpr float kHeadroom = 8.f;       // a row's reference maximum moves when it is outgrown by more than 2^8
 constexpr float kLift = 7.f;           // probabilities stand as 2^7 p: at most 2^15, and 2^-31 of the reference is not lost yet
 
@@ -63,8 +66,11 @@ constexpr int kOffRaw = kOffKExt + kRing * kExt;
 constexpr int kOffScratch = kOffRaw + kRaw * kRawBytes;            // 2 KB per softmax warp: partial rows on their way out
 constexpr int kOffML = kOffScratch + 8 * 2048;                     // per row, both groups: reference; sum; scale of O
 constexpr int kOffQF = kOffML + 3 * 2 * 128 * 4;                   // per row: the factor of its scores
-constexpr int kOffInfo = kOffQF + 128 * 4;                         // TokenInfo [kInfo][4]
-constexpr int kOffBar = kOffInfo + kInfo * 4 * 16;
+constexpr int kOffInfo = kOffQF + 128 * 4;                         // [kInfo][4] of 32 tokens: K stands scaled by 1 / x, V by 2^-y; z: those whose V
+                                                                   // is not finite (it stands as zero, a row that sees one is NaN); w: 1, 2 where
+                                                                   // K, V of every token stand on a scale of their own (x is 1, y the largest)
+constexpr int kOffExp = kOffInfo + kInfo * 4 * 16;                 // [kInfo][128] those scales: two signed bytes
+constexpr int kOffBar = kOffExp + kInfo * 128 * 2;
 constexpr int kNumBars = 2 * kRaw + 4 * kRing + 3 + 2 + 4 + 3;
 constexpr int kSmemBytes = kOffBar + kNumBars * 8 + 16;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
@@ -114,22 +120,27 @@ __device__ __forceinline__ bool wait_asleep(uint64_t* bar, uint32_t parity) {
   return false;
 }
 
-struct TokenInfo {       // of 32 tokens
-  float k_scale;         // K stands scaled by 1 / k_scale
-  int v_exp;             // V stands scaled by 2^-v_exp
-  uint32_t v_bad;        // tokens whose V is not finite: it stands as zero, and a row that sees one of them is NaN
-  int pad;
-};
-
 // Multiples of eight E with 2^-E v in [1, 2^8) for the v whose exponent field is `field` (clamped where a factor 2^E or 2^-E would
 // not be a normal number, or products of two not)
 __device__ __forceinline__ int scale_exp(int field) { return max(-56, min(120, ((field - 127) >> 3) << 3)); }
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
-// the scale of V of the 32 tokens whose {step, minimum} a warp's lanes hold
-__device__ __forceinline__ int v_scale(uint32_t pair, bool* bad) {
+// The scales of 32 tokens, a token a lane, of which `top` is the largest value (0: nothing that has to be held).
+struct Scale {
+  int all, own;
+  bool loses;      // this token is two steps of 2^8 or more below the scale of all
+};
+__device__ __forceinline__ Scale token_scale(float top) {
+  Scale s;
+  const int field = __float_as_int(top) >> 23;
+  s.own = scale_exp(field);
+  s.all = scale_exp(__reduce_max_sync(0xffffffffu, field));
+  s.loses = top > 0.f && s.own + 8 < s.all;
+  return s;
+}
+// the largest value of V of a token with this {step, minimum}
+__device__ __forceinline__ float v_top(uint32_t pair, bool* bad) {
   *bad = (pair & 0x7f80u) == 0x7f80u;
-  const float top = *bad ? 0.f : fmaxf(fabsf(kv4_min(pair)), fabsf(fmaf(15.f, kv4_step(pair), kv4_min(pair))));
-  return scale_exp(__reduce_max_sync(0xffffffffu, __float_as_int(top) >> 23));
+  return *bad ? 0.f : fmaxf(fabsf(kv4_min(pair)), fabsf(fmaf(15.f, kv4_step(pair), kv4_min(pair))));
 }
 __device__ __forceinline__ uint32_t h2_bits(const __half2& h) { return reinterpret_cast<const uint32_t&>(h); }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { return h2_bits(__floats2half2_rn(lo, hi)); }
@@ -394,11 +405,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
         const uint32_t vp = there ? *reinterpret_cast<const uint32_t*>(pg + kv4_v_pairs(D) + 4 * (lane & 15)) : 0u;
         const float k_mid = fmaf(8.f, kv4_step(kp), kv4_min(kp));                       // m + 8 s
         const float k_top = (kp & 0x7f80u) == 0x7f80u ? 0.f : fmaxf(fabsf(k_mid), 8.f * kv4_step(kp));
-        const int ke = scale_exp(__reduce_max_sync(0xffffffffu, __float_as_int(k_top) >> 23));
-        const float ks = pow2(-ke);
         bool v_bad;
-        const int ve = v_scale(vp, &v_bad);
+        const Scale k_scale = token_scale(k_top), v_scale = token_scale(v_top(vp, &v_bad));
         const unsigned bad = __ballot_sync(0xffffffffu, v_bad);
+        int apart = 0;
+        if (__any_sync(0xffffffffu, k_scale.loses || v_scale.loses))
+          apart = (__any_sync(0xffffffffu, k_scale.loses) ? 1 : 0) | (__any_sync(0xffffffffu, v_scale.loses) ? 2 : 0);
+        const float ks = pow2(-((apart & 1) ? k_scale.own : k_scale.all));
         const float mid = k_mid * ks, hi = __half2float(__float2half_rn(mid));
         const uint32_t terms = pack_f16(hi, mid - hi);                                  // met by {a, a, b, b} of the row's sum a + b
         const uint32_t k_step = pack_f16(kv4_step(kp) * ks, kv4_step(kp) * ks);
@@ -406,7 +419,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
         // (A ring of four stages is enough: the S product of stage blk - 2, whose K stood here, was issued behind the P V products of
         // stage blk - 4, which had waited for every softmax warp.)
         if (lane == 0)
-          reinterpret_cast<int4*>(smem + kOffInfo)[(blk % kInfo) * 4 + wq] = make_int4(__float_as_int(pow2(ke)), ve, (int)bad, 0);
+          reinterpret_cast<int4*>(smem + kOffInfo)[(blk % kInfo) * 4 + wq] =
+              make_int4(__float_as_int((apart & 1) ? 1.f : pow2(k_scale.all)), v_scale.all, (int)bad, apart);
+        if (apart) reinterpret_cast<char2*>(smem + kOffExp)[(blk % kInfo) * 128 + 32 * wq + lane] = make_char2((char)k_scale.own, (char)v_scale.own);
         *reinterpret_cast<uint4*>(smem + kOffKExt + s * kExt + ext_row(32 * wq + lane)) = make_uint4(terms, terms, 0, 0);
         // unit: 16 bytes = values [32 q, 32 q + 32) of a token; atom (token group, q >> 1), chunks (q & 1) * 4 + word
         const int q = lane & 3, r = lane >> 2;
@@ -484,7 +499,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
         const bool there = tok_begin + n * kBT + 32 * wq + lane < tok_end;
         uint32_t vp = there ? *reinterpret_cast<const uint32_t*>(raw + (lane >> 4) * kBlock + kv4_v_pairs(D) + 4 * (lane & 15)) : 0u;
         bool v_bad;
-        const float vs = pow2(-v_scale(vp, &v_bad));
+        const Scale v_scale = token_scale(v_top(vp, &v_bad));
+        const float vs = pow2(-(__any_sync(0xffffffffu, v_scale.loses) ? v_scale.own : v_scale.all));
         if (v_bad) vp = 0;
         const uint32_t v_pair = pack_f16(kv4_step(vp) * vs, kv4_min(vp) * vs);
         lazy_wait(&v_empty[s], ((blk / kRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
@@ -541,10 +557,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
       const float qf = qf_smem[row];               // (a row that does not exist: whatever)
       __syncwarp();
       if (lane == 0) mbar_arrive(q_empty);
-      // Reference maximum (powers of two, a whole number: adding exponents to it is exact) and sum of the row; and the scale of O, which
-      // all of a group's rows share.
+      // Reference maximum (powers of two, a whole number: adding exponents to it is exact), sum and scale of O of the row.
       float m_ref = rvalid ? kNoRef : 0.f, l_run = 0.f;
-      int o_exp = -1000;
+      int o_exp = kNoScale;
 
       for (int n = 0; n < nblk; ++n, ++cs) {
         const uint32_t s_buf = s_addr + (cs & 1) * kBT;
@@ -560,8 +575,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
           for (int c = 0; c < 2; ++c) tmem_ld32_nowait(s_buf + c * 32, sr[c]);
           tmem_ld_wait();
           const int lim = min(climit, tok_end - 1);
-          const bool need_mask = __any_sync(0xffffffffu, rvalid && (pos0 + 63 > lim));
+          const int apart[2] = {i0.w, i1.w};
+          // words of two tokens: scales of K and V of the first, of K and V of the second
+          const uint32_t* scales = reinterpret_cast<const uint32_t*>(smem + kOffExp) + (cs % kInfo) * 64 + g * 32;
+          const bool need_mask = __any_sync(0xffffffffu, (rvalid && pos0 + 63 > lim) || (apart[0] | apart[1]));
           unsigned bad[2] = {(unsigned)i0.z, (unsigned)i1.z};
+          int ev[2] = {i0.y, i1.y};            // the largest scale of V among those of the 32 tokens that the row sees
           if (need_mask) {
             // visible tokens of this row within the 64: [0, a] and [b, c), as a 64-bit mask over tokens
             const int a = lim - pos0, b = vlo - pos0, cc = min(vhi, tok_end) - pos0;
@@ -569,6 +588,21 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
             const unsigned long long see = ones(a + 1) | (ones(cc) & ~ones(b));
             bad[0] &= (unsigned)see;
             bad[1] &= (unsigned)(see >> 32);
+            if ((unsigned)see == 0u) ev[0] = kNoScale;
+            if ((unsigned)(see >> 32) == 0u) ev[1] = kNoScale;
+            if (apart[0] | apart[1]) {
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                int most = kNoScale;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                  const int both = (int)(scales[c * 16 + (i >> 1)] << ((i & 1) ? 0 : 16)), k = (both << 8) >> 24, v = both >> 24;
+                  if (apart[c] & 1) sr[c][i] = __float_as_uint(__uint_as_float(sr[c][i]) * pow2(k));
+                  if ((see >> (c * 32 + i)) & 1ull) most = max(most, v);
+                }
+                if (apart[c] & 2) ev[c] = most;
+              }
+            }
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -589,14 +623,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
             const float z = fmaxf(__fmul_rn(fmaxf(mx[0][0], mx[0][1]), f[0]), __fmul_rn(fmaxf(mx[1][0], mx[1][1]), f[1]));
             if (m_ref == kNoRef && z > m_ref) m_ref = rintf(z);
           }
-          const int e_new = max(o_exp, max(i0.y, i1.y));
-          bool rescale = n > 0 && e_new != o_exp;
+          const int e_new = max(o_exp, max(ev[0], ev[1]));
+          const bool rescale = n > 0 && e_new != o_exp && o_exp != kNoScale;      // (without a scale it is zero)
           // (see attention_tc.cu: probabilities relative to the standing reference; a stage in which a row outgrows it is done again)
 #pragma unroll 1
           for (int pass = 0; pass < 2; ++pass) {
             float2 lsa[2][2] = {};
             float mxa[2][2];
-            const int lower[2] = {max(-64, i0.y - e_new), max(-64, i1.y - e_new)};     // (at -64 nothing of P is left)
+            const int lower[2] = {max(-64, ev[0] - e_new), max(-64, ev[1] - e_new)};     // (at -64 nothing of P is left)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               const float2 f2 = make_float2(f[c], f[c]);
@@ -639,6 +673,27 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv4_tc_kernel(const __g
               tmem_st16(o_addr + c * 16, r);
             }
             tmem_st_wait();
+          }
+          // the tokens' own scales of V, on P as it stands.  (This code and that for K in front of the masks is rarely run, and takes 6 us of
+          // 184 for 1001 rows over 6000 tokens of 40 / 8 heads by being there; inside of the loop it took 18.)
+          if ((apart[0] | apart[1]) & 2) {
+            tmem_st_wait();
+#pragma unroll 1
+            for (int c = 0; c < 2; ++c) {
+              if (!((c ? apart[1] : apart[0]) & 2)) continue;
+              const int most = c ? ev[1] : ev[0];
+              auto by = [&](int v) { return __int_as_float(max(127 + min(v - most, 0), 0) << 23); };      // (one that the row does not see: P is 0)
+              uint32_t pk[16];
+              tmem_ld16(s_buf + c * 16, pk);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int both = (int)scales[c * 16 + i];
+                const float2 p = __half22float2(reinterpret_cast<const __half2&>(pk[i]));
+                pk[i] = pack_f16(p.x * by((both << 16) >> 24), p.y * by(both >> 24));
+              }
+              tmem_st16(s_buf + c * 16, pk);
+            }
           }
           o_exp = e_new;
           if (bad[0] | bad[1]) l_run = __int_as_float(0x7fc00000);      // the row sees V that is not finite

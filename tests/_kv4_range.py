@@ -3,10 +3,11 @@ neighbours share.
 
 fp16 rounds by 2^-11 of a value down to 2^-14 and by 2^-25 below.  With x = m + s c for a row of K or V:
 many rows  (the tcgen05 kernel)
-    scales: K and V of 32 tokens 2^e, e a multiple of 8 that brings the largest |end of a row| (K: |m + 8 s| and 8 s) to [1, 2^8); a row of
-    Q likewise by itself; e is not below -56
+    scales: K and V of 32 tokens 2^e, e a multiple of 8 that brings the largest |end of a row| (K: |m + 8 s| and 8 s) to [1, 2^8), or, where
+    some token's own is lower by 16 or more, of every token its own; a row of Q likewise by itself; e is not below -56
     V     s, m and m + s c are rounded: 2^-11 |x|, and (15 + 1 + 1) 2^-25 2^e
-    P     stands as 2^7 p 2^(e_j - e), e the largest e_j up to there: 2^-11 p, and 2^-25 of it, which is 2^-32 2^(e - e_j) of p
+    P     stands as 2^7 p 2^(e_j - e), e the largest e_j that the row has seen: 2^-11 p, and 2^-25 of it, which is 2^-32 2^(e - e_j) of p
+          (twice where tokens have scales of their own: it is rounded before that is applied, and behind)
     K     s (c - 8), of a rounded s, and the second term of m + 8 s: (8 + 1 + 1) 2^-25 2^e a value (of sum |q|)
     Q     2^-25 2^e a value (of sum |s (c - 8)|), and 2^-25 2^e for the second term of its sum (of |m + 8 s|)
 few rows, and gathered weights
@@ -14,8 +15,6 @@ few rows, and gathered weights
           a value
     P s   stands as 2^7 p s / s_top, s_top a power of two above the largest step that the row has seen so far, at most twice the largest:
           2^-11 p s, and 2^-32 s_top
-The largest of many rows are those of all tokens that the kernel has at hand, whether the row in question sees them or not; the bounds take
-all of the request's.
 
 Everything else is fp32: a score's sum takes eight or nine steps in an accumulator that drops what is below 2^-22 of its largest term (2^-19
 of the terms' sum, which is taken with c - 8 by many rows and with c by few), 2^x and its argument are good to 2^-21, sums over tokens to 2^-17."""
@@ -28,11 +27,14 @@ def scale_exp(top):
     return np.clip(np.floor(e / 8) * 8, -56, 120)
 
 
-def of_32(per_token):
-    """The largest of every aligned group of 32 tokens, for each of its tokens.  per_token [L]."""
-    L = len(per_token)
-    pad = np.concatenate([per_token, np.zeros(-L % 32)])
-    return np.repeat(pad.reshape(-1, 32).max(-1), 32)[:L]
+def token_scales(top):
+    """The scale on which the kernel of many rows has every token, and whether it is the token's own.  top [L]: a token's largest value."""
+    L = len(top)
+    own = np.concatenate([scale_exp(top), np.full(-L % 32, -56.0)]).reshape(-1, 32)
+    held = np.concatenate([top > 0, np.zeros(-L % 32, dtype=bool)]).reshape(-1, 32)
+    most = own.max(-1, keepdims=True)
+    apart = (held & (own + 8 < most)).any(-1, keepdims=True)
+    return np.where(apart, own, most).reshape(-1)[:L], np.broadcast_to(apart, own.shape).reshape(-1)[:L]
 
 
 def score_bounds(q, ck, sk, mk, many, top_q):
@@ -43,7 +45,7 @@ def score_bounds(q, ck, sk, mk, many, top_q):
     if many:
         c8, mid = sk[:, None] * np.abs(ck - 8), np.abs(mk + 8 * sk)
         size = aq @ c8.T + np.abs(q.sum(-1))[:, None] * mid[None]
-        ek, eq = scale_exp(of_32(np.maximum(mid, 8 * sk))), scale_exp(aq.max(-1))
+        ek, eq = token_scales(np.maximum(mid, 8 * sk))[0], scale_exp(aq.max(-1))
         lost = 10 * 2.0 ** -25 * aq.sum(-1)[:, None] * 2.0 ** ek + 2.0 ** -25 * 2.0 ** eq[:, None] * (c8.sum(-1) + mid)[None]
     else:
         sc = sk[:, None] * ck
@@ -75,9 +77,10 @@ def attention(q, k_codes, v_codes, see, many):
         pd_o = np.where((top[:, 0] - second > 2 * off.max(-1) + 30)[:, None], 0.0, pd)
         coded, held, low = p @ (s_v[:, None] * cv[:, kh]), p @ np.abs(x), p @ np.abs(m_v)[:, None]
         if many:
-            ev = scale_exp(of_32(np.maximum(np.abs(m_v), np.abs(m_v + 15 * s_v))))
+            ev, apart = token_scales(np.maximum(np.abs(m_v), np.abs(m_v + 15 * s_v)))
+            seen = np.where(see, ev, -1000.0).max(-1, keepdims=True)
             # (a row's reference is a whole number next to its largest score so far: the sum is at least 2^-.5)
-            lost = np.sqrt(2) / total * (np.where(see, 2.0 ** -32 * 2.0 ** (ev.max() - ev), 0.0) @ np.abs(x)) + 17 * 2.0 ** -25 * p @ (2.0 ** ev)[:, None]
+            lost = np.sqrt(2) / total * (np.where(see, (1 + apart) * 2.0 ** -32 * 2.0 ** np.maximum(seen - ev, 0), 0.0) @ np.abs(x)) + 17 * 2.0 ** -25 * p @ (2.0 ** ev)[:, None]
             rounded = 2 * 2.0 ** -11 * held
         else:
             lost = see.sum(-1, keepdims=True) / total * 15 * 2.0 ** -32 * 2 * np.where(see, s_v, 0.0).max(-1, keepdims=True)

@@ -151,13 +151,24 @@ def test_large_values_that_hardly_count(path, gap):
     run(path, 8, keys, lambda r, v: times(v, np.where(far(len(v)), gap, 0)), queries)
 
 
-@pytest.mark.parametrize("path,gap", [(p, g) for p in ("many rows", "row groups", "head_dim 64, row groups") for g in (8, 12, 30, 100)
-                                      if p != "many rows" or g < 30])
-def test_large_values_that_others_see(path, gap):
-    """The rows of a branch hold V of 2^gap and K of 2^3, which the rows outside of it do not see."""
+@pytest.mark.parametrize("path,k_gap", [("many rows", 3), ("many rows", 20), ("row groups", 3), ("row groups", 100), ("head_dim 64, row groups", 3),
+                                        ("head_dim 64, row groups", 100)])
+@pytest.mark.parametrize("gap", [8, 12, 30, 100])
+def test_large_values_that_others_see(path, gap, k_gap):
+    """The rows of a branch hold V of 2^gap and K of 2^k_gap, which the rows outside of it do not see."""
     L, v, b = PATHS[path][1][0]
 
     def scaled(e):
         return lambda r, x: times(x, np.where((r == 0) & (np.arange(len(x)) >= L + v + b), e, 0))
 
-    run(path, 9, scaled(3), scaled(gap), lambda q: q, corr=[(2, 5), ()])
+    run(path, 9, scaled(k_gap), scaled(gap), lambda q: q, corr=[(2, 5), ()], weights=k_gap == 3)
+
+
+@pytest.mark.parametrize("before", [0, 5, 31])
+@pytest.mark.parametrize("path", ["many rows", "many rows, five heads", "row groups", "head_dim 64, row groups"])
+def test_rows_that_grow(path, before):
+    """The causal rows of a chunk hold V that grows by 2^4 and K that grows by 2 a position, to 2^100 and 2^20."""
+    def grown(by, most):
+        return lambda r, x: times(x, np.clip((np.arange(len(x)) - (PATHS[path][1][r][0] - before)) * by, 0, most))
+
+    run(path, 11, grown(1, 20), grown(4, 100), lambda q: q, weights=False)
