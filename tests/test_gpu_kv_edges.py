@@ -112,3 +112,41 @@ def test_in_place_lists_of_requests_that_are_not_cut(flags, head_dim):
         ctx.recg_sync()
     assert torch.equal(pool.view(torch.uint8), bytes_before)
     ctx.recg_free()
+
+
+@pytest.mark.parametrize("flags,far", [(0, 40000), (binding.FLAG_KV_4BIT, 150000)])
+def test_pages_behind_four_gigabytes(flags, far):
+    """The last pages of a pool of two layers that takes more than 2^32 bytes: what every operation gives for the first pages of a small one."""
+    nq, nkv, d, L, n = 32, 8, 128, 300, 3
+    got = []
+    for n_pages in (64, far):
+        ctx = make(2, flags, heads=(nq, nkv, d), stride=20, max_req=1, max_tokens=64)
+        assert n_pages == 64 or ctx.kv_pool_bytes(n_pages) > 2 ** 32 + 2 ** 30
+        pool, w = binding.alloc_kv_pool(ctx, n_pages, fill=None), torch.zeros((2, n_pages, nkv, 16), device="cuda")
+        table, other = (n_pages - 1 - np.arange(20))[None], (n_pages - 21 - np.arange(20))[None]
+        k, v = (t.cuda() for t in synth.kv_values(L + n, nkv, d, seed=3))
+        ctx.recg_kv_write(pool, n_pages, 1, table[0], 0, k, v)
+        batch = binding.Batch([L], [n], [0], None, table, pool, n_pages)
+        ctx.recg_kv_append(batch, 1, k[:n], v[:n])
+        out = list(ctx.recg_kv_rows(None, 1)) + list(ctx.recg_kv_read(pool, n_pages, 1, table[0], 0, L + n))
+        for rows in (n, 40):                                           # both attention kernels of a 4-bit pool
+            few = binding.Batch([L + n - rows], [rows], [0], None, table, pool, n_pages)
+            q = synth.queries(rows, nq, d, seed=5).cuda()
+            o, lse = torch.empty_like(q), torch.empty((rows, nq), device="cuda")
+            ctx.recg_attention(few, 1, q, o, lse)
+            ctx.recg_kv_weights(few, 1, q, lse, w, w)
+            out += [o, lse]
+        keep = torch.empty((1, 1, nkv, 100), dtype=torch.int32, device="cuda")
+        for dst in (other, None):
+            ev = binding.Eviction([L], [100], table, pool, n_pages, w, 4, 16, dst, (1, 2))
+            ctx.recg_kv_select(ev, keep)
+            ctx.recg_kv_compact(ev, keep)
+            to = torch.from_numpy((table if dst is None else dst)[0, :7].copy()).cuda()
+            out += [keep.clone(), w[1, to]] + list(ctx.recg_kv_read(pool, n_pages, 1, to.cpu().numpy(), 0, 100))
+        ctx.recg_sync()
+        ctx.recg_free()
+        got.append([t.cpu() for t in out])
+        del pool, w
+        torch.cuda.empty_cache()
+    for i, (a, b) in enumerate(zip(*got)):
+        assert torch.equal(a, b), i
