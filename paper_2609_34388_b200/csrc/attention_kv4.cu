@@ -93,9 +93,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return reinterpret_cast<const uint32_t&>(h);
 }
-__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
 template <int N>
 __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
   if constexpr (N == 4) {
@@ -106,7 +103,6 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
     w[0] = t.x; w[1] = t.y;
   }
 }
-__device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
 __device__ __forceinline__ float inverse(float power) { return __int_as_float(0x7f000000 - __float_as_int(power)); }       // of 2^e
 
 template <int D, int NT>

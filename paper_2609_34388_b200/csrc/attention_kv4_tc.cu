@@ -123,7 +123,6 @@ __device__ __forceinline__ bool wait_asleep(uint64_t* bar, uint32_t parity) {
 // Multiples of eight E with 2^-E v in [1, 2^8) for the v whose exponent field is `field` (clamped where a factor 2^E or 2^-E would
 // not be a normal number, or products of two not)
 __device__ __forceinline__ int scale_exp(int field) { return max(-56, min(120, ((field - 127) >> 3) << 3)); }
-__device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
 // The scales of 32 tokens, a token a lane, of which `top` is the largest value (0: nothing that has to be held).
 struct Scale {
   int all, own;

@@ -29,6 +29,10 @@ __host__ __device__ __forceinline__ size_t kv4_block_base(int64_t n_pages, int n
 __host__ __device__ __forceinline__ int kv4_k_word(int tok, int j, int d) { return tok * (d >> 1) + 4 * j; }
 __host__ __device__ __forceinline__ int kv4_v_word(int tok, int j, int odd, int d) { return kv4_v_codes(d) + (tok >> 1) * d + 8 * j + 4 * odd; }
 
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }       // 2^e, a normal number
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 // {s, m} of a row
 __device__ __forceinline__ float kv4_step(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float kv4_min(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }

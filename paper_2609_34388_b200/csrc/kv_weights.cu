@@ -68,9 +68,6 @@ struct Shape {
   static_assert(kPage % 16 == 0 && kTotal % 16 == 0, "16-byte pieces");
 };
 
-__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
 // d (+)= a b; FIRST: the accumulator starts from zero
 template <bool HALF, bool FIRST>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -88,7 +85,6 @@ __device__ __forceinline__ uint32_t scaled_f16(uint32_t pair, float by) {
   const __half2 h = __floats2half2_rn(__uint_as_float(pair << 16) * by, __uint_as_float(pair & 0xffff0000u) * by);
   return reinterpret_cast<const uint32_t&>(h);
 }
-__device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
 
 template <int D, bool FOUR>
 __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel(const __grid_constant__ Params P) {
@@ -307,7 +303,8 @@ __global__ void __launch_bounds__(Shape<D, FOUR>::kThreads, 1) kv_weights_kernel
       first_tok = s_next[0];
       const int staged = s_row0[nseg - 1] + s_rows8[nseg - 1];
       // (chunk c of a row: its values 8 c .. 8 c + 7)
-      constexpr int kPer = kChunkRows * kChunks / kThreads + 1;
+      constexpr int kPer = kChunkRows * kChunks / kThreads;
+      static_assert(kPer * kThreads == kChunkRows * kChunks, "a turn stages whole rows");
       uint4 raw[kPer];
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
