@@ -114,7 +114,7 @@ def test_in_place_lists_of_requests_that_are_not_cut(flags, head_dim):
     ctx.recg_free()
 
 
-@pytest.mark.parametrize("flags,far", [(0, 40000), (binding.FLAG_KV_4BIT, 150000)])
+@pytest.mark.parametrize("flags,far", [(0, 45000), (binding.FLAG_KV_4BIT, 160000)])
 def test_pages_behind_four_gigabytes(flags, far):
     """The last pages of a pool of two layers that takes more than 2^32 bytes: what every operation gives for the first pages of a small one."""
     nq, nkv, d, L, n = 32, 8, 128, 300, 3
