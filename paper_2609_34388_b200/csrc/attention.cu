@@ -555,10 +555,13 @@ size_t attention_smem_bytes(int head_dim) {
   return head_dim == 64 ? AttnSmem<64>::kTotal : AttnSmem<128>::kTotal;
 }
 
-// Attention over a 4-bit pool, head_dim 128: row tiles of at most this many query rows take the mma.sync kernel, which unpacks fewer codes per
-// byte than the tensor cores want as operands but needs eight columns of products for eight rows.  Sixteen requests of 512 to 8192 tokens, 4, 8,
-// 12 and 32 rows a kv head: 25.5, 26.3, 50.6 and 68.3 us with mma.sync, 48.8, 48.9, 49.3 and 50.3 with tcgen05; one request of 4096: 8.7, 9.1,
-// 14.7, 17.3 and 13.7, 14.2, 14.3, 14.5.
+// Attention over a 4-bit pool, head_dim 128: batches whose row tiles have at most this many query rows take the mma.sync kernel, which unpacks
+// fewer codes per byte than the tensor cores want as operands but needs eight columns of products for eight rows.  Sixteen requests of 512 to
+// 8192 tokens, 4, 8, 12 and 32 rows a kv head: 24.0, 24.5, 46.8 and 65.9 us with mma.sync, 47.7, 47.9, 48.2 and 49.5 with tcgen05; one request
+// of 4096: 9.0, 9.1, 14.9, 17.4 and 13.5, 14.0, 14.1, 14.3.  One kernel takes all of a batch, so its largest tile decides: fifteen requests of one
+// row beside one of 16 + 16 take 197 us with mma.sync and 50 with tcgen05, 63 beside one 669 and 178 (on a bf16 pool 46 and 170).  Rounds whose
+// lengths are on the device always take tcgen05 for that reason, and where they decode, it loses: 64 requests of one row, eight layers,
+// 2526 us instead of the 1668 of a round that the host lays out.
 constexpr int kFewRows = 8;
 void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, const void* kv_pool,
                       int64_t n_pages, float* part_o, float* part_ml, int tok_per_tile, int n_sm, int* status,

@@ -27,7 +27,10 @@ __device__ __forceinline__ int upper_request(const int* cu, int n_req, int t) {
 // preceded by virtual blocks that stand for the fixed cost of starting an item (fetching Q, refilling and draining the
 // pipeline; kItemCostPair, kItemCostSingle, in blocks: the blocks of a pair take less time, every second one comes from L2.
 // Attention of a layer with 4 for both / 6 and 4 / 8 and 4: two chunks of 1000 prompt tokens 158 / 143 / 143 us, eight requests
-// with two branches each 79.9 / 73.9 / 72.6, sixteen requests 66.7 / 66.7 / 68.0; 6 for both: the last one 67.5):
+// with two branches each 79.9 / 73.9 / 72.6, sixteen requests 66.7 / 66.7 / 68.0; 6 for both: the last one 67.5.  The kernels over a
+// 4-bit pool share them; 3 and 2 / 6 and 4 / 10 and 8 / 16 and 14: one row each of sixteen requests 31.8 / 26.1 / 26.3 / 23.6, one row
+// behind 131071 tokens 35.2 / 34.9 / 34.6 / 33.5, a round of sixteen requests with a branch each 100.1 / 95.7 / 95.9 / 98.8, one request
+// of 16 + 16 rows 18.4 / 15.3 / 15.3 / 16.3, 1001 rows over 6000 tokens 184.8 / 184.0 / 183.7 / 185.2):
 //   line A holds one segment per sibling PAIR and is cut into equal contiguous ranges, one per pair of CTAs
 //          (2 p, 2 p + 1): the even CTA works on the first sibling and the odd CTA on the second sibling of the SAME
 //          block ranges, at the same time, so that the second reader of a K/V block finds it in L2;
