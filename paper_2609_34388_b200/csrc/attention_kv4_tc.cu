@@ -6,8 +6,8 @@
 // is exact up to fp32 sums: the second term is one more step of 16 of the contraction, in which both factors stand as sums of
 // two fp16 numbers.  (K as m + s c rounded to 16 bits would leave the log-sum-exp of a few tokens good to 1e-4 only; steps applied
 // in fp32 behind the product have to be broadcast to every row's thread, and that alone took more of the shared memory's
-// bandwidth than all operands: 325 us instead of 192 us for 1001 rows over 6000 tokens of 40 / 8 heads.)  V stands as m + s c
-// rounded once, and P as fp16 too: 2^-11 of each term by either, a quarter of the rounding of the result together.
+// bandwidth than all operands: 325 us instead of the 192 us that this took then, for 1001 rows over 6000 tokens of 40 / 8 heads.)
+// V stands as m + s c rounded once, and P as fp16 too: 2^-11 of each term by either, a quarter of the rounding of the result together.
 //
 // Range.  fp16 has five bits of exponent, so everything is scaled by powers of two, in steps of 2^8: a query row by its own largest
 // value, K and V of 32 tokens by theirs, or, where tokens lie 2^16 apart, each by its own (a row may see one and not the other).  The
