@@ -64,6 +64,15 @@ enum {
                                 value taken to the nearest (ties to the even level); a row with a value that is not finite
                                 reads back as NaN.  recg_kv_pool_bytes() and everything that takes the pool follow it, steps too
                                 (RECG_FLAG_CHAIN has no effect with it)                            */
+  RECG_FLAG_KV_8BIT = 128,   /* the KV pool holds 8 bits a value, half the bytes: of every page and kv head K and V are each held as e4m3 numbers
+                                times 2^e, e the least whole number for which no value exceeds 448 2^e (within -60 .. 120); a row with a value
+                                that is not finite reads back as NaN.  Rows that come into a page behind others take these along: e follows all
+                                of them and what was held is rounded again, which changes only what is below 2^-14 of the page's largest.
+                                Rows of the page behind the last one written are cleared, so a request is written front to back, and a page that
+                                takes new rows belongs to one request alone (a call whose rows go into one page from two requests is refused; of
+                                a device-resident round the caller sees to that).  recg_kv_pool_bytes() and everything that takes the pool follow it, steps too
+                                (RECG_FLAG_CHAIN has no effect with it); recg_kv_weights(), recg_kv_track() and recg_kv_compact()
+                                refuse it, as recg_init() refuses it beside RECG_FLAG_KV_4BIT */
   RECG_FLAG_DEBUG_CHECKS = 8 /* guard bands behind every workspace region, checked by recg_sync() (RECG_ERR_INTERNAL
                                 if a kernel wrote past the end of one), and a host check that no page which receives
                                 new rows is named by two requests (RECG_ERR_INVALID_ARG)          */
@@ -236,6 +245,14 @@ recg_status recg_verify(recg_ctx *ctx, const recg_batch *batch, const void *logi
 recg_status recg_attention(recg_ctx *ctx, const recg_batch *batch, int32_t layer, const void *q, void *o);
 /* The same, and lse[t, h] = ln of the sum over the visible positions of exp(q . k / sqrt(head_dim)): DEVICE float32 [T, n_q_heads]. */
 recg_status recg_attention_lse(recg_ctx *ctx, const recg_batch *batch, int32_t layer, const void *q, void *o, float *lse);
+/*
+ * Rows look back a window: from now on, in recg_attention(), recg_attention_lse() and steps, a row at position p (in the request's cache; of
+ * a branch token the position that it hypothesises) sees position j of what the mask of Eq. 1 shows it only if j < n_sink or j > p - window.
+ * What no row sees is not read.  window = 0: everything again.  A batch that was laid out before is seen through the new window by the next
+ * recg_attention() without one.  Captured calls keep the window that they were captured with, and are for work lists of the same.
+ * Refused with RECG_FLAG_KV_4BIT and while weights are gathered (recg_kv_track()), as recg_kv_track() and recg_kv_weights() are with a window.
+ */
+recg_status recg_window(recg_ctx* ctx, int32_t n_sink, int32_t window);
 
 /*
  * Move logical K/V rows of one request into / out of the pool.  k, v: DEVICE bf16
@@ -259,6 +276,17 @@ recg_status recg_kv_read(recg_ctx *ctx, const void *kv_pool, int64_t kv_pool_pag
  */
 recg_status recg_kv_append(recg_ctx *ctx, const recg_batch *batch, int32_t layer, const void *k, const void *v, int64_t row_stride);
 recg_status recg_kv_rows(recg_ctx *ctx, const recg_batch *batch, int32_t layer, void *k, void *v, int64_t row_stride);
+
+/*
+ * recg_kv_append() for rows as a projection leaves them: q and k are rotated to their positions on the way (pairing (i, i + head_dim/2), base
+ * cfg.rope_base; a branch token to the position that it hypothesises, positions moved by recg_kv_shift()), and rounded once to bf16 (what a
+ * pool in fewer bits holds follows from that).  Angles, and the products of k, in 64 bits.  With it recg_attention() is a layer's attention
+ * behind any projection: recg_kv_append_rotary(), then recg_attention(q_out).
+ *   q [T, n_q_heads, head_dim], rows q_stride elements apart; q_out [T, n_q_heads, head_dim] without gaps, which may be q where q has none.
+ *   Both NULL: K and V only.  k, v [T, n_kv_heads, head_dim], rows kv_stride elements apart.  Strides and alignment as above.
+ */
+recg_status recg_kv_append_rotary(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, int64_t q_stride, void* q_out,
+                                  const void* k, const void* v, int64_t kv_stride);
 
 /*
  * The batch that batch == NULL stands for in the operations on the pool: its rows (n_rows; of a device-resident round max_tokens, the rows it

@@ -21,7 +21,7 @@ RECG_OK = 0
 DTYPE_BF16, DTYPE_F32 = 0, 1
 MEM_DEVICE, MEM_HOST = 0, 1
 FLAG_LOGITS_BF16, FLAG_SIMT_GEMM, FLAG_SIMT_ATTENTION, FLAG_DEBUG_CHECKS, FLAG_FOLD_NORM, FLAG_CHAIN = 1, 2, 4, 8, 16, 32
-FLAG_KV_4BIT = 64
+FLAG_KV_4BIT, FLAG_KV_8BIT = 64, 128
 STATUS_NAMES = {0: "RECG_OK", 1: "RECG_ERR_INVALID_ARG", 2: "RECG_ERR_SHAPE", 3: "RECG_ERR_CAPACITY",
                 4: "RECG_ERR_CUDA", 5: "RECG_ERR_TIMEOUT", 6: "RECG_ERR_INTERNAL"}
 
@@ -120,6 +120,9 @@ def lib() -> C.CDLL:
         rows = [C.c_void_p, C.POINTER(recg_batch), C.c_int32, C.c_void_p, C.c_void_p, C.c_int64]
         L.recg_kv_append.argtypes = rows
         L.recg_kv_rows.argtypes = rows
+        L.recg_window.argtypes = [C.c_void_p, C.c_int32, C.c_int32]
+        L.recg_kv_append_rotary.argtypes = [C.c_void_p, C.POINTER(recg_batch), C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                            C.c_int64]
         L.recg_kv_weights.argtypes = [C.c_void_p, C.POINTER(recg_batch), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
                                       C.c_void_p, C.c_void_p]
         L.recg_kv_select.argtypes = [C.c_void_p, C.POINTER(recg_eviction), C.c_void_p, C.c_int32]
@@ -149,7 +152,7 @@ def lib() -> C.CDLL:
         L.recg_debug_map_cache_selftest.restype = C.c_int32
         for f in ("recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write", "recg_kv_read",
                   "recg_attention_lse", "recg_kv_append", "recg_kv_rows", "recg_kv_weights", "recg_kv_select", "recg_kv_compact", "recg_kv_track",
-           "recg_kv_shift", "recg_layout_info",
+           "recg_kv_shift", "recg_layout_info", "recg_kv_append_rotary", "recg_window",
            "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_timing_enable", "recg_timing_read",
                   "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
                   "recg_step_device", "recg_next_round"):
@@ -160,7 +163,7 @@ def lib() -> C.CDLL:
 
 EXPORTS = ("recg_kv_pool_bytes", "recg_init", "recg_step", "recg_verify", "recg_attention", "recg_kv_write",
            "recg_attention_lse", "recg_kv_read", "recg_kv_append", "recg_kv_rows", "recg_kv_weights", "recg_kv_select", "recg_kv_compact", "recg_kv_track",
-           "recg_kv_shift", "recg_layout_info",
+           "recg_kv_shift", "recg_layout_info", "recg_kv_append_rotary", "recg_window",
            "recg_linear", "recg_debug_buffer", "recg_sync", "recg_free", "recg_last_error",
            "recg_timing_enable", "recg_timing_read", "recg_row_stats_static", "recg_row_stats_static_error",
            "recg_policy_load", "recg_policy_step", "recg_debug_gemm_config", "recg_debug_gemm_plan", "recg_debug_wait_timeout",
@@ -380,6 +383,10 @@ class Context:
             raise ValueError(f"lse must be contiguous CUDA float32 [{n_tok}, {self.cfg.n_q_heads}]")
         self._check(lib().recg_attention_lse(self.h, b, layer, q.data_ptr(), o.data_ptr(), lse.data_ptr()))
 
+    def recg_window(self, n_sink: int, window: int):
+        """From now on rows see, of what their mask shows them, the first n_sink positions and those less than `window` away (0: everything)."""
+        self._check(lib().recg_window(self.h, int(n_sink), int(window)))
+
     def recg_kv_write(self, pool: torch.Tensor, n_pages: int, layer: int, page_row, pos0: int, k: torch.Tensor,
                       v: torch.Tensor):
         row = _i32(page_row)
@@ -418,6 +425,20 @@ class Context:
         """k, v [T, n_kv_heads, head_dim]: rows of the batch (None: the one laid out last); rows may lie in a wider array."""
         b, kp, vp, stride = self._kv_rows_args(batch, k, v)
         self._check(lib().recg_kv_append(self.h, b, layer, kp, vp, stride))
+
+    def recg_kv_append_rotary(self, batch: Optional[Batch], layer: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                              q_out: Optional[torch.Tensor] = None):
+        """recg_kv_append of k and v with k rotated to the rows' positions, and q [T, n_q_heads, head_dim] rotated into q_out (which may be q
+        itself; both None: K and V only).  Rows of q, k and v may lie in wider arrays."""
+        b, kp, vp, stride = self._kv_rows_args(batch, k, v)
+        qp = op = q_stride = 0
+        if q is not None or q_out is not None:
+            want = (k.shape[0], self.cfg.n_q_heads, self.cfg.head_dim)
+            if q is None or q_out is None or q.dtype is not torch.bfloat16 or q_out.dtype is not torch.bfloat16 or not q.is_cuda or \
+                    not q_out.is_cuda or q.shape != want or q_out.shape != want or q.stride()[1:] != (want[2], 1) or not q_out.is_contiguous():
+                raise ValueError(f"q and q_out must be CUDA bf16 {list(want)}, q with contiguous rows and q_out contiguous")
+            qp, op, q_stride = q.data_ptr(), q_out.data_ptr(), q.stride(0) if want[0] > 1 else 0
+        self._check(lib().recg_kv_append_rotary(self.h, b, layer, qp, q_stride, op, kp, vp, stride))
 
     def recg_kv_rows(self, batch: Optional[Batch], layer: int, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
         """The K and V rows of the batch as the pool holds them, into k and v or into new tensors."""

@@ -34,12 +34,15 @@ struct AttnSmem {
 
 struct AttnParams {
   const AttnItem* items;
+  const int* item_gap;
   const int* cta_off;
   const int* page_table;
   int pt_stride;
   const int* tok_climit;
   const int* tok_lo;
   const int* tok_hi;
+  const int* tok_first;
+  int n_sink, sink_blocks;   // a window: first tokens, and the blocks that hold them
   const __nv_bfloat16* q;
   __nv_bfloat16* o;
   float* lse;         // log-sum-exp of every row and head (null: not wanted)
@@ -55,7 +58,8 @@ struct AttnParams {
 __device__ __forceinline__ void consumer_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // (LSE, here and in the kernels below: the log-sum-exp is wanted.  Asked at run time it took 0.2 us a call from those that do not want it.)
-template <int D, bool LSE>
+// WIN: rows look back a window (recg_window); an item's blocks behind the first tokens' lie `gap` further on.
+template <int D, bool LSE, bool WIN>
 __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P) {
   using SM = AttnSmem<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -80,6 +84,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P
   const int range_n0 = r4.y - r4.x;
   const int item_begin = 0, item_end = range_n0 + (r4.w - r4.z);
   auto item_at = [&](int i) { return i < range_n0 ? r4.x + i : r4.z + (i - range_n0); };
+  auto gap_of = [&](int i) { return WIN ? P.item_gap[item_at(i)] : 0; };
+  auto place = [&](int block, int gap) { return WIN && block >= P.sink_blocks ? block + gap : block; };
   uint32_t it = 0;  // running block counter, identical in producer and consumers
   bool aborted = false;
 
@@ -87,13 +93,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P
     // ------------------------------ producer ------------------------------
     for (int item = item_begin; item < item_end && !aborted; ++item) {
       const AttnItem w = P.items[item_at(item)];
+      const int gap = gap_of(item);
       const int n_req_pages = (w.kv_len + kPageSize - 1) / kPageSize;
       const int* pt = P.page_table + (size_t)w.req * P.pt_stride;
       // lanes 0..3 each own one page of the block; ids are fetched one block ahead of their use
       auto fetch_page = [&](int n) -> int {
         int pg = -1;
         if (lane < kPagesPerBlock && n < w.blk_end) {
-          const int lp = n * kPagesPerBlock + lane;
+          const int lp = place(n, gap) * kPagesPerBlock + lane;
           if (lp < n_req_pages) pg = __ldg(pt + lp);   // validated when used
         }
         return pg;
@@ -143,6 +150,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P
 
   for (int item = item_begin; item < item_end; ++item) {
     const AttnItem w = P.items[item_at(item)];
+    const int gap = gap_of(item);
     const int R = w.ntok * P.group;
     const int RW = (R + 15) >> 4;
     const int KW = RW == 1 ? 8 : (RW == 2 ? 4 : (RW <= 4 ? 2 : 1));
@@ -151,7 +159,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P
 
     // Q fragments and per-row visibility for this thread's two rows (g and g + 8 of the warp's 16)
     uint32_t qf[D / 16][4];
-    int climit[2], vlo[2], vhi[2];
+    int climit[2], vlo[2], vhi[2], vfirst[2];
     int qrow_tok[2], qrow_head[2];
     bool rvalid[2];
 #pragma unroll
@@ -165,6 +173,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P
       climit[hh] = rvalid[hh] ? P.tok_climit[t] : -1;
       vlo[hh] = rvalid[hh] ? P.tok_lo[t] : 0;
       vhi[hh] = rvalid[hh] ? P.tok_hi[t] : 0;
+      vfirst[hh] = WIN && rvalid[hh] ? P.tok_first[t] : 0;
     }
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
@@ -212,11 +221,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P
           }
         }
         // ---- visibility (only blocks that reach past the mask-free prefix) ----
-        const int pos0 = n * kBlockTokens;
+        const int pos0 = place(n, gap) * kBlockTokens;
         const int min_limit = min(climit[0], climit[1]);
         // every row of the tile sees all positions <= its climit; the block is mask-free when it ends
         // at or before the smallest climit of the warp's rows (invalid rows carry -1 and force the test)
-        const bool need_mask = __any_sync(0xffffffffu, pos0 + kBlockTokens - 1 > min_limit);
+        const bool need_mask = __any_sync(0xffffffffu, pos0 + kBlockTokens - 1 > min_limit || (WIN && pos0 < max(vfirst[0], vfirst[1])));
         if (need_mask) {
 #pragma unroll
           for (int nt = 0; nt < 8; ++nt) {
@@ -224,7 +233,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attention_kernel(AttnParams P
             for (int e = 0; e < 4; ++e) {
               const int hh = e >> 1;
               const int pos = pos0 + nt * 8 + q4 * 2 + (e & 1);
-              const bool vis = pos <= climit[hh] || (pos >= vlo[hh] && pos < vhi[hh]);
+              const bool vis = (pos <= climit[hh] || (pos >= vlo[hh] && pos < vhi[hh])) && (!WIN || pos < P.n_sink || pos >= vfirst[hh]);
               if (!vis) sc[nt][e] = -INFINITY;
             }
           }
@@ -521,11 +530,15 @@ void launch_attention_t(const BatchLayout& bl, const Dims& dm, int layer, const 
                         cudaStream_t st, bool whole, int tiles, bool step) {
   static bool configured[kMaxDevices] = {false};
   if (first_use_on_device(configured))
-    for (auto* kernel : {attention_kernel<D, false>, attention_kernel<D, true>})
+    for (auto* kernel : {attention_kernel<D, false, false>, attention_kernel<D, true, false>, attention_kernel<D, false, true>, attention_kernel<D, true, true>})
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnSmem<D>::kTotal);
 
   AttnParams P;
   P.items = bl.items;
+  P.item_gap = bl.item_gap;
+  P.tok_first = bl.tok_first;
+  P.n_sink = bl.n_sink;
+  P.sink_blocks = (bl.n_sink + kBlockTokens - 1) / kBlockTokens;
   P.cta_off = bl.cta_off;
   P.page_table = bl.page_table;
   P.pt_stride = bl.pt_stride;
@@ -545,7 +558,8 @@ void launch_attention_t(const BatchLayout& bl, const Dims& dm, int layer, const 
   P.part_o = part_o;
   P.part_ml = part_ml;
   P.status = status;
-  launch_pdl(lse ? attention_kernel<D, true> : attention_kernel<D, false>, dim3(n_sm), dim3(kAttnThreads), AttnSmem<D>::kTotal, st, P);
+  launch_pdl(bl.window ? (lse ? attention_kernel<D, true, true> : attention_kernel<D, false, true>)
+                       : (lse ? attention_kernel<D, true, false> : attention_kernel<D, false, false>), dim3(n_sm), dim3(kAttnThreads), AttnSmem<D>::kTotal, st, P);
   if (!whole) launch_combine<D>(bl, dm, o, lse, part_o, part_ml, n_sm, st, tiles, step, 0);
 }
 
@@ -565,11 +579,13 @@ size_t attention_smem_bytes(int head_dim) {
 constexpr int kFewRows = 8;
 void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, const void* kv_pool,
                       int64_t n_pages, float* part_o, float* part_ml, int tok_per_tile, int n_sm, int* status,
-                      cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, bool four, float* lse, int max_rows) {
-  if (four || (use_tc && dm.head_dim == 128)) {
+                      cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, int bits, float* lse, int max_rows) {
+  const bool four = bits == 4;
+  if (bits != 16 || (use_tc && dm.head_dim == 128)) {
     if (four && use_tc && dm.head_dim == 128 && max_rows > kFewRows &&
         launch_attention_kv4_tc(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st)) {
-    } else if (four) launch_attention_kv4(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, max_rows, status, st, layout_settled);
+    } else if (bits == 8) launch_attention_kv8(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, max_rows, status, st, layout_settled);
+    else if (four) launch_attention_kv4(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, max_rows, status, st, layout_settled);
     else launch_attention_tc_main(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st, layout_settled);
     // (the kernel in front signals its dependents when the list is settled)
     if (!whole) (dm.head_dim == 64 ? launch_combine<64> : launch_combine<128>)(bl, dm, o, lse, part_o, part_ml, n_sm, st, tiles, step, 1);

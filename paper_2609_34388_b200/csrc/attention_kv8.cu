@@ -1,0 +1,500 @@
+// Hybrid-mask paged attention over a pool in 8 bits, few query rows per kv head or head_dim 64 (mma.sync).
+//
+// Work items, masks and the combine kernel are those of attention.cu.  With codes c and exponents f (K) and e (V) of a page (kv8.cuh)
+//   x_j = log2(e) / sqrt(d) 2^f q . c_K,   y_j = x_j + e_j,   o = sum_j 2^(y_j - r) c_V / sum_j 2^(x_j - r)
+// V's scales become part of the probabilities' exponents, and the reference r of a row is the maximum of the y of what it sees: the
+// largest of the numbers that the product with V takes stands near the top of fp16's range whatever the scales are, what falls below its
+// end (2^-39 of it) is that much smaller a contribution, and a row depends on nothing that it does not see.  The sum below is
+// kept in fp32 from the probabilities before they are rounded, times 2^-e_j.
+// Codes are converted to fp16, which holds them exactly.  Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T, since there
+// are fewer rows (the 8 columns of a product) than tokens or values (its 16 rows).  P^T turns from accumulators to operand by one
+// movmatrix per eight tokens.
+//
+// A warp works on 64 tokens, four pages, at a time: row g of a product is token 4 s + g % 2 (and row g + 8 the token two further) of page
+// g / 2 in product s, so that a lane's four 16-byte reads of V per value pair, one page each, are the operands of four products.  It is
+// alone with its pages: it requests them itself, 16 bytes a lane into a ring of its own, and runs ahead of itself into the next item.  The
+// warps are divided among the item's row groups, those of a group share its blocks among themselves, and their results are merged at the
+// end of the item.
+#include <cuda_fp16.h>
+
+#include "kernels.h"
+#include "kv8.cuh"
+
+namespace recg {
+
+namespace {
+
+constexpr float kNoRef = -1e30f;       // reference maximum of a row that has seen no token yet
+constexpr float kHeadroom = 8.f;       // a row's reference maximum moves when it is outgrown by more than 2^8
+constexpr float kLift = 7.f;           // probabilities stand as 2^7 p: at most 2^15
+constexpr int kPages = 4, kBlockTokens = kPages * kPageSize;
+
+// NT: groups of eight query rows a warp has.
+template <int D, int NT>
+struct Shape {
+  static constexpr int kWarps = D == 128 && NT == 1 ? 6 : 8;
+  static constexpr int kThreads = kWarps * 32;
+  static constexpr int kSlots = D == 64 || NT == 1 ? 2 : 1;        // blocks that a warp has on their way
+  static constexpr int kPitch = kv8_block_bytes(D) + 32;           // a page in the ring: its codes, its header (the lanes of a product read four pages at once)
+  static constexpr int kSlot = kPages * kPitch;
+  static constexpr int kRing = kWarps * kSlots * kSlot;
+  static constexpr int kRowPad = D + 4;                            // floats from row to row of a merged part
+  static constexpr int kRows = 8 * NT;
+  static constexpr int kMerge = kWarps * kRows * kRowPad * 4;      // [warp][row][value]; values D and D + 1: reference maximum, sum
+  static constexpr int kItemsOff = kRing + kMerge;
+  static constexpr int kItems = 24;                                // items of the CTA whose descriptors are kept on chip
+  static constexpr int kTotal = kItemsOff + kItems * (int)sizeof(AttnItem);
+  static_assert(kTotal <= 227 * 1024, "shared memory budget");
+  static_assert(kWarps * kRows >= 128 || NT == 1, "every row of a tile has a warp");
+};
+
+struct Params {
+  const AttnItem* items;
+  const int* item_gap;
+  const int* cta_off;
+  const int* page_table;
+  int pt_stride;
+  const int* tok_climit;
+  const int* tok_lo;
+  const int* tok_hi;
+  const int* tok_first;
+  const __nv_bfloat16* q;
+  __nv_bfloat16* o;
+  float* lse;         // may be null
+  const uint8_t* pool;     // of the layer
+  int64_t n_pages;
+  int n_q, n_kv, group, inv_group;      // inv_group: (rho * inv_group) >> 16 is rho / group for the rows of a tile
+  int n_sink, sink_blocks;              // a window: first tokens, and the blocks that hold them
+  float scale_log2;   // log2(e) / sqrt(d)
+  float* part_o;      // [part][128][D]
+  float* part_ml;     // [part][128][2]
+  int* status;
+  int early_desc;     // the work list is settled: it may be read before the wait for the kernel in front of this one
+};
+
+// D(16x8, f32) += A(16x16, f16, row) * B(16x8, f16, col)
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return reinterpret_cast<const uint32_t&>(h);
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// WIN: rows look back a window (recg_window)
+template <int D, int NT, bool WIN>
+__global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kernel(Params P) {
+  using SH = Shape<D, NT>;
+  constexpr int NW = D / 32;             // 16-byte pieces of a quarter of a row of Q; words of codes: 2 NW
+  constexpr int W = SH::kWarps, kSlots = SH::kSlots;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  uint8_t* ring = smem + warp * kSlots * SH::kSlot;
+  float* merge = reinterpret_cast<float*>(smem + SH::kRing);
+  // (pages that are not requested, behind a request's end: whatever the slot holds is numbers)
+  for (int i = threadIdx.x; i < SH::kRing / 16; i += SH::kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+  // (where the work list is settled all reads of it, and of page ids, overlap the end of the kernel in front)
+  if (!P.early_desc) griddep_wait();
+
+  // the CTA walks two ranges of the item list one after the other (see the layout kernel)
+  const int4 r4 = *reinterpret_cast<const int4*>(P.cta_off + 4 * blockIdx.x);
+  const int range_n0 = r4.y - r4.x, item_end = range_n0 + (r4.w - r4.z);
+  auto item_at = [&](int i) { return i < range_n0 ? r4.x + i : r4.z + (i - range_n0); };
+  static_assert(sizeof(AttnItem) == 32, "two 16-byte pieces");
+  uint4* kept = reinterpret_cast<uint4*>(smem + SH::kItemsOff);
+  for (int i = threadIdx.x; i < 2 * min(item_end, SH::kItems); i += SH::kThreads)
+    kept[i] = reinterpret_cast<const uint4*>(P.items + item_at(i >> 1))[i & 1];
+  __syncthreads();
+  auto item_of = [&](int i) { return i < SH::kItems ? reinterpret_cast<const AttnItem*>(kept)[i] : P.items[item_at(i)]; };
+  // of an item: warps per row group; this warp's group; its first block and the end of all
+  struct Share { int warps, group, block, end; };
+  auto share_of = [&](const AttnItem& w) {
+    Share s;
+    if (NT == 1) {                       // (one group)
+      s.warps = W;
+      s.group = 0;
+    } else {
+      s.warps = W / ((w.ntok * P.group + SH::kRows - 1) / SH::kRows);
+      s.group = warp / s.warps;
+    }
+    s.end = s.group * SH::kRows < w.ntok * P.group ? w.blk_end : 0;
+    s.block = w.blk_begin + warp - s.group * s.warps;
+    return s;
+  };
+  // an item's blocks behind the first tokens' lie `gap` further on
+  auto gap_of = [&](int i) { return WIN ? P.item_gap[item_at(i)] : 0; };
+  auto place = [&](int block, int gap) { return WIN && block >= P.sink_blocks ? block + gap : block; };
+
+  // ---- what the warp requests next: a block of an item.  Page ids are fetched 32 at a time, a lane one of them ----
+  int f_item = -1, f_block = 0, f_step = 0, f_end = 0, f_used = 0, f_ids = 0, f_pages = 0, f_gap = 0;
+  const int* f_table = nullptr;
+  const uint8_t* f_base = nullptr;       // this lane's 16 bytes of the head's block in page 0
+  const uint8_t* f_header = nullptr;
+  const unsigned page_bytes = (unsigned)P.n_kv * kv8_block_bytes(D), n_pages = (unsigned)min(P.n_pages, (int64_t)0x7fffffff);
+  const uint32_t ring_at = smem_u32(ring) + lane * 16;
+  auto load_ids = [&]() {
+    f_used = 0;
+    const int block = f_block + (lane / kPages) * f_step, page = place(block, f_gap) * kPages + lane % kPages;
+    f_ids = block < f_end && page < f_pages ? __ldg(f_table + page) : -1;
+  };
+  auto next_item = [&]() {
+    do {
+      if (++f_item >= item_end) {
+        f_end = -1;
+        return;
+      }
+      const AttnItem w = item_of(f_item);
+      const Share s = share_of(w);
+      f_block = s.block;
+      f_step = s.warps;
+      f_end = s.end;
+      f_gap = gap_of(f_item);
+      f_pages = (w.kv_len + kPageSize - 1) / kPageSize;
+      f_table = P.page_table + (size_t)w.req * P.pt_stride;
+      f_base = P.pool + (size_t)w.kv_head * kv8_block_bytes(D) + lane * 16;
+      f_header = P.pool + kv8_headers(P.n_pages, P.n_kv, D) + (size_t)w.kv_head * 8;
+    } while (f_block >= f_end);
+    load_ids();
+  };
+  auto request = [&](uint32_t slot_at) {        // one group of copies per call, be it empty
+    if (f_end >= 0) {
+#pragma unroll
+      for (int i = 0; i < kPages; ++i) {
+        const int id = __shfl_sync(0xffffffffu, f_ids, f_used + i);
+        if ((unsigned)id >= n_pages) {
+          if (id >= 0 || place(f_block, f_gap) * kPages + i < f_pages) set_status(P.status, DEV_BAD_INDEX);
+          continue;
+        }
+        const uint8_t* src = f_base + (uint64_t)(unsigned)id * page_bytes;
+        const uint32_t dst = ring_at + slot_at + i * SH::kPitch;
+#pragma unroll
+        for (int x = 0; x < kv8_block_bytes(D) / 512; ++x) copy16(dst + x * 512, src + x * 512);
+        if (lane == 0) copy8(dst + kv8_block_bytes(D), f_header + (uint64_t)(unsigned)id * (8u * P.n_kv));
+      }
+      f_block += f_step;
+      f_used += kPages;
+      if (f_block >= f_end) next_item();
+      else if (f_used >= 32) load_ids();
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  next_item();
+  if (P.early_desc) griddep_wait();
+  griddep_launch();
+
+  // The rows of a warp's group in an item, read ahead of their use: column g of row group nt, of which lane t holds the values
+  // [D / 4 t, D / 4 (t + 1)); and what the rows 2 t and 2 t + 1 see
+  uint4 raw[NT][NW];
+  int climit[NT][2], vlo[NT][2], vhi[NT][2], vfirst[NT][2];
+  auto load_rows = [&](const AttnItem& w) {
+    const int R = w.ntok * P.group, row0 = share_of(w).group * SH::kRows;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int rho = row0 + nt * 8 + g, j = (rho * P.inv_group) >> 16;
+      const bool there = rho < R;
+      const uint4* src = reinterpret_cast<const uint4*>(P.q + ((size_t)(w.tok0 + (there ? j : 0)) * P.n_q + w.kv_head * P.group + (there ? rho - j * P.group : 0)) * D) + t * NW;
+#pragma unroll
+      for (int k = 0; k < NW; ++k) raw[nt][k] = there ? __ldg(src + k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int rv = row0 + nt * 8 + 2 * t + e, tok = w.tok0 + ((rv * P.inv_group) >> 16);
+        const bool is = rv < R;      // (a row that does not exist needs no mask: nobody reads it)
+        climit[nt][e] = is ? P.tok_climit[tok] : 0x7fffffff;
+        vlo[nt][e] = is ? P.tok_lo[tok] : 0;
+        vhi[nt][e] = is ? P.tok_hi[tok] : 0;
+        vfirst[nt][e] = WIN && is ? P.tok_first[tok] : 0;
+      }
+    }
+  };
+  if (item_end > 0) load_rows(item_of(0));
+  for (int s = 0; s < kSlots; ++s) request(s * SH::kSlot);
+
+  uint32_t slot_at = 0;   // the slot of the next block
+  for (int item = 0; item < item_end; ++item) {
+    const AttnItem w = item_of(item);
+    const int R = w.ntok * P.group, gap = gap_of(item);
+    const Share sh = share_of(w);
+    // ---- Q as B operands, every row times a power of two of its own, its largest value in [2^8, 2^9): k-step 2 k + u takes the pairs 2 u and
+    // 2 u + 1 of piece k.  A value is off by 2^-34 of the row's largest at most, where fp16 ends ----
+    uint32_t qf[NT][D / 16][2];
+    float back[NT][2];                   // what makes a product of scaled Q and codes a score in powers of two, before K's exponent
+    int lim = 0x7fffffff, from = 0;      // the positions between which every row of the warp sees everything
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      uint32_t top = 0;                  // largest value of this quarter of row g
+#pragma unroll
+      for (int k = 0; k < NW; ++k) {
+        const uint32_t u[4] = {raw[nt][k].x, raw[nt][k].y, raw[nt][k].z, raw[nt][k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, max(u[i] & 0x7fffu, (u[i] >> 16) & 0x7fffu));
+      }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // (as far as the exponent allows: a factor and its inverse are normal numbers)
+      const int e = max(-100, min(100, (int)(top >> 7) - 127 - 8));
+      const float down = kv8_pow2(-e);
+#pragma unroll
+      for (int k = 0; k < NW; ++k) {
+        const uint4 v = raw[nt][k];
+        qf[nt][2 * k][0] = pack_f16(__uint_as_float(v.x << 16) * down, __uint_as_float(v.x & 0xffff0000u) * down);
+        qf[nt][2 * k][1] = pack_f16(__uint_as_float(v.y << 16) * down, __uint_as_float(v.y & 0xffff0000u) * down);
+        qf[nt][2 * k + 1][0] = pack_f16(__uint_as_float(v.z << 16) * down, __uint_as_float(v.z & 0xffff0000u) * down);
+        qf[nt][2 * k + 1][1] = pack_f16(__uint_as_float(v.w << 16) * down, __uint_as_float(v.w & 0xffff0000u) * down);
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        back[nt][c] = kv8_pow2(__shfl_sync(0xffffffffu, e, (2 * t + c) * 4)) * P.scale_log2;
+        lim = min(lim, climit[nt][c]);
+        from = max(from, vfirst[nt][c]);
+      }
+    }
+    lim = __reduce_min_sync(0xffffffffu, lim);
+    from = __reduce_max_sync(0xffffffffu, from);
+
+    float o[NT][D / 16][4];              // O^T: values 16 i + g and 16 i + g + 8, columns 2 t and 2 t + 1
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
+    // per row (columns 2 t, 2 t + 1; the same in all lanes of a column): reference maximum in powers of two, less kLift; this lane's
+    // part of the sum of probabilities
+    float ref[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      ref[nt][0] = ref[nt][1] = kNoRef;
+      l[nt][0] = l[nt][1] = 0.f;
+    }
+
+    for (int block = sh.block; block < sh.end; block += sh.warps) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 1) : "memory");
+      __syncwarp();
+      const uint8_t* pg = ring + slot_at;
+      const int pos0 = place(block, gap) * kBlockTokens;
+      // this lane's page (g / 2 of the block): both its tokens of a product are there
+      const int page_pos = pos0 + (g >> 1) * kPageSize + (g & 1);
+      const uint2 head = *reinterpret_cast<const uint2*>(pg + (g >> 1) * SH::kPitch + kv8_block_bytes(D));
+      // ---- S^T = C_K Q^T ----
+      float sc[4][NT][4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sc[s][nt][0] = sc[s][nt][1] = sc[s][nt][2] = sc[s][nt][3] = 0.f;
+        const uint8_t* rows = pg + (g >> 1) * SH::kPitch;
+        const int tok = 4 * s + (g & 1);
+#pragma unroll
+        for (int c = 0; c < NW / 2; ++c) {
+          const uint4 k0 = *reinterpret_cast<const uint4*>(rows + kv8_k_chunk<D>(tok, t * (NW / 2) + c));
+          const uint4 k1 = *reinterpret_cast<const uint4*>(rows + kv8_k_chunk<D>(tok + 2, t * (NW / 2) + c));
+          const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t a0 = e4m3_to_f16(w0[x] & 0xffffu), a1 = e4m3_to_f16(w1[x] & 0xffffu), a2 = e4m3_to_f16(w0[x] >> 16), a3 = e4m3_to_f16(w1[x] >> 16);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_f16(sc[s][nt], a0, a1, a2, a3, qf[nt][4 * c + x][0], qf[nt][4 * c + x][1]);
+          }
+        }
+      }
+      // ---- y = x + e, -inf where the row does not see the token; NaN where K's row is none ----
+      const float k_scale = kv8_pow2(kv8_exponent(head.x)), v_exp = (float)kv8_exponent(head.y), v_back = kv8_pow2(-kv8_exponent(head.y));
+      const uint32_t k_bad = kv8_flags(head.x), v_bad = kv8_flags(head.y);
+      const bool some_bad = __any_sync(0xffffffffu, (k_bad | v_bad) != 0);
+      const bool masked = pos0 + kBlockTokens - 1 > lim || (WIN && pos0 < from);
+      float top = -INFINITY;
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            // (the product with a power of two is exact: a sum rounded once)
+            float y = fmaf(__fmul_rn(sc[s][nt][e], back[nt][e & 1]), k_scale, v_exp);
+            if (some_bad && (k_bad >> (4 * s + 2 * (e >> 1) + (g & 1))) & 1) y = NAN;
+            if (masked) {
+              const int pos = page_pos + 4 * s + 2 * (e >> 1), c = e & 1;
+              const bool sees = (pos <= climit[nt][c] || (pos >= vlo[nt][c] && pos < vhi[nt][c])) && (!WIN || pos < P.n_sink || pos >= vfirst[nt][c]);
+              if (!sees) y = -INFINITY;
+            }
+            sc[s][nt][e] = y;
+            top = fmaxf(top, __fsub_rn(y, ref[nt][e & 1]));
+          }
+      if (__any_sync(0xffffffffu, top > kHeadroom + kLift)) {
+        // some row's reference moves: what has been summed up is scaled to the new one
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float z = -INFINITY;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) z = fmaxf(z, fmaxf(sc[s][nt][c], sc[s][nt][2 + c]));
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, x));
+            const float to = z - kLift;
+            const float next = to > ref[nt][c] + kHeadroom || ref[nt][c] == kNoRef ? fmaxf(ref[nt][c], to) : ref[nt][c];
+            const float f = exp2f(ref[nt][c] - next);
+            ref[nt][c] = next;
+            l[nt][c] *= f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+              o[nt][i][c] *= f;
+              o[nt][i][2 + c] *= f;
+            }
+          }
+      }
+      // ---- probabilities; O^T += C_V^T P^T ----
+      uint32_t b[4][NT][2];
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            p[e] = exp2f(__fsub_rn(sc[s][nt][e], ref[nt][e & 1]));
+            l[nt][e & 1] = fmaf(p[e], v_back, l[nt][e & 1]);
+            // (a row of V that is none makes those that see it none, not their sums)
+            if (some_bad && (v_bad >> (4 * s + 2 * (e >> 1) + (g & 1))) & 1 && sc[s][nt][e] != -INFINITY) p[e] = NAN;
+          }
+          b[s][nt][0] = transpose8x8(pack_f16(p[0], p[1]));
+          b[s][nt][1] = transpose8x8(pack_f16(p[2], p[3]));
+        }
+      const uint8_t* values = pg + t * SH::kPitch + 16 * D + g * 16;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const uint4 v0 = *reinterpret_cast<const uint4*>(values + i * 256), v1 = *reinterpret_cast<const uint4*>(values + i * 256 + 128);
+        const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const uint32_t a0 = e4m3_to_f16(w0[s] & 0xffffu), a1 = e4m3_to_f16(w1[s] & 0xffffu), a2 = e4m3_to_f16(w0[s] >> 16), a3 = e4m3_to_f16(w1[s] >> 16);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][i], a0, a1, a2, a3, b[s][nt][0], b[s][nt][1]);
+        }
+      }
+      __syncwarp();
+      request(slot_at);
+      slot_at = slot_at == (kSlots - 1) * SH::kSlot ? 0 : slot_at + SH::kSlot;
+    }
+
+    if (item + 1 < item_end) load_rows(item_of(item + 1));
+    __syncthreads();      // (the parts of the item before have been read)
+    // ---- the warps' parts meet: row (column 2 t + c of group nt), the values g and g + 8 of every sixteen that this lane holds ----
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float ls = l[nt][c];
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) ls += __shfl_xor_sync(0xffffffffu, ls, x);
+        float* row = merge + (warp * SH::kRows + nt * 8 + 2 * t + c) * SH::kRowPad;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          row[16 * i + g] = o[nt][i][c];
+          row[16 * i + 8 + g] = o[nt][i][2 + c];
+        }
+        if (g == 0) {
+          row[D] = ref[nt][c];
+          row[D + 1] = ls;
+        }
+      }
+    __syncthreads();
+    // a warp takes every kWarps-th row, a lane D / 32 consecutive values of it
+    for (int rr = warp; rr < R; rr += W) {
+      const float* part = merge + ((size_t)(rr / SH::kRows) * sh.warps * SH::kRows + rr % SH::kRows) * SH::kRowPad;   // of the group's first warp
+      constexpr int kPart = SH::kRows * SH::kRowPad;
+      const float m_mine = lane < sh.warps ? part[lane * kPart + D] : kNoRef, l_mine = lane < sh.warps ? part[lane * kPart + D + 1] : 0.f;
+      float m_all = m_mine;
+#pragma unroll
+      for (int x = 16; x; x >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, x));
+      const float f_mine = exp2f(m_mine - m_all);
+      float l_all = f_mine * l_mine;
+#pragma unroll
+      for (int x = 16; x; x >>= 1) l_all += __shfl_xor_sync(0xffffffffu, l_all, x);
+      constexpr int E = D / 32;
+      float acc[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll 4
+      for (int k = 0; k < sh.warps; ++k) {
+        const float f = __shfl_sync(0xffffffffu, f_mine, k);
+        const float* src = part + k * kPart + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(f, src[e], acc[e]);
+      }
+      const int rho = rr, j = rho / P.group;
+      if (w.part < 0) {
+        const size_t row = (size_t)(w.tok0 + j) * P.n_q + w.kv_head * P.group + rho - j * P.group;
+        const float inv = l_all > 0.f ? 1.f / l_all : 0.f * l_all;
+        uint32_t* dst = reinterpret_cast<uint32_t*>(P.o + row * D + lane * E);
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) dst[e] = pack_bf16(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+        if (P.lse && lane == 0) P.lse[row] = log_sum_exp(m_all, l_all);
+      } else {
+        float* dst = P.part_o + ((size_t)w.part * 128 + rho) * D + lane * E;
+        if constexpr (E == 4) *reinterpret_cast<float4*>(dst) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        else *reinterpret_cast<float2*>(dst) = make_float2(acc[0], acc[1]);
+        if (lane == 0) *reinterpret_cast<float2*>(P.part_ml + ((size_t)w.part * 128 + rho) * 2) = make_float2(m_all, l_all);
+      }
+    }
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+template <int D, int NT, bool WIN>
+void launch_rows(const Params& P, int n_sm, cudaStream_t st) {
+  static bool configured[kMaxDevices] = {false};
+  if (first_use_on_device(configured))
+    cudaFuncSetAttribute(attention_kv8_kernel<D, NT, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D, NT>::kTotal);
+  launch_pdl(attention_kv8_kernel<D, NT, WIN>, dim3(n_sm), dim3(Shape<D, NT>::kThreads), Shape<D, NT>::kTotal, st, P);
+}
+template <bool WIN>
+void launch_shape(int head_dim, int max_rows, const Params& P, int n_sm, cudaStream_t st) {
+  if (head_dim == 64) (max_rows <= 8 ? launch_rows<64, 1, WIN> : launch_rows<64, 2, WIN>)(P, n_sm, st);
+  else (max_rows <= 8 ? launch_rows<128, 1, WIN> : launch_rows<128, 2, WIN>)(P, n_sm, st);
+}
+
+}  // namespace
+
+void launch_attention_kv8(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
+                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int max_rows, int* status, cudaStream_t st, bool list_settled) {
+  Params P;
+  P.items = bl.items;
+  P.item_gap = bl.item_gap;
+  P.cta_off = bl.cta_off;
+  P.page_table = bl.page_table;
+  P.pt_stride = bl.pt_stride;
+  P.tok_climit = bl.tok_climit;
+  P.tok_lo = bl.tok_lo;
+  P.tok_hi = bl.tok_hi;
+  P.tok_first = bl.tok_first;
+  P.q = static_cast<const __nv_bfloat16*>(q);
+  P.o = static_cast<__nv_bfloat16*>(o);
+  P.lse = lse;
+  P.pool = static_cast<const uint8_t*>(kv_pool) + layer * kv8_layer_bytes(n_pages, dm.n_kv, dm.head_dim);
+  P.n_pages = n_pages;
+  P.n_q = dm.n_q;
+  P.n_kv = dm.n_kv;
+  P.group = dm.n_q / dm.n_kv;
+  P.inv_group = 65536 / P.group + 1;
+  P.n_sink = bl.n_sink;
+  P.sink_blocks = (bl.n_sink + kBlockTokens - 1) / kBlockTokens;
+  P.scale_log2 = 1.4426950408889634f / sqrtf((float)dm.head_dim);
+  P.part_o = part_o;
+  P.part_ml = part_ml;
+  P.status = status;
+  P.early_desc = list_settled ? 1 : 0;
+  (bl.window ? launch_shape<true> : launch_shape<false>)(dm.head_dim, max_rows, P, n_sm, st);
+}
+
+}  // namespace recg

@@ -81,12 +81,15 @@ static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
 
 struct TcAttnParams {
   const AttnItem* items;
+  const int* item_gap;
   const int* cta_off;
   const int* page_table;
   int pt_stride;
   const int* tok_climit;
   const int* tok_lo;
   const int* tok_hi;
+  const int* tok_first;
+  int n_sink, sink_blocks;   // a window: first tokens, and the 64-token blocks that hold them
   __nv_bfloat16* o;
   float* lse;         // log-sum-exp of every row and head (null: not wanted)
   const __nv_bfloat16* pool;
@@ -104,8 +107,9 @@ __device__ __forceinline__ int col_token(int c) { return c; }
 __device__ __forceinline__ void softmax_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 
-// LSE: the log-sum-exp of the rows is wanted
-template <bool LSE>
+// LSE: the log-sum-exp of the rows is wanted.  WIN: rows look back a window (recg_window); an item's 64-token blocks behind the first
+// tokens' lie `gap` further on, so that the two halves of a stage need not be neighbours.
+template <bool LSE, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_constant__ CUtensorMap qmap, TcAttnParams P) {
   extern __shared__ __align__(1024) uint8_t smem[];
   if (smem_u32(smem) & 1023u) {          // the swizzled operand layouts need a 1 KB aligned base
@@ -153,6 +157,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
   int item_end = 0;
   auto item_at = [&](int i) { return i < range_n0 ? range_b0 + i : range_b1 + (i - range_n0); };
   AttnItem w_next = {};
+  auto gap_of = [&](int i) { return WIN ? P.item_gap[item_at(i)] : 0; };
+  auto place = [&](int block, int gap) { return WIN && block >= P.sink_blocks ? block + gap : block; };
   if (warp == 0) {
     // (early_desc: an attention kernel has run since the work list was written, so the reads below overlap the kernel in front
     // of this one instead of following it.  Otherwise all warps meet behind this wait before any of them signals the dependents)
@@ -226,15 +232,21 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
         if (item + 1 < item_end) w_next = P.items[item_at(item + 1)];
         const int tok_begin = w.blk_begin * 64;
         const int tok_end = min(w.blk_end * 64, w.kv_len);
-        const int nblk = (tok_end - tok_begin + kBT - 1) / kBT;
+        const int nblk = WIN ? (w.blk_end - w.blk_begin + 1) / 2 : (tok_end - tok_begin + kBT - 1) / kBT;
+        const int gap = gap_of(item);
+        // the logical page of lane p < 8 in stage n, and whether the item has it
+        auto page_of = [&](int n) {
+          const int block = w.blk_begin + 2 * n + (lane >> 2);
+          return WIN ? (block < w.blk_end ? place(block, gap) * 4 + (lane & 3) : 1 << 30) : tok_begin / kPageSize + n * kPagesPerBT + lane;
+        };
         const int n_req_pages = (w.kv_len + kPageSize - 1) / kPageSize;
         const int* pt = P.page_table + (size_t)w.req * P.pt_stride;
         // page ids are fetched by lanes 0..7 in parallel, one iteration ahead of their use
         auto fetch_page = [&](int n) -> int {
           int pg = -1;
           if (lane < kPagesPerBT && n < nblk) {
-            const int lp = tok_begin / kPageSize + n * kPagesPerBT + lane;
-            if (lp < n_req_pages && lp * kPageSize < tok_end) pg = __ldg(pt + lp);   // validated when used
+            const int lp = page_of(n);
+            if (lp < n_req_pages && (WIN || lp * kPageSize < tok_end)) pg = __ldg(pt + lp);   // validated when used
           }
           return pg;
         };
@@ -262,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             my_pg = -1;
           }
           // lane p < 8 owns page p of the block: full pages go by bulk copy, the rest by hand
-          const int first_tok = tok_begin + (n * kPagesPerBT + lane) * kPageSize;
+          const int first_tok = WIN ? min(page_of(n), n_req_pages) * kPageSize : tok_begin + (n * kPagesPerBT + lane) * kPageSize;
           const int my_valid = (lane < kPagesPerBT && my_pg >= 0) ? min(kPageSize, w.kv_len - first_tok) : 0;
           // K: every existing page goes by bulk copy (rows beyond the request's end are masked in S).
           // V: full pages by bulk copy; the one partly filled page by hand with its stale rows zeroed (0 * stale
@@ -345,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
           if (item + 1 < item_end) w_next = P.items[item_at(item + 1)];
           const int tok_begin = w.blk_begin * 64;
           const int tok_end = min(w.blk_end * 64, w.kv_len);
-          const int nblk = (tok_end - tok_begin + kBT - 1) / kBT;
+          const int nblk = WIN ? (w.blk_end - w.blk_begin + 1) / 2 : (tok_end - tok_begin + kBT - 1) / kBT;
           const int buf = item_cnt & 1;
           const uint64_t dq0 = desc_kmajor(smem_base + kOffQ + buf * kQBytes);
           bwait(&q_full[buf], (item_cnt >> 1) & 1, DEV_TIMEOUT_FULL);
@@ -388,16 +400,17 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
     const uint32_t s_addr = lane_addr + g * 64, o_addr = lane_addr + kTmemO + g * D;
     uint32_t cs = 0, item_cnt = 0;   // stages and items so far
     // visibility triple of this thread's row, fetched one item ahead
-    auto row_vis = [&](const AttnItem& it, int& cl, int& lo, int& hi) {
-      cl = -1; lo = 0; hi = 0;
+    auto row_vis = [&](const AttnItem& it, int& cl, int& lo, int& hi, int& from) {
+      cl = -1; lo = 0; hi = 0; from = 0;
       if (row < it.ntok * P.group) {
         const int t = it.tok0 + row / P.group;
         cl = P.tok_climit[t];
         lo = P.tok_lo[t];
         hi = P.tok_hi[t];
+        if (WIN) from = P.tok_first[t];
       }
     };
-    int nx_cl = -1, nx_lo = 0, nx_hi = 0;
+    int nx_cl = -1, nx_lo = 0, nx_hi = 0, nx_from = 0;
     // The first turn of the loop is the one without effect: no row exists, nothing is waited for, signalled or stored but this
     // group's own O accumulator, which the first product overwrites.
     for (int item = item_begin - 1; item < item_end; ++item) {
@@ -410,10 +423,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
       const int R = w.ntok * P.group;
       const int tok_begin = w.blk_begin * 64;
       const int tok_end = min(w.blk_end * 64, w.kv_len);
-      const int nblk = dry ? 1 : (tok_end - tok_begin + kBT - 1) / kBT;
+      const int nblk = dry ? 1 : WIN ? (w.blk_end - w.blk_begin + 1) / 2 : (tok_end - tok_begin + kBT - 1) / kBT;
+      const int gap = dry ? 0 : gap_of(item);
       const bool rvalid = row < R;
       const bool warp_valid = dry || quad * 32 < R;
-      const int climit = nx_cl, vlo = nx_lo, vhi = nx_hi;
+      const int climit = nx_cl, vlo = nx_lo, vhi = nx_hi, vfirst = nx_from;
       // the row's reference maximum (in powers of two), the sum of its probabilities, the score above which the reference moves
       float m_ref = rvalid ? kNoRef : 0.f, l_run = 0.f, outgrown = INFINITY;
       const float inv_scale = 1.f / P.scale_log2;
@@ -424,21 +438,24 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
         const uint32_t s_buf = dry ? o_addr : s_addr + (cs & 1) * kBT;
         if (!dry) bwait(&s_full[cs & 1], (cs >> 1) & 1, DEV_TIMEOUT_MMA);
         tc_fence_after();
-        const int pos0 = tok_begin + n * kBT + g * 64;
+        const int block = w.blk_begin + 2 * n + g;
+        const int pos0 = WIN ? place(block, gap) * 64 : tok_begin + n * kBT + g * 64;
         uint32_t sr[2][32];   // the S row of this thread: 64 scores
         if (warp_valid) {
 #pragma unroll
           for (int c = 0; c < 2; ++c) tmem_ld32_nowait(s_buf + c * 32, sr[c]);
           tmem_ld_wait();
-          const int lim = min(climit, tok_end - 1);
-          const bool need_mask = __any_sync(0xffffffffu, rvalid && (pos0 + 63 > lim));
+          // (with a window: blk_end counts blocks, not positions; a block that the item does not have is seen by no row)
+          const int lim = WIN ? (block < w.blk_end ? climit : -1) : min(climit, tok_end - 1), end = WIN ? (block < w.blk_end ? vhi : -1) : min(vhi, tok_end);
+          const bool need_mask = __any_sync(0xffffffffu, rvalid && (pos0 + 63 > lim || (WIN && pos0 < vfirst)));
           if (need_mask) {
             // visible tokens of this row within the 64: [0, a] and [b, c), as a 64-bit mask over tokens
-            const int a = lim - pos0, b = vlo - pos0, cc = min(vhi, tok_end) - pos0;
+            const int a = lim - pos0, b = vlo - pos0, cc = end - pos0;
             auto ones = [](int n) -> unsigned long long {      // n lowest bits set, n clamped to [0, 64]
               return n <= 0 ? 0ull : (n >= 64 ? ~0ull : ((1ull << n) - 1ull));
             };
-            const unsigned long long m0 = ones(a + 1) | (ones(cc) & ~ones(b));
+            unsigned long long m0 = ones(a + 1) | (ones(cc) & ~ones(b));
+            if (WIN) m0 &= ones(P.n_sink - pos0) | ~ones(vfirst - pos0);
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -525,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
         if (lane == 0) mbar_arrive(&p_full[2 * g + (cs & 1)]);
         if (first) {      // the next item's descriptor has arrived by now: fetch its rows' visibility for later
           first = false;
-          if (item + 1 < item_end) row_vis(w_next, nx_cl, nx_lo, nx_hi);
+          if (item + 1 < item_end) row_vis(w_next, nx_cl, nx_lo, nx_hi, nx_from);
         }
       }
 
@@ -619,7 +636,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
       softmax_bar();          // the (max, sum) exchange area may be rewritten
       if (dry) {
         griddep_wait();
-        if (item_begin < item_end) row_vis(w_next, nx_cl, nx_lo, nx_hi);
+        if (item_begin < item_end) row_vis(w_next, nx_cl, nx_lo, nx_hi, nx_from);
       }
     }
   }
@@ -692,11 +709,15 @@ void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, 
                               cudaStream_t st, bool layout_settled) {
   static bool configured[kMaxDevices] = {false};
   if (first_use_on_device(configured))
-    for (auto* kernel : {attention_tc_kernel<false>, attention_tc_kernel<true>})
+    for (auto* kernel : {attention_tc_kernel<false, false>, attention_tc_kernel<true, false>, attention_tc_kernel<false, true>, attention_tc_kernel<true, true>})
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
 
   TcAttnParams P;
   P.items = bl.items;
+  P.item_gap = bl.item_gap;
+  P.tok_first = bl.tok_first;
+  P.n_sink = bl.n_sink;
+  P.sink_blocks = (bl.n_sink + 63) / 64;
   P.cta_off = bl.cta_off;
   P.page_table = bl.page_table;
   P.pt_stride = bl.pt_stride;
@@ -724,7 +745,8 @@ void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, 
     if (status) cudaMemcpyAsync(status, &code, sizeof(int), cudaMemcpyHostToDevice, st);
     return;
   }
-  launch_pdl(lse ? attention_tc_kernel<true> : attention_tc_kernel<false>, dim3(n_sm), dim3(kThreads), kSmemBytes, st, qmap, P);
+  launch_pdl(bl.window ? (lse ? attention_tc_kernel<true, true> : attention_tc_kernel<false, true>)
+                       : (lse ? attention_tc_kernel<true, false> : attention_tc_kernel<false, false>), dim3(n_sm), dim3(kThreads), kSmemBytes, st, qmap, P);
 }
 
 }  // namespace recg

@@ -51,8 +51,12 @@ struct BatchLayout {
   int* tok_climit;  // sees every cache position <= climit ...
   int* tok_lo;      // ... and every cache position in [lo, hi)
   int* tok_hi;
+  // recg_window(): a row sees, of what its mask shows, the first n_sink positions and those from tok_first on (window = 0: everything)
+  int n_sink, window;
+  int* tok_first;
   // attention work list
   AttnItem* items;
+  int* item_gap;    // with a window: blk_begin, blk_end leave out this many blocks behind those of the first n_sink positions
   AttnTile* tiles;
   int* cta_off;     // [4 n_ctas] per CTA of the persistent attention grid: the two item index ranges [b0, e0), [b1, e1) it walks
 #ifdef __CUDACC__
@@ -87,7 +91,7 @@ struct SmallDesc {
 void launch_layout(const BatchLayout& bl, const Dims& dm, int tok_per_tile, int n_ctas, bool whole, int64_t n_pages,
                    int* status, bool tokens, int* desc_dev, const SmallDesc* desc, cudaStream_t st, bool list = true);
 // HOST arrays [n_req]; rows: rows per request
-bool attention_whole_tiles(int n_req, const int* ctx_len, const int* rows, int n_kv, int tok_per_tile, int n_ctas);
+bool attention_whole_tiles(int n_req, const int* ctx_len, const int* rows, int n_kv, int tok_per_tile, int n_ctas, int n_sink, int window);
 // the layout kernel keeps five ints per request in shared memory: requests per step are bounded by this
 constexpr int kMaxLayoutRequests = 4096;
 size_t layout_smem_bytes(int n_req, int n_ctas);
@@ -218,10 +222,11 @@ bool launch_gemm_chain(void* s, const ChainOp* ops, int n_ops, int M, const Chai
 // layout_settled: an attention kernel has been enqueued behind the kernel that wrote the work list (and has waited for it):
 // the tcgen05 kernel then reads its work range before it waits for its predecessor
 // whole: the work list was laid out with whole tiles
+// bits: of the pool
 // tiles: the row tiles of all kv heads, cut or not (0: known on the device only); step: a projection follows
 void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, const void* kv_pool,
                       int64_t n_pages, float* part_o, float* part_ml, int tok_per_tile, int n_sm, int* status,
-                      cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, bool four = false,
+                      cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, int bits = 16,
                       float* lse = nullptr, int max_rows = 128);
 void launch_attention_tc_main(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse,
                               const void* kv_pool, int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status,
@@ -233,6 +238,10 @@ void launch_attention_kv4(const BatchLayout& bl, const Dims& dm, int layer, cons
 // ... on the tcgen05 tensor cores (head_dim 128); false: not launched (no tensor map over q)
 bool launch_attention_kv4_tc(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
                              int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status, cudaStream_t st);
+// the same over a pool in 8 bits: few rows, or head_dim 64
+void launch_attention_kv8(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
+                          int64_t n_pages, float* part_o, float* part_ml, int n_sm, int max_rows, int* status, cudaStream_t st,
+                          bool list_settled);
 size_t attention_smem_bytes(int head_dim);
 
 // S9b + S10
@@ -274,6 +283,15 @@ void launch_kv4_io(bool write, void* pool, int64_t n_pages, int layer, const Dim
 // K/V rows of the batch laid out last, rows row_stride elements apart, to or from their slots; four: a pool in 4 bits
 void launch_kv_rows(bool write, bool four, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, void* k,
                     void* v, int64_t row_stride, cudaStream_t st);
+
+// The same two for a pool in 8 bits.  staged: row t of k and v lies in slot t of a bf16 pool of row_stride pages, which k points to.
+void launch_kv8_io(bool write, void* pool, int64_t n_pages, int layer, const Dims& dm, const int* page_row, int pos0, int n_pos,
+                   void* k, void* v, cudaStream_t st);
+void launch_kv8_rows(bool write, bool staged, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, void* k, void* v,
+                     int64_t row_stride, cudaStream_t st);
+// q and k of the batch laid out last turned to their positions, k and v into the pool; q may be null
+void launch_append_rotary(int bits, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, const void* q, int64_t q_stride,
+                          void* q_out, const void* k, const void* v, int64_t kv_stride, cudaStream_t st);
 
 // The rows of a round that the QKV projection has left in a bf16 staging pool (row t in slot t of it) into a pool in 4 bits
 void launch_kv_stage(const BatchLayout& bl, const void* stage, int stage_pages, void* pool, int64_t n_pages, int layer, const Dims& dm,

@@ -1,0 +1,153 @@
+// The KV pool in 8 bits (RECG_FLAG_KV_8BIT).
+//
+// A block is the K (or V) of 16 tokens, a page, and one kv head.  With a the largest magnitude among its values
+//   e = the least whole number with a <= 448 2^e, within -60 .. 120 (0 where a is 0),  c = the e4m3 number nearest to x 2^-e
+// and a value stands for c 2^e, which is a bf16 number.  A scale that is a power of two costs no digits, as e4m3 is a floating-point
+// format itself: it decides only where values become too small for four digits (2^-6 2^e and below, 2^-14.8 of the largest) or
+// vanish (2^-24.8 of it).  So rounding a block again, to the e of rows that have come in, loses nothing above that line; and scales
+// leave the matrix products as exponents: they are added to scores in powers of two.
+// At e = 120 codes end at 240: 256 2^120 is no bf16 number.  A row (one token) with a value that is not finite has a flag, codes of 0, no part in e, and
+// reads back as NaN; so every code is a number, and 0 times a code is 0 wherever a mask or the end of a request makes a probability 0.
+//
+// Pool = [layer], each [page][kv_head] blocks of 32 d bytes, K codes and V codes, then [page][kv_head] headers of eight bytes:
+// K's e (16 bits, signed) and its rows' flags above it, the same of V; zeros are a block of zeros.  (Beside the codes a header would move every block off the 32-byte sectors.)
+//   K: token t at t d; at d = 128 the eight 16-byte chunks of a row are XOR-swizzled with t & 7: a page is two of the tensor core's
+//      canonical 128-byte-swizzle atoms, K-major, and a row-wise 16-byte read of the lanes of a warp is free of bank conflicts.
+//   V: value i of token t at 16 i + t: a lane finds the tokens of a page, along which V is contracted, in one 16-byte read.
+#pragma once
+#include "common.cuh"
+#include "kernels.h"
+
+namespace recg {
+
+__host__ __device__ constexpr int kv8_block_bytes(int d) { return 32 * d; }
+__host__ __device__ __forceinline__ size_t kv8_headers(int64_t n_pages, int n_kv, int d) { return (size_t)n_pages * n_kv * kv8_block_bytes(d); }
+__host__ __device__ __forceinline__ size_t kv8_layer_bytes(int64_t n_pages, int n_kv, int d) {
+  return (kv8_headers(n_pages, n_kv, d) + (size_t)n_pages * n_kv * 8 + 127) & ~(size_t)127;
+}
+template <int D>
+__device__ __forceinline__ int kv8_k_chunk(int tok, int c) { return tok * D + ((D == 128 ? c ^ (tok & 7) : c) << 4); }
+
+constexpr int kKv8Least = -60, kKv8Most = 120;
+__device__ __forceinline__ float kv8_pow2(int e) { return __int_as_float((127 + e) << 23); }       // 2^e, a normal number
+__device__ __forceinline__ int kv8_exponent(uint32_t header) { return (int)(int16_t)header; }
+__device__ __forceinline__ uint32_t kv8_flags(uint32_t header) { return header >> 16; }
+__device__ __forceinline__ uint32_t e4m3_to_f16(uint32_t two) {      // two codes (the low 16 bits) as a pair of fp16
+  uint32_t d;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((uint16_t)two));
+  return d;
+}
+__device__ __forceinline__ uint32_t e4m3_from(float lo, float hi) {
+  uint16_t d;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ float2 f16_pair(uint32_t h) {
+  float2 f;
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}" : "=f"(f.x), "=f"(f.y) : "r"(h));
+  return f;
+}
+
+// A block in the registers of a warp: of each of its 16 rows a lane has the values [D / 32 lane, D / 32 (lane + 1)), as pairs of bf16.
+template <int D>
+struct Kv8Block {
+  static constexpr int N = D / 64;
+  uint32_t x[16][N];
+};
+
+// Rows [0, n) as the pool holds them, and their flags.  K: codes in rows; V: a row of codes per value.
+template <int D, bool V>
+__device__ __forceinline__ uint32_t kv8_load(Kv8Block<D>& b, const uint8_t* codes, uint32_t header, int n, int lane) {
+  constexpr int N = Kv8Block<D>::N;
+  const float scale = kv8_pow2(kv8_exponent(header));
+  const uint32_t flags = kv8_flags(header);
+  uint32_t w[16];                                  // row's codes: 2 N of them
+  if (V) {
+    uint4 t[2 * N];
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i) t[i] = *reinterpret_cast<const uint4*>(codes + (2 * N * lane + i) * 16);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {                  // tokens 4 q .. 4 q + 3: a word of each of the lane's values
+      uint32_t a[2 * N];
+#pragma unroll
+      for (int i = 0; i < 2 * N; ++i) a[i] = q == 0 ? t[i].x : q == 1 ? t[i].y : q == 2 ? t[i].z : t[i].w;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t lo = __byte_perm(a[0], a[1], u | ((4 + u) << 4));
+        if constexpr (N == 2) w[4 * q + u] = __byte_perm(lo, __byte_perm(a[2], a[3], u | ((4 + u) << 4)), 0x5410);
+        else w[4 * q + u] = lo & 0xffffu;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      if constexpr (N == 2) w[r] = r < n ? *reinterpret_cast<const uint32_t*>(codes + kv8_k_chunk<D>(r, lane >> 2) + 4 * (lane & 3)) : 0u;
+      else w[r] = r < n ? *reinterpret_cast<const uint16_t*>(codes + kv8_k_chunk<D>(r, lane >> 3) + 2 * (lane & 7)) : 0u;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float2 f = f16_pair(e4m3_to_f16(i ? w[r] >> 16 : w[r] & 0xffffu));
+      b.x[r][i] = r >= n ? 0u : (flags >> r) & 1 ? 0x7fc07fc0u : pack_bf16(f.x * scale, f.y * scale);
+    }
+  return flags & ((1u << n) - 1u);
+}
+
+// Stores rows [0, n) as codes, the others as 0, and returns the header.
+template <int D, bool V>
+__device__ __forceinline__ uint32_t kv8_store(const Kv8Block<D>& b, uint8_t* codes, int n, int lane) {
+  constexpr int N = Kv8Block<D>::N;
+  uint32_t bad = 0;
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t a = b.x[r][i] & 0x7fff7fffu;
+      if ((a & 0xffffu) >= 0x7f80u || a >= 0x7f800000u) bad |= 1u << r;
+    }
+  bad = __reduce_or_sync(0xffffffffu, bad) & ((1u << n) - 1u);
+  uint32_t top = 0;                                // largest magnitude, as the bits of a bf16 number
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (r < n && !((bad >> r) & 1)) top = __vmaxu2(top, b.x[r][i] & 0x7fff7fffu);
+  top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+  // 2^(f - 127) (1 + m / 128) <= 1.75 2^8 2^e
+  const int e = top == 0 ? 0 : max(kKv8Least, min(kKv8Most, (int)(top >> 7) - 127 - 8 + ((top & 127) > 96 ? 1 : 0)));
+  const float down = kv8_pow2(-e), end = e == kKv8Most ? 240.f : 448.f;
+  uint32_t w[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const bool live = r < n && !((bad >> r) & 1);
+    w[r] = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float lo = __uint_as_float(b.x[r][i] << 16) * down, hi = __uint_as_float(b.x[r][i] & 0xffff0000u) * down;
+      w[r] |= e4m3_from(fmaxf(-end, fminf(end, lo)), fmaxf(-end, fminf(end, hi))) << (16 * i);
+    }
+    if (!live) w[r] = 0;
+    if constexpr (!V) {
+      if constexpr (N == 2) *reinterpret_cast<uint32_t*>(codes + kv8_k_chunk<D>(r, lane >> 2) + 4 * (lane & 3)) = w[r];
+      else *reinterpret_cast<uint16_t*>(codes + kv8_k_chunk<D>(r, lane >> 3) + 2 * (lane & 7)) = (uint16_t)w[r];
+    }
+  }
+  if constexpr (V) {
+    uint32_t t[2 * N][4];                          // of each of the lane's values the 16 tokens
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int i = 0; i < 2 * N; ++i) {
+        const uint32_t sel = i | ((4 + i) << 4);
+        t[i][q] = __byte_perm(__byte_perm(w[4 * q], w[4 * q + 1], sel), __byte_perm(w[4 * q + 2], w[4 * q + 3], sel), 0x5410);
+      }
+#pragma unroll
+    for (int i = 0; i < 2 * N; ++i)
+      *reinterpret_cast<uint4*>(codes + (2 * N * lane + i) * 16) = make_uint4(t[i][0], t[i][1], t[i][2], t[i][3]);
+  }
+  return (uint32_t)(e & 0xffff) | (bad << 16);
+}
+
+}  // namespace recg

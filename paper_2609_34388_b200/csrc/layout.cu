@@ -1,4 +1,6 @@
 // Ragged layout (per-token arrays + attention work list), embedding gather, RMSNorm, KV import/export.
+#include <algorithm>
+
 #include "common.cuh"
 #include "kernels.h"
 
@@ -102,6 +104,7 @@ __device__ __forceinline__ TokenPos layout_token(const BatchLayout& bl, int r, i
     lo = first;
     hi = q == 0 ? first + 1 : first + span;
   }
+  bl.tok_first[t] = bl.window ? max(pos - bl.window + 1, 0) : 0;
   if (bl.pos_shift) pos += bl.pos_shift[r];
   bl.tok_weight[t] = j < v ? 1.f : 0.f;
   bl.tok_req[t] = r;
@@ -182,7 +185,9 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, 
   }
   __syncthreads();
   // segment s of a line: its request, kv head, (first) tile and KV blocks
-  struct Seg { int r, kvh, tile, nb; };
+  // (gap: of a window, the blocks behind those of the first tokens that no row of the tiles sees)
+  struct Seg { int r, kvh, tile, nb, gap; };
+  const int sink_blocks = (bl.n_sink + 63) / 64;
   auto segment = [&](const int* first, int s, bool pair) {
     Seg g;
     g.r = upper_request(first, C, s);
@@ -193,6 +198,12 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, 
     // the last of the segment's rows: causal up to itself if it is a verify row, else anything up to the request's end
     const int last_row = min(n, (g.tile + (pair ? 2 : 1)) * tok_per_tile);
     g.nb = (ctx[g.r] + (last_row <= vis[g.r] ? last_row : n) + 63) / 64;
+    g.gap = 0;
+    if (bl.window) {        // rows stand one behind the other, but for those of branches, whose positions lie behind ctx
+      const int first = ctx[g.r] + (last_row <= vis[g.r] + bl.block_size[g.r] ? g.tile * tok_per_tile : 0) - bl.window + 1;
+      g.gap = max(0, first / 64 - sink_blocks);
+      g.nb -= g.gap;
+    }
     return g;
   };
   for (int line = 0; line < 2; ++line) {
@@ -235,7 +246,7 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, 
     int off = 0, pieces = 0;             // cost units and pieces of the line so far
     for (int s0 = 0; s0 < n_seg; s0 += kLayoutThreads) {
       const int s = s0 + tid;
-      Seg g{0, 0, 0, 0};
+      Seg g{0, 0, 0, 0, 0};
       if (s < n_seg) g = segment(first, s, pair);
       Scan3 tot;
       const Scan3 e1 = block_scan(Scan3{s < n_seg ? g.nb + item_cost : 0, 0, 0}, &tot, scratch);
@@ -278,7 +289,10 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, 
           a.blk_end = whole ? g.nb : min(g0 + g.nb, (c + 1) * per) - g0;
           a.part = np > 1 ? part++ : -1;
           a.kv_len = kv_len;
-          if (at + (c - c_first) < bl.max_items && a.part < bl.max_parts) bl.items[at + (c - c_first)] = a;
+          if (at + (c - c_first) < bl.max_items && a.part < bl.max_parts) {
+            bl.items[at + (c - c_first)] = a;
+            bl.item_gap[at + (c - c_first)] = g.gap;
+          }
         }
       }
     }
@@ -544,11 +558,14 @@ size_t layout_smem_bytes(int n_req, int n_ctas) {
 // partial results, the combine kernel and its boundary, about 2.5 us.  Measured (one request, 16 rows, a layer's attention): 64
 // tokens of context 6.3 us whole, 8.8 cut; 256 tokens 8.7 and 9.1; 512 tokens 10.8 and 10.3; with head_dim 64 4.3 and 5.8, 5.8
 // and 6.0, 7.8 and 6.4.
-bool attention_whole_tiles(int n_req, const int* ctx_len, const int* rows, int n_kv, int tok_per_tile, int n_ctas) {
+// (With a window a tile has the blocks of the first tokens and of its window, more or less.)
+bool attention_whole_tiles(int n_req, const int* ctx_len, const int* rows, int n_kv, int tok_per_tile, int n_ctas, int n_sink, int window) {
   long long tiles = 0, cost = 0;
   int longest = 0;
   for (int r = 0; r < n_req; ++r) {
-    const int rt = (rows[r] + tok_per_tile - 1) / tok_per_tile, nb = (ctx_len[r] + rows[r] + 63) / 64;
+    const int rt = (rows[r] + tok_per_tile - 1) / tok_per_tile;
+    int nb = (ctx_len[r] + rows[r] + 63) / 64;
+    if (window) nb = (int)std::min<long long>(nb, ((long long)n_sink + window + std::min(rows[r], 2 * tok_per_tile)) / 64 + 2);
     tiles += (long long)n_kv * rt;
     cost += (long long)n_kv * (rt * nb + (rt & ~1) * kItemCostPair + (rt & 1) * kItemCostSingle);
     if (nb > longest) longest = nb;

@@ -10,6 +10,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "kv4.cuh"
+#include "kv8.cuh"
 
 using namespace recg;
 
@@ -59,6 +60,7 @@ struct recg_ctx {
   bool layout_valid = false;
   bool layout_has_pages = false;
   bool list_pending = false;     // its work list has not been built: only operations on rows have asked for the batch so far
+  bool window_pending = false;   // neither have what its rows see and its work list been built for the window of recg_window()
   bool layout_whole = false;     // no attention tile was cut: no combine kernel
   int layout_rows = 128;         // query rows of its largest row tile (128: the lengths are on the device)
   int layout_tiles = 0;          // its row tiles, all kv heads (0: the lengths are on the device)
@@ -97,7 +99,7 @@ struct recg_ctx {
   std::vector<int> h_rows;
   SmallDesc small_desc{};        // the descriptor laid out last, where it is small enough to travel with the launches (n > 0)
   std::vector<int> h_page_owner;   // debug checks: which request names a page
-  // RECG_FLAG_KV_4BIT: the QKV projection writes a round's rows to a bf16 pool of their own, row t in slot t, from where they are coded
+  // RECG_FLAG_KV_4BIT, _8BIT: the QKV projection writes a round's rows to a bf16 pool of their own, row t in slot t, from where they are coded
   void* stage = nullptr;
   int stage_pages = 0;
   int* d_stage_slot = nullptr;
@@ -109,6 +111,7 @@ struct recg_ctx {
   std::vector<int> h_evict;
   std::vector<int> h_page_seen;    // per page the set of pages (a number) that it was put into last
   int page_set = 0;
+  int pages_taken = -1;            // whether a page that takes new rows of it is named twice
   int pages_shared = -1;           // whether the batch laid out last names a page twice (-1: not looked at yet)
   // optional per-class timing
   bool timing = false;
@@ -146,6 +149,8 @@ recg_status fail(recg_ctx* c, recg_status s, const std::string& msg) {
   } while (0)
 
 bool four_bits(const recg_ctx* ctx) { return ctx->cfg.flags & RECG_FLAG_KV_4BIT; }
+bool eight_bits(const recg_ctx* ctx) { return ctx->cfg.flags & RECG_FLAG_KV_8BIT; }
+int kv_bits(const recg_ctx* ctx) { return four_bits(ctx) ? 4 : eight_bits(ctx) ? 8 : 16; }
 // Layers of a pool that operations are given (a context without layers runs them on a pool of one).
 int pool_layers(const recg_ctx* ctx) { return ctx->cfg.n_layers > 0 ? ctx->cfg.n_layers : 1; }
 
@@ -167,6 +172,8 @@ size_t carve(recg_ctx* c, DeviceArena& A) {
   bl.max_parts = 4 * c->target_items;      // two lines of work, each cut at fewer than target_items places (see layout.cu)
   bl.max_items = (int)(4 * c->target_items + max_tiles);
   bl.items = A.take<AttnItem>(bl.max_items);
+  bl.item_gap = A.take<int>(bl.max_items);
+  bl.tok_first = A.take<int>(Tm);
   bl.tiles = A.take<AttnTile>(max_tiles);
   bl.cta_off = A.take<int>(4 * (c->target_items + 1));
   bl.counts = A.take<int>(4);
@@ -210,7 +217,7 @@ size_t carve(recg_ctx* c, DeviceArena& A) {
     const size_t esz = (g.flags & RECG_FLAG_LOGITS_BF16) ? 2 : 4;
     c->logits = A.take<uint8_t>(Tm * (size_t)d.vocab * esz);
     c->lse = A.take<float>(Tm * d.n_q);
-    if (four_bits(c)) {
+    if (kv_bits(c) < 16) {
       c->stage_pages = (int)((Tm + kPageSize - 1) / kPageSize);
       c->stage = A.take<__nv_bfloat16>((size_t)c->stage_pages * d.n_kv * 2 * kv_tile_elems(d.head_dim));
       c->d_stage_slot = A.take<int>(Tm);
@@ -260,8 +267,8 @@ recg_status pack_batch(recg_ctx* ctx, const recg_batch* b, bool need_pages, bool
   const bool pages = b->page_table != nullptr;
   if (need_pages && (!pages || !b->kv_pool || b->kv_pool_pages <= 0))
     return fail(ctx, RECG_ERR_INVALID_ARG, "batch: page_table and kv_pool are required");
-  if (four_bits(ctx) && (reinterpret_cast<uintptr_t>(b->kv_pool) & 15))
-    return fail(ctx, RECG_ERR_INVALID_ARG, "batch: a KV pool in 4 bits must be 16-byte aligned");
+  if (kv_bits(ctx) < 16 && (reinterpret_cast<uintptr_t>(b->kv_pool) & 15))
+    return fail(ctx, RECG_ERR_INVALID_ARG, "batch: a KV pool in 4 or 8 bits must be 16-byte aligned");
   if (pages && (b->page_table_stride <= 0 || b->page_table_stride > ctx->cfg.max_pages_per_request))
     return fail(ctx, RECG_ERR_CAPACITY, "batch: page_table_stride exceeds max_pages_per_request");
   if (b->n_corr && (!b->corr_index || !b->corr_token || !b->corr_block))
@@ -414,12 +421,14 @@ recg_status upload_and_layout(recg_ctx* ctx, const recg_batch* b, bool need_page
     ctx->layout_rows = most * (ctx->dm.n_q / ctx->dm.n_kv);
     tiles *= ctx->dm.n_kv;
     ctx->layout_tiles = tiles < (1 << 20) ? (int)tiles : 1 << 20;
-    ctx->layout_whole = attention_whole_tiles(b->n_req, b->ctx_len, ctx->h_rows.data(), ctx->dm.n_kv, ctx->tok_per_tile, ctx->target_items);
+    ctx->layout_whole = attention_whole_tiles(b->n_req, b->ctx_len, ctx->h_rows.data(), ctx->dm.n_kv, ctx->tok_per_tile, ctx->target_items,
+                                              ctx->bl.n_sink, ctx->bl.window);
     launch_layout(ctx->bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, ctx->layout_whole, n_pages, ctx->d_status,
                   !forward, ctx->d_desc, small ? &ctx->small_desc : nullptr, ctx->stream, list);
     ctx->list_settled = false;
     ctx->list_pending = !list;
-    ctx->pages_shared = -1;
+    ctx->window_pending = false;
+    ctx->pages_shared = ctx->pages_taken = -1;
     if (forward) embed_tokens(ctx, n_pages);
   }
   CU(cudaGetLastError());
@@ -452,6 +461,29 @@ recg_status gathers(recg_ctx* ctx, const char* who) {
   return RECG_OK;
 }
 
+// Whether the rows of the batch laid out last can go into a pool in 8 bits: a page that takes new rows is written whole, so it must not take
+// another request's as well.  (Of a device-resident round nothing looks for this, as above.)
+recg_status appends(recg_ctx* ctx, const char* who) {
+  if (!eight_bits(ctx) || ctx->bl.dyn) return RECG_OK;
+  if (ctx->pages_taken < 0) {
+    const int C = ctx->bl.n_req, stride = ctx->bl.pt_stride;
+    const int* table = ctx->h_desc.data() + ctx->h_desc.size() - (size_t)C * stride;
+    int taken = 0;
+    try {
+      new_pages(ctx);
+      for (int r = 0; r < C && !taken; ++r)
+        for (int i = ctx->h_desc[r] / kPageSize; i <= (ctx->h_desc[r] + ctx->h_rows[r] - 1) / kPageSize; ++i)
+          taken |= page_seen(ctx, table[(size_t)r * stride + i]);
+    } catch (const std::bad_alloc&) {
+      return fail(ctx, RECG_ERR_CAPACITY, std::string(who) + ": out of host memory");
+    }
+    ctx->pages_taken = taken;
+  }
+  if (ctx->pages_taken)
+    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": a page of a pool in 8 bits that takes new rows is named twice");
+  return RECG_OK;
+}
+
 recg_status run_gemm(recg_ctx* ctx, const GemmArgs& a, int* ss_slots_out = nullptr) {
   bool done = false;
   if (!(ctx->cfg.flags & RECG_FLAG_SIMT_GEMM)) done = launch_gemm_tc(a, ctx->tc_state, ctx->d_status, ctx->stream, ss_slots_out);
@@ -479,6 +511,7 @@ size_t recg_kv_pool_bytes(const recg_config* cfg, int64_t n_pages) {
   if (!cfg || n_pages <= 0) return 0;
   if (cfg->flags & RECG_FLAG_KV_4BIT)
     return (size_t)cfg->n_layers * (size_t)n_pages * cfg->n_kv_heads * kv4_block_bytes(cfg->head_dim);
+  if (cfg->flags & RECG_FLAG_KV_8BIT) return (size_t)cfg->n_layers * kv8_layer_bytes(n_pages, cfg->n_kv_heads, cfg->head_dim);
   return (size_t)cfg->n_layers * (size_t)n_pages * cfg->n_kv_heads * 2 * kPageSize * cfg->head_dim * 2;
 }
 
@@ -501,6 +534,8 @@ recg_status recg_init(recg_ctx** out, const recg_config* cfg, const recg_weights
   if (group > 16) return fail(ctx, RECG_ERR_SHAPE, "recg_init: at most 16 query heads per kv head");
   if (g.hidden % 64 || g.ffn % 64 || g.vocab % 16 || ((g.n_q_heads + 2 * g.n_kv_heads) * g.head_dim) % 128)
     return fail(ctx, RECG_ERR_SHAPE, "recg_init: hidden and ffn must be multiples of 64, vocab of 16, qkv width of 128");
+  if ((g.flags & RECG_FLAG_KV_4BIT) && (g.flags & RECG_FLAG_KV_8BIT))
+    return fail(ctx, RECG_ERR_INVALID_ARG, "recg_init: a KV pool is in 4 bits or in 8, not both");
   if (g.mask_token_id >= g.vocab) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_init: mask_token_id outside the vocabulary");
   if (w && g.n_layers > 0 &&
       (!w->embed || !w->final_norm || !w->lm_head || !w->attn_norm || !w->wqkv || !w->wo || !w->ffn_norm ||
@@ -666,8 +701,8 @@ static recg_status run_forward(recg_ctx* ctx, void* kv_pool, int64_t kv_pool_pag
   // (RECG_FLAG_CHAIN: steps of at most 128 rows run the projections between two attention calls as one persistent kernel)
   cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
   // (not with a staged or observed K/V: the chain has the next layer's QKV projection inside)
-  const bool four = four_bits(ctx);
-  const bool chain = ctx->chain_state && !four && !ctx->track && !bl.dyn && T <= 128 && d.n_layers > 0 && (d.n_q * d.head_dim) % 64 == 0 &&
+  const bool four = four_bits(ctx), staged = kv_bits(ctx) < 16;
+  const bool chain = ctx->chain_state && !staged && !ctx->track && !bl.dyn && T <= 128 && d.n_layers > 0 && (d.n_q * d.head_dim) % 64 == 0 &&
                      d.hidden % 128 == 0 && d.ffn % 64 == 0 &&
                      cudaStreamIsCapturing(st, &cap) == cudaSuccess && cap == cudaStreamCaptureStatusNone;
   const bool fold = folds_norm(ctx);
@@ -707,18 +742,19 @@ static recg_status run_forward(recg_ctx* ctx, void* kv_pool, int64_t kv_pool_pag
     a.w = ctx->wqkv[l]; a.out = ctx->q;
     a.M = T; a.N = (d.n_q + 2 * d.n_kv) * d.head_dim; a.epi = EPI_QKV_ROPE;
     a.tok_pos = bl.tok_pos;
-    a.tok_slot = four ? ctx->d_stage_slot : bl.tok_slot;
-    a.kv_pool = four ? ctx->stage : kv_pool;
-    a.n_pages = four ? ctx->stage_pages : kv_pool_pages;
-    a.layer = four ? 0 : l; a.n_q = d.n_q; a.n_kv = d.n_kv; a.head_dim = d.head_dim; a.rope_cs = ctx->rope_cs;
+    a.tok_slot = staged ? ctx->d_stage_slot : bl.tok_slot;
+    a.kv_pool = staged ? ctx->stage : kv_pool;
+    a.n_pages = staged ? ctx->stage_pages : kv_pool_pages;
+    a.layer = staged ? 0 : l; a.n_q = d.n_q; a.n_kv = d.n_kv; a.head_dim = d.head_dim; a.rope_cs = ctx->rope_cs;
     if ((s = run_gemm(ctx, a)) != RECG_OK) return s;
     if (four) launch_kv_stage(bl, ctx->stage, ctx->stage_pages, kv_pool, kv_pool_pages, l, d, st);
-    ctx->mark(2, four ? 2 : 1);
+    else if (staged) launch_kv8_rows(true, true, bl, kv_pool, kv_pool_pages, l, d, ctx->stage, nullptr, ctx->stage_pages, st);
+    ctx->mark(2, staged ? 2 : 1);
     }
     // (the first layer's attention kernel may be resident while the work list is still being built: idle lanes of a projection
     // signal its dependents before the projection has waited)
     launch_attention(bl, d, l, ctx->q, ctx->o, kv_pool, kv_pool_pages, ctx->part_o, ctx->part_ml, ctx->tok_per_tile, ctx->n_sm,
-                     ctx->d_status, st, !(ctx->cfg.flags & RECG_FLAG_SIMT_ATTENTION), ctx->list_settled, ctx->layout_whole, ctx->layout_tiles, true, four,
+                     ctx->d_status, st, !(ctx->cfg.flags & RECG_FLAG_SIMT_ATTENTION), ctx->list_settled, ctx->layout_whole, ctx->layout_tiles, true, kv_bits(ctx),
                      ctx->track ? ctx->lse : nullptr, ctx->layout_rows);
     if (ctx->track)
       launch_kv_weights(bl, d, l, ctx->q, ctx->lse, bl.tok_weight, ctx->track_decay, ctx->track, ctx->track, kv_pool, kv_pool_pages, four,
@@ -802,6 +838,7 @@ recg_status recg_step(recg_ctx* ctx, const recg_batch* batch, recg_logits* logit
   ctx->mark(-1);
   recg_status s = upload_and_layout(ctx, batch, true, true, true);
   if (s == RECG_OK && ctx->track) s = gathers(ctx, "recg_step");
+  if (s == RECG_OK) s = appends(ctx, "recg_step");
   if (s != RECG_OK) return s;
   return run_forward(ctx, batch->kv_pool, batch->kv_pool_pages, 0, logits);
 }
@@ -811,7 +848,7 @@ static recg_status check_device_batch(recg_ctx* ctx, const recg_device_batch* b,
   if (!b || b->n_req <= 0 || !b->ctx_len || !b->verify_len || !b->block_size || !b->verify_tokens || !b->page_table ||
       !b->kv_pool || b->kv_pool_pages <= 0)
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": null array, n_req <= 0 or no KV pool");
-  if ((four_bits(ctx) || ctx->track) && !aligned16(b->kv_pool, b->kv_pool))
+  if ((kv_bits(ctx) < 16 || ctx->track) && !aligned16(b->kv_pool, b->kv_pool))
     return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": kv_pool must be 16-byte aligned");
   if (b->n_req > ctx->cfg.max_requests) return fail(ctx, RECG_ERR_CAPACITY, std::string(who) + ": n_req exceeds max_requests");
   if (b->max_verify < 1 || b->max_verify > ctx->cfg.max_tokens)
@@ -867,7 +904,7 @@ recg_status recg_step_device(recg_ctx* ctx, const recg_device_batch* b, recg_log
   ctx->layout_rows = 128;
   launch_layout(bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, false, b->kv_pool_pages, ctx->d_status, false, ctx->d_desc, nullptr, ctx->stream);
   ctx->list_settled = false;
-  ctx->list_pending = false;
+  ctx->list_pending = ctx->window_pending = false;
   ctx->small_desc.n = 0;
   embed_tokens(ctx, b->kv_pool_pages);
   CU(cudaGetLastError());
@@ -1040,27 +1077,30 @@ static recg_status operation_batch(recg_ctx* ctx, const recg_batch* batch, int32
     return s;
   }
   if (!has_batch(ctx)) return no_batch(ctx, who);
-  if (list && ctx->list_pending) {
+  if (list && (ctx->list_pending || ctx->window_pending)) {
     // (the descriptor is in device memory by now; a captured launch builds nothing yet, so the list stays pending)
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
     CU(cudaStreamIsCapturing(ctx->stream, &cap));
-    launch_layout(ctx->bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, ctx->layout_whole, ctx->last_pool_pages, ctx->d_status, false,
-                  ctx->d_desc, nullptr, ctx->stream);
+    if (ctx->window_pending && !ctx->bl.dyn)
+      ctx->layout_whole = attention_whole_tiles(ctx->bl.n_req, ctx->h_desc.data(), ctx->h_rows.data(), ctx->dm.n_kv, ctx->tok_per_tile,
+                                                ctx->target_items, ctx->bl.n_sink, ctx->bl.window);
+    launch_layout(ctx->bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, ctx->layout_whole, ctx->last_pool_pages, ctx->d_status,
+                  ctx->window_pending, ctx->d_desc, nullptr, ctx->stream);
     CU(cudaGetLastError());
     ctx->list_settled = false;
-    ctx->list_pending = cap != cudaStreamCaptureStatusNone;
+    if (cap == cudaStreamCaptureStatusNone) ctx->list_pending = ctx->window_pending = false;
   }
   return RECG_OK;
 }
 
 
 static recg_status attention(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, void* o, float* lse, const char* who) {
-  if (four_bits(ctx) && !aligned16(q, o)) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": q and o must be 16-byte aligned");
+  if (kv_bits(ctx) < 16 && !aligned16(q, o)) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": q and o must be 16-byte aligned");
   recg_status s = operation_batch(ctx, batch, layer, who);
   if (s != RECG_OK) return s;
   launch_attention(ctx->bl, ctx->dm, layer, q, o, ctx->last_pool, ctx->last_pool_pages, ctx->part_o, ctx->part_ml,
                    ctx->tok_per_tile, ctx->n_sm, ctx->d_status, ctx->stream, !(ctx->cfg.flags & RECG_FLAG_SIMT_ATTENTION),
-                   ctx->list_settled, ctx->layout_whole, ctx->layout_tiles, false, four_bits(ctx), lse, ctx->layout_rows);
+                   ctx->list_settled, ctx->layout_whole, ctx->layout_tiles, false, kv_bits(ctx), lse, ctx->layout_rows);
   CU(cudaGetLastError());
   ctx->list_settled = true;
   return RECG_OK;
@@ -1081,13 +1121,13 @@ static recg_status kv_io(recg_ctx* ctx, bool write, void* pool, int64_t n_pool_p
   if (pos0 < 0 || n_pos < 0 || n_table <= 0 || n_table > ctx->cfg.max_pages_per_request || layer < 0 ||
       layer >= pool_layers(ctx) || n_pool_pages <= 0)
     return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_*: bad position range, layer or table length");
-  if (four_bits(ctx) && (!aligned16(k, v) || !aligned16(pool, pool)))
+  if (kv_bits(ctx) < 16 && (!aligned16(k, v) || !aligned16(pool, pool)))
     return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_*: k, v and the pool must be 16-byte aligned");
   if (n_pos == 0) return RECG_OK;
   if (((int64_t)pos0 + n_pos - 1) / kPageSize >= n_table) return fail(ctx, RECG_ERR_CAPACITY, "recg_kv_*: positions beyond the page table row");
   for (int i = pos0 / kPageSize; i <= (pos0 + n_pos - 1) / kPageSize; ++i)
     if (row[i] < 0 || row[i] >= n_pool_pages) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_*: page id outside the pool");
-  (four_bits(ctx) ? launch_kv4_io : launch_kv_io)(write, pool, n_pool_pages, layer, ctx->dm, row, pos0, n_pos, k, v, ctx->stream);
+  (four_bits(ctx) ? launch_kv4_io : eight_bits(ctx) ? launch_kv8_io : launch_kv_io)(write, pool, n_pool_pages, layer, ctx->dm, row, pos0, n_pos, k, v, ctx->stream);
   CU(cudaGetLastError());
   return RECG_OK;
 }
@@ -1116,7 +1156,9 @@ static recg_status kv_rows(recg_ctx* ctx, bool write, const recg_batch* batch, i
   recg_status s = operation_batch(ctx, batch, layer, who, write);
   if (s != RECG_OK) return s;
   if (!aligned16(ctx->last_pool, ctx->last_pool)) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": the KV pool must be 16-byte aligned");
-  launch_kv_rows(write, four_bits(ctx), ctx->bl, ctx->last_pool, ctx->last_pool_pages, layer, ctx->dm, k, v, row_stride, ctx->stream);
+  if (write && (s = appends(ctx, who)) != RECG_OK) return s;
+  if (eight_bits(ctx)) launch_kv8_rows(write, false, ctx->bl, ctx->last_pool, ctx->last_pool_pages, layer, ctx->dm, k, v, row_stride, ctx->stream);
+  else launch_kv_rows(write, four_bits(ctx), ctx->bl, ctx->last_pool, ctx->last_pool_pages, layer, ctx->dm, k, v, row_stride, ctx->stream);
   CU(cudaGetLastError());
   return RECG_OK;
 }
@@ -1127,9 +1169,32 @@ recg_status recg_kv_rows(recg_ctx* ctx, const recg_batch* batch, int32_t layer, 
   return kv_rows(ctx, false, batch, layer, k, v, row_stride, "recg_kv_rows");
 }
 
+recg_status recg_kv_append_rotary(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, int64_t q_stride, void* q_out,
+                                  const void* k, const void* v, int64_t kv_stride) {
+  const char* who = "recg_kv_append_rotary";
+  if (!ctx) return RECG_ERR_INVALID_ARG;
+  if (!batch && !has_batch(ctx)) return no_batch(ctx, who);
+  if (!k || !v || !q != !q_out) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": k or v is null, or one of q and q_out");
+  const int64_t q_width = (int64_t)ctx->dm.n_q * ctx->dm.head_dim, kv_width = (int64_t)ctx->dm.n_kv * ctx->dm.head_dim;
+  if (q_stride == 0) q_stride = q_width;
+  if (kv_stride == 0) kv_stride = kv_width;
+  if (kv_stride < kv_width || kv_stride > INT32_MAX || kv_stride % 8 || (q && (q_stride < q_width || q_stride > INT32_MAX || q_stride % 8)) ||
+      !aligned16(k, v) || !aligned16(q, q_out))
+    return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": rows must be 16-byte aligned and at least their heads' elements apart");
+  recg_status s = operation_batch(ctx, batch, layer, who);
+  if (s != RECG_OK) return s;
+  if (!aligned16(ctx->last_pool, ctx->last_pool)) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": the KV pool must be 16-byte aligned");
+  if ((s = appends(ctx, who)) != RECG_OK) return s;
+  launch_append_rotary(kv_bits(ctx), ctx->bl, ctx->last_pool, ctx->last_pool_pages, layer, ctx->dm, q, q_stride, q_out, k, v, kv_stride, ctx->stream);
+  CU(cudaGetLastError());
+  return RECG_OK;
+}
+
 recg_status recg_kv_weights(recg_ctx* ctx, const recg_batch* batch, int32_t layer, const void* q, const float* lse,
                             const float* row_weight, float decay, const float* weights_in, float* weights_out) {
   if (!ctx || !q || !lse || !weights_out) return RECG_ERR_INVALID_ARG;
+  if (ctx->bl.window) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: not with a window (recg_window)");
+  if (eight_bits(ctx)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: not of a pool in 8 bits");
   if (!(decay >= 0.f && decay <= 3e38f)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: decay must be a finite number >= 0");
   if (!aligned16(q, q) || !aligned16(weights_in, weights_out))
     return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_weights: q, weights_in and weights_out must be 16-byte aligned");
@@ -1215,6 +1280,8 @@ static recg_status evict_batch(recg_ctx* ctx, const recg_eviction* e, int32_t ke
 recg_status recg_kv_track(recg_ctx* ctx, float* weights, float decay) {
   if (!ctx) return RECG_ERR_INVALID_ARG;
   if (!ctx->has_weights) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_track: the context was created without weights");
+  if (weights && ctx->bl.window) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_track: not with a window (recg_window)");
+  if (weights && eight_bits(ctx)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_track: not of a pool in 8 bits");
   if (!aligned16(weights, weights)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_track: weights must be 16-byte aligned");
   if (!(decay >= 0.f && decay <= 3e38f)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_track: decay must be a finite number >= 0");
   ctx->track = weights;
@@ -1237,6 +1304,18 @@ recg_status recg_kv_shift(recg_ctx* ctx, int32_t n_req, const int32_t* shift) {
   ctx->bl.pos_shift = n_req ? ctx->d_pos_shift : nullptr;      // (zeros are uploaded all the same: a captured step may read them)
   return RECG_OK;
 }
+recg_status recg_window(recg_ctx* ctx, int32_t n_sink, int32_t window) {
+  if (!ctx) return RECG_ERR_INVALID_ARG;
+  if (n_sink < 0 || window < 0 || n_sink > (1 << 30) || window > (1 << 30))
+    return fail(ctx, RECG_ERR_INVALID_ARG, "recg_window: n_sink and window must be 0 .. 2^30");
+  if (window && four_bits(ctx)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_window: not over a pool in 4 bits");
+  if (window && ctx->track) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_window: not while weights are gathered (recg_kv_track)");
+  if (!window) n_sink = 0;
+  if (n_sink != ctx->bl.n_sink || window != ctx->bl.window) ctx->window_pending = true;
+  ctx->bl.n_sink = n_sink;
+  ctx->bl.window = window;
+  return RECG_OK;
+}
 recg_status recg_kv_select(recg_ctx* ctx, const recg_eviction* e, int32_t* keep, int32_t keep_stride) {
   if (!ctx || !keep) return RECG_ERR_INVALID_ARG;
   if (e && !e->weights) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_select: weights is null");
@@ -1255,6 +1334,7 @@ recg_status recg_kv_select(recg_ctx* ctx, const recg_eviction* e, int32_t* keep,
 }
 recg_status recg_kv_compact(recg_ctx* ctx, const recg_eviction* e, const int32_t* keep, int32_t keep_stride) {
   if (!ctx || !keep) return RECG_ERR_INVALID_ARG;
+  if (eight_bits(ctx)) return fail(ctx, RECG_ERR_INVALID_ARG, "recg_kv_compact: not of a pool in 8 bits");
   EvictDesc E;
   int max_keep = 0, max_pages = 0;
   recg_status s;
