@@ -41,40 +41,81 @@ __device__ __forceinline__ void store_row(const uint32_t (&x)[Kv8Block<D>::N], u
   else *reinterpret_cast<uint32_t*>(row + lane * 4) = x[0];
 }
 
-// K (V: V) of one page and kv head: rows [first, end) of it, which `row(r)` finds in memory, written or read by a warp.
-// `turn(x, r)`: what happens to a row of K on its way.
-template <int D, bool V, bool WRITE, typename Row, typename Turn>
-__device__ __forceinline__ void move_block(uint8_t* layer, int64_t n_pages, int n_kv, int64_t page, int h, int first, int end, int lane,
-                                           Row row, Turn turn) {
-  uint8_t* codes = layer + (page * n_kv + h) * kv8_block_bytes(D) + (V ? 16 * D : 0);
-  uint32_t* header = reinterpret_cast<uint32_t*>(layer + kv8_headers(n_pages, n_kv, D)) + (page * n_kv + h) * 2 + (V ? 1 : 0);
+// Where row r of a block is in memory: pitch bytes from one row to the next, or (STAGED) in slot t0 + r of a bf16 pool with pitch bytes from page
+// to page, of which a lane finds its values by itself (they are less than a chunk of the swizzled row).
+template <int D, bool STAGED>
+struct RowsAt {
+  uint8_t* at;
+  int64_t pitch;
+  int t0;
+  __device__ __forceinline__ uint8_t* operator()(int r, int lane) const {
+    if (!STAGED) return at + r * pitch;
+    const int t = t0 + r;
+    return at + t / kPageSize * pitch + 2 * (kv_tile_offset(t % kPageSize, lane * (D / 32), D) - lane * (D / 32));
+  }
+};
+// cos and sin of an angle: the nearest floats, and what is missing
+struct Angle { float c, s, c_rest, s_rest; };
+// x cos - other sin in the first half of a row, x cos + other sin in the second: what 64 bits give, rounded to 32
+__device__ __forceinline__ float turned(float x, float other, const Angle& a, bool second) {
+  const float y = second ? other : -other;
+  const float p = __fmul_rn(x, a.c), q = __fmul_rn(y, a.s), t = __fadd_rn(p, q), u = __fsub_rn(t, p);
+  const float lost = __fadd_rn(__fsub_rn(p, __fsub_rn(t, u)), __fsub_rn(q, u));                   // (p + q) - t
+  const float rest = __fadd_rn(__fmaf_rn(x, a.c, -p), __fmaf_rn(y, a.s, -q));                     // of the products
+  return __fadd_rn(t, __fadd_rn(lost, __fmaf_rn(x, a.c_rest, __fmaf_rn(y, a.s_rest, rest))));
+}
+__device__ __forceinline__ float turned(float x, float other, const float2& cs, bool second) { return x * cs.x + (second ? cs.y : -cs.y) * other; }
+template <typename T>
+__device__ __forceinline__ uint32_t turned_pair(uint32_t x, uint32_t other, const T& a0, const T& a1, bool second) {
+  return pack_bf16(turned(__uint_as_float(x << 16), __uint_as_float(other << 16), a0, second),
+                   turned(__uint_as_float(x & 0xffff0000u), __uint_as_float(other & 0xffff0000u), a1, second));
+}
+
+// K (V: V) of one page and kv head: rows [first, end) of it are written to the pool or read from it by a warp.  TURN: rows of K are rotated on
+// their way; angles: [16 rows][D / 2], of row `first` on, in the order that append_rotary_kernel explains.
+// (A function of its own: inlined into a loop over blocks the compiler moved sixteen addresses and predicates out of that, 167 registers a
+// thread instead of 80 at most.)
+template <int D, bool V, bool WRITE, bool STAGED, bool TURN>
+__device__ __noinline__ void move_block(uint8_t* codes, uint32_t* header, int first, int end, RowsAt<D, STAGED> row, const Angle* angles) {
+  constexpr int N = Kv8Block<D>::N;
+  const int lane = threadIdx.x & 31;
   Kv8Block<D> b;
   if (WRITE) {
     if (first > 0) kv8_load<D, V>(b, codes, *header, first, lane);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      if (r >= first && r < end) load_row<D>(b.x[r], row(r), lane);
+      if (r >= first && r < end) load_row<D>(b.x[r], row(r, lane), lane);
       else if (r >= end || first == 0)
 #pragma unroll
-        for (int i = 0; i < Kv8Block<D>::N; ++i) b.x[r][i] = 0;
+        for (int i = 0; i < N; ++i) b.x[r][i] = 0;
     }
-    if (!V)
+    if (TURN)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (r >= first && r < end) turn(b.x[r], r);
+        if (r >= first && r < end) {
+          const Angle* a = angles + (r - first) * (D / 2) + (lane & 15);
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            b.x[r][i] = turned_pair(b.x[r][i], __shfl_xor_sync(0xffffffffu, b.x[r][i], 16), a[2 * i * 16], a[(2 * i + 1) * 16], lane >= 16);
+        }
     const uint32_t to = kv8_store<D, V>(b, codes, end, lane);
     if (lane == 0) *header = to;
   } else {
     kv8_load<D, V>(b, codes, *header, end, lane);
 #pragma unroll
     for (int r = 0; r < 16; ++r)
-      if (r >= first && r < end) store_row<D>(b.x[r], row(r), lane);
+      if (r >= first && r < end) store_row<D>(b.x[r], row(r, lane), lane);
   }
 }
-struct AsItIs {
-  template <int N>
-  __device__ __forceinline__ void operator()(uint32_t (&)[N], int) const {}
-};
+// Block h of a page, V where `v` is set
+template <int D, bool WRITE, bool STAGED, bool TURN>
+__device__ __forceinline__ void move_block(bool v, uint8_t* layer, int64_t n_pages, int n_kv, int64_t page, int h, int first, int end,
+                                           const RowsAt<D, STAGED>& row, const Angle* angles) {
+  uint8_t* codes = layer + (page * n_kv + h) * kv8_block_bytes(D);
+  uint32_t* header = reinterpret_cast<uint32_t*>(layer + kv8_headers(n_pages, n_kv, D)) + (page * n_kv + h) * 2;
+  if (v) move_block<D, true, WRITE, STAGED, false>(codes + 16 * D, header + 1, first, end, row, nullptr);
+  else move_block<D, false, WRITE, STAGED, TURN>(codes, header, first, end, row, angles);
+}
 
 // Positions [pos0, pos0 + n_pos) of a request; k, v [n_pos][n_kv][D].
 template <int D, bool WRITE, int N>
@@ -82,16 +123,13 @@ __global__ void __launch_bounds__(kThreads) kv8_io_kernel(uint8_t* layer, int64_
                                                           int pos0, int n_pos, uint8_t* k, uint8_t* v) {
   griddep_launch();
   const unsigned task = blockIdx.x * kWarps + (threadIdx.x >> 5), unit = task >> 1;
-  const int lane = threadIdx.x & 31, p = (int)(unit / (unsigned)n_kv), h = (int)(unit - (unsigned)p * (unsigned)n_kv);
+  const int p = (int)(unit / (unsigned)n_kv), h = (int)(unit - (unsigned)p * (unsigned)n_kv);
   const int start = (pages.first + p) * kPageSize, first = max(pos0 - start, 0), end = min(pos0 + n_pos - start, kPageSize);
   if (end <= first) return griddep_wait();
-  const int64_t page = pages.ids[p];
-  uint8_t* at = ((task & 1) ? v : k) + (size_t)h * (2 * D);
-  const size_t stride = (size_t)n_kv * (2 * D);
-  const auto row = [&](int r) { return at + (size_t)(start + r - pos0) * stride; };
+  const int64_t page = pages.ids[p], stride = n_kv * (2 * D);
+  const RowsAt<D, false> row{((task & 1) ? v : k) + (int64_t)(start - pos0) * stride + h * (2 * D), stride, 0};
   griddep_wait();
-  if (task & 1) move_block<D, true, WRITE>(layer, n_pages, n_kv, page, h, first, end, lane, row, AsItIs());
-  else move_block<D, false, WRITE>(layer, n_pages, n_kv, page, h, first, end, lane, row, AsItIs());
+  move_block<D, WRITE, false, false>(task & 1, layer, n_pages, n_kv, page, h, first, end, row, nullptr);
 }
 
 // What a CTA has of a batch: one page of one request, of which the rows [first, end) are the batch's rows t0 ..  A request with n rows touches
@@ -124,30 +162,26 @@ __device__ __forceinline__ PageRows page_rows(const BatchLayout& bl, unsigned un
 
 // Rows of a batch.  STAGED: row t of k and v lies in slot t of a bf16 pool of row_stride pages (v is not used).
 template <int D, bool WRITE, bool STAGED>
-__global__ void __launch_bounds__(kThreads) kv8_rows_kernel(const __grid_constant__ BatchLayout bl, uint8_t* layer, int64_t n_pages, int n_kv,
+__global__ void __launch_bounds__(kThreads, 3) kv8_rows_kernel(const __grid_constant__ BatchLayout bl, uint8_t* layer, int64_t n_pages, int n_kv,
                                                             uint8_t* k, uint8_t* v, int64_t row_stride) {
   griddep_launch();
   griddep_wait();
   const PageRows p = page_rows(bl, blockIdx.x);
   if (p.page < 0) return;
-  const int lane = threadIdx.x & 31;
   for (int task = blockIdx.y * kWarps + (threadIdx.x >> 5); task < 2 * n_kv; task += kWarps * gridDim.y) {
-    const int h = task >> 1;
-    const auto row = [&](int r) {
-      const int t = p.t0 + r - p.first;
-      if (STAGED)      // (a lane finds its values in the swizzled row by itself: they are less than a chunk)
-        return k + 2 * (kv_tile_base(row_stride, n_kv, D, 0, t / kPageSize, h) + ((task & 1) ? kv_tile_elems(D) : 0) +
-                        kv_tile_offset(t % kPageSize, lane * (D / 32), D) - lane * (D / 32));
-      return ((task & 1) ? v : k) + ((size_t)t * row_stride + (size_t)h * D) * 2;
-    };
-    if (task & 1) move_block<D, true, WRITE>(layer, n_pages, n_kv, p.page, h, p.first, p.end, lane, row, AsItIs());
-    else move_block<D, false, WRITE>(layer, n_pages, n_kv, p.page, h, p.first, p.end, lane, row, AsItIs());
+    const int h = task >> 1, t0 = p.t0 - p.first;
+    const int64_t pitch = STAGED ? (int64_t)(4 * kv_tile_elems(D)) * n_kv : row_stride * 2;
+    const RowsAt<D, STAGED> row{STAGED ? k + 2 * (kv_tile_base(row_stride, n_kv, D, 0, 0, h) + ((task & 1) ? kv_tile_elems(D) : 0))
+                                       : ((task & 1) ? v : k) + t0 * pitch + h * (2 * D), pitch, t0};
+    move_block<D, WRITE, STAGED, false>(task & 1, layer, n_pages, n_kv, p.page, h, p.first, p.end, row, nullptr);
   }
 }
 
 // ---- rotation and append -------------------------------------------------------------------------------------------------------
-// The angles of the page's rows once per CTA, in 64 bits, for all heads.  K is rotated in 64 bits too (the result goes on to be rounded to
-// codes, where the last bit of a sum next to a border decides between two of them), q in 32.
+// The angles of the page's rows once per CTA, in 64 bits, for all heads.  K's sums go on to be rounded to codes, where the last bit of a sum
+// next to a border decides between two of them, so they are formed as if in 64 bits: factors in two floats, products and sum with their
+// errors.  (Double instructions would do, but converting to them and back takes the unit of the exponentials: 16001 rows of 32 / 8 heads
+// 310 us, 85 % of that unit's time.)  q in 32.
 struct RotaryArgs {
   const uint8_t *q, *k, *v;
   uint8_t* q_out;                    // [n_tok][n_q][D]; q may be null
@@ -157,76 +191,61 @@ struct RotaryArgs {
   int layer, n_q, n_kv;
   double turn[64];                   // base^(-2 i / D)
 };
-// y = x cos - (partner) sin in the first half of a row, x cos + (partner) sin in the second
-__device__ __forceinline__ float turned(float x, float other, double2 cs, bool second) {
-  return (float)((double)x * cs.x + (second ? cs.y : -cs.y) * (double)other);
-}
-__device__ __forceinline__ float turned(float x, float other, float2 cs, bool second) {
-  return x * cs.x + (second ? cs.y : -cs.y) * other;
-}
-template <typename T>
-__device__ __forceinline__ uint32_t turned_pair(uint32_t x, uint32_t other, const T* cs, bool second) {
-  return pack_bf16(turned(__uint_as_float(x << 16), __uint_as_float(other << 16), cs[0], second),
-                   turned(__uint_as_float(x & 0xffff0000u), __uint_as_float(other & 0xffff0000u), cs[1], second));
-}
-// Eight values of a row, chunk j of LANES that consecutive lanes hold
+// Eight values of a row, chunk j of LANES that consecutive lanes hold; a: the angles of those values
 template <int LANES, typename T>
-__device__ __forceinline__ uint4 turned_chunk(const uint4& x, const T* row, int j) {
+__device__ __forceinline__ uint4 turned_chunk(const uint4& x, const T (&a)[8], int j) {
   const uint32_t in[4] = {x.x, x.y, x.z, x.w};
   const bool second = j >= LANES / 2;
-  const T* cs = row + 8 * (j % (LANES / 2));
   uint32_t out[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) out[i] = turned_pair(in[i], __shfl_xor_sync(0xffffffffu, in[i], LANES / 2), cs + 2 * i, second);
+  for (int i = 0; i < 4; ++i) out[i] = turned_pair(in[i], __shfl_xor_sync(0xffffffffu, in[i], LANES / 2), a[2 * i], a[2 * i + 1], second);
   return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
-// BITS: of the pool.
+// BITS: of the pool.  A lane finds the angles of its values one stride apart, that of the lanes which share a row, so that these read
+// consecutive ones: angle i of a row lies at (i % E) (D / 2 / E) + i / E, E = D / 32 for blocks of 8 bits and 8 for chunks.
 template <int D, int BITS>
-__global__ void __launch_bounds__(kThreads) append_rotary_kernel(const __grid_constant__ BatchLayout bl, const __grid_constant__ RotaryArgs A) {
-  constexpr int kLanes = D / 8;
-  __shared__ double2 exact[kPageSize][D / 2];
-  __shared__ float2 plain[kPageSize][D / 2];
+__global__ void __launch_bounds__(kThreads, BITS == 8 ? 3 : 4) append_rotary_kernel(const __grid_constant__ BatchLayout bl, const __grid_constant__ RotaryArgs A) {
+  constexpr int kLanes = D / 8, kHalf = D / 2, E = BITS == 8 ? D / 32 : 8;
+  __shared__ Angle exact[kPageSize][kHalf];
+  __shared__ float2 plain[kPageSize][kHalf];
   griddep_launch();
   griddep_wait();
   const PageRows p = page_rows(bl, blockIdx.x);
   const int rows = p.end - p.first;
   if (rows <= 0) return;
-  for (int i = threadIdx.x; i < rows * (D / 2); i += kThreads) {
-    const double angle = (double)bl.tok_pos[p.t0 + i / (D / 2)] * A.turn[i % (D / 2)];
-    double2 cs;
-    sincos(angle, &cs.y, &cs.x);
-    exact[i / (D / 2)][i % (D / 2)] = cs;
-    plain[i / (D / 2)][i % (D / 2)] = make_float2((float)cs.x, (float)cs.y);
+  for (int i = threadIdx.x; i < rows * kHalf; i += kThreads) {
+    const int r = i / kHalf, f = i % kHalf;
+    double sn, cn;
+    sincos((double)bl.tok_pos[p.t0 + r] * A.turn[f], &sn, &cn);
+    const Angle a{(float)cn, (float)sn, (float)(cn - (double)(float)cn), (float)(sn - (double)(float)sn)};
+    exact[r][(f % E) * (kHalf / E) + f / E] = a;
+    plain[r][(f % 8) * (kHalf / 8) + f / 8] = make_float2(a.c, a.s);
   }
   __syncthreads();
   const int warp = blockIdx.y * kWarps + (threadIdx.x >> 5), n_warps = kWarps * gridDim.y, lane = threadIdx.x & 31, j = lane % kLanes;
-  constexpr int kRows = 32 / kLanes;       // row heads that a warp moves at once
-  int done = 0;                            // tasks that have been handed out, a warp each
+  constexpr int kRows = 32 / kLanes;       // heads of a row that a warp moves at once
   // ---- K and V ----
   if (BITS == 8) {
     const int tasks = p.page < 0 ? 0 : 2 * A.n_kv;
     for (int task = warp; task < tasks; task += n_warps) {
       const int h = task >> 1;
-      const auto row = [&](int r) { return const_cast<uint8_t*>((task & 1) ? A.v : A.k) + ((size_t)(p.t0 + r - p.first) * A.kv_stride + (size_t)h * D) * 2; };
-      const auto turn = [&](uint32_t (&x)[Kv8Block<D>::N], int r) {
-        const double2* cs = exact[r - p.first] + (D / 32) * (lane & 15);
-#pragma unroll
-        for (int i = 0; i < Kv8Block<D>::N; ++i) x[i] = turned_pair(x[i], __shfl_xor_sync(0xffffffffu, x[i], 16), cs + 2 * i, lane >= 16);
-      };
-      if (task & 1) move_block<D, true, true>(A.pool, A.n_pages, A.n_kv, p.page, h, p.first, p.end, lane, row, AsItIs());
-      else move_block<D, false, true>(A.pool, A.n_pages, A.n_kv, p.page, h, p.first, p.end, lane, row, turn);
+      const int64_t pitch = A.kv_stride * 2;
+      const RowsAt<D, false> row{const_cast<uint8_t*>((task & 1) ? A.v : A.k) + (p.t0 - p.first) * pitch + h * (2 * D), pitch, 0};
+      move_block<D, true, false, true>(task & 1, A.pool, A.n_pages, A.n_kv, p.page, h, p.first, p.end, row, exact[0]);
     }
-    done = tasks;
   } else {
-    const int units = p.page < 0 ? 0 : rows * A.n_kv, tasks = (units + kRows - 1) / kRows;
+    const int per_row = (A.n_kv + kRows - 1) / kRows, tasks = p.page < 0 ? 0 : rows * per_row;
     for (int task = warp; task < tasks; task += n_warps) {
-      const int unit = task * kRows + lane / kLanes, r = unit / A.n_kv, h = unit - r * A.n_kv, tok = p.first + r;
-      const bool mine = unit < units;
+      const int r = task / per_row, h = (task - r * per_row) * kRows + lane / kLanes, tok = p.first + r;
+      const bool mine = h < A.n_kv;
       const size_t at = ((size_t)(p.t0 + r) * A.kv_stride + (size_t)h * D + 8 * j) * 2;
       const uint4 none = make_uint4(0, 0, 0, 0);
       uint4 k = mine ? *reinterpret_cast<const uint4*>(A.k + at) : none, v = mine ? *reinterpret_cast<const uint4*>(A.v + at) : none;
-      k = turned_chunk<kLanes>(k, exact[mine ? r : 0], j);
+      Angle a[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = exact[r][i * (kHalf / 8) + j % (kLanes / 2)];
+      k = turned_chunk<kLanes>(k, a, j);
       if (BITS == 16) {
         if (!mine) continue;
         uint8_t* tile = A.pool + 2 * (kv_tile_base(A.n_pages, A.n_kv, D, A.layer, p.page, h) + kv_tile_offset(tok, 8 * j, D));
@@ -246,19 +265,32 @@ __global__ void __launch_bounds__(kThreads) append_rotary_kernel(const __grid_co
         }
       }
     }
-    done = tasks;
   }
-  // ---- q (its tasks go on where those of K and V have ended) ----
+  // ---- q: the warps are divided among the rows, those of a row share its heads; from the last warp on, which has had less of K and V ----
   if (!A.q) return;
-  const int units = rows * A.n_q, tasks = (units + kRows - 1) / kRows;
-  for (int task = (warp + n_warps - done % n_warps) % n_warps; task < tasks; task += n_warps) {
-    const int unit = task * kRows + lane / kLanes, r = unit / A.n_q, h = unit - r * A.n_q;
-    const bool mine = unit < units;
-    const size_t t = p.t0 + (mine ? r : 0);
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (mine) x = *reinterpret_cast<const uint4*>(A.q + (t * A.q_stride + (size_t)h * D + 8 * j) * 2);
-    x = turned_chunk<kLanes>(x, plain[mine ? r : 0], j);
-    if (mine) *reinterpret_cast<uint4*>(A.q_out + ((t * A.n_q + h) * D + 8 * j) * 2) = x;
+  const int share = max(n_warps / rows, 1), back = n_warps - 1 - warp;
+  for (int r = back / share; r < rows; r += (n_warps + share - 1) / share) {
+    float2 a[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = plain[r][i * (kHalf / 8) + j % (kLanes / 2)];
+    const size_t t = p.t0 + r;
+    const uint8_t* from = A.q + (t * A.q_stride + 8 * j) * 2;
+    uint8_t* to = A.q_out + (t * A.n_q * D + 8 * j) * 2;
+    constexpr int kAhead = 4;              // loads on their way at once
+    for (int h0 = back % share * kRows + lane / kLanes; h0 - lane / kLanes < A.n_q; h0 += kAhead * share * kRows) {
+      uint4 x[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int h = h0 + i * share * kRows;
+        x[i] = h < A.n_q ? *reinterpret_cast<const uint4*>(from + (size_t)h * (2 * D)) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int h = h0 + i * share * kRows;
+        x[i] = turned_chunk<kLanes>(x[i], a, j);
+        if (h < A.n_q) *reinterpret_cast<uint4*>(to + (size_t)h * (2 * D)) = x[i];
+      }
+    }
   }
 }
 
