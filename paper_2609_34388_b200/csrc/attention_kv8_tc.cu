@@ -1,0 +1,674 @@
+// Hybrid-mask paged attention over a pool in 8 bits on the 5th-generation tensor cores (head_dim 128, many query rows per kv head).
+//
+// Work items, masks and the combine kernel are those of attention_tc.cu, the mathematics those of attention_kv8.cu: the exponent of a block
+// of K is part of the factor of its scores, that of V of the exponents of its probabilities, relative to a row's reference, the largest of the
+// sums that the row has seen.
+//
+// S = Q K^T takes K's codes as they lie in the pool: e4m3 products, whose rate is twice that of 16 bits.  A bf16 number has eight digits and
+// e4m3 four, so a row of Q, scaled by a power of two, is the sum of two e4m3 rows, exactly but for values below 2^-10 of its largest, which
+// are off by 2^-19 of that: two products, as long as one in bf16 together, and no conversion of K.
+// P has no such form (its values span more powers of two than e4m3 holds): V's codes are converted to fp16, exactly, by a warpgroup
+// beside the softmax, and P V is a product in fp16, P rounded to 2^-11.
+//
+// Per CTA (16 warps = 4 warpgroups, one CTA per SM, persistent over the work list), stages of 128 tokens:
+//   warps 0, 2  stream the codes of K (operands as they arrive) and of V, one bulk copy of 2 KB per page each; warp 0 leaves the headers of the
+//               pages for the softmax
+//   warp 1      one elected lane issues S = Q K^T (two stages ahead) and per softmax group O_g += P_g V_g (P from TMEM)
+//   warps 4-7 and 8-11  two softmax groups: group g takes tokens [64 g, 64 g + 64) of every stage, one thread one query row, its own O
+//               accumulator and running (reference, sum); merged at the end of an item
+//   warps 12-15 turn codes of V into the operand (K-major, a thread one of the 128 values, 16 tokens of a page at a time: 16-byte reads and
+//               stores without bank conflicts) and the rows of Q of the next item into theirs
+// The registers are moved to the softmax warps: 4 x (56 + 168 + 168 + 120) x 32, which are those of the launch.
+// Every wait is bounded; a wait that runs out raises a CTA-wide flag after which no wait blocks, so the kernel always ends.
+#include <cuda_fp16.h>
+
+#include "attention_tc.cuh"
+#include "kernels.h"
+#include "kv8.cuh"
+
+namespace recg {
+
+namespace {
+
+constexpr int D = 128;
+constexpr int kBT = 128;                         // tokens per stage
+constexpr int kPages = kBT / kPageSize;
+constexpr int kTile = kPageSize * D;             // 2 KB: the codes of K or V of a page and head
+constexpr int kCodes = kBT * D;                  // 16 KB: of a stage; a row of Q has two such operands
+constexpr int kVBytes = kBT * D * 2;             // 32 KB: V of a stage in fp16
+constexpr int kKRing = 3, kRawRing = 2, kVRing = 2;
+constexpr int kHeadRing = 8;                     // stages whose headers are kept: the softmax may be four behind warp 0
+constexpr int kThreads = 512;
+constexpr uint32_t kSpin = 1u << 22;             // polls of a wait
+constexpr int kTmemCols = 512;                   // two S buffers of 128 columns; O of group g at 256 + 128 g
+constexpr int kTmemO = 2 * kBT;
+constexpr float kNoRef = -1e30f;       // reference of a row that has seen no token yet
+constexpr float kHeadroom = 8.f;       // a row's reference moves when it is outgrown by more than 2^8
+constexpr float kLift = 7.f;           // probabilities stand as 2^7 p: at most 2^15
+
+constexpr int kOffQ = 0;                                           // two items' rows: [hi | lo] each
+constexpr int kOffK = kOffQ + 4 * kCodes;
+constexpr int kOffRaw = kOffK + kKRing * kCodes;
+constexpr int kOffV = kOffRaw + kRawRing * kCodes;
+constexpr int kOffML = kOffV + kVRing * kVBytes;                   // per row, both groups: reference; sum (negative: O is none)
+constexpr int kOffQF = kOffML + 2 * 2 * 128 * 4;                   // per row, two items: the factor of its scores
+constexpr int kOffHead = kOffQF + 2 * 128 * 4;                     // [kHeadRing][8 pages] headers
+constexpr int kOffBar = kOffHead + kHeadRing * kPages * 8;
+constexpr int kNumBars = 2 * kKRing + 2 * kRawRing + 2 * kVRing + 4 + 2 + 4 + 3;
+constexpr int kSmemBytes = kOffBar + kNumBars * 8 + 16;
+static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
+
+struct Params {
+  const AttnItem* items;
+  const int* item_gap;
+  const int* cta_off;
+  const int* page_table;
+  int pt_stride;
+  const int* tok_climit;
+  const int* tok_lo;
+  const int* tok_hi;
+  const int* tok_first;
+  int n_sink, sink_blocks;
+  const __nv_bfloat16* q;
+  __nv_bfloat16* o;
+  float* lse;
+  const uint8_t* pool;     // of the layer
+  int64_t n_pages;
+  int n_q, n_kv, group;
+  float scale_log2;
+  float* part_o;
+  float* part_ml;
+  int* status;
+  int early_desc;     // the work list is settled: it may be read before the wait for the kernel in front of this one
+};
+
+__device__ __forceinline__ void softmax_bar() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// e4m3 operands, both K-major, fp32 accumulators, M = N = 128 (32 values of the contraction an instruction); fp16 operands
+constexpr uint32_t kIdescE4m3 = (1u << 4) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+constexpr uint32_t kIdescF16 = kIdescQK & ~((1u << 7) | (1u << 10));
+__device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+      :
+      : "r"(tmem_d), "l"(da), "l"(db), "r"(kIdescE4m3), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return reinterpret_cast<const uint32_t&>(h);
+}
+// A bounded wait that sleeps between polls: warps that poll take issue slots from those that work.
+template <int NS>
+__device__ __forceinline__ bool wait_asleep(uint64_t* bar, uint32_t parity) {
+#pragma unroll 1
+  for (uint32_t i = 0; i < kSpin; ++i) {
+    __nanosleep(NS);
+    if (mbar_test_wait(bar, parity)) return true;
+  }
+  return false;
+}
+
+// WIN: rows look back a window (recg_window); an item's 64-token blocks behind the first tokens' lie `gap` further on.
+template <bool WIN>
+__global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  if (smem_u32(smem) & 1023u) {          // the swizzled operand layouts need a 1 KB aligned base
+    if (threadIdx.x == 0) set_status(P.status, DEV_BAD_INDEX);
+    return;
+  }
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBar);
+  uint64_t* k_full = bars;                       // [kKRing]
+  uint64_t* k_empty = k_full + kKRing;
+  uint64_t* raw_full = k_empty + kKRing;         // [kRawRing]
+  uint64_t* raw_empty = raw_full + kRawRing;     //            the four converting warps
+  uint64_t* v_full = raw_empty + kRawRing;       // [kVRing]   the four converting warps
+  uint64_t* v_empty = v_full + kVRing;
+  uint64_t* q_ready = v_empty + kVRing;          // [2]   per Q buffer: the four converting warps
+  uint64_t* q_empty = q_ready + 2;               // [2]   the eight softmax warps, at the end of an item
+  uint64_t* s_full = q_empty + 2;                // [2]   per S buffer
+  uint64_t* p_full = s_full + 2;                 // [4]   2 g + (stage & 1)
+  uint64_t* pv_done = p_full + 4;
+  uint64_t* o_full = pv_done + 1;
+  uint64_t* o_empty = o_full + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* ml_smem = reinterpret_cast<float*>(smem + kOffML);
+  float* qf_smem = reinterpret_cast<float*>(smem + kOffQF);
+  int2* head_smem = reinterpret_cast<int2*>(smem + kOffHead);
+  // (the MMA issuer and the softmax warps, whom the stage waits for, poll more often)
+  auto bwait = [&](uint64_t* bar, uint32_t parity, int code) {
+    if (mbar_test_wait(bar, parity) || *abort_flag) return;
+    if (!wait_asleep<20>(bar, parity)) {
+      set_status(P.status, code);
+      *abort_flag = 1;
+    }
+  };
+  auto lazy_wait = [&](uint64_t* bar, uint32_t parity, int code) {
+    if (mbar_test_wait(bar, parity) || *abort_flag) return;
+    if (!wait_asleep<100>(bar, parity)) {
+      set_status(P.status, code);
+      *abort_flag = 1;
+    }
+  };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    for (int s = 0; s < kKRing; ++s) {
+      mbar_init(&k_full[s], 1);
+      mbar_init(&k_empty[s], 1);
+    }
+    for (int s = 0; s < kRawRing; ++s) {
+      mbar_init(&raw_full[s], 1);
+      mbar_init(&raw_empty[s], 4);
+    }
+    for (int s = 0; s < kVRing; ++s) {
+      mbar_init(&v_full[s], 4);
+      mbar_init(&v_empty[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&q_ready[s], 4);
+      mbar_init(&q_empty[s], 8);
+      mbar_init(&s_full[s], 1);
+    }
+    for (int s = 0; s < 4; ++s) mbar_init(&p_full[s], 4);
+    mbar_init(pv_done, 1);
+    mbar_init(o_full, 1);
+    mbar_init(o_empty, 8);
+    fence_barrier_init();
+  }
+  // Codes of pages that are not requested, behind a request's end: whatever the rings hold is numbers.
+  for (int i = threadIdx.x; i < (kKRing + kRawRing) * kCodes / 16; i += kThreads)
+    reinterpret_cast<uint4*>(smem + kOffK)[i] = make_uint4(0, 0, 0, 0);
+  fence_proxy_async();
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, kTmemCols);
+    tmem_relinquish();
+  }
+  // (where the work list is settled it is read ahead of the wait for the kernel in front, and so are page ids)
+  if (!P.early_desc) griddep_wait();
+  // the CTA walks two ranges of the item list one after the other (see the layout kernel)
+  const int4 r4 = *reinterpret_cast<const int4*>(P.cta_off + 4 * blockIdx.x);
+  const int range_n0 = r4.y - r4.x, item_end = range_n0 + (r4.w - r4.z);
+  auto item_at = [&](int i) { return i < range_n0 ? r4.x + i : r4.z + (i - range_n0); };
+  auto gap_of = [&](int i) { return WIN ? P.item_gap[item_at(i)] : 0; };
+  auto place = [&](int block, int gap) { return WIN && block >= P.sink_blocks ? block + gap : block; };
+  auto stages_of = [&](const AttnItem& w) { return (w.blk_end - w.blk_begin + 1) / 2; };
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const uint32_t smem_base = smem_u32(smem);
+
+  if (warp < 4) {
+    regs_dec<56>();
+    if (warp == 0 || warp == 2) {
+      // ------------------------------------ producers: warp 0 codes of K and headers, warp 2 codes of V ------------------------------------
+      const bool v = warp == 2;
+      const int ring = v ? kRawRing : kKRing;
+      uint64_t* full = v ? raw_full : k_full;
+      uint64_t* empty = v ? raw_empty : k_empty;
+      uint8_t* to = smem + (v ? kOffRaw : kOffK);
+      const uint8_t* codes = P.pool + (v ? kTile : 0);
+      const int2* heads = reinterpret_cast<const int2*>(P.pool + kv8_headers(P.n_pages, P.n_kv, D));
+      // The stages of all items are one line: `f` runs two ahead with page ids, one ahead with headers.
+      int f_item = -1, f_n = 0, f_nblk = 0, f_gap = 0;
+      AttnItem f = {};
+      struct Page { int id, head; bool stage; };      // of lanes 0..7: the page, or -1; its kv head; whether there is such a stage
+      auto fetch_page = [&]() {
+        Page p{-1, 0, false};
+        while (f_n >= f_nblk) {
+          if (f_item + 1 >= item_end) return p;
+          ++f_item;
+          f = P.items[item_at(f_item)];
+          f_n = 0;
+          f_nblk = stages_of(f);
+          f_gap = gap_of(f_item);
+        }
+        p.stage = true;
+        const int block = f.blk_begin + 2 * f_n++ + (lane >> 2);
+        const int lp = place(block, f_gap) * 4 + (lane & 3);
+        if (lane < kPages && block < f.blk_end && lp * kPageSize < f.kv_len) {
+          p.id = __ldg(P.page_table + (size_t)f.req * P.pt_stride + lp);
+          p.head = f.kv_head;
+          if (p.id < 0 || p.id >= P.n_pages) {
+            set_status(P.status, DEV_BAD_INDEX);
+            p.id = -1;
+          }
+        }
+        return p;
+      };
+      auto fetch_head = [&](const Page& p) { return !v && p.id >= 0 ? __ldg(heads + (size_t)p.id * P.n_kv + p.head) : make_int2(0, 0); };
+      Page now = fetch_page(), next = fetch_page();
+      griddep_wait();
+      int2 head = fetch_head(now);
+      for (uint32_t blk = 0; now.stage; ++blk) {
+        const int2 head_next = fetch_head(next);
+        const Page after = fetch_page();
+        const int s = blk % ring;
+        lazy_wait(&empty[s], ((blk / ring) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
+        if (!v && lane < kPages) head_smem[(blk % kHeadRing) * kPages + lane] = head;
+        const unsigned mask = __ballot_sync(0xffffffffu, now.id >= 0);
+        if (lane == 0) {
+          if (mask == 0) mbar_arrive(&full[s]);
+          else mbar_arrive_expect_tx(&full[s], __popc(mask) * kTile);
+        }
+        __syncwarp();
+        if (now.id >= 0)
+          bulk_g2s(to + s * kCodes + lane * kTile, codes + ((size_t)now.id * P.n_kv + now.head) * kv8_block_bytes(D), kTile, &full[s]);
+        __syncwarp();
+        now = next;
+        next = after;
+        head = head_next;
+      }
+      if (*abort_flag && lane == 0) {     // gave up somewhere: let the copies in flight land before exiting
+        for (int s = 0; s < ring; ++s)
+          for (uint32_t i = 0; i < (1u << 14); ++i) {
+            if (mbar_try_wait(&full[s], 0) || mbar_try_wait(&full[s], 1)) break;
+            __nanosleep(64);
+          }
+      }
+    } else if (warp == 1) {
+      // ------------------------------------ MMA issuer ------------------------------------
+      griddep_wait();
+      if (elect_one()) {
+        uint32_t blk = 0;
+        int next = item_end > 0 ? stages_of(P.items[item_at(0)]) : 0;
+        for (int item = 0; item < item_end; ++item) {
+          const int nblk = next;
+          if (item + 1 < item_end) next = stages_of(P.items[item_at(item + 1)]);
+          const uint64_t dq0 = desc_kmajor(smem_base + kOffQ + (item & 1) * 2 * kCodes);
+          auto issue_qk = [&](uint32_t b) {
+            const int s = b % kKRing;
+            bwait(&k_full[s], (b / kKRing) & 1, DEV_TIMEOUT_FULL);
+            tc_fence_after();
+            const uint64_t dk0 = desc_kmajor(smem_base + kOffK + s * kCodes);
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+              for (int kk = 0; kk < D / 32; ++kk)
+                umma_e4m3(tmem_base + (b & 1) * kBT, dq0 + (uint64_t)((half * kCodes + kk * 32) >> 4), dk0 + (uint64_t)((kk * 32) >> 4),
+                          half | kk ? 1u : 0u);
+            umma_commit(&s_full[b & 1]);
+            umma_commit(&k_empty[s]);
+          };
+          bwait(&q_ready[item & 1], (item >> 1) & 1, DEV_TIMEOUT_FULL);
+          tc_fence_after();
+          issue_qk(blk);
+          if (nblk > 1) issue_qk(blk + 1);
+          for (int n = 0; n < nblk; ++n, ++blk) {
+            const int s = blk % kVRing;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              const uint64_t dv0 = desc_kmajor(smem_base + kOffV + s * kVBytes + g * (kVBytes / 2));
+              bwait(&p_full[2 * g + (blk & 1)], (blk >> 1) & 1, DEV_TIMEOUT_MMA);
+              if (g == 0) {
+                if (n == 0) bwait(o_empty, (item & 1) ^ 1, DEV_TIMEOUT_MMA);
+                bwait(&v_full[s], (blk / kVRing) & 1, DEV_TIMEOUT_FULL);
+              }
+              tc_fence_after();
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk)
+                umma_bf16_ts(tmem_base + kTmemO + g * D, tmem_base + (blk & 1) * kBT + g * 64 + kk * 8, dv0 + (uint64_t)((kk * 32) >> 4), kIdescF16,
+                             (n | kk) ? 1u : 0u);
+            }
+            umma_commit(pv_done);
+            umma_commit(&v_empty[s]);
+            if (n == nblk - 1) umma_commit(o_full);
+            if (n + 2 < nblk) issue_qk(blk + 2);
+          }
+        }
+      }
+    }
+  } else if (warp >= 12) {
+    // ------------------------------------ codes to V; the rows of Q ------------------------------------
+    regs_dec<120>();
+    griddep_wait();
+    const int me = threadIdx.x - 384;            // row of Q; value of V
+    AttnItem w = {};
+    auto turn_rows = [&](int item) {
+      w = P.items[item_at(item)];
+      const int buf = item & 1;
+      lazy_wait(&q_empty[buf], ((item >> 1) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
+      // A row x = 2^e (hi + lo): its largest value goes to [2^7, 2^8), hi and lo are the nearest e4m3 numbers to it and to what is left.
+      if (me < w.ntok * P.group) {               // (what other rows hold reaches nobody)
+        const uint4* src = reinterpret_cast<const uint4*>(P.q + ((size_t)(w.tok0 + me / P.group) * P.n_q + w.kv_head * P.group + me % P.group) * D);
+        uint4 x[16];
+#pragma unroll
+        for (int c = 0; c < 16; ++c) x[c] = __ldg(src + c);
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+          const uint32_t u[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = max(top, max(u[i] & 0x7fffu, (u[i] >> 16) & 0x7fffu));
+        }
+        const bool none = top >= 0x7f80u;
+        const int e = max(-100, min(100, (int)(top >> 7) - 127 - 7));
+        const float down = kv8_pow2(-e);
+        uint8_t* hi = smem + kOffQ + buf * 2 * kCodes + me * D;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          uint32_t h[4], l[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint4 v = x[2 * c + (i >> 1)];
+            const uint32_t u[2] = {(i & 1) ? v.z : v.x, (i & 1) ? v.w : v.y};
+            h[i] = l[i] = 0;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float a = __uint_as_float(u[k] << 16) * down, b = __uint_as_float(u[k] & 0xffff0000u) * down;
+              const uint32_t two = e4m3_from(a, b);
+              const float2 back = f16_pair(e4m3_to_f16(two));
+              h[i] |= two << (16 * k);
+              l[i] |= e4m3_from(a - back.x, b - back.y) << (16 * k);
+            }
+          }
+          const int at = (c ^ (me & 7)) << 4;
+          *reinterpret_cast<uint4*>(hi + at) = make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(hi + kCodes + at) = make_uint4(l[0], l[1], l[2], l[3]);
+        }
+        qf_smem[buf * 128 + me] = none ? __int_as_float(0x7fc00000) : P.scale_log2 * kv8_pow2(e);
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_ready[buf]);
+    };
+    if (item_end > 0) turn_rows(0);
+    uint32_t blk = 0;
+    for (int item = 0; item < item_end; ++item) {
+      const int nblk = stages_of(w);
+      for (int n = 0; n < nblk; ++n, ++blk) {
+        const int rs = blk % kRawRing, s = blk % kVRing;
+        lazy_wait(&raw_full[rs], (blk / kRawRing) & 1, DEV_TIMEOUT_FULL);
+        lazy_wait(&v_empty[s], ((blk / kVRing) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
+        const uint8_t* src = smem + kOffRaw + rs * kCodes + me * 16;
+        uint8_t* dst = smem + kOffV + s * kVBytes + me * 128;
+#pragma unroll
+        for (int p = 0; p < kPages; ++p) {
+          const uint4 v = *reinterpret_cast<const uint4*>(src + p * kTile);
+          uint8_t* at = dst + (p >> 2) * (kVBytes / 2);
+          const int c = (p & 3) * 2;
+          *reinterpret_cast<uint4*>(at + ((c ^ (me & 7)) << 4)) =
+              make_uint4(e4m3_to_f16(v.x & 0xffffu), e4m3_to_f16(v.x >> 16), e4m3_to_f16(v.y & 0xffffu), e4m3_to_f16(v.y >> 16));
+          *reinterpret_cast<uint4*>(at + (((c + 1) ^ (me & 7)) << 4)) =
+              make_uint4(e4m3_to_f16(v.z & 0xffffu), e4m3_to_f16(v.z >> 16), e4m3_to_f16(v.w & 0xffffu), e4m3_to_f16(v.w >> 16));
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&raw_empty[rs]);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&v_full[s]);
+      }
+      if (item + 1 < item_end) turn_rows(item + 1);
+    }
+  } else {
+    // ------------------------------------ softmax ------------------------------------
+    regs_inc<168>();
+    griddep_wait();
+    const int g = (warp - 4) >> 2;             // softmax group: takes tokens [64 g, 64 g + 64) of every stage
+    const int quad = warp & 3;
+    const int row = quad * 32 + lane;          // query row of the tile = TMEM lane
+    const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
+    const uint32_t s_addr = lane_addr + g * 64, o_addr = lane_addr + kTmemO + g * D;
+    uint32_t cs = 0;                           // stages so far
+    AttnItem w_next = item_end > 0 ? P.items[item_at(0)] : AttnItem{};
+    for (int item = 0; item < item_end; ++item) {
+      const AttnItem w = w_next;
+      if (item + 1 < item_end) w_next = P.items[item_at(item + 1)];
+      const int R = w.ntok * P.group, nblk = stages_of(w), gap = gap_of(item), buf = item & 1;
+      const bool rvalid = row < R, warp_valid = quad * 32 < R;
+      int climit = -1, vlo = 0, vhi = 0, vfirst = 0;
+      if (rvalid) {
+        const int t = w.tok0 + row / P.group;
+        climit = P.tok_climit[t];
+        vlo = P.tok_lo[t];
+        vhi = P.tok_hi[t];
+        if (WIN) vfirst = P.tok_first[t];
+      }
+      bwait(&q_ready[buf], (item >> 1) & 1, DEV_TIMEOUT_FULL);
+      const float qf = qf_smem[buf * 128 + row];               // (a row that does not exist: whatever)
+      // The row's reference (powers of two, a whole number: adding exponents to it is exact) and sum; whether it sees V that is none.
+      // (a query that is not finite: neither is)
+      float m_ref = rvalid ? kNoRef : 0.f, l_run = qf == qf ? 0.f : qf;
+      bool o_none = false;
+
+      for (int n = 0; n < nblk; ++n, ++cs) {
+        const uint32_t s_buf = s_addr + (cs & 1) * kBT;
+        bwait(&s_full[cs & 1], (cs >> 1) & 1, DEV_TIMEOUT_MMA);
+        tc_fence_after();
+        const int block = w.blk_begin + 2 * n + g, pos0 = place(block, gap) * 64;
+        if (warp_valid) {
+          uint32_t sr[2][32];   // the S row of this thread: 64 scores, in units of 1 / f of their page
+#pragma unroll
+          for (int c = 0; c < 2; ++c) tmem_ld32_nowait(s_buf + c * 32, sr[c]);
+          const int2* heads = head_smem + (cs % kHeadRing) * kPages + 4 * g;
+          int2 head[4];
+          float f[4], ve[4];
+          uint32_t bad = 0;
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            head[p] = heads[p];
+            f[p] = fminf(fmaxf(qf * kv8_pow2(kv8_exponent(head[p].x)), 1e-37f), 3e38f);      // (times -inf it stays that)
+            ve[p] = (float)kv8_exponent(head[p].y);
+            bad |= kv8_flags(head[p].x) | kv8_flags(head[p].y);
+          }
+          tmem_ld_wait();
+          // (a block that the item does not have is seen by no row)
+          const int lim = block < w.blk_end ? climit : -1, end = block < w.blk_end ? vhi : -1;
+          const bool need_mask = __any_sync(0xffffffffu, rvalid && (pos0 + 63 > lim || (WIN && pos0 < vfirst)));
+          if (need_mask || bad) {
+            // visible tokens of this row within the 64: [0, a] and [b, c), as a 64-bit mask over tokens
+            const int a = lim - pos0, b = vlo - pos0, cc = end - pos0;
+            auto ones = [](int k) -> unsigned long long { return k <= 0 ? 0ull : (k >= 64 ? ~0ull : ((1ull << k) - 1ull)); };
+            unsigned long long see = ones(a + 1) | (ones(cc) & ~ones(b));
+            if (WIN) see &= ones(P.n_sink - pos0) | ~ones(vfirst - pos0);
+            if (bad) {           // rows of K that are none make a score none, rows of V the result
+              const unsigned long long k_bad = (unsigned long long)(kv8_flags(head[0].x) | kv8_flags(head[1].x) << 16) |
+                                               (unsigned long long)(kv8_flags(head[2].x) | kv8_flags(head[3].x) << 16) << 32;
+              const unsigned long long v_bad = (unsigned long long)(kv8_flags(head[0].y) | kv8_flags(head[1].y) << 16) |
+                                               (unsigned long long)(kv8_flags(head[2].y) | kv8_flags(head[3].y) << 16) << 32;
+              o_none |= (v_bad & see) != 0;
+              if (k_bad & see) l_run = __int_as_float(0x7fc00000);
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (((see >> (c * 32 + i)) & 1ull) == 0ull) sr[c][i] = 0xff800000u;   // -inf
+          }
+          if (__any_sync(0xffffffffu, m_ref == kNoRef)) {      // a row that has seen no token yet: what it has summed up is nothing
+            float z = -INFINITY;
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+              float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+              for (int i = 0; i < 16; ++i) mx[i & 1] = fmaxf(mx[i & 1], __uint_as_float(sr[p >> 1][(p & 1) * 16 + i]));
+              z = fmaxf(z, fmaf(fmaxf(mx[0], mx[1]), f[p], ve[p]));
+            }
+            if (m_ref == kNoRef && z > m_ref) m_ref = rintf(z);
+          }
+          // (see attention_tc.cu: probabilities relative to the standing reference; a stage in which a row outgrows it is done again)
+#pragma unroll 1
+          for (int pass = 0; pass < 2; ++pass) {
+            float ls = 0.f, z = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              uint32_t pk[16];     // 32 tokens -> 16 packed columns over the start of this S buffer
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int p = 2 * c + h;
+                const float shift = kLift + ve[p] - m_ref;
+                const float2 f2 = make_float2(f[p], f[p]), shift2 = make_float2(shift, shift);
+                float2 lsa[2] = {};
+                float mxa[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                  const int k = (i >> 1) & 1;
+                  const float2 t = make_float2(__uint_as_float(sr[c][h * 16 + i]), __uint_as_float(sr[c][h * 16 + i + 1])), y = fma2(t, f2, shift2);
+                  mxa[k] = fmaxf(mxa[k], fmaxf(t.x, t.y));
+                  const float2 pr = make_float2(exp2f(y.x), exp2f(y.y));   // exp2(-inf) = 0 for masked
+                  lsa[k] = add2(lsa[k], pr);
+                  pk[h * 8 + (i >> 1)] = pack_f16(pr.x, pr.y);
+                }
+                const float2 l2 = add2(lsa[0], lsa[1]);
+                ls = fmaf(l2.x + l2.y, kv8_pow2(-kv8_exponent(head[p].y)), ls);
+                z = fmaxf(z, fmaf(fmaxf(mxa[0], mxa[1]), f[p], ve[p]));
+              }
+              tmem_st16(s_buf + c * 16, pk);
+            }
+            const bool grow = rvalid && n > 0 && z > m_ref + kHeadroom;
+            if (pass == 1 || !__any_sync(0xffffffffu, grow)) {
+              l_run += ls;
+              break;
+            }
+            // O is rescaled in TMEM, once the group's P V of the previous stage has completed
+            bwait(pv_done, (cs - 1) & 1, DEV_TIMEOUT_MMA);
+            tc_fence_after();
+            const float m_new = grow ? rintf(z) : m_ref;
+            const float fl = exp2f(m_ref - m_new);
+            m_ref = m_new;
+            l_run *= fl;
+#pragma unroll 1
+            for (int c = 0; c < D / 16; ++c) {
+              uint32_t r[16];
+              tmem_ld16(o_addr + c * 16, r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * fl);
+              tmem_st16(o_addr + c * 16, r);
+            }
+            tmem_st_wait();
+          }
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[2 * g + (cs & 1)]);
+      }
+
+      // ---- merge the two groups' partial attentions and write out: this group finishes dims [64 g, 64 g + 64) ----
+      bwait(o_full, item & 1, DEV_TIMEOUT_MMA);
+      tc_fence_after();
+      // (the sum is of lifted probabilities, relative to a reference lower by as much; its sign says whether O is none)
+      ml_smem[g * 128 + row] = m_ref - kLift;
+      ml_smem[256 + g * 128 + row] = o_none ? -l_run : l_run;
+      softmax_bar();
+      if (warp_valid) {
+        const float r0 = ml_smem[row], r1 = ml_smem[128 + row], m_all = fmaxf(r0, r1);
+        const float w0 = exp2f(r0 - m_all), w1 = exp2f(r1 - m_all);
+        const float l0 = ml_smem[256 + row], l1 = ml_smem[384 + row];
+        const bool none = __float_as_int(l0) < 0 || __float_as_int(l1) < 0;
+        const float l_all = fabsf(l0) * w0 + fabsf(l1) * w1;
+        const float inv = none ? __int_as_float(0x7fc00000) : (w.part < 0) ? (l_all > 0.f ? 1.f / l_all : 0.f * l_all) : (l_all == l_all ? 1.f : l_all);
+        const float f0 = w0 * inv, f1 = w1 * inv;
+        const size_t orow = (size_t)(w.tok0 + row / P.group) * P.n_q + w.kv_head * P.group + row % P.group;
+        // all products of the item are complete, so its Q buffer is free: 4 KB of it per warp serve as transposition space
+        float4* s4 = reinterpret_cast<float4*>(smem + kOffQ + buf * 2 * kCodes + (warp - 4) * 4096);
+        const int nrow = min(32, R - quad * 32);
+#pragma unroll 1
+        for (int cc = 0; cc < 2; ++cc) {
+          const int c = 2 * g + cc;               // 32-dim chunk of the output row
+          uint32_t ra[32], rb[32];
+          tmem_ld32_nowait(lane_addr + kTmemO + c * 32, ra);
+          tmem_ld32_nowait(lane_addr + kTmemO + D + c * 32, rb);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) ra[i] = __float_as_uint(fmaf(__uint_as_float(rb[i]), f1, __uint_as_float(ra[i]) * f0));
+          if (w.part < 0) {
+            if (rvalid) {
+              uint4* dst = reinterpret_cast<uint4*>(P.o + orow * D + c * 32);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float* v = reinterpret_cast<const float*>(ra) + 8 * i;
+                dst[i] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+              }
+            }
+          } else {
+            // fp32 partial rows: chunk q of row r at position q ^ (r & 7), so that a store writes four whole 128-byte row segments
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              s4[lane * 8 + (q ^ (lane & 7))] = make_float4(__uint_as_float(ra[4 * q]), __uint_as_float(ra[4 * q + 1]), __uint_as_float(ra[4 * q + 2]),
+                                                           __uint_as_float(ra[4 * q + 3]));
+            __syncwarp();
+            const int rq = lane >> 3, q = lane & 7;
+            float4* dst = reinterpret_cast<float4*>(P.part_o + ((size_t)w.part * 128 + quad * 32) * D + c * 32) + q;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int rr = 4 * j + rq;
+              const float4 t = s4[rr * 8 + (q ^ (rr & 7))];
+              if (rr < nrow) __stcg(dst + (size_t)rr * (D / 4), t);
+            }
+            __syncwarp();
+          }
+        }
+        if (g == 0 && rvalid) {
+          if (w.part >= 0) {
+            P.part_ml[((size_t)w.part * 128 + row) * 2 + 0] = m_all;
+            P.part_ml[((size_t)w.part * 128 + row) * 2 + 1] = l_all;
+          } else if (P.lse) {
+            P.lse[orow] = log_sum_exp(m_all, l_all);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(o_empty);
+        mbar_arrive(&q_empty[buf]);
+      }
+      softmax_bar();          // the exchange area may be rewritten
+    }
+  }
+
+  griddep_launch();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+}  // namespace
+
+void launch_attention_kv8_tc(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
+                             int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status, cudaStream_t st, bool list_settled) {
+  static bool configured[kMaxDevices] = {false};
+  if (first_use_on_device(configured))
+    for (auto* kernel : {attention_kv8_tc_kernel<false>, attention_kv8_tc_kernel<true>})
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  Params P;
+  P.items = bl.items;
+  P.item_gap = bl.item_gap;
+  P.cta_off = bl.cta_off;
+  P.page_table = bl.page_table;
+  P.pt_stride = bl.pt_stride;
+  P.tok_climit = bl.tok_climit;
+  P.tok_lo = bl.tok_lo;
+  P.tok_hi = bl.tok_hi;
+  P.tok_first = bl.tok_first;
+  P.n_sink = bl.n_sink;
+  P.sink_blocks = (bl.n_sink + 63) / 64;
+  P.q = static_cast<const __nv_bfloat16*>(q);
+  P.o = static_cast<__nv_bfloat16*>(o);
+  P.lse = lse;
+  P.pool = static_cast<const uint8_t*>(kv_pool) + layer * kv8_layer_bytes(n_pages, dm.n_kv, D);
+  P.n_pages = n_pages;
+  P.n_q = dm.n_q;
+  P.n_kv = dm.n_kv;
+  P.group = dm.n_q / dm.n_kv;
+  P.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
+  P.part_o = part_o;
+  P.part_ml = part_ml;
+  P.status = status;
+  P.early_desc = list_settled ? 1 : 0;
+  launch_pdl(bl.window ? attention_kv8_tc_kernel<true> : attention_kv8_tc_kernel<false>, dim3(n_sm), dim3(kThreads), kSmemBytes, st, P);
+}
+
+}  // namespace recg

@@ -242,6 +242,9 @@ bool launch_attention_kv4_tc(const BatchLayout& bl, const Dims& dm, int layer, c
 void launch_attention_kv8(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
                           int64_t n_pages, float* part_o, float* part_ml, int n_sm, int max_rows, int* status, cudaStream_t st,
                           bool list_settled);
+// ... on the tcgen05 tensor cores (head_dim 128)
+void launch_attention_kv8_tc(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, float* lse, const void* kv_pool,
+                             int64_t n_pages, float* part_o, float* part_ml, int n_sm, int* status, cudaStream_t st, bool list_settled);
 size_t attention_smem_bytes(int head_dim);
 
 // S9b + S10
