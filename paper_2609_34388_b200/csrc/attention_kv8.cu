@@ -10,11 +10,15 @@
 // are fewer rows (the 8 columns of a product) than tokens or values (its 16 rows).  P^T turns from accumulators to operand by one
 // movmatrix per eight tokens.
 //
-// A warp works on 64 tokens, four pages, at a time: row g of a product is token 4 s + g % 2 (and row g + 8 the token two further) of page
-// g / 2 in product s, so that a lane's four 16-byte reads of V per value pair, one page each, are the operands of four products.  It is
-// alone with its pages: it requests them itself, 16 bytes a lane into a ring of its own, and runs ahead of itself into the next item.  The
-// warps are divided among the item's row groups, those of a group share its blocks among themselves, and their results are merged at the
-// end of the item.
+// A warp works on 32 tokens, two pages, at a time: row g of a product is token 8 (g / 2 % 2) + 4 s + g % 2 (and row g + 8 the second token
+// after that) of page g / 4 in product s, so that a lane's 8-byte reads of V are the operands of both products.  It is alone with its pages:
+// it requests them itself, 16 bytes a lane into a ring of its own, and runs ahead of itself into the next item.  The warps are divided among
+// the item's row groups, those of a group share its pieces among themselves, and their results are merged at the end of the item.
+//
+// Single rows are bound by the bytes of the cache.  One row each of sixteen requests of 512 to 8192 tokens, and one behind 131071 tokens, 32 / 8
+// heads: 27.5 and 50.8 us (floors 17.4 and 41.0; the copies alone 23.9 and 46.2).  With 64 tokens at a time, two pieces on their way and six
+// warps 28.8 and 52.0 (a request's end waits for the last of them), one piece and ten warps 39.0 and 64.4; 32 tokens, six warps with four pieces 29.0
+// and 52.2, ten with two 28.3 and 52.5.  Codes of V unpacked by ALU instructions instead of conversions: 32.3 and 57.2 instead of 29.3 and 52.6.
 #include <cuda_fp16.h>
 
 #include "kernels.h"
@@ -27,22 +31,24 @@ namespace {
 constexpr float kNoRef = -1e30f;       // reference maximum of a row that has seen no token yet
 constexpr float kHeadroom = 8.f;       // a row's reference maximum moves when it is outgrown by more than 2^8
 constexpr float kLift = 7.f;           // probabilities stand as 2^7 p: at most 2^15
-constexpr int kPages = 4, kBlockTokens = kPages * kPageSize;
+constexpr int kPages = 2, kTokens = kPages * kPageSize;      // that a warp works on at a time
+constexpr int kParts = 64 / kTokens;                            // of a block of the work list
+constexpr int kProducts = kTokens / 16;
 
 // NT: groups of eight query rows a warp has.
 template <int D, int NT>
 struct Shape {
-  static constexpr int kWarps = D == 128 && NT == 1 ? 6 : 8;
+  static constexpr int kWarps = D == 128 && NT == 1 ? 7 : 8;
   static constexpr int kThreads = kWarps * 32;
-  static constexpr int kSlots = D == 64 || NT == 1 ? 2 : 1;        // blocks that a warp has on their way
-  static constexpr int kPitch = kv8_block_bytes(D) + 32;           // a page in the ring: its codes, its header (the lanes of a product read four pages at once)
+  static constexpr int kSlots = D == 64 || NT == 1 ? 3 : 2;        // pieces that a warp has on their way
+  static constexpr int kPitch = kv8_block_bytes(D) + 64;           // a page in the ring: its codes, its header (the lanes of a product read four pages at once)
   static constexpr int kSlot = kPages * kPitch;
   static constexpr int kRing = kWarps * kSlots * kSlot;
   static constexpr int kRowPad = D + 4;                            // floats from row to row of a merged part
   static constexpr int kRows = 8 * NT;
   static constexpr int kMerge = kWarps * kRows * kRowPad * 4;      // [warp][row][value]; values D and D + 1: reference maximum, sum
   static constexpr int kItemsOff = kRing + kMerge;
-  static constexpr int kItems = 24;                                // items of the CTA whose descriptors are kept on chip
+  static constexpr int kItems = 8;                                // items of the CTA whose descriptors are kept on chip
   static constexpr int kTotal = kItemsOff + kItems * (int)sizeof(AttnItem);
   static_assert(kTotal <= 227 * 1024, "shared memory budget");
   static_assert(kWarps * kRows >= 128 || NT == 1, "every row of a tile has a warp");
@@ -104,8 +110,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint8_t* ring = smem + warp * kSlots * SH::kSlot;
   float* merge = reinterpret_cast<float*>(smem + SH::kRing);
-  // (pages that are not requested, behind a request's end: whatever the slot holds is numbers)
-  for (int i = threadIdx.x; i < SH::kRing / 16; i += SH::kThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
   // (where the work list is settled all reads of it, and of page ids, overlap the end of the kernel in front)
   if (!P.early_desc) griddep_wait();
 
@@ -119,8 +123,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
     kept[i] = reinterpret_cast<const uint4*>(P.items + item_at(i >> 1))[i & 1];
   __syncthreads();
   auto item_of = [&](int i) { return i < SH::kItems ? reinterpret_cast<const AttnItem*>(kept)[i] : P.items[item_at(i)]; };
-  // of an item: warps per row group; this warp's group; its first block and the end of all
-  struct Share { int warps, group, block, end; };
+  // of an item: warps per row group; this warp's group; its first piece and the end of all
+  struct Share { int warps, group, piece, end; };
   auto share_of = [&](const AttnItem& w) {
     Share s;
     if (NT == 1) {                       // (one group)
@@ -130,16 +134,16 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
       s.warps = W / ((w.ntok * P.group + SH::kRows - 1) / SH::kRows);
       s.group = warp / s.warps;
     }
-    s.end = s.group * SH::kRows < w.ntok * P.group ? w.blk_end : 0;
-    s.block = w.blk_begin + warp - s.group * s.warps;
+    s.end = s.group * SH::kRows < w.ntok * P.group ? kParts * w.blk_end : 0;
+    s.piece = kParts * w.blk_begin + warp - s.group * s.warps;
     return s;
   };
   // an item's blocks behind the first tokens' lie `gap` further on
   auto gap_of = [&](int i) { return WIN ? P.item_gap[item_at(i)] : 0; };
-  auto place = [&](int block, int gap) { return WIN && block >= P.sink_blocks ? block + gap : block; };
+  auto place = [&](int piece, int gap) { return WIN && piece >= kParts * P.sink_blocks ? piece + kParts * gap : piece; };
 
-  // ---- what the warp requests next: a block of an item.  Page ids are fetched 32 at a time, a lane one of them ----
-  int f_item = -1, f_block = 0, f_step = 0, f_end = 0, f_used = 0, f_ids = 0, f_pages = 0, f_gap = 0;
+  // ---- what the warp requests next: a piece of an item.  Page ids are fetched 32 at a time, a lane one of them ----
+  int f_item = -1, f_piece = 0, f_step = 0, f_end = 0, f_used = 0, f_ids = 0, f_pages = 0, f_gap = 0;
   const int* f_table = nullptr;
   const uint8_t* f_base = nullptr;       // this lane's 16 bytes of the head's block in page 0
   const uint8_t* f_header = nullptr;
@@ -147,8 +151,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
   const uint32_t ring_at = smem_u32(ring) + lane * 16;
   auto load_ids = [&]() {
     f_used = 0;
-    const int block = f_block + (lane / kPages) * f_step, page = place(block, f_gap) * kPages + lane % kPages;
-    f_ids = block < f_end && page < f_pages ? __ldg(f_table + page) : -1;
+    const int piece = f_piece + (lane / kPages) * f_step, page = place(piece, f_gap) * kPages + lane % kPages;
+    f_ids = piece < f_end && page < f_pages ? __ldg(f_table + page) : -1;
   };
   auto next_item = [&]() {
     do {
@@ -158,7 +162,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
       }
       const AttnItem w = item_of(f_item);
       const Share s = share_of(w);
-      f_block = s.block;
+      f_piece = s.piece;
       f_step = s.warps;
       f_end = s.end;
       f_gap = gap_of(f_item);
@@ -166,7 +170,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
       f_table = P.page_table + (size_t)w.req * P.pt_stride;
       f_base = P.pool + (size_t)w.kv_head * kv8_block_bytes(D) + lane * 16;
       f_header = P.pool + kv8_headers(P.n_pages, P.n_kv, D) + (size_t)w.kv_head * 8;
-    } while (f_block >= f_end);
+    } while (f_piece >= f_end);
     load_ids();
   };
   auto request = [&](uint32_t slot_at) {        // one group of copies per call, be it empty
@@ -174,8 +178,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
 #pragma unroll
       for (int i = 0; i < kPages; ++i) {
         const int id = __shfl_sync(0xffffffffu, f_ids, f_used + i);
-        if ((unsigned)id >= n_pages) {
-          if (id >= 0 || place(f_block, f_gap) * kPages + i < f_pages) set_status(P.status, DEV_BAD_INDEX);
+        if ((unsigned)id >= n_pages) {          // (none behind the request's end: what stands in for it is numbers)
+          if (id >= 0 || place(f_piece, f_gap) * kPages + i < f_pages) set_status(P.status, DEV_BAD_INDEX);
+          for (int x = lane; x < SH::kPitch / 16; x += 32) reinterpret_cast<uint4*>(ring + slot_at + i * SH::kPitch)[x] = make_uint4(0, 0, 0, 0);
           continue;
         }
         const uint8_t* src = f_base + (uint64_t)(unsigned)id * page_bytes;
@@ -184,9 +189,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
         for (int x = 0; x < kv8_block_bytes(D) / 512; ++x) copy16(dst + x * 512, src + x * 512);
         if (lane == 0) copy8(dst + kv8_block_bytes(D), f_header + (uint64_t)(unsigned)id * (8u * P.n_kv));
       }
-      f_block += f_step;
+      f_piece += f_step;
       f_used += kPages;
-      if (f_block >= f_end) next_item();
+      if (f_piece >= f_end) next_item();
       else if (f_used >= 32) load_ids();
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -222,7 +227,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
   if (item_end > 0) load_rows(item_of(0));
   for (int s = 0; s < kSlots; ++s) request(s * SH::kSlot);
 
-  uint32_t slot_at = 0;   // the slot of the next block
+  uint32_t slot_at = 0;   // the slot of the next piece
   for (int item = 0; item < item_end; ++item) {
     const AttnItem w = item_of(item);
     const int R = w.ntok * P.group, gap = gap_of(item);
@@ -278,22 +283,22 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
       l[nt][0] = l[nt][1] = 0.f;
     }
 
-    for (int block = sh.block; block < sh.end; block += sh.warps) {
+    for (int piece = sh.piece; piece < sh.end; piece += sh.warps) {
       asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 1) : "memory");
-      __syncwarp();
+      __syncwarp();      // (the zeros of pages that there are not, too)
       const uint8_t* pg = ring + slot_at;
-      const int pos0 = place(block, gap) * kBlockTokens;
-      // this lane's page (g / 2 of the block): both its tokens of a product are there
-      const int page_pos = pos0 + (g >> 1) * kPageSize + (g & 1);
-      const uint2 head = *reinterpret_cast<const uint2*>(pg + (g >> 1) * SH::kPitch + kv8_block_bytes(D));
+      const int pos0 = place(piece, gap) * kTokens;
+      // this lane's tokens of product s: 4 s + my_tok and the second one after that, of page g / 4
+      const int my_tok = ((g << 2) & 8) + (g & 1), page_pos = pos0 + (g >> 2) * kPageSize + my_tok;
+      const uint2 head = *reinterpret_cast<const uint2*>(pg + (g >> 2) * SH::kPitch + kv8_block_bytes(D));
       // ---- S^T = C_K Q^T ----
-      float sc[4][NT][4];
+      float sc[kProducts][NT][4];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
+      for (int s = 0; s < kProducts; ++s) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) sc[s][nt][0] = sc[s][nt][1] = sc[s][nt][2] = sc[s][nt][3] = 0.f;
-        const uint8_t* rows = pg + (g >> 1) * SH::kPitch;
-        const int tok = 4 * s + (g & 1);
+        const uint8_t* rows = pg + (g >> 2) * SH::kPitch;
+        const int tok = 4 * s + my_tok;
 #pragma unroll
         for (int c = 0; c < NW / 2; ++c) {
           const uint4 k0 = *reinterpret_cast<const uint4*>(rows + kv8_k_chunk<D>(tok, t * (NW / 2) + c));
@@ -311,17 +316,17 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
       const float k_scale = kv8_pow2(kv8_exponent(head.x)), v_exp = (float)kv8_exponent(head.y), v_back = kv8_pow2(-kv8_exponent(head.y));
       const uint32_t k_bad = kv8_flags(head.x), v_bad = kv8_flags(head.y);
       const bool some_bad = __any_sync(0xffffffffu, (k_bad | v_bad) != 0);
-      const bool masked = pos0 + kBlockTokens - 1 > lim || (WIN && pos0 < from);
+      const bool masked = pos0 + kTokens - 1 > lim || (WIN && pos0 < from);
       float top = -INFINITY;
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+      for (int s = 0; s < kProducts; ++s)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             // (the product with a power of two is exact: a sum rounded once)
             float y = fmaf(__fmul_rn(sc[s][nt][e], back[nt][e & 1]), k_scale, v_exp);
-            if (some_bad && (k_bad >> (4 * s + 2 * (e >> 1) + (g & 1))) & 1) y = NAN;
+            if (some_bad && (k_bad >> (4 * s + 2 * (e >> 1) + my_tok)) & 1) y = NAN;
             if (masked) {
               const int pos = page_pos + 4 * s + 2 * (e >> 1), c = e & 1;
               const bool sees = (pos <= climit[nt][c] || (pos >= vlo[nt][c] && pos < vhi[nt][c])) && (!WIN || pos < P.n_sink || pos >= vfirst[nt][c]);
@@ -338,7 +343,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
           for (int c = 0; c < 2; ++c) {
             float z = -INFINITY;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) z = fmaxf(z, fmaxf(sc[s][nt][c], sc[s][nt][2 + c]));
+            for (int s = 0; s < kProducts; ++s) z = fmaxf(z, fmaxf(sc[s][nt][c], sc[s][nt][2 + c]));
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, x));
             const float to = z - kLift;
@@ -354,9 +359,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
           }
       }
       // ---- probabilities; O^T += C_V^T P^T ----
-      uint32_t b[4][NT][2];
+      uint32_t b[kProducts][NT][2];
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+      for (int s = 0; s < kProducts; ++s)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float p[4];
@@ -365,18 +370,18 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attention_kv8_kerne
             p[e] = exp2f(__fsub_rn(sc[s][nt][e], ref[nt][e & 1]));
             l[nt][e & 1] = fmaf(p[e], v_back, l[nt][e & 1]);
             // (a row of V that is none makes those that see it none, not their sums)
-            if (some_bad && (v_bad >> (4 * s + 2 * (e >> 1) + (g & 1))) & 1 && sc[s][nt][e] != -INFINITY) p[e] = NAN;
+            if (some_bad && (v_bad >> (4 * s + 2 * (e >> 1) + my_tok)) & 1 && sc[s][nt][e] != -INFINITY) p[e] = NAN;
           }
           b[s][nt][0] = transpose8x8(pack_f16(p[0], p[1]));
           b[s][nt][1] = transpose8x8(pack_f16(p[2], p[3]));
         }
-      const uint8_t* values = pg + t * SH::kPitch + 16 * D + g * 16;
+      const uint8_t* values = pg + (t >> 1) * SH::kPitch + 16 * D + g * 16 + (t & 1) * 8;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
-        const uint4 v0 = *reinterpret_cast<const uint4*>(values + i * 256), v1 = *reinterpret_cast<const uint4*>(values + i * 256 + 128);
-        const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
+        const uint2 v0 = *reinterpret_cast<const uint2*>(values + i * 256), v1 = *reinterpret_cast<const uint2*>(values + i * 256 + 128);
+        const uint32_t w0[2] = {v0.x, v0.y}, w1[2] = {v1.x, v1.y};
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < kProducts; ++s) {
           const uint32_t a0 = e4m3_to_f16(w0[s] & 0xffffu), a1 = e4m3_to_f16(w1[s] & 0xffffu), a2 = e4m3_to_f16(w0[s] >> 16), a3 = e4m3_to_f16(w1[s] >> 16);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][i], a0, a1, a2, a3, b[s][nt][0], b[s][nt][1]);
@@ -488,7 +493,7 @@ void launch_attention_kv8(const BatchLayout& bl, const Dims& dm, int layer, cons
   P.group = dm.n_q / dm.n_kv;
   P.inv_group = 65536 / P.group + 1;
   P.n_sink = bl.n_sink;
-  P.sink_blocks = (bl.n_sink + kBlockTokens - 1) / kBlockTokens;
+  P.sink_blocks = (bl.n_sink + 63) / 64;
   P.scale_log2 = 1.4426950408889634f / sqrtf((float)dm.head_dim);
   P.part_o = part_o;
   P.part_ml = part_ml;
