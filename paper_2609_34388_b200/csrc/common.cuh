@@ -131,6 +131,11 @@ __device__ __forceinline__ float2 fma2(const float2& a, const float2& b, const f
       : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)), "l"(reinterpret_cast<const uint64_t&>(c)));
   return reinterpret_cast<float2&>(d);
 }
+__device__ __forceinline__ float2 mul2(const float2& a, const float2& b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
+  return reinterpret_cast<float2&>(d);
+}
 __device__ __forceinline__ float2 add2(const float2& a, const float2& b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));

@@ -55,12 +55,12 @@ struct Kv8Block {
   uint32_t x[16][N];
 };
 
-// Rows [0, n) as the pool holds them, and their flags.  K: codes in rows; V: a row of codes per value.
+// Rows [0, n) as the pool holds them, the others 0, and their flags.  K: codes in rows; V: a row of codes per value.
 template <int D, bool V>
 __device__ __forceinline__ uint32_t kv8_load(Kv8Block<D>& b, const uint8_t* codes, uint32_t header, int n, int lane) {
   constexpr int N = Kv8Block<D>::N;
   const float scale = kv8_pow2(kv8_exponent(header));
-  const uint32_t flags = kv8_flags(header);
+  const uint32_t flags = kv8_flags(header) & ((1u << n) - 1u);
   uint32_t w[16];                                  // row's codes: 2 N of them
   if (V) {
     uint4 t[2 * N];
@@ -81,54 +81,76 @@ __device__ __forceinline__ uint32_t kv8_load(Kv8Block<D>& b, const uint8_t* code
   } else {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      if constexpr (N == 2) w[r] = r < n ? *reinterpret_cast<const uint32_t*>(codes + kv8_k_chunk<D>(r, lane >> 2) + 4 * (lane & 3)) : 0u;
-      else w[r] = r < n ? *reinterpret_cast<const uint16_t*>(codes + kv8_k_chunk<D>(r, lane >> 3) + 2 * (lane & 7)) : 0u;
+      if constexpr (N == 2) w[r] = *reinterpret_cast<const uint32_t*>(codes + kv8_k_chunk<D>(r, lane >> 2) + 4 * (lane & 3));
+      else w[r] = *reinterpret_cast<const uint16_t*>(codes + kv8_k_chunk<D>(r, lane >> 3) + 2 * (lane & 7));
     }
   }
+  if (n < 16)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (r >= n) w[r] = 0;
 #pragma unroll
   for (int r = 0; r < 16; ++r)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float2 f = f16_pair(e4m3_to_f16(i ? w[r] >> 16 : w[r] & 0xffffu));
-      b.x[r][i] = r >= n ? 0u : (flags >> r) & 1 ? 0x7fc07fc0u : pack_bf16(f.x * scale, f.y * scale);
+      b.x[r][i] = pack_bf16(f.x * scale, f.y * scale);
     }
-  return flags & ((1u << n) - 1u);
+  if (flags)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if ((flags >> r) & 1) b.x[r][i] = 0x7fc07fc0u;
+  return flags;
 }
 
-// Stores rows [0, n) as codes, the others as 0, and returns the header.
+// Stores a block as codes and returns the header.  Rows that are not there are 0.
 template <int D, bool V>
-__device__ __forceinline__ uint32_t kv8_store(const Kv8Block<D>& b, uint8_t* codes, int n, int lane) {
+__device__ __forceinline__ uint32_t kv8_store(Kv8Block<D>& b, uint8_t* codes, int lane) {
   constexpr int N = Kv8Block<D>::N;
-  uint32_t bad = 0;
+  uint32_t top = 0, bad = 0;                       // largest magnitude, as the bits of a bf16 number
 #pragma unroll
   for (int r = 0; r < 16; ++r)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint32_t a = b.x[r][i] & 0x7fff7fffu;
-      if ((a & 0xffffu) >= 0x7f80u || a >= 0x7f800000u) bad |= 1u << r;
-    }
-  bad = __reduce_or_sync(0xffffffffu, bad) & ((1u << n) - 1u);
-  uint32_t top = 0;                                // largest magnitude, as the bits of a bf16 number
-#pragma unroll
-  for (int r = 0; r < 16; ++r)
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (r < n && !((bad >> r) & 1)) top = __vmaxu2(top, b.x[r][i] & 0x7fff7fffu);
+    for (int i = 0; i < N; ++i) top = __vmaxu2(top, b.x[r][i] & 0x7fff7fffu);
   top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+  if (top >= 0x7f80u) {                            // rows that are none, which go, and the largest of the others
+    top = 0;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) m = __vmaxu2(m, b.x[r][i] & 0x7fff7fffu);
+      m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+      if (m < 0x7f80u) {
+        top = max(top, m);
+        continue;
+      }
+      bad |= 1u << r;
+#pragma unroll
+      for (int i = 0; i < N; ++i) b.x[r][i] = 0;
+    }
+  }
   // 2^(f - 127) (1 + m / 128) <= 1.75 2^8 2^e
   const int e = top == 0 ? 0 : max(kKv8Least, min(kKv8Most, (int)(top >> 7) - 127 - 8 + ((top & 127) > 96 ? 1 : 0)));
-  const float down = kv8_pow2(-e), end = e == kKv8Most ? 240.f : 448.f;
+  if (e == kKv8Most)                               // (codes end at 240: magnitudes at 240 2^120)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int i = 0; i < N; ++i) b.x[r][i] = __vminu2(b.x[r][i] & 0x7fff7fffu, 0x7f707f70u) | (b.x[r][i] & 0x80008000u);
+  const float2 down = make_float2(kv8_pow2(-e), kv8_pow2(-e));
   uint32_t w[16];
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    const bool live = r < n && !((bad >> r) & 1);
-    w[r] = 0;
+    uint32_t two[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float lo = __uint_as_float(b.x[r][i] << 16) * down, hi = __uint_as_float(b.x[r][i] & 0xffff0000u) * down;
-      w[r] |= e4m3_from(fmaxf(-end, fminf(end, lo)), fmaxf(-end, fminf(end, hi))) << (16 * i);
+      const float2 f = mul2(make_float2(__uint_as_float(b.x[r][i] << 16), __uint_as_float(b.x[r][i] & 0xffff0000u)), down);
+      two[i] = e4m3_from(f.x, f.y);
     }
-    if (!live) w[r] = 0;
+    if constexpr (N == 2) w[r] = __byte_perm(two[0], two[1], 0x5410);
+    else w[r] = two[0];
     if constexpr (!V) {
       if constexpr (N == 2) *reinterpret_cast<uint32_t*>(codes + kv8_k_chunk<D>(r, lane >> 2) + 4 * (lane & 3)) = w[r];
       else *reinterpret_cast<uint16_t*>(codes + kv8_k_chunk<D>(r, lane >> 3) + 2 * (lane & 7)) = (uint16_t)w[r];
