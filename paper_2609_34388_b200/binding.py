@@ -448,7 +448,7 @@ class Context:
             kv = torch.empty((2, n, heads, d), dtype=torch.bfloat16, device=_CUDA)
             at = kv.data_ptr()
             self._check(lib().recg_kv_rows(self.h, C.byref(batch.c) if batch is not None else None, layer, at, at + 2 * n * heads * d, 0))
-            return kv[0], kv[1]
+            return kv.unbind(0)
         b, kp, vp, stride = self._kv_rows_args(batch, k, v)
         self._check(lib().recg_kv_rows(self.h, b, layer, kp, vp, stride))
         return k, v

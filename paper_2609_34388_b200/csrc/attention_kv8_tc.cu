@@ -52,8 +52,8 @@ constexpr int kOffRaw = kOffK + kKRing * kCodes;
 constexpr int kOffV = kOffRaw + kRawRing * kCodes;
 constexpr int kOffML = kOffV + kVRing * kVBytes;                   // per row, both groups: reference; sum (negative: O is none)
 constexpr int kOffQF = kOffML + 2 * 2 * 128 * 4;                   // per row, two items: the factor of its scores
-constexpr int kOffHead = kOffQF + 2 * 128 * 4;                     // [kHeadRing][8 pages] headers
-constexpr int kOffBar = kOffHead + kHeadRing * kPages * 8;
+constexpr int kOffHead = kOffQF + 2 * 128 * 4;                     // [kHeadRing][8 pages] 2^f of K, e and 2^-e of V, flags of K | V << 16
+constexpr int kOffBar = kOffHead + kHeadRing * kPages * 16;
 constexpr int kNumBars = 2 * kKRing + 2 * kRawRing + 2 * kVRing + 4 + 2 + 4 + 3;
 constexpr int kSmemBytes = kOffBar + kNumBars * 8 + 16;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory budget");
@@ -74,7 +74,7 @@ struct Params {
   float* lse;
   const uint8_t* pool;     // of the layer
   int64_t n_pages;
-  int n_q, n_kv, group;
+  int n_q, n_kv, group, inv_group;      // inv_group: (row * inv_group) >> 16 is row / group for the rows of a tile
   float scale_log2;
   float* part_o;
   float* part_ml;
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* ml_smem = reinterpret_cast<float*>(smem + kOffML);
   float* qf_smem = reinterpret_cast<float*>(smem + kOffQF);
-  int2* head_smem = reinterpret_cast<int2*>(smem + kOffHead);
+  float4* head_smem = reinterpret_cast<float4*>(smem + kOffHead);
   // (the MMA issuer and the softmax warps, whom the stage waits for, poll more often)
   auto bwait = [&](uint64_t* bar, uint32_t parity, int code) {
     if (mbar_test_wait(bar, parity) || *abort_flag) return;
@@ -252,7 +252,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P)
         const Page after = fetch_page();
         const int s = blk % ring;
         lazy_wait(&empty[s], ((blk / ring) & 1) ^ 1, DEV_TIMEOUT_EMPTY);
-        if (!v && lane < kPages) head_smem[(blk % kHeadRing) * kPages + lane] = head;
+        if (!v && lane < kPages) {
+          const int e = kv8_exponent(head.y);
+          head_smem[(blk % kHeadRing) * kPages + lane] =
+              make_float4(kv8_pow2(kv8_exponent(head.x)), (float)e, kv8_pow2(-e), __int_as_float((int)(kv8_flags(head.x) | kv8_flags(head.y) << 16)));
+        }
         const unsigned mask = __ballot_sync(0xffffffffu, now.id >= 0);
         if (lane == 0) {
           if (mask == 0) mbar_arrive(&full[s]);
@@ -418,19 +422,26 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P)
     const uint32_t s_addr = lane_addr + g * 64, o_addr = lane_addr + kTmemO + g * D;
     uint32_t cs = 0;                           // stages so far
     AttnItem w_next = item_end > 0 ? P.items[item_at(0)] : AttnItem{};
+    // what this thread's row sees, fetched one item ahead
+    int nx_climit = -1, nx_lo = 0, nx_hi = 0, nx_first = 0;
+    auto sight = [&]() {
+      nx_climit = -1;
+      nx_lo = nx_hi = nx_first = 0;
+      if (row < w_next.ntok * P.group) {
+        const int t = w_next.tok0 + ((row * P.inv_group) >> 16);
+        nx_climit = P.tok_climit[t];
+        nx_lo = P.tok_lo[t];
+        nx_hi = P.tok_hi[t];
+        if (WIN) nx_first = P.tok_first[t];
+      }
+    };
+    sight();
     for (int item = 0; item < item_end; ++item) {
       const AttnItem w = w_next;
       if (item + 1 < item_end) w_next = P.items[item_at(item + 1)];
       const int R = w.ntok * P.group, nblk = stages_of(w), gap = gap_of(item), buf = item & 1;
       const bool rvalid = row < R, warp_valid = quad * 32 < R;
-      int climit = -1, vlo = 0, vhi = 0, vfirst = 0;
-      if (rvalid) {
-        const int t = w.tok0 + row / P.group;
-        climit = P.tok_climit[t];
-        vlo = P.tok_lo[t];
-        vhi = P.tok_hi[t];
-        if (WIN) vfirst = P.tok_first[t];
-      }
+      const int climit = nx_climit, vlo = nx_lo, vhi = nx_hi, vfirst = nx_first;
       bwait(&q_ready[buf], (item >> 1) & 1, DEV_TIMEOUT_FULL);
       const float qf = qf_smem[buf * 128 + row];               // (a row that does not exist: whatever)
       // The row's reference (powers of two, a whole number: adding exponents to it is exact) and sum; whether it sees V that is none.
@@ -447,16 +458,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P)
           uint32_t sr[2][32];   // the S row of this thread: 64 scores, in units of 1 / f of their page
 #pragma unroll
           for (int c = 0; c < 2; ++c) tmem_ld32_nowait(s_buf + c * 32, sr[c]);
-          const int2* heads = head_smem + (cs % kHeadRing) * kPages + 4 * g;
-          int2 head[4];
-          float f[4], ve[4];
+          const float4* heads = head_smem + (cs % kHeadRing) * kPages + 4 * g;
+          float f[4], ve[4], back[4];
           uint32_t bad = 0;
 #pragma unroll
           for (int p = 0; p < 4; ++p) {
-            head[p] = heads[p];
-            f[p] = fminf(fmaxf(qf * kv8_pow2(kv8_exponent(head[p].x)), 1e-37f), 3e38f);      // (times -inf it stays that)
-            ve[p] = (float)kv8_exponent(head[p].y);
-            bad |= kv8_flags(head[p].x) | kv8_flags(head[p].y);
+            const float4 h = heads[p];
+            f[p] = fminf(fmaxf(qf * h.x, 1e-37f), 3e38f);      // (times -inf it stays that)
+            ve[p] = h.y;
+            back[p] = h.z;
+            bad |= (uint32_t)__float_as_int(h.w);
           }
           tmem_ld_wait();
           // (a block that the item does not have is seen by no row)
@@ -469,10 +480,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P)
             unsigned long long see = ones(a + 1) | (ones(cc) & ~ones(b));
             if (WIN) see &= ones(P.n_sink - pos0) | ~ones(vfirst - pos0);
             if (bad) {           // rows of K that are none make a score none, rows of V the result
-              const unsigned long long k_bad = (unsigned long long)(kv8_flags(head[0].x) | kv8_flags(head[1].x) << 16) |
-                                               (unsigned long long)(kv8_flags(head[2].x) | kv8_flags(head[3].x) << 16) << 32;
-              const unsigned long long v_bad = (unsigned long long)(kv8_flags(head[0].y) | kv8_flags(head[1].y) << 16) |
-                                               (unsigned long long)(kv8_flags(head[2].y) | kv8_flags(head[3].y) << 16) << 32;
+              unsigned long long k_bad = 0, v_bad = 0;
+#pragma unroll
+              for (int p = 0; p < 4; ++p) {
+                const uint32_t flags = (uint32_t)__float_as_int(heads[p].w);
+                k_bad |= (unsigned long long)(flags & 0xffffu) << (16 * p);
+                v_bad |= (unsigned long long)(flags >> 16) << (16 * p);
+              }
               o_none |= (v_bad & see) != 0;
               if (k_bad & see) l_run = __int_as_float(0x7fc00000);
             }
@@ -517,7 +531,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P)
                   pk[h * 8 + (i >> 1)] = pack_f16(pr.x, pr.y);
                 }
                 const float2 l2 = add2(lsa[0], lsa[1]);
-                ls = fmaf(l2.x + l2.y, kv8_pow2(-kv8_exponent(head[p].y)), ls);
+                ls = fmaf(l2.x + l2.y, back[p], ls);
                 z = fmaxf(z, fmaf(fmaxf(mxa[0], mxa[1]), f[p], ve[p]));
               }
               tmem_st16(s_buf + c * 16, pk);
@@ -552,6 +566,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P)
         if (lane == 0) mbar_arrive(&p_full[2 * g + (cs & 1)]);
       }
 
+      if (item + 1 < item_end) sight();
       // ---- merge the two groups' partial attentions and write out: this group finishes dims [64 g, 64 g + 64) ----
       bwait(o_full, item & 1, DEV_TIMEOUT_MMA);
       tc_fence_after();
@@ -567,7 +582,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P)
         const float l_all = fabsf(l0) * w0 + fabsf(l1) * w1;
         const float inv = none ? __int_as_float(0x7fc00000) : (w.part < 0) ? (l_all > 0.f ? 1.f / l_all : 0.f * l_all) : (l_all == l_all ? 1.f : l_all);
         const float f0 = w0 * inv, f1 = w1 * inv;
-        const size_t orow = (size_t)(w.tok0 + row / P.group) * P.n_q + w.kv_head * P.group + row % P.group;
+        const auto row_at = [&](int r) {
+          const int j = (r * P.inv_group) >> 16;
+          return (size_t)(w.tok0 + j) * P.n_q + w.kv_head * P.group + r - j * P.group;
+        };
         // all products of the item are complete, so its Q buffer is free: 4 KB of it per warp serve as transposition space
         float4* s4 = reinterpret_cast<float4*>(smem + kOffQ + buf * 2 * kCodes + (warp - 4) * 4096);
         const int nrow = min(32, R - quad * 32);
@@ -581,14 +599,22 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P)
 #pragma unroll
           for (int i = 0; i < 32; ++i) ra[i] = __float_as_uint(fmaf(__uint_as_float(rb[i]), f1, __uint_as_float(ra[i]) * f0));
           if (w.part < 0) {
-            if (rvalid) {
-              uint4* dst = reinterpret_cast<uint4*>(P.o + orow * D + c * 32);
+            // through shared memory (piece q of row r at q ^ ((r >> 1) & 3)), so that a store writes 64-byte pieces of eight rows
+            uint4* h4 = reinterpret_cast<uint4*>(s4);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float* v = reinterpret_cast<const float*>(ra) + 8 * i;
-                dst[i] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-              }
+            for (int q = 0; q < 4; ++q) {
+              const float* v = reinterpret_cast<const float*>(ra) + 8 * q;
+              h4[lane * 4 + (q ^ ((lane >> 1) & 3))] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
             }
+            __syncwarp();
+            const int q = lane & 3;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int rr = 8 * k + (lane >> 2);
+              const uint4 t = h4[rr * 4 + (q ^ ((rr >> 1) & 3))];
+              if (rr < nrow) reinterpret_cast<uint4*>(P.o + row_at(quad * 32 + rr) * D + c * 32)[q] = t;
+            }
+            __syncwarp();
           } else {
             // fp32 partial rows: chunk q of row r at position q ^ (r & 7), so that a store writes four whole 128-byte row segments
 #pragma unroll
@@ -612,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kv8_tc_kernel(Params P)
             P.part_ml[((size_t)w.part * 128 + row) * 2 + 0] = m_all;
             P.part_ml[((size_t)w.part * 128 + row) * 2 + 1] = l_all;
           } else if (P.lse) {
-            P.lse[orow] = log_sum_exp(m_all, l_all);
+            P.lse[row_at(row)] = log_sum_exp(m_all, l_all);
           }
         }
       }
@@ -663,6 +689,7 @@ void launch_attention_kv8_tc(const BatchLayout& bl, const Dims& dm, int layer, c
   P.n_q = dm.n_q;
   P.n_kv = dm.n_kv;
   P.group = dm.n_q / dm.n_kv;
+  P.inv_group = 65536 / P.group + 1;
   P.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
   P.part_o = part_o;
   P.part_ml = part_ml;

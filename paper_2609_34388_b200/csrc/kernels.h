@@ -292,8 +292,9 @@ void launch_kv8_io(bool write, void* pool, int64_t n_pages, int layer, const Dim
                    void* k, void* v, cudaStream_t st);
 void launch_kv8_rows(bool write, bool staged, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, void* k, void* v,
                      int64_t row_stride, cudaStream_t st);
-// q and k of the batch laid out last turned to their positions, k and v into the pool; q may be null
-void launch_append_rotary(int bits, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, const void* q, int64_t q_stride,
+// q and k of the batch laid out last turned to their positions, k and v into the pool; q may be null.  turn: HOST [head_dim / 2], what a position
+// turns each pair of values by
+void launch_append_rotary(int bits, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, const double* turn, const void* q, int64_t q_stride,
                           void* q_out, const void* k, const void* v, int64_t kv_stride, cudaStream_t st);
 
 // The rows of a round that the QKV projection has left in a bf16 staging pool (row t in slot t of it) into a pool in 4 bits

@@ -5,7 +5,6 @@
 // all of them, and the block is written whole.  The bytes bound it: 4 d in and 2 d out per position and head (K and V) to write, the
 // reverse to read.
 #include <algorithm>
-#include <cmath>
 #include <cstring>
 
 #include "kernels.h"
@@ -383,8 +382,8 @@ void launch_kv8_rows(bool write, bool staged, const BatchLayout& bl, void* pool,
              static_cast<uint8_t*>(k), static_cast<uint8_t*>(v), row_stride);
 }
 
-void launch_append_rotary(int bits, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, const void* q, int64_t q_stride,
-                          void* q_out, const void* k, const void* v, int64_t kv_stride, cudaStream_t st) {
+void launch_append_rotary(int bits, const BatchLayout& bl, void* pool, int64_t n_pages, int layer, const Dims& dm, const double* turn, const void* q,
+                          int64_t q_stride, void* q_out, const void* k, const void* v, int64_t kv_stride, cudaStream_t st) {
   RotaryArgs A;
   A.q = static_cast<const uint8_t*>(q);
   A.k = static_cast<const uint8_t*>(k);
@@ -397,10 +396,7 @@ void launch_append_rotary(int bits, const BatchLayout& bl, void* pool, int64_t n
   A.layer = layer;
   A.n_q = dm.n_q;
   A.n_kv = dm.n_kv;
-  const int half = dm.head_dim / 2;
-  for (int i = 0; i < half; ++i) {
-    A.turn[i] = exp(-log((double)dm.rope_base) * i / half);
-  }
+  memcpy(A.turn, turn, dm.head_dim / 2 * sizeof(double));
   using Kernel = void (*)(const BatchLayout, const RotaryArgs);
   Kernel kernel;
   if (dm.head_dim == 128) kernel = bits == 16 ? append_rotary_kernel<128, 16> : bits == 8 ? append_rotary_kernel<128, 8> : append_rotary_kernel<128, 4>;

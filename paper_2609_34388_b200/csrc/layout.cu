@@ -104,7 +104,7 @@ __device__ __forceinline__ TokenPos layout_token(const BatchLayout& bl, int r, i
     lo = first;
     hi = q == 0 ? first + 1 : first + span;
   }
-  bl.tok_first[t] = bl.window ? max(pos - bl.window + 1, 0) : 0;
+  if (bl.window) bl.tok_first[t] = max(pos - bl.window + 1, 0);
   if (bl.pos_shift) pos += bl.pos_shift[r];
   bl.tok_weight[t] = j < v ? 1.f : 0.f;
   bl.tok_req[t] = r;
@@ -121,6 +121,8 @@ __device__ __forceinline__ TokenPos layout_token(const BatchLayout& bl, int r, i
   return TokenPos{id, pos};
 }
 
+// WIN: rows look back a window.  (As a condition at run time it took .5 to 1.4 us of every call that lays a batch out.)
+template <bool WIN>
 __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, int n_kv, int mask_id, int tok_per_tile,
                                                                 int n_ctas, int whole, int list, int64_t n_pages, int* status, int* desc_dev,
                                                                 const __grid_constant__ SmallDesc desc) {
@@ -199,7 +201,7 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, 
     const int last_row = min(n, (g.tile + (pair ? 2 : 1)) * tok_per_tile);
     g.nb = (ctx[g.r] + (last_row <= vis[g.r] ? last_row : n) + 63) / 64;
     g.gap = 0;
-    if (bl.window) {        // rows stand one behind the other, but for those of branches, whose positions lie behind ctx
+    if (WIN) {        // rows stand one behind the other, but for those of branches, whose positions lie behind ctx
       const int first = ctx[g.r] + (last_row <= vis[g.r] + bl.block_size[g.r] ? g.tile * tok_per_tile : 0) - bl.window + 1;
       g.gap = max(0, first / 64 - sink_blocks);
       g.nb -= g.gap;
@@ -291,7 +293,7 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, 
           a.kv_len = kv_len;
           if (at + (c - c_first) < bl.max_items && a.part < bl.max_parts) {
             bl.items[at + (c - c_first)] = a;
-            bl.item_gap[at + (c - c_first)] = g.gap;
+            if (WIN) bl.item_gap[at + (c - c_first)] = g.gap;
           }
         }
       }
@@ -579,9 +581,10 @@ void launch_layout(const BatchLayout& bl, const Dims& dm, int tok_per_tile, int 
   const size_t smem = layout_smem_bytes(bl.n_req, n_ctas);
   static bool configured[kMaxDevices] = {false};
   if (first_use_on_device(configured))    // room for kMaxLayoutRequests requests (the default limit is 48 KB)
-    cudaFuncSetAttribute(layout_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)layout_smem_bytes(kMaxLayoutRequests, 1024));
+    for (auto* kernel : {layout_kernel<false>, layout_kernel<true>})
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)layout_smem_bytes(kMaxLayoutRequests, 1024));
   const int token_ctas = tokens ? (bl.n_tok + kLayoutThreads - 1) / kLayoutThreads : 0;
-  launch_pdl(layout_kernel, dim3(1 + token_ctas), dim3(kLayoutThreads), smem, st, bl, dm.n_kv, dm.mask_id, tok_per_tile, n_ctas,
+  launch_pdl(bl.window ? layout_kernel<true> : layout_kernel<false>, dim3(1 + token_ctas), dim3(kLayoutThreads), smem, st, bl, dm.n_kv, dm.mask_id, tok_per_tile, n_ctas,
              whole ? 1 : 0, list ? 1 : 0, n_pages, status, desc_dev, desc ? *desc : none);
 }
 

@@ -1,5 +1,6 @@
 // The C ABI: context, workspace, descriptor validation and the per-step launch sequence.
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <new>
@@ -50,6 +51,7 @@ struct recg_ctx {
   std::vector<const void*> attn_norm, wqkv, wo, ffn_norm, w_gate_up, w_down;
   cudaStream_t stream = nullptr;
   int n_sm = 0, tok_per_tile = 0, target_items = 0;
+  double turn[64] = {};          // what a position turns the pairs of values by: base^(-2 i / d)
   std::string err;
 
   DeviceArena arena;
@@ -553,6 +555,7 @@ recg_status recg_init(recg_ctx** out, const recg_config* cfg, const recg_weights
                  g.mask_token_id < 0 ? g.vocab - 1 : g.mask_token_id};
   ctx->stream = static_cast<cudaStream_t>(cuda_stream);
   ctx->n_sm = n_sm;
+  for (int i = 0; i < g.head_dim / 2; ++i) ctx->turn[i] = std::exp(-std::log((double)g.rope_base) * i / (g.head_dim / 2));
   ctx->tok_per_tile = 128 / group;
   ctx->target_items = n_sm;
   ctx->has_weights = w != nullptr;
@@ -604,6 +607,9 @@ recg_status recg_init(recg_ctx** out, const recg_config* cfg, const recg_weights
     ctx->h_vout = nullptr;   // fall back to one copy per output array
   }
   cudaMemsetAsync(ctx->d_status, 0, sizeof(int), ctx->stream);
+  // (a captured call with a window may be replayed over a work list that was built without one)
+  cudaMemsetAsync(ctx->bl.item_gap, 0, ctx->bl.max_items * sizeof(int), ctx->stream);
+  cudaMemsetAsync(ctx->bl.tok_first, 0, g.max_tokens * sizeof(int), ctx->stream);
   if (ctx->d_stage_slot) {
     ctx->h_desc.resize(g.max_tokens);
     for (int t = 0; t < g.max_tokens; ++t) ctx->h_desc[t] = t;
@@ -1185,7 +1191,8 @@ recg_status recg_kv_append_rotary(recg_ctx* ctx, const recg_batch* batch, int32_
   if (s != RECG_OK) return s;
   if (!aligned16(ctx->last_pool, ctx->last_pool)) return fail(ctx, RECG_ERR_INVALID_ARG, std::string(who) + ": the KV pool must be 16-byte aligned");
   if ((s = appends(ctx, who)) != RECG_OK) return s;
-  launch_append_rotary(kv_bits(ctx), ctx->bl, ctx->last_pool, ctx->last_pool_pages, layer, ctx->dm, q, q_stride, q_out, k, v, kv_stride, ctx->stream);
+  launch_append_rotary(kv_bits(ctx), ctx->bl, ctx->last_pool, ctx->last_pool_pages, layer, ctx->dm, ctx->turn, q, q_stride, q_out, k, v,
+                       kv_stride, ctx->stream);
   CU(cudaGetLastError());
   return RECG_OK;
 }
