@@ -250,6 +250,8 @@ recg_status recg_attention_lse(recg_ctx *ctx, const recg_batch *batch, int32_t l
  * a branch token the position that it hypothesises) sees position j of what the mask of Eq. 1 shows it only if j < n_sink or j > p - window.
  * What no row sees is not read.  window = 0: everything again.  A batch that was laid out before is seen through the new window by the next
  * recg_attention() without one.  Captured calls keep the window that they were captured with, and are for work lists of the same.
+ * (Over a bf16 pool V has to be finite in the 64-token blocks at the window's edges, as it has to be wherever a block is read that some rows do
+ * not see whole.)
  * Refused with RECG_FLAG_KV_4BIT and while weights are gathered (recg_kv_track()), as recg_kv_track() and recg_kv_weights() are with a window.
  */
 recg_status recg_window(recg_ctx* ctx, int32_t n_sink, int32_t window);

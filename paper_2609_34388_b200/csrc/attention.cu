@@ -577,6 +577,11 @@ size_t attention_smem_bytes(int head_dim) {
 // lengths are on the device always take tcgen05 for that reason, and where they decode, it loses: 64 requests of one row, eight layers,
 // 2526 us instead of the 1668 of a round that the host lays out.
 constexpr int kFewRows = 8;
+// ... and over an 8-bit pool, whose codes cost few instructions in either kernel.  The same sixteen requests, 4, 8, 12, 16, 32, 64 and 128 rows a
+// kv head: 26.5, 28.1, 36.0, 37.0, 56.1, 95.8 and 180 us with mma.sync, 41.0, 41.2, 42.1, 44.8 and 49.4 from 12 rows on with tcgen05 (bf16 pool: 44.5, 44.5,
+// 45.1, 45.5, 46.6, 48.5 and 53.2); one request of 4096, 4 to 16 and 32 rows: 8.0, 8.5, 10.0, 10.3, 13.0 and from 12 rows on 12.3, 12.4, 12.6.  Fifteen
+// requests of one row beside one of 16 + 16: 166 and 44.
+constexpr int kFewRows8 = 16;
 void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const void* q, void* o, const void* kv_pool,
                       int64_t n_pages, float* part_o, float* part_ml, int tok_per_tile, int n_sm, int* status,
                       cudaStream_t st, bool use_tc, bool layout_settled, bool whole, int tiles, bool step, int bits, float* lse, int max_rows) {
@@ -584,7 +589,7 @@ void launch_attention(const BatchLayout& bl, const Dims& dm, int layer, const vo
   if (bits != 16 || (use_tc && dm.head_dim == 128)) {
     if (four && use_tc && dm.head_dim == 128 && max_rows > kFewRows &&
         launch_attention_kv4_tc(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st)) {
-    } else if (bits == 8 && use_tc && dm.head_dim == 128 && max_rows > kFewRows)
+    } else if (bits == 8 && use_tc && dm.head_dim == 128 && max_rows > kFewRows8)
       launch_attention_kv8_tc(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, status, st, layout_settled);
     else if (bits == 8) launch_attention_kv8(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, max_rows, status, st, layout_settled);
     else if (four) launch_attention_kv4(bl, dm, layer, q, o, lse, kv_pool, n_pages, part_o, part_ml, n_sm, max_rows, status, st, layout_settled);

@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
           tmem_ld_wait();
           // (with a window: blk_end counts blocks, not positions; a block that the item does not have is seen by no row)
           const int lim = WIN ? (block < w.blk_end ? climit : -1) : min(climit, tok_end - 1), end = WIN ? (block < w.blk_end ? vhi : -1) : min(vhi, tok_end);
-          const bool need_mask = __any_sync(0xffffffffu, rvalid && (pos0 + 63 > lim || (WIN && pos0 < vfirst)));
+          const bool need_mask = __any_sync(0xffffffffu, rvalid && (pos0 + 63 > lim || (WIN && pos0 < vfirst && pos0 + 63 >= P.n_sink)));
           if (need_mask) {
             // visible tokens of this row within the 64: [0, a] and [b, c), as a 64-bit mask over tokens
             const int a = lim - pos0, b = vlo - pos0, cc = end - pos0;

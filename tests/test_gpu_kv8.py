@@ -288,3 +288,45 @@ def test_refusals():
     ctx.recg_kv_append_rotary(batch, 0, q, k, k, q)
     ctx.recg_sync()
     ctx.recg_free()
+
+
+def test_pages_behind_four_gigabytes():
+    """Every operation on pages whose blocks and headers lie behind 2^32 bytes, in the second layer."""
+    n_pages = 140000                                                     # 4.6 GB a layer
+    ctx = make(8, 128, 8, max_tokens=64, max_req=2, group=4)
+    assert ctx.kv_pool_bytes(n_pages) // 2 > 2 ** 32
+    pool = binding.alloc_kv_pool(ctx, n_pages, fill=None)
+    pt = n_pages - 1 - np.arange(16).reshape(2, 8) * 3
+    L = [70, 33]
+    caches = []
+    for r, n in enumerate(L):
+        k, v = synth.kv_values(n, 8, 128, seed=r)
+        ctx.recg_kv_write(pool, n_pages, 1, pt[r], 0, k.cuda(), v.cuda())
+        caches.append([_kv8.Cache(8, 128).write(0, k), _kv8.Cache(8, 128).write(0, v)])
+    batch = binding.Batch(L, [5, 1], [12, 0], None, pt, pool, n_pages)
+    x = torch.randn((18, 48, 128), device="cuda").bfloat16()
+    q, k, v = x[:, :32], x[:, 32:40], x[:, 40:]
+    turned, o, lse = torch.empty((18, 32, 128), dtype=torch.bfloat16, device="cuda"), torch.empty((18, 32, 128), dtype=torch.bfloat16, device="cuda"), \
+        torch.empty((18, 32), device="cuda")
+    ctx.recg_kv_append_rotary(batch, 1, q, k, v, turned)
+    p = np.concatenate([np.arange(70, 87), [33]])
+    rk = _kv8.rotated(k, p, BASE)[0]
+    got = ctx.recg_kv_rows(None, 1)
+    for r, (t, n) in enumerate(((0, 17), (17, 1))):
+        caches[r][0].write(L[r], rk[t:t + n])
+        caches[r][1].write(L[r], v[t:t + n])
+        assert same(got[0][t:t + n], caches[r][0].bf16(L[r], n)) and same(got[1][t:t + n], caches[r][1].bf16(L[r], n))
+        for held, c in zip(ctx.recg_kv_read(pool, n_pages, 1, pt[r], 0, L[r] + n), caches[r]):
+            assert same(held, c.bf16(0, L[r] + n))
+    for rows in (2, 1):                                                  # the kernel of many rows, and that of few
+        if rows == 1:
+            batch = binding.Batch([87, 34], [1, 1], [0, 0], None, pt, pool, n_pages)
+            ctx.recg_kv_append(batch, 1, k[:2].contiguous(), v[:2].contiguous())
+            caches = [[c[i].write(n, t[r:r + 1]) for i, t in enumerate((k, v))] for r, (c, n) in enumerate(zip(caches, (87, 34)))]
+        n = 18 if rows == 2 else 2
+        ctx.recg_attention(batch, 1, turned[:n], o[:n], lse[:n])
+        ctx.recg_sync()
+        for r, (t, m, see) in enumerate(((0, 17, _kv4.visible(70, 5, 12)), (17, 1, _kv4.visible(33, 1, 0))) if rows == 2 else
+                                        ((0, 1, _kv4.visible(87, 1, 0)), (1, 1, _kv4.visible(34, 1, 0)))):
+            _kv8.check(f64(o[t:t + m]), f64(lse[t:t + m]), f64(turned[t:t + m]), caches[r][0].held, caches[r][1].held, see)
+    ctx.recg_free()
