@@ -84,14 +84,14 @@ struct SmallDesc {
   int v[kSmallDesc];
 };
 // S1: per-token arrays and the attention work list (batches with a page table: a verify-only batch needs neither).
-// whole: no tile is cut (attention_whole_tiles), and no combine kernel has to follow the attention kernel.
+// whole: no tile is cut, a CTA has at most so many (attention_whole_tiles), and no combine kernel has to follow the attention kernel; 0: tiles are cut.
 // tokens: the per-token arrays as well (else launch_embed follows, which fills them).
 // desc (may be null): the descriptor to be written to desc_dev, where bl points.
 // list: the work list (else the per-token arrays only, and the list may follow by itself).
-void launch_layout(const BatchLayout& bl, const Dims& dm, int tok_per_tile, int n_ctas, bool whole, int64_t n_pages,
+void launch_layout(const BatchLayout& bl, const Dims& dm, int tok_per_tile, int n_ctas, int whole, int64_t n_pages,
                    int* status, bool tokens, int* desc_dev, const SmallDesc* desc, cudaStream_t st, bool list = true);
 // HOST arrays [n_req]; rows: rows per request
-bool attention_whole_tiles(int n_req, const int* ctx_len, const int* rows, int n_kv, int tok_per_tile, int n_ctas, int n_sink, int window);
+int attention_whole_tiles(int n_req, const int* ctx_len, const int* rows, int n_kv, int tok_per_tile, int n_ctas, int n_sink, int window);
 // the layout kernel keeps five ints per request in shared memory: requests per step are bounded by this
 constexpr int kMaxLayoutRequests = 4096;
 size_t layout_smem_bytes(int n_req, int n_ctas);

@@ -40,8 +40,8 @@ __device__ __forceinline__ int upper_request(const int* cu, int n_req, int t) {
 // The CTAs are divided between the two lines in proportion to their work (line A: the first 2 n_pairs_a CTAs), so
 // that every CTA walks ONE range and all carry about the same load.  Each piece that holds real blocks is an item;
 // a tile whose blocks are cut by range boundaries gets one partial slot per piece.
-// Small work lists are not cut at all (`whole`, decided on the host from the same lengths): every tile is one item of a CTA of
-// its own, and no combine kernel follows.
+// Small work lists are not cut at all (`whole`, decided on the host from the same lengths): every tile is one item, a CTA has one of
+// them (`whole` at most), and no combine kernel follows.
 // Items: [line A, first siblings | line A, second siblings (same order) | line B]; cta_off holds, per CTA, two
 // index ranges it walks one after the other (the second one is empty in this division).
 //
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, 
   if (pairs_a > max_pairs) pairs_a = max_pairs;
   if (wb > 0 && n_ctas - 2 * pairs_a < 1) pairs_a = (n_ctas - 1) / 2;
   if (wa == 0) pairs_a = 0;
-  if (whole) pairs_a = n_seg_a;            // (2 n_seg_a + n_seg_b <= n_ctas)
+  if (whole) pairs_a = (n_seg_a + whole - 1) / whole;      // (which leaves CTAs enough for line B)
   const int n_ctas_b = n_ctas - 2 * pairs_a;
   const int per_a = pairs_a > 0 && wa > 0 ? (int)((wa + pairs_a - 1) / pairs_a) : 0x3fffffff;
   const int per_b = n_ctas_b > 0 && wb > 0 ? (int)((wb + n_ctas_b - 1) / n_ctas_b) : 0x3fffffff;
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, 
       const Scan3 e1 = block_scan(Scan3{s < n_seg ? g.nb + item_cost : 0, 0, 0}, &tot, scratch);
       const int g0 = off + e1.a + item_cost;              // cost range of the real blocks: [g0, g0 + nb)
       off += tot.a;
-      const int c_first = whole ? s : g0 / per, c_last = whole ? s : (g0 + g.nb - 1) / per;
+      const int c_first = whole ? s / whole : g0 / per, c_last = whole ? c_first : (g0 + g.nb - 1) / per;
       const int np = s < n_seg ? c_last - c_first + 1 : 0;
       const int cut_tiles = np > 1 ? (pair ? 2 : 1) : 0;
       const Scan3 e2 = block_scan(Scan3{np, cut_tiles * np, cut_tiles}, &tot, scratch);
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kLayoutThreads) layout_kernel(BatchLayout bl, 
       }
       if (pass == 0 || s >= n_seg) continue;
       // first piece of every owner: an owner without pieces starts where the next one does
-      const int c_prev = s == 0 || whole ? s - 1 : (g0 - item_cost - 1) / per;     // owner of the last block of the segment before
+      const int c_prev = s == 0 ? -1 : whole ? (s - 1) / whole : (g0 - item_cost - 1) / per;     // owner of the last block of the segment before
       for (int c = c_prev + 1; c <= c_last && c <= n_owners; ++c) owner_off[c] = c <= c_first ? item0 : item0 + (c - c_first);
       if (s == n_seg - 1)
         for (int c = c_last + 1; c <= n_owners; ++c) owner_off[c] = item0 + np;
@@ -561,21 +561,30 @@ size_t layout_smem_bytes(int n_req, int n_ctas) {
 // tokens of context 6.3 us whole, 8.8 cut; 256 tokens 8.7 and 9.1; 512 tokens 10.8 and 10.3; with head_dim 64 4.3 and 5.8, 5.8
 // and 6.0, 7.8 and 6.4.
 // (With a window a tile has the blocks of the first tokens and of its window, more or less.)
-bool attention_whole_tiles(int n_req, const int* ctx_len, const int* rows, int n_kv, int tok_per_tile, int n_ctas, int n_sink, int window) {
-  long long tiles = 0, cost = 0;
+int attention_whole_tiles(int n_req, const int* ctx_len, const int* rows, int n_kv, int tok_per_tile, int n_ctas, int n_sink, int window) {
+  long long tiles = 0, cost = 0, pairs = 0;
   int longest = 0;
   for (int r = 0; r < n_req; ++r) {
     const int rt = (rows[r] + tok_per_tile - 1) / tok_per_tile;
     int nb = (ctx_len[r] + rows[r] + 63) / 64;
     if (window) nb = (int)std::min<long long>(nb, ((long long)n_sink + window + std::min(rows[r], 2 * tok_per_tile)) / 64 + 2);
     tiles += (long long)n_kv * rt;
+    pairs += (long long)n_kv * (rt / 2);
     cost += (long long)n_kv * (rt * nb + (rt & ~1) * kItemCostPair + (rt & 1) * kItemCostSingle);
     if (nb > longest) longest = nb;
   }
-  return tiles <= n_ctas && longest - (cost + n_ctas - 1) / n_ctas <= kWholeBlocks;
+  const long long even = (cost + n_ctas - 1) / n_ctas;
+  if (tiles <= n_ctas) return longest - even <= kWholeBlocks ? 1 : 0;
+  if (!window) return 0;
+  // Windows are short and all alike: several whole tiles a CTA, if the longest CTA then waits less than cutting costs, which grows with the tiles
+  const long long k = (tiles + n_ctas - 1) / n_ctas, most = 8;
+  for (long long w = k; w <= std::min(k + 1, most); ++w)
+    if (2 * ((pairs + w - 1) / w) + (tiles - 2 * pairs + w - 1) / w <= n_ctas)
+      return w * (longest + (pairs ? kItemCostPair : kItemCostSingle)) - even <= kWholeBlocks * tiles / n_ctas ? (int)w : 0;
+  return 0;
 }
 
-void launch_layout(const BatchLayout& bl, const Dims& dm, int tok_per_tile, int n_ctas, bool whole, int64_t n_pages,
+void launch_layout(const BatchLayout& bl, const Dims& dm, int tok_per_tile, int n_ctas, int whole, int64_t n_pages,
                    int* status, bool tokens, int* desc_dev, const SmallDesc* desc, cudaStream_t st, bool list) {
   static const SmallDesc none{};
   const size_t smem = layout_smem_bytes(bl.n_req, n_ctas);
@@ -585,7 +594,7 @@ void launch_layout(const BatchLayout& bl, const Dims& dm, int tok_per_tile, int 
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)layout_smem_bytes(kMaxLayoutRequests, 1024));
   const int token_ctas = tokens ? (bl.n_tok + kLayoutThreads - 1) / kLayoutThreads : 0;
   launch_pdl(bl.window ? layout_kernel<true> : layout_kernel<false>, dim3(1 + token_ctas), dim3(kLayoutThreads), smem, st, bl, dm.n_kv, dm.mask_id, tok_per_tile, n_ctas,
-             whole ? 1 : 0, list ? 1 : 0, n_pages, status, desc_dev, desc ? *desc : none);
+             whole, list ? 1 : 0, n_pages, status, desc_dev, desc ? *desc : none);
 }
 
 void launch_embed(const BatchLayout& bl, const Dims& dm, const void* embed, float* h, const void* gain, void* x, float* ss,

@@ -63,7 +63,7 @@ struct recg_ctx {
   bool layout_has_pages = false;
   bool list_pending = false;     // its work list has not been built: only operations on rows have asked for the batch so far
   bool window_pending = false;   // neither have what its rows see and its work list been built for the window of recg_window()
-  bool layout_whole = false;     // no attention tile was cut: no combine kernel
+  int layout_whole = 0;          // no attention tile was cut (a CTA has at most so many): no combine kernel
   int layout_rows = 128;         // query rows of its largest row tile (128: the lengths are on the device)
   int layout_tiles = 0;          // its row tiles, all kv heads (0: the lengths are on the device)
   // An attention kernel has been enqueued behind the last layout kernel.  The first one waits for its predecessors before it
@@ -905,10 +905,10 @@ recg_status recg_step_device(recg_ctx* ctx, const recg_device_batch* b, recg_log
   bl.page_table = b->page_table;
   bl.risk_delta = 0.5f;
   launch_pack_device(device_round(ctx, b), ctx->d_desc, ctx->d_dyn, ctx->d_status, ctx->stream);
-  ctx->layout_whole = false;           // (the lengths are on the device)
+  ctx->layout_whole = 0;               // (the lengths are on the device)
   ctx->layout_tiles = 0;
   ctx->layout_rows = 128;
-  launch_layout(bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, false, b->kv_pool_pages, ctx->d_status, false, ctx->d_desc, nullptr, ctx->stream);
+  launch_layout(bl, ctx->dm, ctx->tok_per_tile, ctx->target_items, 0, b->kv_pool_pages, ctx->d_status, false, ctx->d_desc, nullptr, ctx->stream);
   ctx->list_settled = false;
   ctx->list_pending = ctx->window_pending = false;
   ctx->small_desc.n = 0;

@@ -37,6 +37,14 @@ def test_branches(heads, window, flags):
 
 
 @pytest.mark.parametrize("flags", FLAGS)
+@pytest.mark.parametrize("heads,reqs", [(B8, [(900, 700, 0)]), (B8, [(300 + 7 * i, 40, 0) for i in range(9)]), (B8, [(300 + 7 * i, 1, 0) for i in range(60)]),
+                                        (B14, [(500, 1, 0)] * 19 + [(400, 60, 9)] * 7), (TINY, [(500, 300, 0)] * 9), ((16, 1, 128), [(333, 500, 0)] * 5)])
+def test_several_whole_tiles_for_a_cta(heads, reqs, flags):
+    """More tiles than CTAs, all about as long: pairs of tiles and single ones, a last CTA with fewer."""
+    run_case(heads, reqs, seed=71, flags=flags, window=(3, 50))
+
+
+@pytest.mark.parametrize("flags", FLAGS)
 def test_many_short_requests(flags):
     g = np.random.default_rng(9)
     run_case(B8, [(int(x), 1, 0) for x in g.integers(0, 400, 500)], seed=61, flags=flags, window=(3, 50))
