@@ -19,6 +19,10 @@
 //   warps 12-15 turn codes of V into the operand (K-major, a thread one of the 128 values, 16 tokens of a page at a time: 16-byte reads and
 //               stores without bank conflicts) and the rows of Q of the next item into theirs
 // The registers are moved to the softmax warps: 4 x (56 + 168 + 168 + 120) x 32, which are those of the launch.
+//
+// 1001 rows over 6000 tokens of 40 / 8 heads 165 us (floor 80, mma.sync 789), 16 requests of 12 to 96 rows over 512 to 8192 tokens 89 us (27, 386).  Of 2150
+// clocks a stage the softmax of a group takes 2000, the products 1050; without the exponentials 167 us, without V's conversion 160, without
+// maxima, sums and packing 154: what is left is latency, with two softmax warps a scheduler.  V by ALU instructions instead of conversions 172.
 // Every wait is bounded; a wait that runs out raises a CTA-wide flag after which no wait blocks, so the kernel always ends.
 #include <cuda_fp16.h>
 

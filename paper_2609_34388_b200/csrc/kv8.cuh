@@ -4,13 +4,14 @@
 //   e = the least whole number with a <= 448 2^e, within -60 .. 120 (0 where a is 0),  c = the e4m3 number nearest to x 2^-e
 // and a value stands for c 2^e, which is a bf16 number.  A scale that is a power of two costs no digits, as e4m3 is a floating-point
 // format itself: it decides only where values become too small for four digits (2^-6 2^e and below, 2^-14.8 of the largest) or
-// vanish (2^-24.8 of it).  So rounding a block again, to the e of rows that have come in, loses nothing above that line; and scales
+// vanish (2^-18.8 of it).  So rounding a block again, to the e of rows that have come in, loses nothing above that line; and scales
 // leave the matrix products as exponents: they are added to scores in powers of two.
-// At e = 120 codes end at 240: 256 2^120 is no bf16 number.  A row (one token) with a value that is not finite has a flag, codes of 0, no part in e, and
-// reads back as NaN; so every code is a number, and 0 times a code is 0 wherever a mask or the end of a request makes a probability 0.
+// At e = 120 codes end at 240: 256 2^120 is no bf16 number.  A row (one token) with a value that is not finite has a flag, codes of 0, no part in
+// e, and reads back as NaN; so every code is a number, and 0 times a code is 0 wherever a mask or the end of a request makes a probability 0.
 //
 // Pool = [layer], each [page][kv_head] blocks of 32 d bytes, K codes and V codes, then [page][kv_head] headers of eight bytes:
-// K's e (16 bits, signed) and its rows' flags above it, the same of V; zeros are a block of zeros.  (Beside the codes a header would move every block off the 32-byte sectors.)
+// K's e (16 bits, signed) and its rows' flags above it, the same of V; zeros are a block of zeros.  (Beside the codes a header would move every
+// block off the 32-byte sectors.)
 //   K: token t at t d; at d = 128 the eight 16-byte chunks of a row are XOR-swizzled with t & 7: a page is two of the tensor core's
 //      canonical 128-byte-swizzle atoms, K-major, and a row-wise 16-byte read of the lanes of a warp is free of bank conflicts.
 //   V: value i of token t at 16 i + t: a lane finds the tokens of a page, along which V is contracted, in one 16-byte read.
