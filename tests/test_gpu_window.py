@@ -199,3 +199,48 @@ def test_refusals():
     ctx.recg_kv_weights(batch, 0, q, lse, None, w)
     ctx.recg_sync()
     ctx.recg_free()
+
+
+@pytest.mark.parametrize("flags", FLAGS)
+@pytest.mark.parametrize("window", [None, (5, 100)])
+def test_workspace_regions_are_kept(flags, window):
+    """With guard bands behind every region of the workspace, which recg_sync() checks."""
+    flags |= binding.FLAG_DEBUG_CHECKS
+    run_case(B8, [(900, 33, 8), (3, 1, 0), (0, 64, 0)], seed=81, flags=flags, window=window, corr=[(2, 9), (), (63,)])
+    run_case(TINY, [(500, 1, 0)] * 40, seed=82, flags=flags, window=window)
+
+
+def test_two_contexts_on_two_streams():
+    """A pool that two contexts read at once, each with a window of its own."""
+    desc = synth.fixed_descriptor([3000], [16], [16], seed=3)
+    T = desc.n_tokens
+    k, v = synth.kv_values(3000 + T, 8, 128, seed=9)
+    q = synth.queries(T, 32, 128, seed=8).cuda()
+    torch.cuda.synchronize()
+    alone, together = [], []
+    contexts = []
+    for i, window in enumerate(((0, 0), (4, 500))):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            ctx = binding.Context(binding.make_config(shape_of(B8), 1, T, desc.page_table.shape[1], KV8))
+            ctx.recg_window(*window)
+            contexts.append((ctx, stream))
+    pool = binding.alloc_kv_pool(contexts[0][0], desc.n_pages)
+    torch.cuda.synchronize()
+    contexts[0][0].recg_kv_write(pool, desc.n_pages, 0, desc.page_table[0], 0, k.cuda(), v.cuda())
+    contexts[0][0].recg_sync()
+    batch = binding.Batch([3000], [16], [16], None, desc.page_table, pool, desc.n_pages)
+    for out, wait in ((alone, True), (together, False)):
+        outs = [torch.empty_like(q) for _ in contexts]
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for (ctx, _), o in zip(contexts, outs):
+                ctx.recg_attention(batch, 0, q, o)
+                if wait:
+                    ctx.recg_sync()
+        for ctx, _ in contexts:
+            ctx.recg_sync()
+        out += outs
+    assert all(torch.equal(a, b) for a, b in zip(alone, together)) and not torch.equal(alone[0], alone[1])
+    for ctx, _ in contexts:
+        ctx.recg_free()
